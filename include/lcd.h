@@ -411,6 +411,88 @@ lcd_status lcd_linear_host_batch(const lcd_host_problem* problems /* host */, in
                                  void* y_host_all, void* scratch, size_t scratch_bytes, int32_t* status_word_dev,
                                  void* cuda_stream);
 
+/* ----------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point (the OCP "MXFP4" format): a row is cut into blocks of 32 columns, a block is a scale
+ * 2^(byte - 127) (byte 255: NaN) and 32 elements of sign, two exponent bits and one mantissa bit, {0, .5, 1, 1.5, 2, 3, 4, 6}
+ * and their negatives.  For layers whose clustering loses too much, and for weights that change at every step.
+ *   codes:  uint8 [rows][ldc], blocks * 16 bytes a row, blocks = ceil(K / 32); the even column of a pair in the low nibble,
+ *           an element's code = sign << 3 | index into the list above; columns K.. of the last block hold code 0;
+ *   scales: uint8 [rows][lds], blocks bytes a row.
+ * Both start on 16 bytes and ldc, lds are multiples of 16 (LCD_ERR_INVALID_ARG otherwise); bytes between a row's end and the
+ * next row are neither read for their value nor written.
+ * Types of x, y and logits in this and the next section: lcd_dtype.
+ * -------------------------------------------------------------------------------------------- */
+typedef enum {
+  LCD_DTYPE_F32 = 0,
+  LCD_DTYPE_F16 = 1,
+  LCD_DTYPE_BF16 = 2
+} lcd_dtype;
+
+/* t = x * inv_smooth (binary32, one rounding; x itself without inv_smooth).  Per block, A = max |t|:
+ *     scale exponent e = max(floor(log2 A) - 2, -127), A == 0: 0;     element = t * 2^-e rounded to the nearest of the list,
+ *     a tie to the one with a zero mantissa bit, beyond 6 to 6; a block with an infinity or a NaN: byte 255, codes 0.
+ * Reproducible bit for bit.
+ *   x:          device, [M][ldx], ldx >= K, any alignment of the type's own;     inv_smooth: device fp32 [K] or NULL;
+ *   codes, scales: device out. */
+lcd_status lcd_mx_quantize(const void* x, lcd_dtype x_type, int64_t M, int64_t K, int64_t ldx, const float* inv_smooth,
+                           uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, void* cuda_stream);
+
+/* What codes and scales stand for: out[m][k] = element * 2^(byte - 127), rounded once to the output type (fp32 holds every
+ * value, bf16 all of them, fp16 overflows to infinity).  out: device, [M][ldo], ldo >= K. */
+lcd_status lcd_mx_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K,
+                             void* out, lcd_dtype out_type, int64_t ldo, void* cuda_stream);
+
+/* y[m][n] = sum over k of x^[m][k] * w^[n][k], both operands microscaled, sums in fp32, rounded once to y's type.
+ *   w_codes, w_scales: device, N rows;     x_codes, x_scales: device, M rows, the same K;
+ *   y: device out, [M][ldy], ldy >= N;     status_word_dev: as for lcd_lut_linear.
+ * The sums' order is fixed: results are reproducible from run to run. */
+lcd_status lcd_mx_linear(const uint8_t* w_codes, int64_t ldwc, const uint8_t* w_scales, int64_t ldws, int64_t N, int64_t K,
+                         const uint8_t* x_codes, int64_t ldxc, const uint8_t* x_scales, int64_t ldxs, int64_t M, void* y,
+                         lcd_dtype y_type, int64_t ldy, int32_t* status_word_dev, void* cuda_stream);
+
+/* lcd_mx_quantize of x and lcd_mx_linear in one call; y is the same bit for bit.  workspace: device scratch of
+ * lcd_mx_linear_fused_workspace_bytes(M, K) bytes, 16-byte aligned, contents ignored; calls that may overlap on the device
+ * need separate ones. */
+lcd_status lcd_mx_linear_fused_workspace_bytes(int64_t M, int64_t K, size_t* bytes);
+
+lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, const uint8_t* w_scales, int64_t ldws, int64_t N, int64_t K,
+                               const void* x, lcd_dtype x_type, int64_t ldx, const float* inv_smooth, int64_t M, void* y,
+                               lcd_dtype y_type, int64_t ldy, void* workspace, size_t workspace_bytes,
+                               int32_t* status_word_dev, void* cuda_stream);
+
+/* ----------------------------------------------------------------------------------------------
+ * Offline: distillation from a teacher's top logits (Section 3 trains the clustered weights against the full-precision
+ * model), before lcd_reclassify: the loss of a student's logits and its gradient.  Per token, over the entries j whose index
+ * lies in [0, V) (others, -1 for instance, are absent):
+ *     p_j = exp(t_j / temperature - L),  L = log sum_j exp(t_j / temperature), or teacher_lse of the token: the logarithm of
+ *           that sum over the teacher's whole row, so that the p_j are its probabilities and sum to less than one;
+ *     q = softmax(z / temperature) over the V logits;     P = sum_j p_j;
+ *     loss = weight * sum over p_j != 0 of p_j * (log p_j - log q_idx_j);
+ *     dlogits_v = weight / temperature * (P * q_v - sum over j with idx_j = v of p_j).
+ * A token whose weight is 0 is left out: its logits are not read, loss and gradient are 0.  A token without entries has
+ * loss 0 and gradient 0.  Logits of -infinity have probability 0.  The same index twice counts twice.
+ *   logits:         device, [T][ldz], ldz >= V;
+ *   teacher_idx:    device, int32 or int64 (idx_bytes 4 or 8) [T][ldi];   teacher_logits: device, [T][ldt];  1 <= k <= 1024
+ *                   entries a token;
+ *   temperature:    > 0 and finite;     teacher_lse, weight: device fp32 [T] or NULL (all ones);
+ *   loss:           device out, fp32 [T];
+ *   stats:          device out, fp32 [T][2], or NULL: the row's largest logit m and sum_v exp((z_v - m) / temperature), for
+ *                   lcd_distill_grad;
+ *   dlogits:        device out, the logits' type, [T][ldd], or NULL.  May be logits itself (with ldd = ldz).
+ * Sums run in a fixed order: results are reproducible from run to run.
+ * -------------------------------------------------------------------------------------------- */
+lcd_status lcd_distill_loss(const void* logits, lcd_dtype type, int64_t T, int64_t V, int64_t ldz, const void* teacher_idx,
+                            int idx_bytes, int64_t ldi, const void* teacher_logits, lcd_dtype teacher_type, int64_t ldt, int64_t k,
+                            float temperature, const float* teacher_lse, const float* weight, float* loss, float* stats,
+                            void* dlogits, int64_t ldd, void* cuda_stream);
+
+/* The gradient alone, from the stats that lcd_distill_loss wrote for the same logits and temperature; the weights may be
+ * others (a token that was left out there has NaN for stats: its gradient is NaN unless it is left out here too). */
+lcd_status lcd_distill_grad(const void* logits, lcd_dtype type, int64_t T, int64_t V, int64_t ldz, const void* teacher_idx,
+                            int idx_bytes, int64_t ldi, const void* teacher_logits, lcd_dtype teacher_type, int64_t ldt, int64_t k,
+                            float temperature, const float* teacher_lse, const float* weight, const float* stats, void* dlogits,
+                            int64_t ldd, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

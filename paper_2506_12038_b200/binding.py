@@ -32,7 +32,8 @@ EXPORTS = ["lcd_status_string", "lcd_last_cuda_error", "lcd_packed_weights_bytes
            "lcd_linear_host_batch_sizes", "lcd_linear_host_batch", "lcd_lut_linear_act8",
            "lcd_lut_linear_batch_act8", "lcd_linear_fused_batch_workspace_bytes", "lcd_linear_fused_batch",
            "lcd_smoothing_search_workspace_bytes", "lcd_smoothing_search", "lcd_reclassify",
-           "lcd_dbci_workspace_bytes", "lcd_dbci"]
+           "lcd_dbci_workspace_bytes", "lcd_dbci", "lcd_mx_quantize", "lcd_mx_dequantize", "lcd_mx_linear",
+           "lcd_mx_linear_fused_workspace_bytes", "lcd_mx_linear_fused", "lcd_distill_loss", "lcd_distill_grad"]
 STATIC_SCRATCH_BYTES = 4 << 20
 
 
@@ -114,6 +115,16 @@ def _load() -> ctypes.CDLL:
                                                 POINTER(c_size_t)]
     lib.lcd_linear_host_batch.argtypes = [POINTER(HostProblem), c_int, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p,
                                           c_void_p]
+    matrix, scaled = [c_void_p, c_int], [c_void_p, c_int64, c_void_p, c_int64]       # an address and its type; codes and scales
+    lib.lcd_mx_quantize.argtypes = matrix + [c_int64, c_int64, c_int64, c_void_p] + scaled + [c_void_p]
+    lib.lcd_mx_dequantize.argtypes = scaled + [c_int64, c_int64] + matrix + [c_int64, c_void_p]
+    lib.lcd_mx_linear.argtypes = scaled + [c_int64, c_int64] + scaled + [c_int64] + matrix + [c_int64, c_void_p, c_void_p]
+    lib.lcd_mx_linear_fused_workspace_bytes.argtypes = [c_int64, c_int64, POINTER(c_size_t)]
+    lib.lcd_mx_linear_fused.argtypes = scaled + [c_int64, c_int64] + matrix + [c_int64, c_void_p, c_int64] + matrix + [
+        c_int64, c_void_p, c_size_t, c_void_p, c_void_p]
+    distill = matrix + [c_int64, c_int64, c_int64, c_void_p, c_int, c_int64] + matrix + [c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p]
+    lib.lcd_distill_loss.argtypes = distill + [c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
+    lib.lcd_distill_grad.argtypes = distill + [c_void_p, c_void_p, c_int64, c_void_p]
     for name in EXPORTS:
         if name not in ("lcd_status_string", "lcd_last_cuda_error"):
             getattr(lib, name).restype = c_int
@@ -354,6 +365,83 @@ def smoothing_search(x, wmax, alphas, stream=None):
     if r.__class__ is int:
         _check(r, "lcd_smoothing_search")
     return r
+
+
+# --------------------------------------------------------------------- microscaled 4-bit floating point, distillation
+# These run on the device of their tensors, whichever is current; a stream that is given belongs to that device.
+def mx_quantize(x, inv_smooth=None, codes=None, scales=None, stream=None):
+    """x: CUDA fp32, fp16 or bf16 [M,K] (row stride may exceed K), inv_smooth: fp32 [K] -> (codes uint8 [M, 16 * blocks],
+    scales uint8 [M, blocks]), blocks = ceil(K / 32): x * inv_smooth as microscaled 4-bit numbers (include/lcd.h).  Both may be
+    given; their rows start on 16 bytes."""
+    out = (_host_calls or _calls()).mx_quantize(x, inv_smooth, codes, scales, stream)
+    if out.__class__ is int:
+        _check(out, "lcd_mx_quantize")
+    return out
+
+
+def mx_dequantize(codes, scales, K=None, out=None, dtype=None, stream=None):
+    """What codes and scales stand for, as fp32 (or dtype, or in out) [M,K]; without K all 32 * blocks columns."""
+    r = (_host_calls or _calls()).mx_dequantize(codes, scales, K, out, dtype or _float32(), stream)
+    if r.__class__ is int:
+        _check(r, "lcd_mx_dequantize")
+    return r
+
+
+def mx_linear(w_codes, w_scales, x_codes, x_scales, y=None, dtype=None, status_word=None, stream=None):
+    """y[m][n] = sum_k x^[m][k] w^[n][k] of two microscaled matrices with the same K, fp32 sums; y: CUDA [M,N], fp32 or dtype."""
+    r = (_host_calls or _calls()).mx_linear(False, w_codes, w_scales, x_codes, x_scales, y, dtype or _float32(), None, status_word, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_mx_linear")
+    return r
+
+
+def mx_linear_fused(w_codes, w_scales, x, inv_smooth=None, y=None, dtype=None, workspace=None, status_word=None, stream=None):
+    """mx_quantize(x, inv_smooth) and mx_linear in one call, the same y bit for bit.  workspace: CUDA scratch of at least
+    mx_linear_fused_workspace_bytes(M, K) bytes (allocated here if absent)."""
+    r = (_host_calls or _calls()).mx_linear(True, w_codes, w_scales, x, inv_smooth, y, dtype or _float32(), workspace, status_word, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_mx_linear_fused")
+    return r
+
+
+def mx_linear_fused_workspace_bytes(M: int, K: int) -> int:
+    out = c_size_t(0)
+    _check(lib.lcd_mx_linear_fused_workspace_bytes(M, K, byref(out)), "lcd_mx_linear_fused_workspace_bytes")
+    return out.value
+
+
+@functools.cache
+def _float32():
+    import torch
+    return torch.float32
+
+
+def distill_loss(logits, teacher_idx, teacher_logits, temperature: float = 1.0, teacher_lse=None, weight=None, want_stats=False,
+                 want_grad=False, loss=None, stats=None, dlogits=None, stream=None):
+    """Loss of a student's logits (CUDA fp32, fp16 or bf16 [T,V]) against a teacher's top logits (any of those types [T,k], with
+    their int32 or int64 indices [T,k], -1: absent), per token, times weight (fp32 [T]).  teacher_lse (fp32 [T]): the logarithm of
+    the teacher's whole row's sum of exp(t / temperature); without it its probabilities are normalised over the entries.  Returns
+    the loss, fp32 [T], and behind it, if asked for, the stats for distill_grad (fp32 [T,2]) and the gradient of the loss's sum
+    with respect to the logits (their type; dlogits=logits writes it in their place)."""
+    r = (_host_calls or _calls()).distill(logits, teacher_idx, teacher_logits, temperature, teacher_lse, weight, None, loss,
+                                          stats if stats is not None else True if want_stats else None,
+                                          dlogits if dlogits is not None else True if want_grad else None, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_distill_loss")
+    if r[1] is None:
+        return r[0] if r[2] is None else (r[0], r[2])
+    return r[:2] if r[2] is None else r
+
+
+def distill_grad(logits, teacher_idx, teacher_logits, stats, temperature: float = 1.0, teacher_lse=None, weight=None, dlogits=None,
+                 stream=None):
+    """The gradient of distill_loss with respect to the logits, from the stats that it gave for them; weight (fp32 [T]) is the
+    loss's factor of every token, which may be known only now."""
+    r = (_host_calls or _calls()).distill(logits, teacher_idx, teacher_logits, temperature, teacher_lse, weight, stats, None, None,
+                                          True if dlogits is None else dlogits, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_distill_grad")
+    return r[2]
 
 
 def resolve_batch_algo(weights_and_tokens, algo: int = ALGO_AUTO) -> int:

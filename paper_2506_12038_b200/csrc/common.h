@@ -99,5 +99,37 @@ size_t dense_tc_workspace_bytes(const Problem& p);
 lcd_status launch_dense_tc(const Problem& p, bool fp16_operands, void* workspace, size_t workspace_bytes,
                            int32_t* status_word, void* stream);
 
+
+// Microscaled 4-bit floating point and distillation (arguments are checked by api_mx.cu).
+struct MxProduct {
+  const uint8_t *w_codes, *w_scales, *x_codes, *x_scales;
+  int64_t ldwc, ldws, ldxc, ldxs, N, K, M;
+  void* y;
+  lcd_dtype y_type;
+  int64_t ldy;
+};
+lcd_status launch_mx_quantize(const void* x, lcd_dtype type, int64_t M, int64_t K, int64_t ldx, const float* inv_smooth, uint8_t* codes,
+                              int64_t ldc, uint8_t* scales, int64_t lds, void* stream);
+lcd_status launch_mx_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K, void* out,
+                                lcd_dtype type, int64_t ldo, void* stream);
+lcd_status launch_mx_linear(const MxProduct& p, int32_t* status_word, void* stream);
+struct Distillation {
+  const void* logits;
+  lcd_dtype type;
+  int64_t T, V, ldz;
+  const void* teacher_idx;
+  int idx_bytes;
+  int64_t ldi;
+  const void* teacher_logits;
+  lcd_dtype teacher_type;
+  int64_t ldt, k;
+  float temperature;
+  const float *teacher_lse, *weight;
+  float *loss, *stats;        // stats is read by the gradient alone (loss == nullptr)
+  void* dlogits;
+  int64_t ldd;
+};
+lcd_status launch_distill(const Distillation& d, void* stream);
+
 }  // namespace lcd
 #endif

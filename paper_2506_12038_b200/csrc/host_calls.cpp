@@ -11,10 +11,13 @@
 #include <ATen/ops/empty_like.h>
 #include <ATen/ops/zeros.h>
 #include <c10/cuda/CUDACachingAllocator.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <vector>
 
 #include "lcd.h"
@@ -312,6 +315,276 @@ PyObject* smoothing_search(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- microscaled 4-bit floating point and distillation.  These run on their first tensor's device, whichever is current, and
+// every tensor has to lie there.
+bool type_of(at::ScalarType t, lcd_dtype* out) {
+  if (t == at::kFloat) *out = LCD_DTYPE_F32;
+  else if (t == at::kHalf) *out = LCD_DTYPE_F16;
+  else if (t == at::kBFloat16) *out = LCD_DTYPE_BF16;
+  else return false;
+  return true;
+}
+// A matrix of fp32, fp16 or bf16 with unit column stride.
+bool dense(const at::Tensor& t, lcd_dtype* type) {
+  return t.is_cuda() && t.dim() == 2 && type_of(t.scalar_type(), type) && (t.stride(1) == 1 || t.size(1) == 1);
+}
+// Elements from a row to the next.  A single row's stride is whatever its tensor was cut from: any that holds the row will do.
+int64_t row_stride(const at::Tensor& t, int64_t multiple = 1) {
+  return t.size(0) > 1 ? t.stride(0) : (t.size(1) + multiple - 1) / multiple * multiple;
+}
+bool bytes_of(const at::Tensor& t, const at::Device& device, int64_t rows, int64_t columns) {
+  return t.device() == device && t.scalar_type() == at::kByte && t.dim() == 2 && t.size(0) == rows && t.size(1) == columns &&
+         (t.stride(1) == 1 || columns == 1);
+}
+// An fp32 vector of n values, or none.
+bool vector_of(PyObject* o, const char* what, const at::Device& device, int64_t n, const char* expected, const float** out) {
+  *out = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = tensor_of(o, what);
+  if (!t || !require(t->device() == device && t->scalar_type() == at::kFloat && t->numel() == n && t->is_contiguous(), expected)) return false;
+  *out = static_cast<const float*>(t->data_ptr());
+  return true;
+}
+bool status_word_of(PyObject* o, const at::Device& device, int32_t** out) {
+  *out = nullptr;
+  if (o == Py_None) return true;
+  const at::Tensor* t = tensor_of(o, "status_word");
+  if (!t || !require(t->device() == device && t->scalar_type() == at::kInt && t->numel() >= 1, "status_word: int32 on the same device")) return false;
+  *out = static_cast<int32_t*>(t->data_ptr());
+  return true;
+}
+// A dtype argument (torch.float32, float16, bfloat16).
+bool dtype_of(PyObject* o, at::ScalarType* out) {
+  lcd_dtype t;
+  if (!require(THPDtype_Check(o), "dtype: a torch.dtype")) return false;
+  *out = reinterpret_cast<THPDtype*>(o)->scalar_type;
+  return require(type_of(*out, &t), "dtype: torch.float32, torch.float16 or torch.bfloat16");
+}
+// The given tensor of that shape, or a new one.
+bool output_of(PyObject* o, const char* what, at::IntArrayRef shape, const at::TensorOptions& options, const char* expected, at::Tensor* out) {
+  if (o == Py_None) {
+    *out = at::empty(shape, options);
+    return true;
+  }
+  const at::Tensor* t = tensor_of(o, what);
+  if (!t || !require(t->device() == options.device() && t->scalar_type() == c10::typeMetaToScalarType(options.dtype()) && t->sizes() == shape &&
+                         (t->dim() == 0 || t->stride(-1) == 1 || t->size(-1) == 1), expected))
+    return false;
+  *out = *t;
+  return true;
+}
+// A given output is returned as it came.
+PyObject* returned(const CallStream& stream, PyObject* given, const at::Tensor& t) {
+  return given == Py_None ? stream.output(t) : Py_NewRef(given);
+}
+PyObject* pack(std::initializer_list<PyObject*> items) {     // steals the references
+  bool all = true;
+  for (PyObject* o : items) all = all && o;
+  PyObject* r = all ? PyTuple_New((Py_ssize_t)items.size()) : nullptr;
+  Py_ssize_t i = 0;
+  for (PyObject* o : items) {
+    if (r) PyTuple_SET_ITEM(r, i++, o);
+    else Py_XDECREF(o);
+  }
+  return r;
+}
+
+// (x, inv_smooth, codes, scales, stream) -> (codes, scales) or a status
+PyObject* mx_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 5)) return nullptr;
+  const at::Tensor* x = tensor_of(a[0], "x");
+  lcd_dtype type;
+  if (!x || !require(dense(*x, &type), "x: CUDA fp32, fp16 or bf16 [M, K] with unit column stride")) return nullptr;
+  const c10::cuda::CUDAGuard on(x->device());
+  const int64_t M = x->size(0), K = x->size(1), blocks = (K + 31) / 32;
+  const float* inv;
+  if (!vector_of(a[1], "inv_smooth", x->device(), K, "inv_smooth: fp32 [K] on x's device", &inv)) return nullptr;
+  const CallStream stream(a[4]);
+  if (!stream.ok()) return nullptr;
+  const at::TensorOptions bytes = x->options().dtype(at::kByte);
+  at::Tensor codes, scales;
+  if (!output_of(a[2], "codes", {M, 16 * blocks}, bytes, "codes: uint8 [M, 16 * ceil(K / 32)]", &codes)) return nullptr;
+  if (a[3] == Py_None) scales = at::empty({M, (blocks + 15) / 16 * 16}, bytes).narrow(1, 0, blocks);
+  else if (!output_of(a[3], "scales", {M, blocks}, bytes, "scales: uint8 [M, ceil(K / 32)]", &scales)) return nullptr;
+  const lcd_status st = without_gil([&] {
+    return lcd_mx_quantize(x->data_ptr(), type, M, K, row_stride(*x), inv, static_cast<uint8_t*>(codes.data_ptr()), row_stride(codes),
+                           static_cast<uint8_t*>(scales.data_ptr()), row_stride(scales, 16), stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return pack({returned(stream, a[2], codes), returned(stream, a[3], scales)});
+  END_HANDLE_TH_ERRORS
+}
+
+// (codes, scales, K or None, out, dtype, stream) -> out or a status
+PyObject* mx_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 6)) return nullptr;
+  const at::Tensor *codes = tensor_of(a[0], "codes"), *scales = codes ? tensor_of(a[1], "scales") : nullptr;
+  if (!scales || !require(codes->is_cuda() && codes->dim() == 2 && codes->size(1) % 16 == 0, "codes: CUDA uint8 [M, 16 * blocks]")) return nullptr;
+  const int64_t M = codes->size(0), blocks = codes->size(1) / 16;
+  const int64_t K = a[2] == Py_None ? 32 * blocks : PyLong_AsLongLong(a[2]);
+  at::ScalarType type;
+  if (PyErr_Occurred() || !dtype_of(a[4], &type)) return nullptr;
+  if (!require(bytes_of(*codes, codes->device(), M, 16 * blocks) && bytes_of(*scales, codes->device(), M, blocks),
+               "codes: uint8 [M, 16 * blocks], scales: uint8 [M, blocks], on one device") ||
+      !require(K >= 1 && (K + 31) / 32 == blocks, "K: 32 * blocks, or up to 31 less"))
+    return nullptr;
+  const c10::cuda::CUDAGuard on(codes->device());
+  const CallStream stream(a[5]);
+  if (!stream.ok()) return nullptr;
+  at::Tensor out;
+  if (a[3] != Py_None) {
+    const at::Tensor* t = tensor_of(a[3], "out");
+    if (!t) return nullptr;
+    type = t->scalar_type();
+  }
+  lcd_dtype kind;
+  if (!require(type_of(type, &kind), "out: fp32, fp16 or bf16") ||
+      !output_of(a[3], "out", {M, K}, codes->options().dtype(type), "out: [M, K] with unit column stride on the codes' device", &out))
+    return nullptr;
+  const lcd_status st = without_gil([&] {
+    return lcd_mx_dequantize(static_cast<const uint8_t*>(codes->data_ptr()), row_stride(*codes), static_cast<const uint8_t*>(scales->data_ptr()),
+                             row_stride(*scales, 16), M, K, out.data_ptr(), kind, row_stride(out), stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return returned(stream, a[3], out);
+  END_HANDLE_TH_ERRORS
+}
+
+// (fused, w_codes, w_scales, x or x_codes, inv_smooth or x_scales, y, dtype, workspace, status_word, stream) -> y or a status
+PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 10)) return nullptr;
+  const bool fused = PyObject_IsTrue(a[0]) == 1;
+  const at::Tensor *wc = tensor_of(a[1], "w_codes"), *ws = wc ? tensor_of(a[2], "w_scales") : nullptr;
+  const at::Tensor* x = ws ? tensor_of(a[3], fused ? "x" : "x_codes") : nullptr;
+  if (!x || !require(wc->is_cuda() && wc->dim() == 2 && wc->size(1) % 16 == 0, "w_codes: CUDA uint8 [N, 16 * blocks]")) return nullptr;
+  const at::Device device = wc->device();
+  const int64_t N = wc->size(0), blocks = wc->size(1) / 16;
+  if (!require(bytes_of(*wc, device, N, 16 * blocks) && bytes_of(*ws, device, N, blocks),
+               "w_codes: uint8 [N, 16 * blocks], w_scales: uint8 [N, blocks], on one device") ||
+      !require(x->dim() == 2 && x->device() == device, fused ? "x: [M, K] on the weights' device" : "x_codes: [M, 16 * blocks] on the weights' device"))
+    return nullptr;
+  const int64_t M = x->size(0);
+  int64_t K = 32 * blocks;
+  lcd_dtype x_type = LCD_DTYPE_F32, y_type;
+  const at::Tensor* xs = nullptr;
+  const float* inv = nullptr;
+  if (fused) {
+    K = x->size(1);
+    if (!require(dense(*x, &x_type), "x: CUDA fp32, fp16 or bf16 [M, K] with unit column stride") ||
+        !require((K + 31) / 32 == blocks, "x: [M, K], K being 32 * blocks of the weights, or up to 31 less") ||
+        !vector_of(a[4], "inv_smooth", device, K, "inv_smooth: fp32 [K] on x's device", &inv))
+      return nullptr;
+  } else {
+    xs = tensor_of(a[4], "x_scales");
+    if (!xs || !require(bytes_of(*x, device, M, 16 * blocks) && bytes_of(*xs, device, M, blocks),
+                        "x_codes: uint8 [M, 16 * blocks], x_scales: uint8 [M, blocks], blocks as the weights'"))
+      return nullptr;
+  }
+  at::ScalarType type;
+  if (!dtype_of(a[6], &type)) return nullptr;
+  int32_t* word;
+  if (!status_word_of(a[8], device, &word)) return nullptr;
+  const c10::cuda::CUDAGuard on(device);
+  const CallStream stream(a[9]);
+  if (!stream.ok()) return nullptr;
+  if (a[5] != Py_None) {
+    const at::Tensor* t = tensor_of(a[5], "y");
+    if (!t) return nullptr;
+    type = t->scalar_type();
+  }
+  at::Tensor y, space;
+  if (!require(type_of(type, &y_type), "y: fp32, fp16 or bf16") ||
+      !output_of(a[5], "y", {M, N}, x->options().dtype(type), "y: [M, N] with unit column stride on the weights' device", &y))
+    return nullptr;
+  size_t have = 0;
+  if (fused) {
+    size_t need = 0;
+    const lcd_status sized = lcd_mx_linear_fused_workspace_bytes(M, K, &need);
+    if (sized != LCD_OK) return PyLong_FromLong((long)sized);
+    if (a[7] == Py_None) {
+      space = at::empty({(int64_t)need}, x->options().dtype(at::kByte));
+    } else {
+      const at::Tensor* t = tensor_of(a[7], "workspace");
+      if (!t || !require(t->device() == device && t->is_contiguous(), "workspace: contiguous, on the weights' device")) return nullptr;
+      space = *t;
+    }
+    have = (size_t)space.numel() * space.element_size();
+  }
+  const lcd_status st = without_gil([&] {
+    const uint8_t *c = static_cast<const uint8_t*>(wc->data_ptr()), *s = static_cast<const uint8_t*>(ws->data_ptr());
+    const int64_t ldc = row_stride(*wc), lds = row_stride(*ws, 16), ldy = row_stride(y);
+    if (fused)
+      return lcd_mx_linear_fused(c, ldc, s, lds, N, K, x->data_ptr(), x_type, row_stride(*x), inv, M, y.data_ptr(), y_type, ldy,
+                                 space.data_ptr(), have, word, stream.raw());
+    return lcd_mx_linear(c, ldc, s, lds, N, K, static_cast<const uint8_t*>(x->data_ptr()), row_stride(*x),
+                         static_cast<const uint8_t*>(xs->data_ptr()), row_stride(*xs, 16), M, y.data_ptr(), y_type, ldy, word, stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return returned(stream, a[5], y);
+  END_HANDLE_TH_ERRORS
+}
+
+// (logits, teacher_idx, teacher_logits, temperature, teacher_lse, weight, stats in or None, loss, stats out (None, True: a new one),
+//  dlogits (None, True: a new one), stream) -> (loss, stats or None, dlogits or None), or a status.  With stats in: the gradient alone.
+PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 11)) return nullptr;
+  const at::Tensor *z = tensor_of(a[0], "logits"), *idx = z ? tensor_of(a[1], "teacher_idx") : nullptr;
+  const at::Tensor* top = idx ? tensor_of(a[2], "teacher_logits") : nullptr;
+  lcd_dtype type, top_type;
+  if (!top || !require(dense(*z, &type), "logits: CUDA fp32, fp16 or bf16 [T, V] with unit column stride")) return nullptr;
+  const at::Device device = z->device();
+  const int64_t T = z->size(0), V = z->size(1);
+  if (!require(dense(*top, &top_type) && top->device() == device && top->size(0) == T,
+               "teacher_logits: fp32, fp16 or bf16 [T, k] with unit column stride on the logits' device"))
+    return nullptr;
+  const int64_t k = top->size(1);
+  if (!require(idx->device() == device && (idx->scalar_type() == at::kInt || idx->scalar_type() == at::kLong) && idx->dim() == 2 &&
+                   idx->size(0) == T && idx->size(1) == k && (idx->stride(1) == 1 || k == 1),
+               "teacher_idx: int32 or int64 [T, k] with unit column stride on the logits' device"))
+    return nullptr;
+  const double tau = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred()) return nullptr;
+  const float *lse, *weight;
+  if (!vector_of(a[4], "teacher_lse", device, T, "teacher_lse: fp32 [T] on the logits' device", &lse) ||
+      !vector_of(a[5], "weight", device, T, "weight: fp32 [T] on the logits' device", &weight))
+    return nullptr;
+  const bool grad_only = a[6] != Py_None;
+  const c10::cuda::CUDAGuard on(device);
+  const CallStream stream(a[10]);
+  if (!stream.ok()) return nullptr;
+  const at::TensorOptions f32 = z->options().dtype(at::kFloat);
+  PyObject *want_stats = a[8] == Py_True ? Py_None : a[8], *want_grad = a[9] == Py_True ? Py_None : a[9];   // None from here: a new one
+  const bool has_stats = grad_only || a[8] != Py_None, has_grad = a[9] != Py_None;
+  at::Tensor loss, stats, d;
+  if (!grad_only && (!output_of(a[7], "loss", {T}, f32, "loss: fp32 [T] on the logits' device", &loss) ||
+                     !require(loss.is_contiguous(), "loss: contiguous")))
+    return nullptr;
+  if (has_stats && (!output_of(grad_only ? a[6] : want_stats, "stats", {T, 2}, f32, "stats: fp32 [T, 2] on the logits' device", &stats) ||
+                    !require(stats.is_contiguous(), "stats: contiguous")))
+    return nullptr;
+  if (has_grad && !output_of(want_grad, "dlogits", {T, V}, z->options(), "dlogits: as the logits, with unit column stride", &d)) return nullptr;
+  const lcd_status st = without_gil([&] {
+    void* grads = has_grad ? d.data_ptr() : nullptr;
+    const int64_t ldd = has_grad ? row_stride(d) : 0;
+    float* state = has_stats ? static_cast<float*>(stats.data_ptr()) : nullptr;
+    const int width = idx->scalar_type() == at::kInt ? 4 : 8;
+    if (grad_only)
+      return lcd_distill_grad(z->data_ptr(), type, T, V, row_stride(*z), idx->data_ptr(), width, row_stride(*idx), top->data_ptr(), top_type,
+                              row_stride(*top), k, (float)tau, lse, weight, state, grads, ldd, stream.raw());
+    return lcd_distill_loss(z->data_ptr(), type, T, V, row_stride(*z), idx->data_ptr(), width, row_stride(*idx), top->data_ptr(), top_type,
+                            row_stride(*top), k, (float)tau, lse, weight, static_cast<float*>(loss.data_ptr()), state, grads, ldd, stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return pack({grad_only ? Py_NewRef(Py_None) : returned(stream, a[7], loss),
+               grad_only || !has_stats ? Py_NewRef(Py_None) : returned(stream, want_stats, stats),
+               has_grad ? returned(stream, want_grad, d) : Py_NewRef(Py_None)});
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef kMethods[] = {
     {"smooth_quantize_act", reinterpret_cast<PyCFunction>(smooth_quantize_act), METH_FASTCALL, nullptr},
     {"lut_linear", reinterpret_cast<PyCFunction>(lut_linear), METH_FASTCALL, nullptr},
@@ -319,6 +592,10 @@ PyMethodDef kMethods[] = {
     {"linear_batch", reinterpret_cast<PyCFunction>(linear_batch), METH_FASTCALL, nullptr},
     {"reclassify", reinterpret_cast<PyCFunction>(reclassify), METH_FASTCALL, nullptr},
     {"smoothing_search", reinterpret_cast<PyCFunction>(smoothing_search), METH_FASTCALL, nullptr},
+    {"mx_quantize", reinterpret_cast<PyCFunction>(mx_quantize), METH_FASTCALL, nullptr},
+    {"mx_dequantize", reinterpret_cast<PyCFunction>(mx_dequantize), METH_FASTCALL, nullptr},
+    {"mx_linear", reinterpret_cast<PyCFunction>(mx_linear), METH_FASTCALL, nullptr},
+    {"distill", reinterpret_cast<PyCFunction>(distill), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,264 @@
+"""Distillation from a teacher's top logits on the GPU against the float64 oracle, to the bounds derived at check()."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_12038_b200 as lcd
+from oracle import train_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"fp32": torch.float32, "fp16": torch.float16, "bf16": torch.bfloat16}
+
+
+def make(seed, T, V, k, type="fp32", absent=0.0, wide=False, spread=2.5):
+    rng = np.random.default_rng(seed)
+    z = torch.from_numpy(rng.normal(size=(T, V)) * spread).to(TYPES[type]).cuda()
+    teacher = z.double().cpu().numpy() + rng.normal(size=(T, V))
+    idx = np.argsort(-teacher, axis=1)[:, :k]
+    top = torch.from_numpy(np.take_along_axis(teacher, idx, axis=1)).half().cuda()
+    idx = np.where(rng.random(idx.shape) < absent, -1, idx)
+    return z, torch.from_numpy(idx.astype(np.int64 if wide else np.int32)).cuda(), top, teacher
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def check(z, idx, top, tau=1.0, lse=None, weight=None, loss=None, grad=None, stats=None):
+    """With R the largest |value - maximum| / temperature that weighs (beyond 90 a term is below 2^-126 of the largest), an exponent's
+    argument is off by 3 roundings of at most R, the exponential itself by 2^-22 (2 ulp for expf), a sum of n terms by (terms that one
+    thread adds + the levels above) roundings: e = (3 R + V / 256 + 64) * 2^-24 + 2^-21 bounds the relative error of every p, q and of
+    a sum of them; the logarithms add 3 roundings of their own size, at most R + log V.  Gradients are rounded to their type."""
+    ref, dref, sref, size, dsize = O.distill(host(z), idx.cpu().numpy(), host(top), tau, None if lse is None else host(lse),
+                                             None if weight is None else host(weight))
+    zz = host(z)
+    with np.errstate(invalid="ignore"):
+        R = min(90.0, np.nan_to_num(np.abs(zz - zz.max(axis=1, keepdims=True)), posinf=0).max() / tau)
+        R = max(R, min(90.0, np.nan_to_num(np.ptp(host(top)), posinf=90, neginf=90) / tau))
+    e = (3 * R + z.shape[1] / 256 + 64) * 2.0 ** -24 + 2.0 ** -21
+    if loss is not None:
+        bound = (2 * e + 6 * (R + np.log(z.shape[1])) * 2.0 ** -24) * size + 1e-38
+        assert (np.abs(host(loss) - ref) <= bound).all(), (np.abs(host(loss) - ref) / bound).max()
+    if stats is not None:
+        got = host(stats)
+        out = np.isnan(sref)
+        assert np.array_equal(np.isnan(got), out) and np.array_equal(got[:, 0][~out[:, 0]], sref[:, 0][~out[:, 0]])
+        assert (np.abs(got - sref)[~out] <= 2 * e * np.abs(sref[~out])).all()
+    if grad is not None:
+        g = host(grad)
+        step = torch.finfo(grad.dtype).eps / 2
+        tiny = 2.0 ** -25 if grad.dtype == torch.float16 else 1e-38
+        bound = 3 * e * dsize + step * np.abs(dref) * (1 + 1e-3) + tiny
+        assert grad.dtype == z.dtype and (np.abs(g - dref) <= bound).all(), (np.abs(g - dref) / bound).max()
+
+
+def same(a, b):
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
+
+
+def every_path(z, idx, top, **teacher):
+    """Loss alone, loss with gradient and stats, gradient alone: one answer."""
+    loss = lcd.distill_loss(z, idx, top, **teacher)
+    both, stats, grad = lcd.distill_loss(z, idx, top, want_stats=True, want_grad=True, **teacher)
+    assert same(loss, both)
+    again = lcd.distill_grad(z, idx, top, stats, **teacher)
+    assert same(grad, again)
+    return loss, grad, stats
+
+
+SHAPES = [(1, 1, 1), (1, 7, 3), (3, 100, 5), (2, 1000, 64), (5, 4097, 17), (1, 32000, 100), (40, 2003, 1), (3, 50021, 128), (2, 128000, 20),
+          (300, 517, 33), (1, 260001, 1024)]
+
+
+@pytest.mark.parametrize("type", sorted(TYPES))
+@pytest.mark.parametrize("T,V,k", SHAPES)
+def test_loss_and_gradient(T, V, k, type):
+    z, idx, top, _ = make(T + V, T, V, k, type)
+    loss, grad, stats = every_path(z, idx, top)
+    check(z, idx, top, loss=loss, grad=grad, stats=stats)
+
+
+@pytest.mark.parametrize("tau", [2.0, 0.7])
+@pytest.mark.parametrize("whole,wide", [(False, True), (True, False)])
+@pytest.mark.parametrize("T,V,k", [(6, 1001, 40), (700, 333, 12), (3, 40000, 300)])
+def test_temperature_weights_and_absent_entries(T, V, k, tau, whole, wide):
+    z, idx, top, teacher = make(V, T, V, k, "bf16", absent=0.3, wide=wide)
+    rng = np.random.default_rng(T)
+    weight = torch.from_numpy((rng.random(T) * (rng.random(T) < 0.7)).astype(np.float32)).cuda()
+    lse = torch.from_numpy(np.log(np.exp(teacher / tau).sum(axis=1)).astype(np.float32)).cuda() if whole else None
+    args = dict(temperature=tau, teacher_lse=lse, weight=weight)
+    loss, grad, stats = every_path(z, idx, top, **args)
+    check(z, idx, top, tau, lse, weight, loss, grad, stats)
+    out = weight == 0
+    assert not loss[out].any() and not grad[out].any()
+
+
+def test_an_index_twice_and_entries_out_of_range():
+    z, idx, top, _ = make(1, 4, 500, 9)
+    idx[0, 1:5] = idx[0, 0]
+    idx[1, 3], idx[1, 4] = 500, 2 ** 31 - 1
+    idx[2, :] = -1
+    idx[3, 1:] = -5
+    loss, grad, stats = every_path(z, idx, top)
+    check(z, idx, top, loss=loss, grad=grad, stats=stats)
+    assert loss[2] == 0 and not grad[2].any()
+    far = idx.long()
+    far[1, 3] = 2 ** 40 + 7                       # an int64 index whose low half would be in range
+    assert torch.equal(lcd.distill_loss(z, far, top), loss)
+
+
+@pytest.mark.parametrize("type", sorted(TYPES))
+def test_masked_logits(type):
+    z, idx, top, _ = make(2, 6, 777, 8, type)
+    low = torch.finfo(z.dtype).min
+    z[0, 100:700] = -float("inf")
+    z[1, 50:] = low
+    z[2] = low                                       # a uniform row, however low
+    top[3, 2:] = -float("inf")
+    top[4] = torch.finfo(top.dtype).min
+    idx[0], idx[1] = torch.arange(8), torch.arange(10, 18)
+    loss, grad, stats = every_path(z, idx, top)
+    assert torch.isfinite(loss).all() and torch.isfinite(grad).all()
+    check(z[2:], idx[2:], top[2:], loss=loss[2:], grad=grad[2:], stats=stats[2:])
+    # masked columns: those that are left make the row
+    for row, left in ((0, torch.cat([torch.arange(100), torch.arange(700, 777)])), (1, torch.arange(50))):
+        short = z[row:row + 1, left.cuda()].contiguous()
+        check(short, idx[row:row + 1], top[row:row + 1], loss=loss[row:row + 1], grad=grad[row:row + 1, left.cuda()].contiguous())
+        rest = torch.ones(777, dtype=torch.bool)
+        rest[left] = False
+        assert not grad[row, rest.cuda()].any()
+    # the student rules out what the teacher holds likely
+    z[5, idx[5, 0].long()] = -float("inf")
+    loss, grad, _ = every_path(z, idx, top)
+    assert loss[5] == float("inf") and torch.isfinite(grad[5]).all() and grad[5, idx[5, 0].long()] < 0
+
+
+def test_nan_and_infinity_stay_in_their_row():
+    z, idx, top, _ = make(3, 6, 5000, 8)
+    clean = every_path(z, idx, top)
+    z[1, 4321] = float("nan")
+    z[2, 17] = float("inf")
+    z[3] = -float("inf")
+    top[4, 3] = float("nan")
+    loss, grad, _ = every_path(z, idx, top)
+    for row in range(6):
+        if row in (0, 5):
+            assert loss[row] == clean[0][row] and torch.equal(grad[row], clean[1][row])
+        else:
+            assert loss[row].isnan() and grad[row].isnan().any()
+    # a left-out row's logits are not looked at
+    weight = torch.tensor([1.0, 0, 0, 0, 0, 1.0], device="cuda")
+    loss, grad, stats = every_path(z, idx, top, weight=weight)
+    assert not loss[1:5].any() and not grad[1:5].any() and stats[1:5].isnan().all()
+
+
+@pytest.mark.parametrize("type", sorted(TYPES))
+@pytest.mark.parametrize("V,pitch,dpitch", [(501, 3, 0), (2048, 8, 5), (33000, 1, 2)])
+def test_rows_at_any_alignment_and_in_place(type, V, pitch, dpitch):
+    z, idx, top, _ = make(V, 5, V, 12, type)
+    room = torch.full((5, V + pitch), float("nan"), dtype=z.dtype, device="cuda")
+    room[:, :V] = z
+    out = torch.full((5, V + dpitch), 7.0, dtype=z.dtype, device="cuda")
+    loss, grad = lcd.distill_loss(room[:, :V], idx, top, dlogits=out[:, :V])
+    check(z, idx, top, loss=loss, grad=grad)
+    assert (out[:, V:] == 7).all()
+    stats = lcd.distill_loss(room[:, :V], idx, top, want_stats=True)[1]
+    both = room.clone()
+    same = lcd.distill_loss(both[:, :V], idx, top, dlogits=both[:, :V])
+    assert torch.equal(same[0], loss) and torch.equal(both[:, :V], grad) and both[:, V:].isnan().all()
+    both = room.clone()
+    lcd.distill_grad(both[:, :V], idx, top, stats, dlogits=both[:, :V])
+    assert torch.equal(both[:, :V], grad) and both[:, V:].isnan().all()
+
+
+def test_large_logits_keep_their_differences():
+    # z - log s would lose the differences of logits near 10^4
+    z, idx, top, _ = make(4, 3, 3000, 10)
+    shifted = (z * 64).round() / 64 + 8192
+    loss, grad, stats = every_path(shifted, idx, top)
+    check(shifted, idx, top, loss=loss, grad=grad, stats=stats)
+
+
+def test_the_gradient_with_weights_known_later():
+    z, idx, top, _ = make(6, 9, 1234, 10)
+    loss, stats = lcd.distill_loss(z, idx, top, want_stats=True)
+    weight = torch.rand(9, device="cuda")
+    weight[3] = 0
+    check(z, idx, top, weight=weight, grad=lcd.distill_grad(z, idx, top, stats, weight=weight))
+
+
+@pytest.mark.parametrize("T", [1, 64])
+def test_gradient_by_differences(T):
+    # the loss in float64 of the package's own gradient step: dL = grad . dz to second order
+    z, idx, top, _ = make(T, T, 600, 10)
+    _, grad = lcd.distill_loss(z, idx, top, want_grad=True, temperature=1.5)
+    rng = np.random.default_rng(1)
+    d = rng.normal(size=(T, 600)) * 1e-4
+    up, down = (O.distill(host(z) + s * d, idx.cpu().numpy(), host(top), 1.5)[0] for s in (1, -1))
+    want = (host(grad) * d).sum(axis=1)
+    # the third-order term is below |d|^3 per logit, and the gradient's own error as in check()
+    assert np.allclose((up - down) / 2, want, rtol=0, atol=600 * (4e-4) ** 3 + 1e-5 * np.abs(host(grad) * d).sum(axis=1).max())
+
+
+def test_results_do_not_change_and_graphs_replay():
+    z, idx, top, _ = make(8, 37, 30011, 50, "bf16")
+    loss, grad, _ = every_path(z, idx, top)
+    for _ in range(3):
+        l2, g2, _ = every_path(z, idx, top)
+        assert torch.equal(loss, l2) and torch.equal(grad, g2)
+    buf, out_l, out_g = torch.zeros_like(z), torch.zeros_like(loss), torch.zeros_like(grad)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        lcd.distill_loss(buf, idx, top, loss=out_l, dlogits=out_g)
+    for k in range(2):
+        buf.copy_(z if k else z.flip(0))
+        g.replay()
+        torch.cuda.synchronize()
+    assert torch.equal(out_l, loss) and torch.equal(out_g, grad)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    l3 = lcd.distill_loss(z, idx, top, stream=side)
+    side.synchronize()
+    assert torch.equal(l3, loss)
+
+
+def test_a_student_with_a_microscaled_head():
+    # the pieces as a training loop uses them: head quantised, logits, loss and gradient against the teacher's stored top logits,
+    # the master weights' gradient, an update, quantised again
+    rng = np.random.default_rng(12)
+    T, H, V, k = 48, 256, 1500, 20
+    h = torch.from_numpy(rng.normal(size=(T, H)).astype(np.float32)).cuda().bfloat16()
+    master = torch.from_numpy((rng.normal(size=(V, H)) * 0.1).astype(np.float32)).cuda()
+    top, idx = (h.float() @ (master + 0.05 * torch.randn(V, H, device="cuda")).t()).topk(k, dim=1)
+    for _ in range(2):
+        codes, scales = lcd.mx_quantize(master)
+        y = lcd.mx_linear_fused(codes, scales, h)
+        xc, xs = lcd.mx_quantize(h)
+        seen, weights = lcd.mx_dequantize(xc, xs), lcd.mx_dequantize(codes, scales)
+        ref = seen.double() @ weights.double().t()
+        assert (y - ref).abs().max() <= 16 * 2.0 ** -22 * (seen.abs().double() @ weights.abs().double().t()).max()
+        loss, dy = lcd.distill_loss(y, idx, top, want_grad=True)
+        check(y, idx, top, loss=loss, grad=dy)
+        dw = dy.t() @ seen
+        # the gradient of the head's weights against differences, in float64, along a random direction
+        d = torch.from_numpy(rng.normal(size=(V, H))).cuda() * 1e-4
+        up, down = (O.distill(host(seen.double() @ (weights.double() + s * d).t()), idx.cpu().numpy(), host(top))[0].sum() for s in (1, -1))
+        want = (dw.double() * d).sum().item()
+        assert abs((up - down) / 2 - want) <= 1e-3 * (dw.double() * d).abs().sum().item()
+        master -= 0.1 * dw
+
+
+def test_updates_of_a_clustered_head():
+    # the same loss on the logits of a clustered layer; its weights' gradient becomes the updates that reclassify takes
+    from synth import gen
+    L = gen.random_case(seed=5, N=300, K=256, bits=2, M=16)
+    w = lcd.PackedWeights(lcd.pack_weights(L.idx, L.codebook, 2))
+    a, s = lcd.smooth_quantize_act(torch.from_numpy(L.x).cuda(), torch.from_numpy(L.inv_s).cuda())
+    y = lcd.lut_linear(w, a, s)
+    top, idx = (y + torch.randn_like(y)).topk(12, dim=1)
+    loss, dy = lcd.distill_loss(y, idx, top, want_grad=True)
+    check(y, idx, top, loss=loss, grad=dy)
+    x = torch.from_numpy(L.x).cuda().float() * torch.from_numpy(L.inv_s).cuda()
+    new, _, counts = lcd.reclassify(torch.from_numpy(L.idx).cuda(), torch.from_numpy(np.sort(L.codebook, axis=1)).cuda(), -0.01 * (dy.t() @ x))
+    assert new.shape == (300, 256) and (counts.sum(dim=1) == 256).all()
