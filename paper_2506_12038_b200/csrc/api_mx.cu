@@ -63,8 +63,8 @@ extern "C" lcd_status lcd_mx_linear(const uint8_t* w_codes, int64_t ldwc, const 
   if (!mx_rows(w_codes, ldwc, w_scales, ldws, N, K) || !mx_rows(x_codes, ldxc, x_scales, ldxs, M, K) ||
       !dense_rows(y, y_type, M, N, ldy) || !aligned(status_word_dev, 4))
     return LCD_ERR_INVALID_ARG;
-  return launch_mx_linear({w_codes, w_scales, x_codes, x_scales, ldwc, ldws, ldxc, ldxs, N, K, M, y, y_type, ldy}, status_word_dev,
-                          cuda_stream);
+  return launch_mx_linear({w_codes, w_scales, x_codes, x_scales, ldwc, ldws, ldxc, ldxs, N, K, M, y, y_type, ldy}, false,
+                          status_word_dev, cuda_stream);
 }
 
 extern "C" lcd_status lcd_mx_linear_fused_workspace_bytes(int64_t M, int64_t K, size_t* bytes) {
@@ -89,7 +89,8 @@ extern "C" lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, 
   uint8_t* scales = codes + M * ldc;
   const lcd_status st = launch_mx_quantize(x, x_type, M, K, ldx, inv_smooth, codes, ldc, scales, lds, cuda_stream);
   if (st != LCD_OK) return st;
-  return launch_mx_linear({w_codes, w_scales, codes, scales, ldwc, ldws, ldc, lds, N, K, M, y, y_type, ldy}, status_word_dev, cuda_stream);
+  return launch_mx_linear({w_codes, w_scales, codes, scales, ldwc, ldws, ldc, lds, N, K, M, y, y_type, ldy}, true, status_word_dev,
+                          cuda_stream);
 }
 
 extern "C" lcd_status lcd_distill_loss(const void* logits, lcd_dtype type, int64_t T, int64_t V, int64_t ldz, const void* teacher_idx,

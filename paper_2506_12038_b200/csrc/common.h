@@ -112,7 +112,8 @@ lcd_status launch_mx_quantize(const void* x, lcd_dtype type, int64_t M, int64_t 
                               int64_t ldc, uint8_t* scales, int64_t lds, void* stream);
 lcd_status launch_mx_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K, void* out,
                                 lcd_dtype type, int64_t ldo, void* stream);
-lcd_status launch_mx_linear(const MxProduct& p, int32_t* status_word, void* stream);
+// x_just_written: x's codes come of the kernel launched directly before, which lets this one start early (launch_mx_quantize).
+lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* status_word, void* stream);
 struct Distillation {
   const void* logits;
   lcd_dtype type;

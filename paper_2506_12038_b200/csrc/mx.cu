@@ -21,6 +21,7 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kMxThreads)
 mx_quantize_kernel(const T* __restrict__ x, int64_t K, int64_t ldx, const float* __restrict__ inv, uint8_t* __restrict__ codes,
                    int64_t ldc, uint8_t* __restrict__ scales, int64_t lds, uint32_t units, uint32_t chunks) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the product of the same call may set itself up
   const int64_t row = blockIdx.x / chunks;
   const uint32_t unit = (blockIdx.x % chunks) * kMxThreads + threadIdx.x;
   float t[8];

@@ -1,6 +1,21 @@
 // The product of two microscaled 4-bit matrices (lcd_mx_linear): y[m][n] = sum over blocks b of 2^(sx + sw) times the sum over the
-// block's 32 columns of the elements' products.  Products of elements are multiples of 1/4 up to 36, so a block's sum is exact in
-// binary32 in any order; the blocks are added in binary32.
+// block's 32 columns of the elements' products.  The tensor cores take this format as it is: tcgen05.mma kind::mxf4 multiplies
+// 128 weight rows by BN tokens over 64 columns, codes from shared memory, scales from tensor memory, sums in fp32.  So there
+// is no decoding, and few tokens (weights from HBM) and many (tensor pipe) are one kernel with token tiles of different width.
+//
+// Roles (11 warps):
+//   warp 0      TMA producer of codes: stages of 256 columns, 128-byte swizzle
+//   warp 10     TMA producer of scales: 512 columns (16 bytes a row) at a time
+//   warps 2-5   scales to tensor memory: the unit reads row r's four scale bytes of 128 columns at lane r % 32, column r / 32, in
+//               every quarter of the lanes, so each of the four warps stores all rows' words into its own quarter
+//   warp 1      owns tensor memory; one elected lane issues the MMAs
+//   warps 6-9   epilogue: tensor memory -> y, coalesced along the weight rows
+// Where tiles are few the columns of a tile are cut among the CTAs of a cluster; their partial sums meet in distributed shared
+// memory and are added in the order of the ranks, so results do not depend on timing.
+// Every wait is bounded (status word LCD_ERR_TIMEOUT on expiry; then every role leaves its loop, copies and MMAs in flight are
+// drained, tensor memory is released).
+#include <cuda.h>
+
 #include <type_traits>
 
 #include "common.h"
@@ -11,57 +26,460 @@ namespace lcd {
 
 namespace {
 
-constexpr int kPlainThreads = 128;
+constexpr int kRows = 128;                      // weight rows of a tile = MMA M
+constexpr int kStageK = 256;                    // columns of a stage: 128 bytes of codes a row
+constexpr int kAStage = kRows * kStageK / 2;    // 16 KB
+constexpr int kScaleSlots = 3;
+constexpr int kMmaWarp = 1, kFirstEpiWarp = 6, kScaleCopyWarp = 10;
+constexpr int kThreads = 32 * 11;
+constexpr unsigned long long kWaitNs = 2000000000ull;
 
-// A warp per output; a lane takes every 32nd block of its row pair.
-template <typename T>
-__global__ void __launch_bounds__(kPlainThreads)
-mx_linear_kernel(const uint8_t* __restrict__ wc, int64_t ldwc, const uint8_t* __restrict__ ws, int64_t ldws, int64_t N, int64_t K,
-                 const uint8_t* __restrict__ xc, int64_t ldxc, const uint8_t* __restrict__ xs, int64_t ldxs, T* __restrict__ y, int64_t ldy) {
-  const int64_t n = (int64_t)blockIdx.x * (kPlainThreads / 32) + threadIdx.x / 32, m = blockIdx.y;
-  if (n >= N) return;
-  const int64_t blocks = (K + kMxBlock - 1) / kMxBlock;
-  float sum = 0.0f;
-  for (int64_t b = threadIdx.x & 31; b < blocks; b += 32) {
-    const uint4 w = *reinterpret_cast<const uint4*>(wc + n * ldwc + b * 16), x = *reinterpret_cast<const uint4*>(xc + m * ldxc + b * 16);
-    const uint32_t wv[4] = {w.x, w.y, w.z, w.w}, xv[4] = {x.x, x.y, x.z, x.w};
-    float part = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float a[8], c[8];
-      mx_elements8(wv[i], a);
-      mx_elements8(xv[i], c);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) part += a[j] * c[j];
+template <int BN>
+struct Cfg {
+  static constexpr int kBStage = BN * kStageK / 2;
+  static constexpr int kStages = BN <= 32 ? 5 : BN == 256 ? 4 : BN == 128 ? 6 : 4;
+  static constexpr int kScaleBytes = (kRows + BN) * 16;
+  static constexpr int kSfbCols = BN / 32 < 4 ? 4 : BN / 32;             // tensor-memory columns of the tokens' scales, per 128 columns
+  static constexpr int kSfCols = 4 * (4 + kSfbCols);                     // of a scale slot: 512 columns
+  static constexpr int kDBuffers = 2 * BN + 2 * kSfCols <= 512 ? 2 : 1;  // accumulators
+  static constexpr int kUsed = kDBuffers * BN + 2 * kSfCols;
+  static constexpr int kTmemCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+  static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 256;
+  static constexpr int kPerSm = BN <= 64 ? 2 : 1;
+  static_assert(kUsed <= kTmemCols && kTmemCols * kPerSm <= 512, "tensor memory");
+  static_assert(kSmem <= 227 * 1024 && kPerSm * (kSmem + 1024) <= 228 * 1024, "shared memory");
+  static_assert(BN * 512 <= kStages * (kAStage + kBStage), "partial sums lie in the stages");
+};
+
+struct Args {
+  void* y;
+  long long ldy;
+  int y_type, M, N, n_ks, n_ss, n_tiles_m, n_tiles, early;
+  int32_t* status;
+};
+
+__device__ __forceinline__ unsigned long long timer_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ bool elect() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred P;\nelect.sync _|P, 0xffffffff;\nselp.u32 %0, 1, 0, P;\n}" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Bounded: false when another role gave up or after kWaitNs, when the flag is raised for everybody.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (bar_try(bar, parity)) return true;
+  const unsigned long long t0 = timer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (bar_try(bar, parity)) return true;
+    if ((it & 255u) == 0) {
+      if (*abort_flag) return false;
+      if (timer_ns() - t0 > kWaitNs) { *abort_flag = 1; return false; }
     }
-    sum += part * mx_scale_value(ws[n * ldws + b]) * mx_scale_value(xs[m * ldxs + b]);
   }
-  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if ((threadIdx.x & 31) == 0) y[m * ldy + n] = from_f32<T>(sum);
+}
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+  const unsigned long long t0 = timer_ns();
+  for (uint32_t it = 1; !bar_try(bar, parity); ++it)
+    if ((it & 255u) == 0 && timer_ns() - t0 > kWaitNs) return;
+}
+__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, int x, int row, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(bar) : "memory");
+}
+// Shared-memory matrix descriptor: K-major, 128-byte swizzle, 8-row groups 1024 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(1024u >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Instruction descriptor of kind::mxf4: both operands E2M1 (1), K-major, M = 128, N = n, UE8M0 scales; `pair`: the bytes of a scale
+// word that the instruction's two blocks use, 0 and 1 or 2 and 3.
+__host__ __device__ constexpr uint32_t instr_desc(int n, int pair) {
+  return (uint32_t)(2 * pair) << 4 | 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | 1u << 23 | (uint32_t)(kRows >> 4) << 24 |
+         (uint32_t)(2 * pair) << 29;
+}
+__device__ __forceinline__ void mma_mx(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void store_y(const Args& P, long long m, int n, float v) {
+  const long long at = m * P.ldy + n;
+  if (P.y_type == LCD_DTYPE_F32) static_cast<float*>(P.y)[at] = v;
+  else if (P.y_type == LCD_DTYPE_F16) static_cast<__half*>(P.y)[at] = __float2half_rn(v);
+  else static_cast<__nv_bfloat16*>(P.y)[at] = __float2bfloat16_rn(v);
 }
 
-template <typename T>
-lcd_status launch_typed(const MxProduct& p, cudaStream_t s) {
-  for (int64_t m = 0; m < p.M; m += 65535) {
-    const int64_t rows = p.M - m < 65535 ? p.M - m : 65535;
-    mx_linear_kernel<T><<<dim3((unsigned)((p.N + kPlainThreads / 32 - 1) / (kPlainThreads / 32)), (unsigned)rows), kPlainThreads, 0, s>>>(
-        p.w_codes, p.ldwc, p.w_scales, p.ldws, p.N, p.K, p.x_codes + m * p.ldxc, p.ldxc, p.x_scales + m * p.ldxs, p.ldxs,
-        static_cast<T*>(p.y) + m * p.ldy, p.ldy);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+// Scales of 512 columns of `groups` groups of 32 rows, [row][16 bytes] in shared memory, to COLS tensor-memory columns per 128
+// columns: word j of row 32 g + lane goes to column j * COLS + g.
+template <int GROUPS, int COLS>
+__device__ __forceinline__ void scales_to_tmem(const uint8_t* rows, uint32_t taddr, int lane) {
+  uint32_t v[4 * COLS];
+#pragma unroll
+  for (int i = 0; i < 4 * COLS; ++i) v[i] = 0u;
+#pragma unroll
+  for (int g = 0; g < (GROUPS < 1 ? 1 : GROUPS); ++g) {
+    if (GROUPS >= 1 || lane < 16) {             // a tile of 16 tokens fills half a group
+      const uint4 w = *reinterpret_cast<const uint4*>(rows + (32 * g + lane) * 16);
+      v[g] = w.x;
+      v[COLS + g] = w.y;
+      v[2 * COLS + g] = w.z;
+      v[3 * COLS + g] = w.w;
+    }
   }
+#pragma unroll
+  for (int i = 0; i < 4 * COLS; i += 16) tmem_st16(taddr + i, v + i);
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kThreads, Cfg<BN>::kPerSm)
+mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                 const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const Args P) {
+  using C = Cfg<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw_addr = (uint32_t)__cvta_generic_to_shared(smem_raw);
+  const uint32_t base = (raw_addr + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - raw_addr);
+  constexpr uint32_t kScaleAt = C::kStages * (kAStage + C::kBStage), kBarAt = kScaleAt + kScaleSlots * C::kScaleBytes;
+  const uint32_t a_base = base, b_base = base + C::kStages * kAStage, s_base = base + kScaleAt, bars = base + kBarAt;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (C::kStages + s); };
+  auto sc_full = [&](int s) { return bars + 8u * (2 * C::kStages + s); };
+  auto sc_empty = [&](int s) { return bars + 8u * (2 * C::kStages + kScaleSlots + s); };
+  constexpr int kB0 = 2 * C::kStages + 2 * kScaleSlots;
+  auto ts_full = [&](int b) { return bars + 8u * (kB0 + b); };
+  auto ts_empty = [&](int b) { return bars + 8u * (kB0 + 2 + b); };
+  auto d_full = [&](int b) { return bars + 8u * (kB0 + 4 + b); };
+  auto d_empty = [&](int b) { return bars + 8u * (kB0 + 6 + b); };
+  const uint32_t drain = bars + 8u * (kB0 + 8);
+  static_assert(8 * (kB0 + 9) + 8 <= 256, "barriers");
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + kBarAt + 8 * (kB0 + 9));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+  uint32_t rank, split;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+  const int ss0 = (int)((long long)P.n_ss * rank / split), ss1 = (int)((long long)P.n_ss * (rank + 1) / split);   // this CTA's columns
+  const int ks0 = 2 * ss0, ks1 = min(P.n_ks, 2 * ss1);
+  const int tile0 = blockIdx.x / split, tile_step = gridDim.x / split;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      bar_init(full(s), 1);
+      bar_init(empty(s), 1);
+    }
+    for (int s = 0; s < kScaleSlots; ++s) {
+      bar_init(sc_full(s), 1);
+      bar_init(sc_empty(s), 4);
+    }
+    for (int b = 0; b < 2; ++b) {
+      bar_init(ts_full(b), 4);
+      bar_init(ts_empty(b), 1);
+      bar_init(d_full(b), 1);
+      bar_init(d_empty(b), 4);
+    }
+    bar_init(drain, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"((uint32_t)__cvta_generic_to_shared(tmem_holder)), "r"((uint32_t)C::kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *tmem_holder;
+  const uint32_t sf_tmem = tmem + C::kDBuffers * BN;
+
+  if (warp == 0 || warp == kScaleCopyWarp) {
+    // ---------------------------------------------------------------- TMA producers.  With P.early the kernel before this one wrote x's
+    // codes and nothing else that is read here, so the weights' first copies do not wait for it.
+    const bool codes = warp == 0;
+    if (elect()) {
+      const int from = codes ? ks0 : ss0, to = codes ? ks1 : ss1, slots = codes ? C::kStages : kScaleSlots;
+      const uint32_t bytes = codes ? kAStage + C::kBStage : C::kScaleBytes;
+      auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
+      auto copy_w = [&](int s, int k, int row) {
+        if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full(s));
+        else copy_tile(s_base + s * C::kScaleBytes, &map_ws, k * 16, row, sc_full(s));
+      };
+      auto copy_x = [&](int s, int k, int row) {
+        if (codes) copy_tile(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), row, full(s));
+        else copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, row, sc_full(s));
+      };
+      const int ahead = P.early && tile0 < P.n_tiles ? min(slots, to - from) : 0;
+      for (int i = 0; i < ahead; ++i) {
+        bar_expect_tx(full_of(i), bytes);
+        copy_w(i, from + i, tile0 / P.n_tiles_m * kRows);
+      }
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      int it = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step) {
+        const int n0 = tile / P.n_tiles_m * kRows, m0 = tile % P.n_tiles_m * BN;
+        for (int k = from; k < to; ++k, ++it) {
+          const int s = it % slots;
+          if (it >= ahead) {
+            ok = bar_wait(codes ? empty(s) : sc_empty(s), ((it / slots) & 1u) ^ 1u, abort_flag);
+            if (!ok) break;
+            bar_expect_tx(full_of(s), bytes);
+            copy_w(s, k, n0);
+          }
+          copy_x(s, k, m0);
+        }
+      }
+      // nothing this thread issued may be in flight when the CTA exits
+      const int back = min(it, slots);
+      for (int i = 1; i <= back; ++i) bar_drain(full_of((it - i) % slots), ((it - i) / slots) & 1u);
+    }
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    if (elect()) {
+      constexpr uint32_t idesc[2] = {instr_desc(BN, 0), instr_desc(BN, 1)};
+      const uint64_t a_desc0 = smem_desc(a_base), b_desc0 = smem_desc(b_base);
+      uint32_t it = 0, sit = 0, tl = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+        const uint32_t buf = tl % C::kDBuffers;
+        ok = bar_wait(d_empty(buf), ((tl / C::kDBuffers) & 1u) ^ 1u, abort_flag);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + buf * BN;
+        for (int ss = ss0; ss < ss1 && ok; ++ss, ++sit) {
+          const uint32_t sb = sit & 1u;
+          ok = bar_wait(ts_full(sb), (sit >> 1) & 1u, abort_flag);
+          if (!ok) break;
+          const uint32_t sfa = sf_tmem + sb * C::kSfCols, sfb = sfa + 16;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (2 * ss + h >= P.n_ks) break;
+            const uint32_t slot = it % C::kStages;
+            ok = bar_wait(full(slot), (it / C::kStages) & 1u, abort_flag);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint64_t ad = a_desc0 + (uint64_t)(slot * kAStage >> 4), bd = b_desc0 + (uint64_t)(slot * C::kBStage >> 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              mma_mx(d, ad + 2 * i, bd + 2 * i, idesc[i & 1], sfa + (2 * h + i / 2) * 4, sfb + (2 * h + i / 2) * C::kSfbCols,
+                     (uint32_t)(ss != ss0 || h != 0 || i != 0));
+            mma_commit(empty(slot));
+            ++it;
+          }
+          mma_commit(ts_empty(sb));
+        }
+        if (ok) mma_commit(d_full(buf));
+      }
+      // every MMA must have finished before tensor memory is released
+      mma_commit(drain);
+      bar_drain(drain, 0);
+    }
+    __syncwarp();
+  } else if (warp < kFirstEpiWarp) {
+    // ---------------------------------------------------------------- scales to tensor memory
+    const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16;
+    uint32_t sit = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step)
+      for (int ss = ss0; ss < ss1; ++ss, ++sit) {
+        const uint32_t slot = sit % kScaleSlots, sb = sit & 1u;
+        ok = __all_sync(0xffffffffu, bar_wait(sc_full(slot), (sit / kScaleSlots) & 1u, abort_flag) &&
+                                         bar_wait(ts_empty(sb), ((sit >> 1) & 1u) ^ 1u, abort_flag));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint8_t* rows = gen + kScaleAt + slot * C::kScaleBytes;
+        const uint32_t at = sf_tmem + sb * C::kSfCols + quarter;
+        scales_to_tmem<4, 4>(rows, at, lane);
+        scales_to_tmem<BN / 32, C::kSfbCols>(rows + kRows * 16, at + 16, lane);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          bar_arrive(sc_empty(slot));
+          bar_arrive(ts_full(sb));
+        }
+        __syncwarp();
+      }
+  } else {
+    // ---------------------------------------------------------------- epilogue
+    const int quad = warp & 3;
+    const uint32_t quarter = (uint32_t)(32 * quad) << 16;
+    uint32_t tl = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+      const uint32_t buf = tl % C::kDBuffers;
+      const int n = tile / P.n_tiles_m * kRows + 32 * quad + lane, m0 = tile % P.n_tiles_m * BN;
+      const int tokens = min(BN, P.M - m0);
+      ok = __all_sync(0xffffffffu, bar_wait(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      for (int c = 0; c < tokens; c += 16) {
+        uint32_t v[16];
+        tmem_ld16(tmem + quarter + buf * BN + c, v);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        if (split > 1) {            // every copy into the stages has landed and been read: they hold the partial sums
+          float* part = reinterpret_cast<float*>(gen) + (size_t)c * kRows + 32 * quad + lane;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) part[j * kRows] = __uint_as_float(v[j]);
+        } else if (n < P.N) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (c + j < tokens) store_y(P, m0 + c + j, n, __uint_as_float(v[j]));
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) bar_arrive(d_empty(buf));
+      __syncwarp();
+    }
+  }
+  if (split > 1) {
+    // Token t of the tile is added up by rank t % split.
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    const int n0 = tile0 / P.n_tiles_m * kRows, m0 = tile0 % P.n_tiles_m * BN;
+    const int tokens = min(BN, P.M - m0), row = threadIdx.x % kRows;
+    if (threadIdx.x < 2 * kRows && n0 + row < P.N) {
+      for (int t = rank + split * (threadIdx.x / kRows); t < tokens; t += 2 * split) {
+        float sum = 0.0f;
+        for (uint32_t r = 0; r < split; ++r) {
+          uint32_t at;
+          float v;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + (uint32_t)(t * kRows + row) * 4u), "r"(r));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+          sum = r ? sum + v : v;
+        }
+        store_y(P, m0 + t, n0 + row, sum);
+      }
+    }
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::kTmemCols) : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
+}
+
+bool encode_rows(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t rows, int64_t ld, int box_bytes, int box_rows, bool swizzled) {
+  const EncodeTiledFn encode = encode_tiled();
+  const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
+  const cuuint32_t box[2] = {(cuuint32_t)box_bytes, (cuuint32_t)box_rows}, one[2] = {1, 1};
+  return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(p), dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN>
+lcd_status launch_width(const MxProduct& p, bool early, int32_t* status, cudaStream_t s) {
+  using C = Cfg<BN>;
+  auto kern = mx_linear_kernel<BN>;
+  static PerDeviceFlag attr_set;
+  int dev;
+  if (attr_set.first(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+    attr_set.done(dev);
+  }
+  const int64_t blocks = (p.K + kMxBlock - 1) / kMxBlock;
+  const int64_t n_tiles_m = (p.M + BN - 1) / BN, tiles = n_tiles_m * ((p.N + kRows - 1) / kRows);
+  if (tiles > 0x7fffffff) return LCD_ERR_UNSUPPORTED;
+  CUtensorMap w, x, ws, xs;
+  if (!encode_rows(&w, p.w_codes, blocks * 16, p.N, p.ldwc, kStageK / 2, kRows, true) ||
+      !encode_rows(&x, p.x_codes, blocks * 16, p.M, p.ldxc, kStageK / 2, BN, true) ||
+      !encode_rows(&ws, p.w_scales, blocks, p.N, p.ldws, 16, kRows, false) ||
+      !encode_rows(&xs, p.x_scales, blocks, p.M, p.ldxs, 16, BN, false)) {
+    set_cuda_error((int)cudaErrorInvalidValue);
+    return LCD_ERR_CUDA;
+  }
+  Args a = {};
+  a.y = p.y;
+  a.ldy = p.ldy;
+  a.y_type = (int)p.y_type;
+  a.M = (int)p.M;
+  a.N = (int)p.N;
+  a.n_ks = (int)((blocks * kMxBlock + kStageK - 1) / kStageK);
+  a.n_ss = (a.n_ks + 1) / 2;
+  a.n_tiles_m = (int)n_tiles_m;
+  a.n_tiles = (int)tiles;
+  a.early = early;
+  a.status = status;
+  const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
+  int64_t split = tiles < room ? room / tiles : 1;
+  split = split > 8 ? 8 : split;
+  split = split > a.n_ss ? a.n_ss : split;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (early) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (split > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)split;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = (unsigned)n;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, w, x, ws, xs, a);
+  if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
 
 }  // namespace
 
-lcd_status launch_mx_linear(const MxProduct& p, int32_t*, void* stream) {
+lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* status_word, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  switch (p.y_type) {
-    case LCD_DTYPE_F32: return launch_typed<float>(p, s);
-    case LCD_DTYPE_F16: return launch_typed<__half>(p, s);
-    default: return launch_typed<__nv_bfloat16>(p, s);
-  }
+  if (p.M <= 16) return launch_width<16>(p, x_just_written, status_word, s);
+  if (p.M <= 32) return launch_width<32>(p, x_just_written, status_word, s);
+  if (p.M <= 64) return launch_width<64>(p, x_just_written, status_word, s);
+  if (p.M <= 128) return launch_width<128>(p, x_just_written, status_word, s);
+  return launch_width<256>(p, x_just_written, status_word, s);
 }
 
 }  // namespace lcd
