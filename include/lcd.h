@@ -469,7 +469,7 @@ lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, const uint8
  *     q = softmax(z / temperature) over the V logits;     P = sum_j p_j;
  *     loss = weight * sum over p_j != 0 of p_j * (log p_j - log q_idx_j);
  *     dlogits_v = weight / temperature * (P * q_v - sum over j with idx_j = v of p_j).
- * A token whose weight is 0 is left out: its logits are not read, loss and gradient are 0.  A token without entries has
+ * A token whose weight is 0 is left out: loss and gradient are 0 whatever its logits are.  A token without entries has
  * loss 0 and gradient 0.  Logits of -infinity have probability 0.  The same index twice counts twice.
  *   logits:         device, [T][ldz], ldz >= V;
  *   teacher_idx:    device, int32 or int64 (idx_bytes 4 or 8) [T][ldi];   teacher_logits: device, [T][ldt];  1 <= k <= 1024
@@ -479,7 +479,7 @@ lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, const uint8
  *   stats:          device out, fp32 [T][2], or NULL: the row's largest logit m and sum_v exp((z_v - m) / temperature), for
  *                   lcd_distill_grad;
  *   dlogits:        device out, the logits' type, [T][ldd], or NULL.  May be logits itself (with ldd = ldz).
- * Sums run in a fixed order: results are reproducible from run to run.
+ * Sums run in a fixed order: results are reproducible from run to run (which order may go by whether dlogits is given).
  * -------------------------------------------------------------------------------------------- */
 lcd_status lcd_distill_loss(const void* logits, lcd_dtype type, int64_t T, int64_t V, int64_t ldz, const void* teacher_idx,
                             int idx_bytes, int64_t ldi, const void* teacher_logits, lcd_dtype teacher_type, int64_t ldt, int64_t k,
