@@ -2,8 +2,10 @@
 // Per block of 32 columns: A = max |t|, e = floor(log2 A) - 2, element = round(t * 2^-e).  Scaling by a power of two is exact,
 // so the rounding to 4 bits is the only one after t itself and results are the same bit for bit everywhere.
 //
-// Four lanes share a block and eight consecutive columns are a lane's: one 16-byte load of 16-bit values (two of fp32), the
-// block's maximum by two shuffles, four code bytes out, so that loads and stores of a warp are contiguous.
+// Four lanes share a block and eight consecutive columns, a unit, are a lane's: one 16-byte load of 16-bit values (two of fp32), the
+// block's maximum by two shuffles, four code bytes out, so that loads and stores of a warp are contiguous.  What bounds both
+// kernels is memory: a thread has its unit of kRowsEach rows in flight at once (one of few rows).  Rows that do not start on 16 bytes go
+// through shared memory, element by element and contiguous in memory.
 #include <type_traits>
 
 #include "common.h"
@@ -15,71 +17,129 @@ namespace lcd {
 namespace {
 
 constexpr int kMxThreads = 256;
+constexpr int kRowsEach = 4;
 
-// VEC: rows of x and the factors start on 16 bytes.  A unit is a lane's eight columns; chunks = CTAs a row.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kMxThreads)
-mx_quantize_kernel(const T* __restrict__ x, int64_t K, int64_t ldx, const float* __restrict__ inv, uint8_t* __restrict__ codes,
-                   int64_t ldc, uint8_t* __restrict__ scales, int64_t lds, uint32_t units, uint32_t chunks) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the product of the same call may set itself up
-  const int64_t row = blockIdx.x / chunks;
-  const uint32_t unit = (blockIdx.x % chunks) * kMxThreads + threadIdx.x;
-  float t[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) t[i] = 0.0f;
-  const int64_t k0 = (int64_t)unit * 8;
-  const T* p = x + row * ldx + k0;
-  if (VEC && k0 + 8 <= K) {
-    load8(p, t);
-    if (inv) {
-      float f[8];
-      load8(inv + k0, f);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t[i] = __fmul_rn(t[i], f[i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (k0 + i < K) t[i] = inv ? __fmul_rn(to_f32(p[i]), inv[k0 + i]) : to_f32(p[i]);
-  }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(t[i]) & 0x7fffffffu);
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-  if (unit >= units) return;
-  const uint32_t byte = mx_scale_byte(top);
-  uint32_t c = 0;
-  if (byte != 255u) {
-    const float m = mx_inverse_scale(byte);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = __fmul_rn(t[i], m);
-    c = mx_codes8(t);
-  }
-  *reinterpret_cast<uint32_t*>(codes + row * ldc + (int64_t)unit * 4) = c;
-  if ((unit & 3u) == 0) scales[row * lds + (unit >> 2)] = (uint8_t)byte;
+// The CTA's threads as (unit, row): blockDim.x units of blockDim.y rows.  A thread has unit blockIdx.y * blockDim.x + threadIdx.x of
+// EACH rows, blockDim.y apart.
+struct Place {
+  uint32_t unit;
+  int64_t row0;
+};
+template <int EACH>
+__device__ __forceinline__ Place place() {
+  return {blockIdx.y * blockDim.x + threadIdx.x, (int64_t)blockIdx.x * EACH * blockDim.y + threadIdx.y};
 }
 
-template <typename T, bool VEC>
+// VEC: rows of x and the factors start on 16 bytes.
+template <typename T, bool VEC, int EACH>
 __global__ void __launch_bounds__(kMxThreads)
-mx_dequantize_kernel(const uint8_t* __restrict__ codes, int64_t ldc, const uint8_t* __restrict__ scales, int64_t lds, int64_t K,
-                     T* __restrict__ out, int64_t ldo, uint32_t units, uint32_t chunks) {
-  const int64_t row = blockIdx.x / chunks;
-  const uint32_t unit = (blockIdx.x % chunks) * kMxThreads + threadIdx.x;
-  if (unit >= units) return;
-  float v[8];
-  mx_elements8(*reinterpret_cast<const uint32_t*>(codes + row * ldc + (int64_t)unit * 4), v);
-  const float s = mx_scale_value(scales[row * lds + (unit >> 2)]);
+mx_quantize_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ldx, const float* __restrict__ inv, uint8_t* __restrict__ codes,
+                   int64_t ldc, uint8_t* __restrict__ scales, int64_t lds, uint32_t units) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the product of the same call may set itself up
+  __shared__ T s_x[VEC ? 1 : kMxThreads * 8];
+  const Place at = place<EACH>();
+  const int64_t k0 = (int64_t)at.unit * 8;
+  float t[8], f[8];
+  const bool whole = VEC && k0 + 8 <= K;
+  Raw8<T> raw[EACH];
+  if (whole) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], s);
-  const int64_t k0 = (int64_t)unit * 8;
-  T* p = out + row * ldo + k0;
-  if (VEC && k0 + 8 <= K) {
-    store8(p, v);
-  } else {
+    for (int u = 0; u < EACH; ++u) raw[u] = load8(x + min(at.row0 + u * blockDim.y, M - 1) * ldx + k0);
+  }
+  if (inv) {
+    if (whole) {
+      values8(load8(inv + k0), f);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (k0 + i < K) p[i] = from_f32<T>(v[i]);
+      for (int i = 0; i < 8; ++i) f[i] = k0 + i < K ? inv[k0 + i] : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int64_t row = at.row0 + u * blockDim.y;
+    if (whole) {
+      values8(raw[u], t);
+    } else if (VEC) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = row < M && k0 + i < K ? to_f32(x[row * ldx + k0 + i]) : 0.0f;
+    } else {
+      const int n = blockDim.x * 8;
+      T* line = s_x + threadIdx.y * n;
+      const int64_t from = (int64_t)blockIdx.y * n;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t e = from + i * blockDim.x + threadIdx.x;
+        line[i * blockDim.x + threadIdx.x] = row < M && e < K ? x[row * ldx + e] : from_f32<T>(0.0f);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = to_f32(line[threadIdx.x * 8 + i]);
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (inv) t[i] = __fmul_rn(t[i], f[i]);
+      top = max(top, __float_as_uint(t[i]) & 0x7fffffffu);
+    }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    if (at.unit >= units || row >= M) continue;
+    const uint32_t byte = mx_scale_byte(top);
+    uint32_t c = 0;
+    if (byte != 255u) {
+      const float m = mx_inverse_scale(byte);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = __fmul_rn(t[i], m);
+      c = mx_codes8(t);
+    }
+    *reinterpret_cast<uint32_t*>(codes + row * ldc + (int64_t)at.unit * 4) = c;
+    if ((at.unit & 3u) == 0) scales[row * lds + (at.unit >> 2)] = (uint8_t)byte;
+  }
+}
+
+template <typename T, bool VEC, int EACH>
+__global__ void __launch_bounds__(kMxThreads)
+mx_dequantize_kernel(const uint8_t* __restrict__ codes, int64_t ldc, const uint8_t* __restrict__ scales, int64_t lds, int64_t M, int64_t K,
+                     T* __restrict__ out, int64_t ldo, uint32_t units) {
+  __shared__ T s_out[VEC ? 1 : kMxThreads * 8];
+  const Place at = place<EACH>();
+  const int64_t k0 = (int64_t)at.unit * 8;
+  uint32_t c[EACH], byte[EACH];
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int64_t row = at.row0 + u * blockDim.y;
+    const bool there = row < M && at.unit < units;
+    c[u] = there ? *reinterpret_cast<const uint32_t*>(codes + row * ldc + (int64_t)at.unit * 4) : 0u;
+    byte[u] = there ? scales[row * lds + (at.unit >> 2)] : 0u;
+  }
+#pragma unroll
+  for (int u = 0; u < EACH; ++u) {
+    const int64_t row = at.row0 + u * blockDim.y;
+    float v[8];
+    mx_elements8(c[u], v);
+    const float s = mx_scale_value(byte[u]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], s);
+    T* p = out + row * ldo + k0;
+    if (VEC && k0 + 8 <= K) {
+      if (row < M) store8(p, v);
+    } else if (VEC) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (row < M && k0 + i < K) p[i] = from_f32<T>(v[i]);
+    } else {
+      const int n = blockDim.x * 8;
+      T* line = s_out + threadIdx.y * n;
+      const int64_t from = (int64_t)blockIdx.y * n;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) line[threadIdx.x * 8 + i] = from_f32<T>(v[i]);
+      __syncthreads();
+      if (row < M)
+        for (int e = threadIdx.x; e < n; e += blockDim.x)
+          if (from + e < K) out[row * ldo + from + e] = line[e];
+    }
   }
 }
 
@@ -93,22 +153,43 @@ lcd_status launched() {
   return LCD_OK;
 }
 
+// CTAs as wide as a row, a warp at least, of as many rows as make up their threads.
+struct Shape {
+  dim3 grid, block;
+  bool each;           // kRowsEach rows a thread
+};
+Shape shape_of(int64_t rows, uint32_t units) {
+  uint32_t x = 32;
+  while (x < kMxThreads && x < units) x *= 2;
+  const uint32_t y = kMxThreads / x, columns = (units + x - 1) / x;
+  const bool each = (rows + y - 1) / y * columns >= 8 * (int64_t)current_sm_count();    // every SM full without
+  const int64_t per = each ? (int64_t)y * kRowsEach : y;
+  return {dim3((unsigned)((rows + per - 1) / per), columns), dim3(x, y), each};
+}
+
 template <typename T>
 lcd_status quantize_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc,
                          uint8_t* scales, int64_t lds, cudaStream_t s) {
-  const uint32_t units = (uint32_t)((K + kMxBlock - 1) / kMxBlock * 4), chunks = (units + kMxThreads - 1) / kMxThreads;
+  const uint32_t units = (uint32_t)((K + kMxBlock - 1) / kMxBlock * 4);
+  const Shape q = shape_of(M, units);
+  if (q.grid.y > 65535) return LCD_ERR_UNSUPPORTED;
   const bool vec = on16(x, ldx, sizeof(T), M) && (!inv || reinterpret_cast<uintptr_t>(inv) % 16 == 0);
-  auto kern = vec ? mx_quantize_kernel<T, true> : mx_quantize_kernel<T, false>;
-  kern<<<(unsigned)(M * chunks), kMxThreads, 0, s>>>(static_cast<const T*>(x), K, ldx, inv, codes, ldc, scales, lds, units, chunks);
+  auto kern = vec ? (q.each ? mx_quantize_kernel<T, true, kRowsEach> : mx_quantize_kernel<T, true, 1>)
+                  : (q.each ? mx_quantize_kernel<T, false, kRowsEach> : mx_quantize_kernel<T, false, 1>);
+  kern<<<q.grid, q.block, 0, s>>>(static_cast<const T*>(x), M, K, ldx, inv, codes, ldc, scales, lds, units);
   return launched();
 }
 
 template <typename T>
 lcd_status dequantize_rows(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K, void* out,
                            int64_t ldo, cudaStream_t s) {
-  const uint32_t units = (uint32_t)((K + 7) / 8), chunks = (units + kMxThreads - 1) / kMxThreads;
-  auto kern = on16(out, ldo, sizeof(T), M) ? mx_dequantize_kernel<T, true> : mx_dequantize_kernel<T, false>;
-  kern<<<(unsigned)(M * chunks), kMxThreads, 0, s>>>(codes, ldc, scales, lds, K, static_cast<T*>(out), ldo, units, chunks);
+  const uint32_t units = (uint32_t)((K + 7) / 8);
+  const Shape q = shape_of(M, units);
+  if (q.grid.y > 65535) return LCD_ERR_UNSUPPORTED;
+  const bool vec = on16(out, ldo, sizeof(T), M);
+  auto kern = vec ? (q.each ? mx_dequantize_kernel<T, true, kRowsEach> : mx_dequantize_kernel<T, true, 1>)
+                  : (q.each ? mx_dequantize_kernel<T, false, kRowsEach> : mx_dequantize_kernel<T, false, 1>);
+  kern<<<q.grid, q.block, 0, s>>>(codes, ldc, scales, lds, M, K, static_cast<T*>(out), ldo, units);
   return launched();
 }
 

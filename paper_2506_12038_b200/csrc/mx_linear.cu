@@ -30,6 +30,7 @@ constexpr int kRows = 128;                      // weight rows of a tile = MMA M
 constexpr int kStageK = 256;                    // columns of a stage: 128 bytes of codes a row
 constexpr int kAStage = kRows * kStageK / 2;    // 16 KB
 constexpr int kScaleSlots = 3;
+constexpr int kMostSplit = 8;                  // a cluster's CTAs
 constexpr int kMmaWarp = 1, kFirstEpiWarp = 6, kScaleCopyWarp = 10;
 constexpr int kThreads = 32 * 11;
 constexpr unsigned long long kWaitNs = 2000000000ull;
@@ -37,12 +38,13 @@ constexpr unsigned long long kWaitNs = 2000000000ull;
 template <int BN>
 struct Cfg {
   static constexpr int kBStage = BN * kStageK / 2;
-  static constexpr int kStages = BN <= 32 ? 5 : BN == 256 ? 4 : BN == 128 ? 6 : 4;
+  static constexpr int kStages = BN <= 32 ? 5 : BN == 256 ? 4 : BN == 192 ? 5 : BN == 128 ? 6 : 4;
   static constexpr int kScaleBytes = (kRows + BN) * 16;
-  static constexpr int kSfbCols = BN / 32 < 4 ? 4 : BN / 32;             // tensor-memory columns of the tokens' scales, per 128 columns
+  static constexpr int kSfbCols = (BN + 127) / 128 * 4;                   // tensor-memory columns of the tokens' scales, per 128 columns
   static constexpr int kSfCols = 4 * (4 + kSfbCols);                     // of a scale slot: 512 columns
   static constexpr int kDBuffers = 2 * BN + 2 * kSfCols <= 512 ? 2 : 1;  // accumulators
-  static constexpr int kUsed = kDBuffers * BN + 2 * kSfCols;
+  static constexpr int kSfSlots = 2;                                     // (four were no faster)
+  static constexpr int kUsed = kDBuffers * BN + kSfSlots * kSfCols;
   static constexpr int kTmemCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
   static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 256;
   static constexpr int kPerSm = BN <= 64 ? 2 : 1;
@@ -136,11 +138,12 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
         "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
       : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void store_y(const Args& P, long long m, int n, float v) {
-  const long long at = m * P.ldy + n;
-  if (P.y_type == LCD_DTYPE_F32) static_cast<float*>(P.y)[at] = v;
-  else if (P.y_type == LCD_DTYPE_F16) static_cast<__half*>(P.y)[at] = __float2half_rn(v);
-  else static_cast<__nv_bfloat16*>(P.y)[at] = __float2bfloat16_rn(v);
+// f(y as a pointer to its type): the type is looked at once, not for every output.
+template <typename F>
+__device__ __forceinline__ void by_type(const Args& P, F&& f) {
+  if (P.y_type == LCD_DTYPE_F32) f(static_cast<float*>(P.y));
+  else if (P.y_type == LCD_DTYPE_F16) f(static_cast<__half*>(P.y));
+  else f(static_cast<__nv_bfloat16*>(P.y));
 }
 
 // Scales of 512 columns of `groups` groups of 32 rows, [row][16 bytes] in shared memory, to COLS tensor-memory columns per 128
@@ -180,14 +183,14 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   auto empty = [&](int s) { return bars + 8u * (C::kStages + s); };
   auto sc_full = [&](int s) { return bars + 8u * (2 * C::kStages + s); };
   auto sc_empty = [&](int s) { return bars + 8u * (2 * C::kStages + kScaleSlots + s); };
-  constexpr int kB0 = 2 * C::kStages + 2 * kScaleSlots;
+  constexpr int kB0 = 2 * C::kStages + 2 * kScaleSlots, kB1 = kB0 + 2 * C::kSfSlots;
   auto ts_full = [&](int b) { return bars + 8u * (kB0 + b); };
-  auto ts_empty = [&](int b) { return bars + 8u * (kB0 + 2 + b); };
-  auto d_full = [&](int b) { return bars + 8u * (kB0 + 4 + b); };
-  auto d_empty = [&](int b) { return bars + 8u * (kB0 + 6 + b); };
-  const uint32_t drain = bars + 8u * (kB0 + 8);
-  static_assert(8 * (kB0 + 9) + 8 <= 256, "barriers");
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + kBarAt + 8 * (kB0 + 9));
+  auto ts_empty = [&](int b) { return bars + 8u * (kB0 + C::kSfSlots + b); };
+  auto d_full = [&](int b) { return bars + 8u * (kB1 + b); };
+  auto d_empty = [&](int b) { return bars + 8u * (kB1 + 2 + b); };
+  const uint32_t drain = bars + 8u * (kB1 + 4);
+  static_assert(8 * (kB1 + 5) + 8 <= 256, "barriers");
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + kBarAt + 8 * (kB1 + 5));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
   uint32_t rank, split;
@@ -206,9 +209,11 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       bar_init(sc_full(s), 1);
       bar_init(sc_empty(s), 4);
     }
-    for (int b = 0; b < 2; ++b) {
+    for (int b = 0; b < C::kSfSlots; ++b) {
       bar_init(ts_full(b), 4);
       bar_init(ts_empty(b), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
       bar_init(d_full(b), 1);
       bar_init(d_empty(b), 4);
     }
@@ -283,8 +288,8 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + buf * BN;
         for (int ss = ss0; ss < ss1 && ok; ++ss, ++sit) {
-          const uint32_t sb = sit & 1u;
-          ok = bar_wait(ts_full(sb), (sit >> 1) & 1u, abort_flag);
+          const uint32_t sb = sit % C::kSfSlots;
+          ok = bar_wait(ts_full(sb), (sit / C::kSfSlots) & 1u, abort_flag);
           if (!ok) break;
           const uint32_t sfa = sf_tmem + sb * C::kSfCols, sfb = sfa + 16;
 #pragma unroll
@@ -318,9 +323,9 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     bool ok = true;
     for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step)
       for (int ss = ss0; ss < ss1; ++ss, ++sit) {
-        const uint32_t slot = sit % kScaleSlots, sb = sit & 1u;
+        const uint32_t slot = sit % kScaleSlots, sb = sit % C::kSfSlots;
         ok = __all_sync(0xffffffffu, bar_wait(sc_full(slot), (sit / kScaleSlots) & 1u, abort_flag) &&
-                                         bar_wait(ts_empty(sb), ((sit >> 1) & 1u) ^ 1u, abort_flag));
+                                         bar_wait(ts_empty(sb), ((sit / C::kSfSlots) & 1u) ^ 1u, abort_flag));
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint8_t* rows = gen + kScaleAt + slot * C::kScaleBytes;
@@ -349,19 +354,63 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       ok = __all_sync(0xffffffffu, bar_wait(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (int c = 0; c < tokens; c += 16) {
-        uint32_t v[16];
-        tmem_ld16(tmem + quarter + buf * BN + c, v);
-        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        if (split > 1) {            // every copy into the stages has landed and been read: they hold the partial sums
-          float* part = reinterpret_cast<float*>(gen) + (size_t)c * kRows + 32 * quad + lane;
-#pragma unroll
-          for (int j = 0; j < 16; ++j) part[j * kRows] = __uint_as_float(v[j]);
-        } else if (n < P.N) {
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (c + j < tokens) store_y(P, m0 + c + j, n, __uint_as_float(v[j]));
+      // The next columns are on their way while these are stored.
+      const uint32_t from = tmem + quarter + buf * BN;
+      auto drain_tile = [&](auto&& store) {       // store(first token of the tile, 16 tokens' sums)
+        uint32_t v[16], w[16];
+        if (BN <= 64) {                           // (two CTAs an SM have no registers for it)
+#pragma unroll 1
+          for (int c = 0; c < tokens; c += 16) {
+            tmem_ld16(from + c, v);
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            store(c, v);
+          }
+          return;
         }
+        tmem_ld16(from, v);
+#pragma unroll 1
+        for (int c = 0;; c += 32) {
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (c + 16 < tokens) tmem_ld16(from + c + 16, w);
+          store(c, v);
+          if (c + 16 >= tokens) break;
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (c + 32 < tokens) tmem_ld16(from + c + 32, v);
+          store(c + 16, w);
+          if (c + 32 >= tokens) break;
+        }
+      };
+      if (split > 1) {            // every copy into the stages has landed and been read: they hold the partial sums
+        float* part = reinterpret_cast<float*>(gen) + 32 * quad + lane;
+        drain_tile([&](int c, const uint32_t (&v)[16]) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) part[(c + j) * kRows] = __uint_as_float(v[j]);
+        });
+      } else {
+        by_type(P, [&](auto* y) {
+          using T = std::remove_pointer_t<decltype(y)>;
+          T* at = y + (size_t)m0 * P.ldy + n;
+          const bool inside = n < P.N;
+          drain_tile([&](int c, const uint32_t (&v)[16]) {
+            // (the address is kept from being formed for all sixteen at once, which takes 32 registers)
+            if (!inside) return;
+            if (c + 16 <= tokens) {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                *at = from_f32<T>(__uint_as_float(v[j]));
+                at += P.ldy;
+                asm volatile("" : "+l"(at));
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                if (c + j < tokens) *at = from_f32<T>(__uint_as_float(v[j]));
+                at += P.ldy;
+                asm volatile("" : "+l"(at));
+              }
+            }
+          });
+        });
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -370,23 +419,39 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     }
   }
   if (split > 1) {
-    // Token t of the tile is added up by rank t % split.
+    // Token t of the tile is added up by rank t % split, a warp for 32 rows; the loads from all ranks are on their way together.
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
     const int n0 = tile0 / P.n_tiles_m * kRows, m0 = tile0 % P.n_tiles_m * BN;
-    const int tokens = min(BN, P.M - m0), row = threadIdx.x % kRows;
-    if (threadIdx.x < 2 * kRows && n0 + row < P.N) {
-      for (int t = rank + split * (threadIdx.x / kRows); t < tokens; t += 2 * split) {
-        float sum = 0.0f;
-        for (uint32_t r = 0; r < split; ++r) {
+    const int tokens = min(BN, P.M - m0);
+    constexpr int kBatch = BN == 16 ? 1 : 4;           // groups of 32 rows that a warp adds at a time
+    for (int item = warp;; item += kThreads / 32) {
+      const int t = rank + split * (item * kBatch / 4), row = item * kBatch % 4 * 32 + lane;
+      if (t >= tokens) break;
+      float v[kMostSplit][kBatch];
+#pragma unroll
+      for (int r = 0; r < kMostSplit; ++r) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) v[r][j] = 0.0f;
+        if (r < (int)split) {
           uint32_t at;
-          float v;
           asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + (uint32_t)(t * kRows + row) * 4u), "r"(r));
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-          sum = r ? sum + v : v;
+#pragma unroll
+          for (int j = 0; j < kBatch; ++j) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r][j]) : "r"(at + 128 * j) : "memory");
         }
-        store_y(P, m0 + t, n0 + row, sum);
       }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+#pragma unroll
+        for (int r = 1; r < kMostSplit; ++r) v[0][j] += v[r][j];
+      }
+      by_type(P, [&](auto* y) {
+        using T = std::remove_pointer_t<decltype(y)>;
+        T* to = y + (size_t)(m0 + t) * P.ldy + n0 + row;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+          if (n0 + row + 32 * j < P.N) to[32 * j] = from_f32<T>(v[0][j]);
+      });
     }
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -409,8 +474,39 @@ bool encode_rows(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t rows
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// How a product is cut: the width of the token tiles and the CTAs that share a tile's columns.
+struct Plan { int width, split; };
+
+// Estimated in microseconds, from products timed alone on B200: 0.31 to 0.39 a stage (bound by shared memory's bandwidth: operands are
+// written once and read by the tensor core), an epilogue that only the widest tile cannot overlap with the next one's columns, and for a
+// shared tile the cluster's barrier and 1 us a 64 tokens to add up.  512 x 5120 x 5120: 192 tokens 12.2, 256 13.9, 128 17.8; 2048 x
+// 13824 x 5120: 68 with 256, 75 with 192; 333 x 5003 x 5001 14.7 with 128, 20.5 with 256; 1 x 4096 x 4096: 8.6 / 7.1 / 6.0 / 7.2
+// with 1 / 2 / 4 / 8 CTAs a tile, the last being more than one an SM.
+Plan plan(int64_t M, int64_t N, int64_t n_ks) {
+  static constexpr struct { int width; double stage, epilogue; } kWidths[] = {
+      {16, 0.33, 0.1}, {32, 0.33, 0.2}, {64, 0.34, 0.4}, {128, 0.31, 0.4}, {192, 0.39, 0.2}, {256, 0.35, 2.9}};
+  const int64_t sms = current_sm_count(), n_ss = (n_ks + 1) / 2;
+  Plan best = {256, 1};
+  double least = 1e300;
+  for (const auto& w : kWidths) {
+    if (M > w.width && w.width < 128) continue;           // few tokens: one tile of them
+    const int64_t tiles = (M + w.width - 1) / w.width * ((N + kRows - 1) / kRows);
+    const int64_t waves = (tiles + sms - 1) / sms;
+    for (int s = 1; s <= kMostSplit && s <= n_ss && (s == 1 || tiles * s <= sms); ++s) {
+      if (s > 4 && (w.width >= 128 || tiles * s > sms / 2)) break;      // clusters of more than four do not fill the GPU
+      const double time = waves * (2 * w.stage * ((n_ss + s - 1) / s) + w.epilogue) + (s > 1 ? 2.0 + (M < w.width ? M : w.width) / (64.0 * s) : 0.0);
+      if (time < least) {
+        least = time;
+        best = {w.width, s};
+      }
+    }
+    if (M <= w.width && w.width < 128) break;
+  }
+  return best;
+}
+
 template <int BN>
-lcd_status launch_width(const MxProduct& p, bool early, int32_t* status, cudaStream_t s) {
+lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* status, cudaStream_t s) {
   using C = Cfg<BN>;
   auto kern = mx_linear_kernel<BN>;
   static PerDeviceFlag attr_set;
@@ -444,9 +540,6 @@ lcd_status launch_width(const MxProduct& p, bool early, int32_t* status, cudaStr
   a.early = early;
   a.status = status;
   const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
-  int64_t split = tiles < room ? room / tiles : 1;
-  split = split > 8 ? 8 : split;
-  split = split > a.n_ss ? a.n_ss : split;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room));
   cfg.blockDim = dim3(kThreads);
@@ -475,11 +568,15 @@ lcd_status launch_width(const MxProduct& p, bool early, int32_t* status, cudaStr
 
 lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* status_word, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (p.M <= 16) return launch_width<16>(p, x_just_written, status_word, s);
-  if (p.M <= 32) return launch_width<32>(p, x_just_written, status_word, s);
-  if (p.M <= 64) return launch_width<64>(p, x_just_written, status_word, s);
-  if (p.M <= 128) return launch_width<128>(p, x_just_written, status_word, s);
-  return launch_width<256>(p, x_just_written, status_word, s);
+  const Plan w = plan(p.M, p.N, ((p.K + kMxBlock - 1) / kMxBlock * kMxBlock + kStageK - 1) / kStageK);
+  switch (w.width) {
+    case 16: return launch_width<16>(p, w.split, x_just_written, status_word, s);
+    case 32: return launch_width<32>(p, w.split, x_just_written, status_word, s);
+    case 64: return launch_width<64>(p, w.split, x_just_written, status_word, s);
+    case 128: return launch_width<128>(p, w.split, x_just_written, status_word, s);
+    case 192: return launch_width<192>(p, w.split, x_just_written, status_word, s);
+    default: return launch_width<256>(p, w.split, x_just_written, status_word, s);
+  }
 }
 
 }  // namespace lcd
