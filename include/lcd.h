@@ -450,9 +450,9 @@ lcd_status lcd_mx_linear(const uint8_t* w_codes, int64_t ldwc, const uint8_t* w_
                          const uint8_t* x_codes, int64_t ldxc, const uint8_t* x_scales, int64_t ldxs, int64_t M, void* y,
                          lcd_dtype y_type, int64_t ldy, int32_t* status_word_dev, void* cuda_stream);
 
-/* lcd_mx_quantize of x and lcd_mx_linear in one call; y is the same bit for bit.  workspace: device scratch of
- * lcd_mx_linear_fused_workspace_bytes(M, K) bytes, 16-byte aligned, contents ignored; calls that may overlap on the device
- * need separate ones. */
+/* lcd_mx_quantize of x and lcd_mx_linear in one call (one launch for up to four tokens of ordinary rows); y is the same bit for bit.  workspace:
+ * device scratch of lcd_mx_linear_fused_workspace_bytes(M, K) bytes, 16-byte aligned, contents ignored (may be NULL when that size
+ * is 0); calls that may overlap on the device need separate ones. */
 lcd_status lcd_mx_linear_fused_workspace_bytes(int64_t M, int64_t K, size_t* bytes);
 
 lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, const uint8_t* w_scales, int64_t ldws, int64_t N, int64_t K,

@@ -67,7 +67,7 @@ def build_calls() -> None:
                sysconfig.get_paths()["include"], os.path.join(cuda, "include"), os.path.join(ROOT, "include")]
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", *(f"-I{d}" for d in include),
                            os.path.join(CSRC, "host_calls.cpp"), "-o", CALLS, f"-L{HERE}", "-l:" + os.path.basename(LIB),
-                           f"-L{os.path.join(torch_dir, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10",
+                           f"-L{os.path.join(torch_dir, 'lib')}", "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10_cuda", "-lc10",
                            "-Wl,-rpath,$ORIGIN"])
 
 

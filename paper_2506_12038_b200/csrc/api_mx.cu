@@ -69,7 +69,7 @@ extern "C" lcd_status lcd_mx_linear(const uint8_t* w_codes, int64_t ldwc, const 
 
 extern "C" lcd_status lcd_mx_linear_fused_workspace_bytes(int64_t M, int64_t K, size_t* bytes) {
   if (!bytes || M < 1 || M > kMostRows || K < 1 || K > kMostColumns) return LCD_ERR_INVALID_ARG;
-  *bytes = (size_t)M * (size_t)(16 * blocks_of(K) + on_16(blocks_of(K)));
+  *bytes = mx_linear_quantizes(M, K) ? 0 : (size_t)M * (size_t)(16 * blocks_of(K) + on_16(blocks_of(K)));
   return LCD_OK;
 }
 
@@ -83,7 +83,10 @@ extern "C" lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, 
       lcd_mx_linear_fused_workspace_bytes(M, K, &need) != LCD_OK)
     return LCD_ERR_INVALID_ARG;
   if (!countable(M, K)) return LCD_ERR_UNSUPPORTED;
-  if (!workspace || workspace_bytes < need) return LCD_ERR_BUFFER_TOO_SMALL;
+  if (need > 0 && (!workspace || workspace_bytes < need)) return LCD_ERR_BUFFER_TOO_SMALL;
+  if (mx_linear_quantizes(M, K))
+    return launch_mx_linear({w_codes, w_scales, nullptr, nullptr, ldwc, ldws, 0, 0, N, K, M, y, y_type, ldy, x, x_type, ldx, inv_smooth},
+                            false, status_word_dev, cuda_stream);
   const int64_t ldc = 16 * blocks_of(K), lds = on_16(blocks_of(K));
   uint8_t* codes = static_cast<uint8_t*>(workspace);
   uint8_t* scales = codes + M * ldc;

@@ -107,7 +107,13 @@ struct MxProduct {
   void* y;
   lcd_dtype y_type;
   int64_t ldy;
+  // x as it is in place of x_codes and x_scales, where mx_linear_quantizes(M, K)
+  const void* x = nullptr;
+  lcd_dtype x_type = LCD_DTYPE_F32;
+  int64_t ldx = 0;
+  const float* inv_smooth = nullptr;
 };
+bool mx_linear_quantizes(int64_t M, int64_t K);
 lcd_status launch_mx_quantize(const void* x, lcd_dtype type, int64_t M, int64_t K, int64_t ldx, const float* inv_smooth, uint8_t* codes,
                               int64_t ldc, uint8_t* scales, int64_t lds, void* stream);
 lcd_status launch_mx_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K, void* out,

@@ -7,6 +7,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <ATen/ops/zeros.h>
@@ -317,6 +318,10 @@ PyObject* smoothing_search(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // ---- microscaled 4-bit floating point and distillation.  These run on their first tensor's device, whichever is current, and
 // every tensor has to lie there.
+// A new tensor, without the dispatcher (0.5 us each, of a call of 5).
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, const at::Device& device) {
+  return at::detail::empty_cuda(shape, type, device, std::nullopt);
+}
 bool type_of(at::ScalarType t, lcd_dtype* out) {
   if (t == at::kFloat) *out = LCD_DTYPE_F32;
   else if (t == at::kHalf) *out = LCD_DTYPE_F16;
@@ -361,13 +366,14 @@ bool dtype_of(PyObject* o, at::ScalarType* out) {
   return require(type_of(*out, &t), "dtype: torch.float32, torch.float16 or torch.bfloat16");
 }
 // The given tensor of that shape, or a new one.
-bool output_of(PyObject* o, const char* what, at::IntArrayRef shape, const at::TensorOptions& options, const char* expected, at::Tensor* out) {
+bool output_of(PyObject* o, const char* what, at::IntArrayRef shape, at::ScalarType type, const at::Device& device, const char* expected,
+               at::Tensor* out) {
   if (o == Py_None) {
-    *out = at::empty(shape, options);
+    *out = fresh(shape, type, device);
     return true;
   }
   const at::Tensor* t = tensor_of(o, what);
-  if (!t || !require(t->device() == options.device() && t->scalar_type() == c10::typeMetaToScalarType(options.dtype()) && t->sizes() == shape &&
+  if (!t || !require(t->device() == device && t->scalar_type() == type && t->sizes() == shape &&
                          (t->dim() == 0 || t->stride(-1) == 1 || t->size(-1) == 1), expected))
     return false;
   *out = *t;
@@ -402,11 +408,10 @@ PyObject* mx_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!vector_of(a[1], "inv_smooth", x->device(), K, "inv_smooth: fp32 [K] on x's device", &inv)) return nullptr;
   const CallStream stream(a[4]);
   if (!stream.ok()) return nullptr;
-  const at::TensorOptions bytes = x->options().dtype(at::kByte);
   at::Tensor codes, scales;
-  if (!output_of(a[2], "codes", {M, 16 * blocks}, bytes, "codes: uint8 [M, 16 * ceil(K / 32)]", &codes)) return nullptr;
-  if (a[3] == Py_None) scales = at::empty({M, (blocks + 15) / 16 * 16}, bytes).narrow(1, 0, blocks);
-  else if (!output_of(a[3], "scales", {M, blocks}, bytes, "scales: uint8 [M, ceil(K / 32)]", &scales)) return nullptr;
+  if (!output_of(a[2], "codes", {M, 16 * blocks}, at::kByte, x->device(), "codes: uint8 [M, 16 * ceil(K / 32)]", &codes)) return nullptr;
+  if (a[3] == Py_None) scales = at::detail::empty_strided_cuda({M, blocks}, {(blocks + 15) / 16 * 16, 1}, at::kByte, x->device());
+  else if (!output_of(a[3], "scales", {M, blocks}, at::kByte, x->device(), "scales: uint8 [M, ceil(K / 32)]", &scales)) return nullptr;
   const lcd_status st = without_gil([&] {
     return lcd_mx_quantize(x->data_ptr(), type, M, K, row_stride(*x), inv, static_cast<uint8_t*>(codes.data_ptr()), row_stride(codes),
                            static_cast<uint8_t*>(scales.data_ptr()), row_stride(scales, 16), stream.raw());
@@ -441,7 +446,7 @@ PyObject* mx_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   lcd_dtype kind;
   if (!require(type_of(type, &kind), "out: fp32, fp16 or bf16") ||
-      !output_of(a[3], "out", {M, K}, codes->options().dtype(type), "out: [M, K] with unit column stride on the codes' device", &out))
+      !output_of(a[3], "out", {M, K}, type, codes->device(), "out: [M, K] with unit column stride on the codes' device", &out))
     return nullptr;
   const lcd_status st = without_gil([&] {
     return lcd_mx_dequantize(static_cast<const uint8_t*>(codes->data_ptr()), row_stride(*codes), static_cast<const uint8_t*>(scales->data_ptr()),
@@ -497,7 +502,7 @@ PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   at::Tensor y, space;
   if (!require(type_of(type, &y_type), "y: fp32, fp16 or bf16") ||
-      !output_of(a[5], "y", {M, N}, x->options().dtype(type), "y: [M, N] with unit column stride on the weights' device", &y))
+      !output_of(a[5], "y", {M, N}, type, device, "y: [M, N] with unit column stride on the weights' device", &y))
     return nullptr;
   size_t have = 0;
   if (fused) {
@@ -505,20 +510,20 @@ PyObject* mx_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const lcd_status sized = lcd_mx_linear_fused_workspace_bytes(M, K, &need);
     if (sized != LCD_OK) return PyLong_FromLong((long)sized);
     if (a[7] == Py_None) {
-      space = at::empty({(int64_t)need}, x->options().dtype(at::kByte));
+      if (need > 0) space = fresh({(int64_t)need}, at::kByte, device);
     } else {
       const at::Tensor* t = tensor_of(a[7], "workspace");
       if (!t || !require(t->device() == device && t->is_contiguous(), "workspace: contiguous, on the weights' device")) return nullptr;
       space = *t;
     }
-    have = (size_t)space.numel() * space.element_size();
+    have = space.defined() ? (size_t)space.numel() * space.element_size() : 0;
   }
   const lcd_status st = without_gil([&] {
     const uint8_t *c = static_cast<const uint8_t*>(wc->data_ptr()), *s = static_cast<const uint8_t*>(ws->data_ptr());
     const int64_t ldc = row_stride(*wc), lds = row_stride(*ws, 16), ldy = row_stride(y);
     if (fused)
       return lcd_mx_linear_fused(c, ldc, s, lds, N, K, x->data_ptr(), x_type, row_stride(*x), inv, M, y.data_ptr(), y_type, ldy,
-                                 space.data_ptr(), have, word, stream.raw());
+                                 have ? space.data_ptr() : nullptr, have, word, stream.raw());
     return lcd_mx_linear(c, ldc, s, lds, N, K, static_cast<const uint8_t*>(x->data_ptr()), row_stride(*x),
                          static_cast<const uint8_t*>(xs->data_ptr()), row_stride(*xs, 16), M, y.data_ptr(), y_type, ldy, word, stream.raw());
   });
@@ -556,17 +561,16 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const c10::cuda::CUDAGuard on(device);
   const CallStream stream(a[10]);
   if (!stream.ok()) return nullptr;
-  const at::TensorOptions f32 = z->options().dtype(at::kFloat);
   PyObject *want_stats = a[8] == Py_True ? Py_None : a[8], *want_grad = a[9] == Py_True ? Py_None : a[9];   // None from here: a new one
   const bool has_stats = grad_only || a[8] != Py_None, has_grad = a[9] != Py_None;
   at::Tensor loss, stats, d;
-  if (!grad_only && (!output_of(a[7], "loss", {T}, f32, "loss: fp32 [T] on the logits' device", &loss) ||
+  if (!grad_only && (!output_of(a[7], "loss", {T}, at::kFloat, device, "loss: fp32 [T] on the logits' device", &loss) ||
                      !require(loss.is_contiguous(), "loss: contiguous")))
     return nullptr;
-  if (has_stats && (!output_of(grad_only ? a[6] : want_stats, "stats", {T, 2}, f32, "stats: fp32 [T, 2] on the logits' device", &stats) ||
+  if (has_stats && (!output_of(grad_only ? a[6] : want_stats, "stats", {T, 2}, at::kFloat, device, "stats: fp32 [T, 2] on the logits' device", &stats) ||
                     !require(stats.is_contiguous(), "stats: contiguous")))
     return nullptr;
-  if (has_grad && !output_of(want_grad, "dlogits", {T, V}, z->options(), "dlogits: as the logits, with unit column stride", &d)) return nullptr;
+  if (has_grad && !output_of(want_grad, "dlogits", {T, V}, z->scalar_type(), device, "dlogits: as the logits, with unit column stride", &d)) return nullptr;
   const lcd_status st = without_gil([&] {
     void* grads = has_grad ? d.data_ptr() : nullptr;
     const int64_t ldd = has_grad ? row_stride(d) : 0;

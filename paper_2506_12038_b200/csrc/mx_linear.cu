@@ -9,7 +9,8 @@
 //   warps 2-5   scales to tensor memory: the unit reads row r's four scale bytes of 128 columns at lane r % 32, column r / 32, in
 //               every quarter of the lanes, so each of the four warps stores all rows' words into its own quarter
 //   warp 1      owns tensor memory; one elected lane issues the MMAs
-//   warps 6-9   epilogue: tensor memory -> y, coalesced along the weight rows
+//   warps 6-9   epilogue: tensor memory -> y, coalesced along the weight rows; up to four tokens come as they are, then these warps
+//               quantise them into the stages first
 // Where tiles are few the columns of a tile are cut among the CTAs of a cluster; their partial sums meet in distributed shared
 // memory and are added in the order of the ranks, so results do not depend on timing.
 // Every wait is bounded (status word LCD_ERR_TIMEOUT on expiry; then every role leaves its loop, copies and MMAs in flight are
@@ -31,6 +32,7 @@ constexpr int kStageK = 256;                    // columns of a stage: 128 bytes
 constexpr int kAStage = kRows * kStageK / 2;    // 16 KB
 constexpr int kScaleSlots = 3;
 constexpr int kMostSplit = 8;                  // a cluster's CTAs
+constexpr int kOwnTokens = 4;                  // tokens that the kernel quantises itself
 constexpr int kMmaWarp = 1, kFirstEpiWarp = 6, kScaleCopyWarp = 10;
 constexpr int kThreads = 32 * 11;
 constexpr unsigned long long kWaitNs = 2000000000ull;
@@ -58,6 +60,10 @@ struct Args {
   long long ldy;
   int y_type, M, N, n_ks, n_ss, n_tiles_m, n_tiles, early;
   int32_t* status;
+  const void* x;         // instances that quantise x themselves: its rows, their pitch, the factors and the columns
+  long long ldx;
+  const float* inv;
+  int K, x_wide;
 };
 
 __device__ __forceinline__ unsigned long long timer_ns() {
@@ -167,7 +173,24 @@ __device__ __forceinline__ void scales_to_tmem(const uint8_t* rows, uint32_t tad
   for (int i = 0; i < 4 * COLS; i += 16) tmem_st16(taddr + i, v + i);
 }
 
-template <int BN>
+// Eight columns of a token from k on, zeros beyond K.  `raw` holds them where they lie on 16 bytes inside the row.
+template <typename X>
+__device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8<X>& raw, float (&t)[8]) {
+  if (P.x_wide && k + 8 <= P.K) {
+    values8(raw, t);
+  } else {
+    const X* p = static_cast<const X*>(P.x) + m * P.ldx + k;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = k + i < P.K ? to_f32(p[i]) : 0.0f;
+  }
+}
+
+// X: the type of x where the kernel quantises its tokens itself (few tokens), void where codes and scales come ready.  Then the
+// epilogue warps, which wait for the sums, take the stages in turn: a CTA needs its own columns of x only and blocks are complete in
+// them, so it can be done in every CTA, and a launch is saved: 1 x 11008 x 4096 9.7 us, 10.8
+// with two launches, 1 x 4096 x 4096 5.9 and 6.1, and 5.4 us on the host in place of 8.1; from eight tokens on it takes longer than the
+// weights' copies (8 x 4096 x 4096 8.4 and 6.9).
+template <int BN, typename X>
 __global__ void __launch_bounds__(kThreads, Cfg<BN>::kPerSm)
 mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                  const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const Args P) {
@@ -199,14 +222,15 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   const int ss0 = (int)((long long)P.n_ss * rank / split), ss1 = (int)((long long)P.n_ss * (rank + 1) / split);   // this CTA's columns
   const int ks0 = 2 * ss0, ks1 = min(P.n_ks, 2 * ss1);
   const int tile0 = blockIdx.x / split, tile_step = gridDim.x / split;
+  constexpr bool kReady = std::is_same<X, void>::value;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
-      bar_init(full(s), 1);
+      bar_init(full(s), kReady ? 1 : 2);            // the copies' thread, and the warp that quantises
       bar_init(empty(s), 1);
     }
     for (int s = 0; s < kScaleSlots; ++s) {
-      bar_init(sc_full(s), 1);
+      bar_init(sc_full(s), kReady ? 1 : 3);         // the copies' thread, and a warp for either half
       bar_init(sc_empty(s), 4);
     }
     for (int b = 0; b < C::kSfSlots; ++b) {
@@ -239,7 +263,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const bool codes = warp == 0;
     if (elect()) {
       const int from = codes ? ks0 : ss0, to = codes ? ks1 : ss1, slots = codes ? C::kStages : kScaleSlots;
-      const uint32_t bytes = codes ? kAStage + C::kBStage : C::kScaleBytes;
+      const uint32_t bytes = codes ? kAStage + (kReady ? C::kBStage : 0) : kReady ? C::kScaleBytes : kRows * 16;
       auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
       auto copy_w = [&](int s, int k, int row) {
         if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full(s));
@@ -267,7 +291,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             bar_expect_tx(full_of(s), bytes);
             copy_w(s, k, n0);
           }
-          copy_x(s, k, m0);
+          if (kReady) copy_x(s, k, m0);
         }
       }
       // nothing this thread issued may be in flight when the CTA exits
@@ -348,6 +372,74 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     uint32_t tl = 0;
     bool ok = true;
     for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+      if constexpr (!kReady) {
+        // Stage i of the CTA's belongs to warp i % 4: a lane has eight columns, four lanes a block, of one token after the other.  The
+        // next stage's columns and factors are asked for when this one's have been taken.
+        const int m0 = tile % P.n_tiles_m * BN, tokens = min(kOwnTokens, P.M - m0), stages = 2 * (ss1 - ss0);
+        Raw8<X> raw[kOwnTokens];
+        float f[8];
+        auto load = [&](int i) {
+          const int k = (ks0 + i) * kStageK + lane * 8;
+          if (P.inv) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = k + e < P.K ? P.inv[k + e] : 0.0f;
+          }
+          if (P.x_wide && k + 8 <= P.K) {
+#pragma unroll
+            for (int j = 0; j < kOwnTokens; ++j) raw[j] = load8(static_cast<const X*>(P.x) + min(m0 + j, P.M - 1) * P.ldx + k);
+          }
+        };
+        load(warp - kFirstEpiWarp);
+        for (int i = warp - kFirstEpiWarp; i < stages; i += 4) {
+          const int k = (ks0 + i) * kStageK + lane * 8;
+          const uint32_t it = tl * (ks1 - ks0) + i, sit = tl * (ss1 - ss0) + i / 2, slot = it % C::kStages, ss = sit % kScaleSlots;
+          const bool there = ks0 + i < ks1;           // (the last 256 columns of 512 may be beyond the row)
+          uint32_t c[kOwnTokens], byte[kOwnTokens];
+#pragma unroll
+          for (int j = 0; j < kOwnTokens; ++j) {
+            if (j >= tokens || !there) break;
+            float t[8];
+            columns8<X>(P, m0 + j, k, raw[j], t);
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (P.inv) t[e] = __fmul_rn(t[e], f[e]);
+              top = max(top, __float_as_uint(t[e]) & 0x7fffffffu);
+            }
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            byte[j] = mx_scale_byte(top);
+            c[j] = 0;
+            if (byte[j] != 255u) {
+              const float s = mx_inverse_scale(byte[j]);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) t[e] = __fmul_rn(t[e], s);
+              c[j] = mx_codes8(t);
+            }
+          }
+          load(i + 4);
+          ok = __all_sync(0xffffffffu, (!there || bar_wait(empty(slot), ((it / C::kStages) & 1u) ^ 1u, abort_flag)) &&
+                                           bar_wait(sc_empty(ss), ((sit / kScaleSlots) & 1u) ^ 1u, abort_flag));
+          if (!ok) break;
+          // 128-byte swizzle: the 16-byte piece's number in the row, exclusive-or the row in its group of eight
+          uint8_t* codes = gen + C::kStages * kAStage + slot * C::kBStage + (lane & 3) * 4;
+          uint8_t* bytes = gen + kScaleAt + ss * C::kScaleBytes + kRows * 16 + (i & 1) * 8 + lane / 4;
+#pragma unroll
+          for (int j = 0; j < kOwnTokens; ++j) {
+            if (j >= tokens || !there) break;
+            *reinterpret_cast<uint32_t*>(codes + j * 128 + ((lane / 4) ^ j) * 16) = c[j];
+            if ((lane & 3) == 0) bytes[j * 16] = (uint8_t)byte[j];
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if (there) bar_arrive(full(slot));
+            bar_arrive(sc_full(ss));
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
+      }
       const uint32_t buf = tl % C::kDBuffers;
       const int n = tile / P.n_tiles_m * kRows + 32 * quad + lane, m0 = tile % P.n_tiles_m * BN;
       const int tokens = min(BN, P.M - m0);
@@ -505,10 +597,10 @@ Plan plan(int64_t M, int64_t N, int64_t n_ks) {
   return best;
 }
 
-template <int BN>
+template <int BN, typename X = void>
 lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* status, cudaStream_t s) {
   using C = Cfg<BN>;
-  auto kern = mx_linear_kernel<BN>;
+  auto kern = mx_linear_kernel<BN, X>;
   static PerDeviceFlag attr_set;
   int dev;
   if (attr_set.first(&dev)) {
@@ -520,14 +612,25 @@ lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* stat
   const int64_t n_tiles_m = (p.M + BN - 1) / BN, tiles = n_tiles_m * ((p.N + kRows - 1) / kRows);
   if (tiles > 0x7fffffff) return LCD_ERR_UNSUPPORTED;
   CUtensorMap w, x, ws, xs;
-  if (!encode_rows(&w, p.w_codes, blocks * 16, p.N, p.ldwc, kStageK / 2, kRows, true) ||
-      !encode_rows(&x, p.x_codes, blocks * 16, p.M, p.ldxc, kStageK / 2, BN, true) ||
-      !encode_rows(&ws, p.w_scales, blocks, p.N, p.ldws, 16, kRows, false) ||
-      !encode_rows(&xs, p.x_scales, blocks, p.M, p.ldxs, 16, BN, false)) {
+  bool encoded = encode_rows(&w, p.w_codes, blocks * 16, p.N, p.ldwc, kStageK / 2, kRows, true) &&
+                 encode_rows(&ws, p.w_scales, blocks, p.N, p.ldws, 16, kRows, false);
+  if (std::is_same<X, void>::value) {
+    encoded = encoded && encode_rows(&x, p.x_codes, blocks * 16, p.M, p.ldxc, kStageK / 2, BN, true) &&
+              encode_rows(&xs, p.x_scales, blocks, p.M, p.ldxs, 16, BN, false);
+  } else {
+    x = w;               // not used
+    xs = ws;
+  }
+  if (!encoded) {
     set_cuda_error((int)cudaErrorInvalidValue);
     return LCD_ERR_CUDA;
   }
   Args a = {};
+  a.x = p.x;
+  a.ldx = p.ldx;
+  a.inv = p.inv_smooth;
+  a.K = (int)p.K;
+  a.x_wide = p.x && reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && (p.M == 1 || p.ldx * (p.x_type == LCD_DTYPE_F32 ? 4 : 2) % 16 == 0);
   a.y = p.y;
   a.ldy = p.ldy;
   a.y_type = (int)p.y_type;
@@ -566,9 +669,19 @@ lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* stat
 
 }  // namespace
 
+// (4 x 8192 x 28672 35 us, 27 with two launches; 1 x 8192 x 28672 27.1 and 26.8; 4 x 4096 x 4096 6.7 and 6.6)
+bool mx_linear_quantizes(int64_t M, int64_t K) { return M <= kOwnTokens && M * K <= 28672; }
+
 lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* status_word, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Plan w = plan(p.M, p.N, ((p.K + kMxBlock - 1) / kMxBlock * kMxBlock + kStageK - 1) / kStageK);
+  if (p.x) {
+    switch (p.x_type) {
+      case LCD_DTYPE_F32: return launch_width<16, float>(p, w.split, false, status_word, s);
+      case LCD_DTYPE_F16: return launch_width<16, __half>(p, w.split, false, status_word, s);
+      default: return launch_width<16, __nv_bfloat16>(p, w.split, false, status_word, s);
+    }
+  }
   switch (w.width) {
     case 16: return launch_width<16>(p, w.split, x_just_written, status_word, s);
     case 32: return launch_width<32>(p, w.split, x_just_written, status_word, s);

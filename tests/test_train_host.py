@@ -59,12 +59,13 @@ def test_invalid_arguments(call, bad):
 
 def test_too_many_entries_and_short_workspaces():
     assert loss(V=5000, ldz=5000, k=1025, ldi=1025, ldt=1025) == 2
-    assert fused(bytes=95) == 3 and fused(space=None) == 3
+    assert fused(M=20, bytes=20 * 48 - 1) == 3 and fused(M=20, space=None) == 3
     need = ctypes.c_size_t()
-    assert lib.lcd_mx_linear_fused_workspace_bytes(2, 64, ctypes.byref(need)) == 0 and need.value == 2 * (32 + 16)
+    assert lib.lcd_mx_linear_fused_workspace_bytes(20, 64, ctypes.byref(need)) == 0 and need.value == 20 * (32 + 16)
+    assert lib.lcd_mx_linear_fused_workspace_bytes(4, 64, ctypes.byref(need)) == 0 and need.value == 0
     assert lib.lcd_mx_linear_fused_workspace_bytes(0, 64, ctypes.byref(need)) == 1
     assert lib.lcd_mx_linear_fused_workspace_bytes(2, 64, None) == 1
-    assert lcd.mx_linear_fused_workspace_bytes(3, 33) == 3 * (32 + 16)
+    assert lcd.mx_linear_fused_workspace_bytes(33, 33) == 33 * (32 + 16)
 
 
 def test_binding_refuses_what_is_no_gpu_matrix():
