@@ -38,6 +38,33 @@ inline int current_sm_count() {
 }
 
 #ifdef __CUDACC__
+// Launches a kernel that begins while the one before it in the stream ends: it passes begin_after_previous() before it touches
+// what another kernel may write or read.  cluster: CTAs of a cluster, 1 for none.
+template <typename... Params, typename... Args>
+inline cudaError_t launch_overlapping(void (*kern)(Params...), dim3 grid, dim3 block, size_t smem, unsigned cluster, cudaStream_t stream,
+                                      Args&&... args) {
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
+}
+// Waits for the kernels before this one and only then lets the next one begin: a kernel that has begun may take everything before
+// its direct predecessor for done.
+__device__ __forceinline__ void begin_after_previous() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // Loads of what an earlier kernel of the stream writes, behind griddepcontrol.wait.  A kernel launched with programmatic
 // stream serialization may be running while that one still writes, and __ldg (ld.global.nc, what loads through const
 // __restrict__ pointers become too) is only for data that nobody writes while the reading kernel runs.

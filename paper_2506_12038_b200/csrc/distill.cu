@@ -234,6 +234,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
   __shared__ Pair s_top[kWarps], s_row[kWarps];
   __shared__ float s_mass[kWarps];
   __shared__ Word s_word[kMaxCluster];
+  begin_after_previous();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const int64_t t = blockIdx.x / P.parts;
   const int rank = blockIdx.x % P.parts;
@@ -455,6 +456,7 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Pair s_top[2][kStreamWarps], s_row[2][kStreamWarps];
   __shared__ float s_mass[2][kStreamWarps];
+  begin_after_previous();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint4* ring = reinterpret_cast<uint4*>(smem) + tid;
   auto entries = [&](int place) {
@@ -767,8 +769,7 @@ lcd_status launch_stream(const Params& p, int64_t rows, bool loss, bool grad, cu
     flag.done(dev);
   }
   const int64_t most = (int64_t)current_sm_count() * kStreamPerSm<THREADS>;
-  kern<<<(unsigned)(rows < most ? rows : most), THREADS, kRing + 3 * 16 * p.k, s>>>(p, rows);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch_overlapping(kern, dim3((unsigned)(rows < most ? rows : most)), dim3(THREADS), kRing + 3 * 16 * p.k, 1, s, p, rows);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
@@ -801,17 +802,7 @@ lcd_status launch_typed(Params p, int64_t rows, bool loss, bool grad, cudaStream
   auto kern = loss ? (grad ? (once ? distill_kernel<T, true, true, true> : distill_kernel<T, true, true, false>)
                            : (once ? distill_kernel<T, true, false, true> : distill_kernel<T, true, false, false>))
                    : (once ? distill_kernel<T, false, true, true> : distill_kernel<T, false, true, false>);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(rows * parts));
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.stream = s;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = (unsigned)parts;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = loss && parts > 1 ? 1 : 0;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p);
+  const cudaError_t e = launch_overlapping(kern, dim3((unsigned)(rows * parts)), dim3((unsigned)threads), 0, loss ? (unsigned)parts : 1u, s, p);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }

@@ -33,9 +33,9 @@ __device__ __forceinline__ Place place() {
 // VEC: rows of x and the factors start on 16 bytes.
 template <typename T, bool VEC, int EACH>
 __global__ void __launch_bounds__(kMxThreads)
-mx_quantize_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ldx, const float* __restrict__ inv, uint8_t* __restrict__ codes,
-                   int64_t ldc, uint8_t* __restrict__ scales, int64_t lds, uint32_t units) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the product of the same call may set itself up
+mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc, uint8_t* scales,
+                   int64_t lds, uint32_t units) {
+  begin_after_previous();       // (no __restrict__: loads of what the kernel before wrote are coherent ones)
   __shared__ T s_x[VEC ? 1 : kMxThreads * 8];
   const Place at = place<EACH>();
   const int64_t k0 = (int64_t)at.unit * 8;
@@ -100,8 +100,9 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t M, int64_t K, int64_t ldx, c
 
 template <typename T, bool VEC, int EACH>
 __global__ void __launch_bounds__(kMxThreads)
-mx_dequantize_kernel(const uint8_t* __restrict__ codes, int64_t ldc, const uint8_t* __restrict__ scales, int64_t lds, int64_t M, int64_t K,
-                     T* __restrict__ out, int64_t ldo, uint32_t units) {
+mx_dequantize_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K, T* out, int64_t ldo,
+                     uint32_t units) {
+  begin_after_previous();
   __shared__ T s_out[VEC ? 1 : kMxThreads * 8];
   const Place at = place<EACH>();
   const int64_t k0 = (int64_t)at.unit * 8;
@@ -147,8 +148,7 @@ bool on16(const void* p, int64_t ld, int64_t size, int64_t rows) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows == 1 || ld * size % 16 == 0);
 }
 
-lcd_status launched() {
-  const cudaError_t e = cudaGetLastError();
+lcd_status launched(cudaError_t e) {
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
@@ -176,8 +176,7 @@ lcd_status quantize_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const
   const bool vec = on16(x, ldx, sizeof(T), M) && (!inv || reinterpret_cast<uintptr_t>(inv) % 16 == 0);
   auto kern = vec ? (q.each ? mx_quantize_kernel<T, true, kRowsEach> : mx_quantize_kernel<T, true, 1>)
                   : (q.each ? mx_quantize_kernel<T, false, kRowsEach> : mx_quantize_kernel<T, false, 1>);
-  kern<<<q.grid, q.block, 0, s>>>(static_cast<const T*>(x), M, K, ldx, inv, codes, ldc, scales, lds, units);
-  return launched();
+  return launched(launch_overlapping(kern, q.grid, q.block, 0, 1, s, static_cast<const T*>(x), M, K, ldx, inv, codes, ldc, scales, lds, units));
 }
 
 template <typename T>
@@ -189,8 +188,7 @@ lcd_status dequantize_rows(const uint8_t* codes, int64_t ldc, const uint8_t* sca
   const bool vec = on16(out, ldo, sizeof(T), M);
   auto kern = vec ? (q.each ? mx_dequantize_kernel<T, true, kRowsEach> : mx_dequantize_kernel<T, true, 1>)
                   : (q.each ? mx_dequantize_kernel<T, false, kRowsEach> : mx_dequantize_kernel<T, false, 1>);
-  kern<<<q.grid, q.block, 0, s>>>(codes, ldc, scales, lds, M, K, static_cast<T*>(out), ldo, units);
-  return launched();
+  return launched(launch_overlapping(kern, q.grid, q.block, 0, 1, s, codes, ldc, scales, lds, M, K, static_cast<T*>(out), ldo, units));
 }
 
 }  // namespace

@@ -259,7 +259,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 
   if (warp == 0 || warp == kScaleCopyWarp) {
     // ---------------------------------------------------------------- TMA producers.  With P.early the kernel before this one wrote x's
-    // codes and nothing else that is read here, so the weights' first copies do not wait for it.
+    // codes and nothing else that is read here, and itself began when all before it was done: the weights' first copies do not wait.
     const bool codes = warp == 0;
     if (elect()) {
       const int from = codes ? ks0 : ss0, to = codes ? ks1 : ss1, slots = codes ? C::kStages : kScaleSlots;
@@ -278,7 +278,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         bar_expect_tx(full_of(i), bytes);
         copy_w(i, from + i, tile0 / P.n_tiles_m * kRows);
       }
-      asm volatile("griddepcontrol.wait;" ::: "memory");
+      begin_after_previous();
       int it = 0;
       bool ok = true;
       for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step) {
@@ -373,6 +373,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     bool ok = true;
     for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
       if constexpr (!kReady) {
+        if (tl == 0) begin_after_previous();
         // Stage i of the CTA's belongs to warp i % 4: a lane has eight columns, four lanes a block, of one token after the other.  The
         // next stage's columns and factors are asked for when this one's have been taken.
         const int m0 = tile % P.n_tiles_m * BN, tokens = min(kOwnTokens, P.M - m0), stages = 2 * (ss1 - ss0);
@@ -643,26 +644,8 @@ lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* stat
   a.early = early;
   a.status = status;
   const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = C::kSmem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  int n = 0;
-  if (early) {
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  if (split > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = (unsigned)split;
-    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
-    ++n;
-  }
-  cfg.attrs = attr;
-  cfg.numAttrs = (unsigned)n;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, w, x, ws, xs, a);
+  const unsigned grid = (unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room);
+  const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(kThreads), C::kSmem, (unsigned)split, s, w, x, ws, xs, a);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
