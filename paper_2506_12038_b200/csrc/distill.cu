@@ -393,8 +393,9 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
 // Many rows: a CTA takes one row after the other and its threads copy ahead (cp.async) into a ring in shared memory, each thread
 // the words that it reads itself, so that nothing is waited for but one's own copies and memory is busy through the reductions,
 // into the next row.  A row of at most kDepth chunks stays in the ring between the sum and the gradient; a longer one is copied
-// twice, the second time out of L2 (the rows in work are kept few enough for that).  The teacher's entries of a row are asked for two
-// reductions ahead: index and logit while the row before is summed up, the student's logit there while its gradient is written.
+// twice, the second time out of L2 (the rows in work are kept few enough for that).  The teacher's entries of a row are asked for
+// while the row before is worked on; the student's logits there when the row has been read, out of L2 (before it is read they are
+// single accesses to DRAM: of 4440 x 32000, k = 128, loss 77 us, 62 so), but for the gradient alone, which may take the row's place.
 constexpr int kStreamSlots = 4;       // words a thread has of a chunk
 template <int THREADS> constexpr int kStreamPerSm = THREADS == 128 ? 6 : 2;
 constexpr int kDepth = 4;             // chunks of the ring
@@ -408,7 +409,7 @@ __device__ __forceinline__ void copy_wait(int newer) {      // all copies but th
 
 struct Entries {         // of three rows in turn, k each: a row's are read until the last warp has left it
   int* idx;
-  float *t, *p, *z;
+  float *p, *z;          // p holds t / temperature first
 };
 // write(index, sum of its p, its logit) for every entry, k / warps of them a warp.  An index that comes twice has all of its p, in the
 // entries' order, and each of its entries writes the same.  Whether any does is seen by counting what is equal to a warp's
@@ -455,15 +456,14 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Pair s_top[2][kStreamWarps], s_row[2][kStreamWarps];
-  __shared__ float s_mass[2][kStreamWarps];
+  __shared__ float s_mass[2][kStreamWarps], s_part[2][kStreamWarps];
   begin_after_previous();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint4* ring = reinterpret_cast<uint4*>(smem) + tid;
   auto entries = [&](int place) {
     Entries n;
-    n.idx = reinterpret_cast<int*>(smem + kDepth * kChunkBytes) + place * 4 * P.k;
-    n.t = reinterpret_cast<float*>(n.idx + P.k);
-    n.p = n.t + P.k;
+    n.idx = reinterpret_cast<int*>(smem + kDepth * kChunkBytes) + place * 3 * P.k;
+    n.p = reinterpret_cast<float*>(n.idx + P.k);
     n.z = n.p + P.k;
     return n;
   };
@@ -577,10 +577,10 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       const float v = teacher_in(e_top);
       const int i = v == -INFINITY ? -1 : index_in(e_idx);     // p = 0: as if it were absent
       n.idx[tid] = i;
-      n.t[tid] = v;
+      n.p[tid] = v;
       if (i >= 0) {
         top = {fmaxf(v, -FLT_MAX), v == v ? 1.0f : v};
-        e_z = row[i];
+        if (!LOSS) e_z = row[i];
       }
 #pragma unroll 1
       for (int j = tid + kStreamThreads; j < P.k; j += kStreamThreads) {
@@ -591,11 +591,11 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
                                                                 : static_cast<const uint16_t*>(P.top)[t * P.ldt + j]);
         const int i2 = v2 == -INFINITY ? -1 : index_in(raw);
         n.idx[j] = i2;
-        n.t[j] = v2;
+        n.p[j] = v2;
         if (i2 >= 0) {
           const float m = fmaxf(top.m, v2);
           top = {m, top.s * exp2_fast((top.m - m) * kLog2e) + exp2_fast((v2 - m) * kLog2e)};
-          n.z[j] = to_f32(row[i2]);
+          if (!LOSS) n.z[j] = to_f32(row[i2]);
         }
       }
     }
@@ -624,6 +624,7 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     while (issued - freed < (uint32_t)kDepth && copy_one(t, w, t_next, w_next)) {}
     const Row row = row_of(t);
     const bool stays = LOSS && GRAD && row.chunks <= kDepth;
+    const T* student = static_cast<const T*>(P.z) + t * P.ldz;
     T* out = GRAD ? static_cast<T*>(P.d) + t * P.ldd : nullptr;
     const bool wide = ((reinterpret_cast<uintptr_t>(out) & 15) == row.off * sizeof(T));
     // makes what lies outside the row -infinity in this thread's words of a chunk
@@ -658,52 +659,50 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
           copy_one(t, w, t_next, w_next);
         }
       }
+      if (tid < P.k && n.idx[tid] >= 0) e_z = student[n.idx[tid]];       // arrives behind the reductions
       all = warp_pair(all, P.c);
       if (lane == 0) s_row[parity][warp] = all;
     }
-    // this row's p, the next row's entries, and one barrier for all three reductions
-    float mass = 0.0f, norm = 0.0f;                    // log p = (t - top.m) - norm
-    Pair top = {};
-    auto normalise = [&]() {
-      top = pair_of<kStreamWarps>(s_top[parity], kLog2e);
-      norm = P.lse ? lse - top.m : logf(top.s);
-    };
+    // this row's p, its share of the loss with the warp's own maximum, the next row's entries, and one barrier for all reductions
+    float mass = 0.0f, part = 0.0f;                    // log p = (t - top.m) - norm
     if (warp * 32 < P.k) {
-      normalise();
-      if (tid < P.k) n.z[tid] = to_f32(e_z);
+      const Pair top = pair_of<kStreamWarps>(s_top[parity], kLog2e);
+      const float norm = P.lse ? lse - top.m : logf(top.s);
       for (int j = tid; j < P.k; j += kStreamThreads) {
-        const float p = n.idx[j] >= 0 ? expf((n.t[j] - top.m) - norm) : 0.0f;
+        const int i = n.idx[j];
+        const float logp = (n.p[j] - top.m) - norm, p = i >= 0 ? expf(logp) : 0.0f;
+        if (!LOSS && j == tid) n.z[j] = to_f32(e_z);
+        if (LOSS && w != 0.0f && i >= 0) {
+          const float z = to_f32(j == tid ? e_z : student[i]);
+          if (p != 0.0f) part += p * (logp - (z - all.m) * P.inv_tau);
+          n.z[j] = z;
+        }
         n.p[j] = p;
         mass += p;
       }
       mass = warp_sum(mass);
+      if (LOSS) part = warp_sum(part);
     }
-    if (lane == 0) s_mass[parity][warp] = mass;
+    if (lane == 0) {
+      s_mass[parity][warp] = mass;
+      s_part[parity][warp] = part;
+    }
     enter(t_next, place, parity ^ 1);
     __syncthreads();
-    const bool turn = warp == (int)(t % kStreamWarps);          // whose warp forms the loss
-    if (GRAD || turn) mass = sum_of<kStreamWarps>(s_mass[parity]);
-    if (LOSS && w == 0.0f && tid == 0) {
-      P.loss[t] = 0.0f;
-      if (P.stats) P.stats[2 * t] = P.stats[2 * t + 1] = NAN;
+    if (GRAD || warp == 0) {
+      mass = sum_of<kStreamWarps>(s_mass[parity]);
+      if (LOSS && w != 0.0f) all = pair_of<kStreamWarps>(s_row[parity], P.c);
     }
-    if (LOSS && w != 0.0f && (GRAD || turn)) {
-      all = pair_of<kStreamWarps>(s_row[parity], P.c);
-      if (turn) {
-        if (warp * 32 >= P.k) normalise();
-        float part = 0.0f;
-        for (int j = lane; j < P.k; j += 32) {
-          const float p = n.p[j];
-          if (p != 0.0f) part += p * (((n.t[j] - top.m) - norm) - (n.z[j] - all.m) * P.inv_tau);
-        }
-        part = warp_sum(part);
-        if (lane == 0) {
-          P.loss[t] = mass == 0.0f ? 0.0f : w * (part + mass * logf(all.s));
-          if (P.stats) {
-            P.stats[2 * t] = all.m;
-            P.stats[2 * t + 1] = all.s;
-          }
-        }
+    if (LOSS && tid == 0) {
+      if (w != 0.0f) {
+        part = mass * logf(all.s);
+        for (int i = 0; i < kStreamWarps; ++i)
+          if (s_mass[parity][i] != 0.0f) part += s_part[parity][i] + s_mass[parity][i] * ((all.m - s_row[parity][i].m) * P.inv_tau);
+      }
+      P.loss[t] = w == 0.0f || mass == 0.0f ? 0.0f : w * part;
+      if (P.stats) {
+        P.stats[2 * t] = w == 0.0f ? NAN : all.m;
+        P.stats[2 * t + 1] = w == 0.0f ? NAN : all.s;
       }
     }
     const bool none = w == 0.0f || mass == 0.0f;      // no gradient
@@ -764,12 +763,14 @@ lcd_status launch_stream(const Params& p, int64_t rows, bool loss, bool grad, cu
   constexpr int kRing = kDepth * THREADS * kStreamSlots * 16;
   PerDeviceFlag& flag = attr_set[loss ? grad : 2];
   if (flag.first(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing + 3 * 16 * kMaxK);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kRing + 3 * 12 * kMaxK);
     if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
     flag.done(dev);
   }
-  const int64_t most = (int64_t)current_sm_count() * kStreamPerSm<THREADS>;
-  const cudaError_t e = launch_overlapping(kern, dim3((unsigned)(rows < most ? rows : most)), dim3(THREADS), kRing + 3 * 16 * p.k, 1, s, p, rows);
+  // as many CTAs as are resident: 1 KB of the system's and up to 0.5 of static shared memory a CTA
+  const int fit = 228 * 1024 / (kRing + 3 * 12 * (int)p.k + 1536);
+  const int64_t most = (int64_t)current_sm_count() * (fit < kStreamPerSm<THREADS> ? fit : kStreamPerSm<THREADS>);
+  const cudaError_t e = launch_overlapping(kern, dim3((unsigned)(rows < most ? rows : most)), dim3(THREADS), kRing + 3 * 12 * p.k, 1, s, p, rows);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
