@@ -392,8 +392,8 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
 // ---------------------------------------------------------------------------------------------------------
 // Many rows: a CTA takes one row after the other and its threads copy ahead (cp.async) into a ring in shared memory, each thread
 // the words that it reads itself, so that nothing is waited for but one's own copies and memory is busy through the reductions,
-// into the next row.  A row of at most kDepth chunks stays in the ring between the sum and the gradient; a longer one is copied
-// twice, the second time out of L2 (the rows in work are kept few enough for that).  The teacher's entries of a row are asked for
+// into the next row.  A row's last kDepth chunks stay in the ring between the sum and the gradient, the others are copied twice,
+// the second time out of L2, as far as the rows in work fit there.  The teacher's entries of a row are asked for
 // while the row before is worked on; the student's logits there when the row has been read, out of L2 (before it is read they are
 // single accesses to DRAM: of 4440 x 32000, k = 128, loss 77 us, 62 so), but for the gradient alone, which may take the row's place.
 constexpr int kStreamSlots = 4;       // words a thread has of a chunk
@@ -490,35 +490,40 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     return r;
   };
 
-  // ---- the copies.  Chunks are numbered in the order in which they are asked for; chunk n lies at place n % kDepth.
-  uint32_t issued = 0, freed = 0;
+  // ---- the copies.  With a gradient a row goes through the ring forwards for the sum, and its last kDepth chunks stay there; then
+  // backwards for the gradient, those first and the others copied again, the latest of them first, which are the likeliest to be in
+  // L2.  So places are taken in one direction by a row's sum and in the other by its gradient and by the next row's sum.  (kDepth
+  // is a power of two.)
+  constexpr bool kTwice = LOSS && GRAD;
+  uint32_t issued = 0, taken = 0;                    // copies asked for, and those that have been waited for
+  int free_places = kDepth, copy_place = 0, copy_dir = 1;
   int64_t copy_t = -1;             // the row that is being copied
   Row copy_row = {};
-  const uint8_t* copy_src = nullptr;                 // this thread's first word of the next chunk
-  int copy_chunk = 0;
-  bool copy_again = false;                           // the row is copied once more
+  int copy_chunk = 0, copy_left = 0;                 // the next chunk, and how many there are of this pass
+  bool copy_again = false;                           // in a row's first pass of two
   auto copy_one = [&](int64_t t, float w_t, int64_t t_next, float w_next) {     // false: nothing to copy now.  There is a free place
-    if (copy_chunk >= copy_row.chunks) {
-      if (copy_again) {
+    while (copy_left == 0) {
+      if (copy_again) {                              // from here on backwards
         copy_again = false;
-      } else {
-        for (;;) {                                   // the row that is worked on, or the next one
-          if (copy_t == t_next) return false;
-          const bool begin = copy_t != t;
-          copy_t = begin ? t : t_next;
-          copy_row.chunks = 0;
-          copy_chunk = 0;
-          if (copy_t < rows && (begin ? w_t : w_next) != 0.0f) {
-            copy_row = row_of(copy_t);
-            copy_again = LOSS && GRAD && copy_row.chunks > kDepth;
-            break;
-          }
-        }
+        copy_dir = -copy_dir;
+        copy_left = max(0, copy_row.chunks - kDepth);
+        copy_chunk = copy_left - 1;
+        // from the last chunk's place on; a row that stays whole leaves the places behind its first chunk to the next row
+        copy_place += copy_row.chunks >= kDepth ? copy_dir : (copy_row.chunks + 1) * copy_dir;
+        continue;
       }
-      copy_chunk = 0;
-      copy_src = copy_row.at + tid * 16;
+      if (copy_t == t_next) return false;            // the row that is worked on, or the next one
+      const bool begin = copy_t != t;
+      copy_t = begin ? t : t_next;
+      if (copy_t < rows && (begin ? w_t : w_next) != 0.0f) {
+        copy_row = row_of(copy_t);
+        copy_chunk = 0;
+        copy_left = copy_row.chunks;
+        copy_again = kTwice;
+      }
     }
-    uint4* dst = ring + (issued % kDepth) * kChunkSlots;
+    uint4* dst = ring + (copy_place & (kDepth - 1)) * kChunkSlots;
+    const uint8_t* copy_src = copy_row.at + (size_t)copy_chunk * kChunkBytes + tid * 16;
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
     if (copy_row.whole(copy_chunk)) {
 #pragma unroll
@@ -543,11 +548,14 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    ++copy_chunk;
-    copy_src += kChunkBytes;
+    copy_chunk += kTwice && !copy_again ? -1 : 1;
+    --copy_left;
+    copy_place += copy_dir;
+    --free_places;
     ++issued;
     return true;
   };
+  int place_now = 0, dir = 1;                        // of the chunk that is worked on
 
   // ---- the teacher's entries.  A thread's first is asked for ahead and lies in registers as it came, since the first instruction that
   // takes it waits for it; those beyond kStreamThreads are loaded when they are entered.
@@ -621,9 +629,8 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     Pair all = {-FLT_MAX, 0.0f};
     if (!LOSS) all = {P.stats[2 * t], P.stats[2 * t + 1]};
     const float lse_next = P.lse && t_next < rows ? P.lse[t_next] : 0.0f;
-    while (issued - freed < (uint32_t)kDepth && copy_one(t, w, t_next, w_next)) {}
+    while (free_places > 0 && copy_one(t, w, t_next, w_next)) {}
     const Row row = row_of(t);
-    const bool stays = LOSS && GRAD && row.chunks <= kDepth;
     const T* student = static_cast<const T*>(P.z) + t * P.ldz;
     T* out = GRAD ? static_cast<T*>(P.d) + t * P.ldd : nullptr;
     const bool wide = ((reinterpret_cast<uintptr_t>(out) & 15) == row.off * sizeof(T));
@@ -643,21 +650,25 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
         }
       }
     };
-    const uint32_t from = freed;
     if (LOSS && w != 0.0f) {
       for (int c = 0; c < row.chunks; ++c) {
-        const uint32_t at = stays ? from + c : freed;
-        copy_wait((int)(issued - at - 1));
-        uint4* src = ring + (at % kDepth) * kChunkSlots;
+        copy_wait((int)(issued - taken - 1));
+        ++taken;
+        uint4* src = ring + (place_now & (kDepth - 1)) * kChunkSlots;
+        place_now += dir;
         if (!row.whole(c)) patch(src, c);
         uint4 x[kStreamSlots];
 #pragma unroll
         for (int u = 0; u < kStreamSlots; ++u) x[u] = src[u * kStreamThreads];
         add_words<T, kStreamSlots>(x, P.c, all);
-        if (!stays) {
-          ++freed;
+        if (!kTwice || c < row.chunks - kDepth) {
+          ++free_places;
           copy_one(t, w, t_next, w_next);
         }
+      }
+      if (kTwice) {
+        place_now -= dir;
+        dir = -dir;
       }
       if (tid < P.k && n.idx[tid] >= 0) e_z = student[n.idx[tid]];       // arrives behind the reductions
       all = warp_pair(all, P.c);
@@ -712,9 +723,14 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     }
     if (GRAD && w != 0.0f) {
       const float wt = w * P.inv_tau, scale = wt * mass / all.s;
-      for (int c = 0; c < row.chunks; ++c) {
-        copy_wait((int)(issued - freed - 1));
-        const uint4* src = ring + (freed % kDepth) * kChunkSlots;
+      for (int n_done = 0; n_done < row.chunks; ++n_done) {
+        const int c = kTwice ? row.chunks - 1 - n_done : n_done;
+        if (!kTwice || n_done >= kDepth) {
+          copy_wait((int)(issued - taken - 1));
+          ++taken;
+        }
+        const uint4* src = ring + (place_now & (kDepth - 1)) * kChunkSlots;
+        place_now += dir;
         if (none) {
         } else if (wide && row.whole(c)) {
           T* to = out - row.off + (size_t)c * kChunkSlots * E + tid * E;
@@ -737,7 +753,7 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
             S::store(out, lo, P.V, wide, v);
           }
         }
-        ++freed;
+        ++free_places;
         copy_one(t, w, t_next, w_next);
       }
       __syncthreads();
