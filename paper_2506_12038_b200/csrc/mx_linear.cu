@@ -3,13 +3,13 @@
 // 128 weight rows by BN tokens over 64 columns, codes from shared memory, scales from tensor memory, sums in fp32.  So there
 // is no decoding, and few tokens (weights from HBM) and many (tensor pipe) are one kernel with token tiles of different width.
 //
-// Roles (11 warps):
+// Roles (11 warps; 15 with tiles of 256 tokens):
 //   warp 0      TMA producer of codes: stages of 256 columns, 128-byte swizzle
 //   warp 10     TMA producer of scales: 512 columns (16 bytes a row) at a time
 //   warps 2-5   scales to tensor memory: the unit reads row r's four scale bytes of 128 columns at lane r % 32, column r / 32, in
 //               every quarter of the lanes, so each of the four warps stores all rows' words into its own quarter
 //   warp 1      owns tensor memory; one elected lane issues the MMAs
-//   warps 6-9   epilogue: tensor memory -> y, coalesced along the weight rows; up to four tokens come as they are, then these warps
+//   warps 6-9, 11-14  epilogue: tensor memory -> y, coalesced along the weight rows; up to four tokens come as they are, then these warps
 //               quantise them into the stages first
 // Where tiles are few the columns of a tile are cut among the CTAs of a cluster; their partial sums meet in distributed shared
 // memory and are added in the order of the ranks, so results do not depend on timing.
@@ -34,7 +34,6 @@ constexpr int kScaleSlots = 3;
 constexpr int kMostSplit = 8;                  // a cluster's CTAs
 constexpr int kOwnTokens = 4;                  // tokens that the kernel quantises itself
 constexpr int kMmaWarp = 1, kFirstEpiWarp = 6, kScaleCopyWarp = 10;
-constexpr int kThreads = 32 * 11;
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
 template <int BN>
@@ -50,6 +49,8 @@ struct Cfg {
   static constexpr int kTmemCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
   static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 256;
   static constexpr int kPerSm = BN <= 64 ? 2 : 1;
+  static constexpr int kEpiHalves = kDBuffers == 1 ? 2 : 1;              // the one accumulator is drained by twice the warps
+  static constexpr int kThreads = 32 * (11 + 4 * (kEpiHalves - 1));
   static_assert(kUsed <= kTmemCols && kTmemCols * kPerSm <= 512, "tensor memory");
   static_assert(kSmem <= 227 * 1024 && kPerSm * (kSmem + 1024) <= 228 * 1024, "shared memory");
   static_assert(BN * 512 <= kStages * (kAStage + kBStage), "partial sums lie in the stages");
@@ -191,7 +192,7 @@ __device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8
 // with two launches, 1 x 4096 x 4096 5.9 and 6.1, and 5.4 us on the host in place of 8.1; from eight tokens on it takes longer than the
 // weights' copies (8 x 4096 x 4096 8.4 and 6.9).
 template <int BN, typename X>
-__global__ void __launch_bounds__(kThreads, Cfg<BN>::kPerSm)
+__global__ void __launch_bounds__(Cfg<BN>::kThreads, Cfg<BN>::kPerSm)
 mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                  const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const Args P) {
   using C = Cfg<BN>;
@@ -239,7 +240,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     }
     for (int b = 0; b < 2; ++b) {
       bar_init(d_full(b), 1);
-      bar_init(d_empty(b), 4);
+      bar_init(d_empty(b), 4 * C::kEpiHalves);
     }
     bar_init(drain, 1);
     *abort_flag = 0;
@@ -449,8 +450,10 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       // The next columns are on their way while these are stored.
       const uint32_t from = tmem + quarter + buf * BN;
+      const int begin = warp > kScaleCopyWarp ? BN / 2 : 0, end = C::kEpiHalves == 2 && !begin ? min(tokens, BN / 2) : tokens;
       auto drain_tile = [&](auto&& store) {       // store(first token of the tile, 16 tokens' sums)
         uint32_t v[16], w[16];
+        if (begin >= end) return;
         if (BN <= 64) {                           // (two CTAs an SM have no registers for it)
 #pragma unroll 1
           for (int c = 0; c < tokens; c += 16) {
@@ -460,17 +463,17 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
           }
           return;
         }
-        tmem_ld16(from, v);
+        tmem_ld16(from + begin, v);
 #pragma unroll 1
-        for (int c = 0;; c += 32) {
+        for (int c = begin;; c += 32) {
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (c + 16 < tokens) tmem_ld16(from + c + 16, w);
+          if (c + 16 < end) tmem_ld16(from + c + 16, w);
           store(c, v);
-          if (c + 16 >= tokens) break;
+          if (c + 16 >= end) break;
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (c + 32 < tokens) tmem_ld16(from + c + 32, v);
+          if (c + 32 < end) tmem_ld16(from + c + 32, v);
           store(c + 16, w);
-          if (c + 32 >= tokens) break;
+          if (c + 32 >= end) break;
         }
       };
       if (split > 1) {            // every copy into the stages has landed and been read: they hold the partial sums
@@ -482,7 +485,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       } else {
         by_type(P, [&](auto* y) {
           using T = std::remove_pointer_t<decltype(y)>;
-          T* at = y + (size_t)m0 * P.ldy + n;
+          T* at = y + (size_t)(m0 + begin) * P.ldy + n;
           const bool inside = n < P.N;
           drain_tile([&](int c, const uint32_t (&v)[16]) {
             // (the address is kept from being formed for all sixteen at once, which takes 32 registers)
@@ -518,7 +521,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const int n0 = tile0 / P.n_tiles_m * kRows, m0 = tile0 % P.n_tiles_m * BN;
     const int tokens = min(BN, P.M - m0);
     constexpr int kBatch = BN == 16 ? 1 : 4;           // groups of 32 rows that a warp adds at a time
-    for (int item = warp;; item += kThreads / 32) {
+    for (int item = warp;; item += C::kThreads / 32) {
       const int t = rank + split * (item * kBatch / 4), row = item * kBatch % 4 * 32 + lane;
       if (t >= tokens) break;
       float v[kMostSplit][kBatch];
@@ -645,7 +648,7 @@ lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* stat
   a.status = status;
   const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
   const unsigned grid = (unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room);
-  const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(kThreads), C::kSmem, (unsigned)split, s, w, x, ws, xs, a);
+  const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(C::kThreads), C::kSmem, (unsigned)split, s, w, x, ws, xs, a);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
