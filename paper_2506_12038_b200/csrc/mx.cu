@@ -2,8 +2,9 @@
 // Per block of 32 columns: A = max |t|, e = floor(log2 A) - 2, element = round(t * 2^-e).  Scaling by a power of two is exact,
 // so the rounding to 4 bits is the only one after t itself and results are the same bit for bit everywhere.
 //
-// Four lanes share a block and eight consecutive columns, a unit, are a lane's: one 16-byte load of 16-bit values (two of fp32), the
-// block's maximum by two shuffles, four code bytes out, so that loads and stores of a warp are contiguous.  What bounds both
+// To quantise, four lanes share a block and eight consecutive columns, a unit, are a lane's: one 16-byte load of 16-bit values (two of
+// fp32), the block's maximum by two shuffles, four code bytes out.  The other way a unit is 16 bytes of the output, so that a
+// warp's store is contiguous (fp32 in units of eight, two stores: 46 us of 11008 x 4096 in place of 35).  What bounds both
 // kernels is memory: a thread has its unit of kRowsEach rows in flight at once (one of few rows).  Rows that do not start on 16 bytes go
 // through shared memory, element by element and contiguous in memory.
 #include <type_traits>
@@ -30,13 +31,13 @@ __device__ __forceinline__ Place place() {
   return {blockIdx.y * blockDim.x + threadIdx.x, (int64_t)blockIdx.x * EACH * blockDim.y + threadIdx.y};
 }
 
-// VEC: rows of x and the factors start on 16 bytes.
+// VEC: rows of x start on 16 bytes.
 template <typename T, bool VEC, int EACH>
 __global__ void __launch_bounds__(kMxThreads)
 mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc, uint8_t* scales,
                    int64_t lds, uint32_t units) {
   begin_after_previous();       // (no __restrict__: loads of what the kernel before wrote are coherent ones)
-  __shared__ T s_x[VEC ? 1 : kMxThreads * 8];
+  __shared__ __align__(16) T s_x[VEC ? 1 : EACH * kMxThreads * 8];
   const Place at = place<EACH>();
   const int64_t k0 = (int64_t)at.unit * 8;
   float t[8], f[8];
@@ -47,12 +48,25 @@ mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* i
     for (int u = 0; u < EACH; ++u) raw[u] = load8(x + min(at.row0 + u * blockDim.y, M - 1) * ldx + k0);
   }
   if (inv) {
-    if (whole) {
+    if (k0 + 8 <= K && (reinterpret_cast<uintptr_t>(inv) & 15) == 0) {
       values8(load8(inv + k0), f);
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = k0 + i < K ? inv[k0 + i] : 0.0f;
     }
+  }
+  if (!VEC) {
+    const int n = blockDim.x * 8;
+    const int64_t from = (int64_t)blockIdx.y * n + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      const int64_t row = at.row0 + u * blockDim.y;
+      T* line = s_x + (u * blockDim.y + threadIdx.y) * n + threadIdx.x;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        line[i * blockDim.x] = row < M && from + i * blockDim.x < K ? x[row * ldx + from + i * blockDim.x] : from_f32<T>(0.0f);
+    }
+    __syncthreads();
   }
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
@@ -63,18 +77,8 @@ mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* i
 #pragma unroll
       for (int i = 0; i < 8; ++i) t[i] = row < M && k0 + i < K ? to_f32(x[row * ldx + k0 + i]) : 0.0f;
     } else {
-      const int n = blockDim.x * 8;
-      T* line = s_x + threadIdx.y * n;
-      const int64_t from = (int64_t)blockIdx.y * n;
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t e = from + i * blockDim.x + threadIdx.x;
-        line[i * blockDim.x + threadIdx.x] = row < M && e < K ? x[row * ldx + e] : from_f32<T>(0.0f);
-      }
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t[i] = to_f32(line[threadIdx.x * 8 + i]);
+      const T* line = s_x + (u * blockDim.y + threadIdx.y) * blockDim.x * 8;
+      values8(load8(line + threadIdx.x * 8), t);
     }
     uint32_t top = 0;
 #pragma unroll
@@ -103,16 +107,18 @@ __global__ void __launch_bounds__(kMxThreads)
 mx_dequantize_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K, T* out, int64_t ldo,
                      uint32_t units) {
   begin_after_previous();
-  __shared__ T s_out[VEC ? 1 : kMxThreads * 8];
+  constexpr int E = 16 / sizeof(T);
+  using Codes = typename std::conditional<E == 8, uint32_t, uint16_t>::type;
+  __shared__ T s_out[VEC ? 1 : EACH * kMxThreads * E];
   const Place at = place<EACH>();
-  const int64_t k0 = (int64_t)at.unit * 8;
+  const int64_t k0 = (int64_t)at.unit * E;
   uint32_t c[EACH], byte[EACH];
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     const int64_t row = at.row0 + u * blockDim.y;
     const bool there = row < M && at.unit < units;
-    c[u] = there ? *reinterpret_cast<const uint32_t*>(codes + row * ldc + (int64_t)at.unit * 4) : 0u;
-    byte[u] = there ? scales[row * lds + (at.unit >> 2)] : 0u;
+    c[u] = there ? *reinterpret_cast<const Codes*>(codes + row * ldc + (int64_t)at.unit * (E / 2)) : 0u;
+    byte[u] = there ? scales[row * lds + at.unit / (kMxBlock / E)] : 0u;
   }
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
@@ -121,25 +127,34 @@ mx_dequantize_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, i
     mx_elements8(c[u], v);
     const float s = mx_scale_value(byte[u]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], s);
+    for (int i = 0; i < E; ++i) v[i] = __fmul_rn(v[i], s);
     T* p = out + row * ldo + k0;
-    if (VEC && k0 + 8 <= K) {
-      if (row < M) store8(p, v);
+    if (VEC && k0 + E <= K) {
+      if (row < M) {
+        if constexpr (E == 8) *reinterpret_cast<uint4*>(p) = pack8<T>(v);
+        else *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+      }
     } else if (VEC) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < E; ++i)
         if (row < M && k0 + i < K) p[i] = from_f32<T>(v[i]);
     } else {
-      const int n = blockDim.x * 8;
-      T* line = s_out + threadIdx.y * n;
-      const int64_t from = (int64_t)blockIdx.y * n;
-      __syncthreads();
+      T* line = s_out + (u * blockDim.y + threadIdx.y) * blockDim.x * E;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) line[threadIdx.x * 8 + i] = from_f32<T>(v[i]);
-      __syncthreads();
-      if (row < M)
-        for (int e = threadIdx.x; e < n; e += blockDim.x)
-          if (from + e < K) out[row * ldo + from + e] = line[e];
+      for (int i = 0; i < E; ++i) line[threadIdx.x * E + i] = from_f32<T>(v[i]);
+    }
+  }
+  if (!VEC) {
+    __syncthreads();
+    const int n = blockDim.x * E;
+    const int64_t from = (int64_t)blockIdx.y * n + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      const int64_t row = at.row0 + u * blockDim.y;
+      const T* line = s_out + (u * blockDim.y + threadIdx.y) * n + threadIdx.x;
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (row < M && from + i * blockDim.x < K) out[row * ldo + from + i * blockDim.x] = line[i * blockDim.x];
     }
   }
 }
@@ -158,10 +173,10 @@ struct Shape {
   dim3 grid, block;
   bool each;           // kRowsEach rows a thread
 };
-Shape shape_of(int64_t rows, uint32_t units) {
+Shape shape_of(int64_t rows, uint32_t units, uint32_t threads) {
   uint32_t x = 32;
-  while (x < kMxThreads && x < units) x *= 2;
-  const uint32_t y = kMxThreads / x, columns = (units + x - 1) / x;
+  while (x < threads && x < units) x *= 2;
+  const uint32_t y = threads / x, columns = (units + x - 1) / x;
   const bool each = (rows + y - 1) / y * columns >= 8 * (int64_t)current_sm_count();    // every SM full without
   const int64_t per = each ? (int64_t)y * kRowsEach : y;
   return {dim3((unsigned)((rows + per - 1) / per), columns), dim3(x, y), each};
@@ -171,9 +186,10 @@ template <typename T>
 lcd_status quantize_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc,
                          uint8_t* scales, int64_t lds, cudaStream_t s) {
   const uint32_t units = (uint32_t)((K + kMxBlock - 1) / kMxBlock * 4);
-  const Shape q = shape_of(M, units);
+  const bool vec = on16(x, ldx, sizeof(T), M);
+  // (2048 x 5120 bf16: 128 threads 7.8 us, 256 8.9; through shared memory, 333 x 5001, 5.1 and 4.2)
+  const Shape q = shape_of(M, units, vec ? kMxThreads / 2 : kMxThreads);
   if (q.grid.y > 65535) return LCD_ERR_UNSUPPORTED;
-  const bool vec = on16(x, ldx, sizeof(T), M) && (!inv || reinterpret_cast<uintptr_t>(inv) % 16 == 0);
   auto kern = vec ? (q.each ? mx_quantize_kernel<T, true, kRowsEach> : mx_quantize_kernel<T, true, 1>)
                   : (q.each ? mx_quantize_kernel<T, false, kRowsEach> : mx_quantize_kernel<T, false, 1>);
   return launched(launch_overlapping(kern, q.grid, q.block, 0, 1, s, static_cast<const T*>(x), M, K, ldx, inv, codes, ldc, scales, lds, units));
@@ -182,8 +198,9 @@ lcd_status quantize_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const
 template <typename T>
 lcd_status dequantize_rows(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K, void* out,
                            int64_t ldo, cudaStream_t s) {
-  const uint32_t units = (uint32_t)((K + 7) / 8);
-  const Shape q = shape_of(M, units);
+  constexpr int E = 16 / sizeof(T);
+  const uint32_t units = (uint32_t)((K + E - 1) / E);
+  const Shape q = shape_of(M, units, kMxThreads);
   if (q.grid.y > 65535) return LCD_ERR_UNSUPPORTED;
   const bool vec = on16(out, ldo, sizeof(T), M);
   auto kern = vec ? (q.each ? mx_dequantize_kernel<T, true, kRowsEach> : mx_dequantize_kernel<T, true, 1>)
