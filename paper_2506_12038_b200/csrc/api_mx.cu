@@ -22,8 +22,6 @@ bool mx_rows(const void* codes, int64_t ldc, const void* scales, int64_t lds, in
 bool dense_rows(const void* p, lcd_dtype t, int64_t rows, int64_t columns, int64_t ld) {
   return p && known(t) && rows >= 1 && rows <= kMostRows && columns >= 1 && columns <= kMostColumns && ld >= columns && aligned(p, size_of(t));
 }
-// A launch's CTAs are numbered in 31 bits; 256 threads take 2048 columns.
-bool countable(int64_t rows, int64_t columns) { return rows * ((columns + 2047) / 2048) <= 0x7fffffffLL; }
 
 lcd_status distillation(const Distillation& d) {
   if (!dense_rows(d.logits, d.type, d.T, d.V, d.ldz) || !d.teacher_idx || !known(d.teacher_type) || d.k < 1) return LCD_ERR_INVALID_ARG;
@@ -46,14 +44,12 @@ using namespace lcd;
 extern "C" lcd_status lcd_mx_quantize(const void* x, lcd_dtype x_type, int64_t M, int64_t K, int64_t ldx, const float* inv_smooth,
                                       uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, void* cuda_stream) {
   if (!dense_rows(x, x_type, M, K, ldx) || !mx_rows(codes, ldc, scales, lds, M, K) || !aligned(inv_smooth, 4)) return LCD_ERR_INVALID_ARG;
-  if (!countable(M, K)) return LCD_ERR_UNSUPPORTED;
   return launch_mx_quantize(x, x_type, M, K, ldx, inv_smooth, codes, ldc, scales, lds, cuda_stream);
 }
 
 extern "C" lcd_status lcd_mx_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K,
                                         void* out, lcd_dtype out_type, int64_t ldo, void* cuda_stream) {
   if (!dense_rows(out, out_type, M, K, ldo) || !mx_rows(codes, ldc, scales, lds, M, K)) return LCD_ERR_INVALID_ARG;
-  if (!countable(M, K)) return LCD_ERR_UNSUPPORTED;
   return launch_mx_dequantize(codes, ldc, scales, lds, M, K, out, out_type, ldo, cuda_stream);
 }
 
@@ -82,7 +78,6 @@ extern "C" lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, 
       !aligned(inv_smooth, 4) || !aligned(workspace, 16) || !aligned(status_word_dev, 4) ||
       lcd_mx_linear_fused_workspace_bytes(M, K, &need) != LCD_OK)
     return LCD_ERR_INVALID_ARG;
-  if (!countable(M, K)) return LCD_ERR_UNSUPPORTED;
   if (need > 0 && (!workspace || workspace_bytes < need)) return LCD_ERR_BUFFER_TOO_SMALL;
   if (mx_linear_quantizes(M, K))
     return launch_mx_linear({w_codes, w_scales, nullptr, nullptr, ldwc, ldws, 0, 0, N, K, M, y, y_type, ldy, x, x_type, ldx, inv_smooth},

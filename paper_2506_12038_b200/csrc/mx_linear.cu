@@ -51,7 +51,10 @@ struct Cfg {
   static constexpr int kPerSm = BN <= 64 ? 2 : 1;
   static constexpr int kEpiHalves = kDBuffers == 1 ? 2 : 1;              // the one accumulator is drained by twice the warps
   static constexpr int kThreads = 32 * (11 + 4 * (kEpiHalves - 1));
+  // Whatever shares an SM has tensor memory enough, so that no CTA of a cluster waits for columns while another CTA of it holds some:
+  // two of the narrow tiles fit, and beside a wide one nothing does (shared memory).
   static_assert(kUsed <= kTmemCols && kTmemCols * kPerSm <= 512, "tensor memory");
+  static_assert(kPerSm == 2 || kSmem > 128 * 1024, "one CTA an SM");
   static_assert(kSmem <= 227 * 1024 && kPerSm * (kSmem + 1024) <= 228 * 1024, "shared memory");
   static_assert(BN * 512 <= kStages * (kAStage + kBStage), "partial sums lie in the stages");
 };

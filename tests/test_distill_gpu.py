@@ -291,3 +291,34 @@ def test_updates_of_a_clustered_head():
     x = torch.from_numpy(L.x).cuda().float() * torch.from_numpy(L.inv_s).cuda()
     new, _, counts = lcd.reclassify(torch.from_numpy(L.idx).cuda(), torch.from_numpy(np.sort(L.codebook, axis=1)).cuda(), -0.01 * (dy.t() @ x))
     assert new.shape == (300, 256) and (counts.sum(dim=1) == 256).all()
+
+
+def test_offsets_beyond_32_bits():
+    T, V, k = 20_000, 110_011, 8                     # 2.2e9 logits
+    z = torch.empty(T, V, dtype=torch.bfloat16, device="cuda").normal_()
+    idx = torch.randint(0, V, (T, k), device="cuda")
+    top = torch.randn(T, k, device="cuda")
+    rows = [0, 9, T - 1]
+    keep = z[rows].clone()
+    loss, stats = lcd.distill_loss(z, idx, top, want_stats=True)
+    both, grad = lcd.distill_loss(z, idx, top, dlogits=z)
+    assert grad is z
+    check(keep, idx[rows], top[rows], loss=loss[rows], stats=stats[rows])
+    check(keep, idx[rows], top[rows], loss=both[rows], grad=z[rows])
+
+
+def test_calls_of_several_threads_and_streams_at_once():
+    import concurrent.futures
+    sizes = [(3, 60000, 20), (64, 5000, 300), (700, 9001, 64), (40, 40000, 5)]
+    made = [make(i, T, V, k, "bf16")[:3] for i, (T, V, k) in enumerate(sizes)]
+    want = [lcd.distill_loss(*m, want_grad=True) for m in made]
+    torch.cuda.synchronize()
+
+    def loop(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            got = [lcd.distill_loss(*made[i], want_grad=True) for _ in range(30)]
+            stream.synchronize()
+            return all(torch.equal(a, b) for g in got for a, b in zip(g, want[i]))
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:
+        assert all(pool.map(loop, range(4)))

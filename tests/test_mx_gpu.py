@@ -243,9 +243,10 @@ def test_weights_that_the_call_before_wrote(M):
             assert torch.equal(lcd.mx_linear_fused(codes, scales, x), y)
 
 
-def test_on_another_stream_and_in_a_graph():
+@pytest.mark.parametrize("M", [3, 40])           # one launch, two
+def test_on_another_stream_and_in_a_graph(M):
     w = random_mx(3, 500, 1000)
-    xs = [random_x(s, 3, 1000) for s in (1, 2)]
+    xs = [random_x(s, M, 1000) for s in (1, 2)]
     want = [lcd.mx_linear_fused(w[0], w[1], x) for x in xs]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -268,3 +269,61 @@ def test_status_word_untouched():
     word = torch.full((1,), 7, dtype=torch.int32, device="cuda")
     lcd.mx_linear(w[0], w[1], x[0], x[1], status_word=word)
     assert word.item() == 7
+
+
+def test_offsets_beyond_32_bits():
+    # 2.3 GB of codes: rows behind the 2^31st byte, against the same rows alone (whole-number sums, exact in any order)
+    N, K = 140_032, 32768
+    codes = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.full((N, K // 32), 127, dtype=torch.uint8, device="cuda")
+    x = random_mx(1, 3, K)
+    x[1].fill_(127)
+    y = lcd.mx_linear(codes, scales, x[0], x[1])
+    for lo in (0, 65536, N - 300):
+        part = lcd.mx_linear(codes[lo:lo + 300], scales[lo:lo + 300], x[0], x[1])
+        assert torch.equal(y[:, lo:lo + 300], part)
+    v = lcd.mx_dequantize(codes, scales, dtype=torch.bfloat16)         # 4.6e9 values
+    assert torch.equal(v[N - 2:], lcd.mx_dequantize(codes[N - 2:], scales[N - 2:], dtype=torch.bfloat16))
+    again = lcd.mx_quantize(v)
+    assert torch.equal(lcd.mx_dequantize(*again, dtype=torch.bfloat16)[N - 2:], v[N - 2:])
+    wide = torch.zeros(2, 2 ** 31 + 64, dtype=torch.bfloat16, device="cuda")[:, :100]     # rows further apart than 2^31 elements
+    wide.copy_(v[:2, :100])
+    c, s = lcd.mx_quantize(wide)
+    assert torch.equal(lcd.mx_dequantize(c, s, 100, dtype=torch.bfloat16), lcd.mx_dequantize(*lcd.mx_quantize(wide.contiguous()), 100, dtype=torch.bfloat16))
+
+
+def test_calls_of_several_threads_and_streams_at_once():
+    import concurrent.futures
+    work = [(1, 700, 3000), (12, 384, 4096), (50, 500, 1000), (300, 512, 2048)]
+    w = [random_mx(i, N, K) for i, (M, N, K) in enumerate(work)]
+    x = [random_x(i, M, K, "bf16") for i, (M, N, K) in enumerate(work)]
+    want = [lcd.mx_linear_fused(a[0], a[1], b) for a, b in zip(w, x)]
+    torch.cuda.synchronize()
+
+    def loop(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            got = [lcd.mx_linear_fused(w[i][0], w[i][1], x[i]) for _ in range(50)]
+            stream.synchronize()
+            return all(torch.equal(g, want[i]) for g in got)
+    with concurrent.futures.ThreadPoolExecutor(4) as pool:
+        assert all(pool.map(loop, range(4)))
+
+
+def test_between_the_lookup_kernels():
+    # kernels that begin before the one ahead of them has ended, of both kinds, in turn
+    from synth import gen
+    L = gen.random_case(seed=9, N=512, K=2048, bits=3, M=12)
+    pw = lcd.PackedWeights(lcd.pack_weights(L.idx, L.codebook, 3))
+    xh, inv = torch.from_numpy(L.x).cuda(), torch.from_numpy(L.inv_s).cuda()
+    w = random_mx(2, 512, 2048)
+
+    def both():
+        a, s = lcd.smooth_quantize_act(xh, inv)
+        y = lcd.lut_linear(pw, a, s)
+        z = lcd.mx_linear_fused(w[0], w[1], y[:, :512].repeat(1, 4), inv)
+        return y, z, lcd.mx_linear_fused(w[0], w[1], xh, inv)
+    want = both()
+    torch.cuda.synchronize()
+    for _ in range(30):
+        assert all(torch.equal(g, v) for g, v in zip(both(), want))
