@@ -9,6 +9,9 @@
  *
  *      y[m][n] = s_q[m] * sum_k q[m][k] * cb[n][idx[n][k]]          (fp32)
  *
+ * Beside it stand what makes such layers offline (smoothing search, centroid initialisation, distillation loss, reclassification) and
+ * the product of layers in microscaled 4-bit floating point.
+ *
  * Conventions for every function:
  *   - returns an lcd_status; never aborts, traps or throws;
  *   - "host" / "device" in a parameter comment says where the pointer must point;
