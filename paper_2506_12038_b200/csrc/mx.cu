@@ -112,19 +112,21 @@ mx_dequantize_kernel(const uint8_t* codes, int64_t ldc, const uint8_t* scales, i
   __shared__ T s_out[VEC ? 1 : EACH * kMxThreads * E];
   const Place at = place<EACH>();
   const int64_t k0 = (int64_t)at.unit * E;
-  uint32_t c[EACH], byte[EACH];
+  Codes c[EACH];
+  uint32_t byte[EACH];
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     const int64_t row = at.row0 + u * blockDim.y;
     const bool there = row < M && at.unit < units;
-    c[u] = there ? *reinterpret_cast<const Codes*>(codes + row * ldc + (int64_t)at.unit * (E / 2)) : 0u;
+    c[u] = there ? *reinterpret_cast<const Codes*>(codes + row * ldc + (int64_t)at.unit * (E / 2)) : Codes(0);
     byte[u] = there ? scales[row * lds + at.unit / (kMxBlock / E)] : 0u;
   }
 #pragma unroll
   for (int u = 0; u < EACH; ++u) {
     const int64_t row = at.row0 + u * blockDim.y;
-    float v[8];
-    mx_elements8(c[u], v);
+    float v[E];
+    if constexpr (E == 8) mx_elements8(c[u], v);
+    else mx_elements4(c[u], v);
     const float s = mx_scale_value(byte[u]);
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = __fmul_rn(v[i], s);
