@@ -177,6 +177,63 @@ __device__ __forceinline__ void scales_to_tmem(const uint8_t* rows, uint32_t tad
   for (int i = 0; i < 4 * COLS; i += 16) tmem_st16(taddr + i, v + i);
 }
 
+// store(first column, 16 columns' sums) for the accumulator's columns begin .. end - 1 of this warp's lanes.  AHEAD: the next columns are on
+// their way while these are stored (two CTAs an SM have no registers for it).
+template <bool AHEAD, typename Store>
+__device__ __forceinline__ void drain_columns(uint32_t from, int begin, int end, Store&& store) {
+  uint32_t v[16], w[16];
+  if (begin >= end) return;
+  if (!AHEAD) {
+#pragma unroll 1
+    for (int c = begin; c < end; c += 16) {
+      tmem_ld16(from + c, v);
+      asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+      store(c, v);
+    }
+    return;
+  }
+  tmem_ld16(from + begin, v);
+#pragma unroll 1
+  for (int c = begin;; c += 32) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    if (c + 16 < end) tmem_ld16(from + c + 16, w);
+    store(c, v);
+    if (c + 16 >= end) break;
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    if (c + 32 < end) tmem_ld16(from + c + 32, v);
+    store(c + 16, w);
+    if (c + 32 >= end) break;
+  }
+}
+// The same to y: this lane's weight row n, tokens m0 + begin .. m0 + end - 1.
+template <bool AHEAD>
+__device__ __forceinline__ void store_columns(const Args& P, uint32_t from, int begin, int end, int m0, int n) {
+  by_type(P, [&](auto* y) {
+    using T = std::remove_pointer_t<decltype(y)>;
+    T* at = y + (size_t)(m0 + begin) * P.ldy + n;
+    const bool inside = n < P.N;
+    drain_columns<AHEAD>(from, begin, end, [&](int c, const uint32_t (&v)[16]) {
+      // (the address is kept from being formed for all sixteen at once, which takes 32 registers)
+      if (!inside) return;
+      if (c + 16 <= end) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          *at = from_f32<T>(__uint_as_float(v[j]));
+          at += P.ldy;
+          asm volatile("" : "+l"(at));
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (c + j < end) *at = from_f32<T>(__uint_as_float(v[j]));
+          at += P.ldy;
+          asm volatile("" : "+l"(at));
+        }
+      }
+    });
+  });
+}
+
 // Eight columns of a token from k on, zeros beyond K.  `raw` holds them where they lie on 16 bytes inside the row.
 template <typename X>
 __device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8<X>& raw, float (&t)[8]) {
@@ -451,65 +508,16 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       ok = __all_sync(0xffffffffu, bar_wait(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      // The next columns are on their way while these are stored.
       const uint32_t from = tmem + quarter + buf * BN;
       const int begin = warp > kScaleCopyWarp ? BN / 2 : 0, end = C::kEpiHalves == 2 && !begin ? min(tokens, BN / 2) : tokens;
-      auto drain_tile = [&](auto&& store) {       // store(first token of the tile, 16 tokens' sums)
-        uint32_t v[16], w[16];
-        if (begin >= end) return;
-        if (BN <= 64) {                           // (two CTAs an SM have no registers for it)
-#pragma unroll 1
-          for (int c = 0; c < tokens; c += 16) {
-            tmem_ld16(from + c, v);
-            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-            store(c, v);
-          }
-          return;
-        }
-        tmem_ld16(from + begin, v);
-#pragma unroll 1
-        for (int c = begin;; c += 32) {
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (c + 16 < end) tmem_ld16(from + c + 16, w);
-          store(c, v);
-          if (c + 16 >= end) break;
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-          if (c + 32 < end) tmem_ld16(from + c + 32, v);
-          store(c + 16, w);
-          if (c + 32 >= end) break;
-        }
-      };
       if (split > 1) {            // every copy into the stages has landed and been read: they hold the partial sums
         float* part = reinterpret_cast<float*>(gen) + 32 * quad + lane;
-        drain_tile([&](int c, const uint32_t (&v)[16]) {
+        drain_columns<(BN > 64)>(from, begin, end, [&](int c, const uint32_t (&v)[16]) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) part[(c + j) * kRows] = __uint_as_float(v[j]);
         });
       } else {
-        by_type(P, [&](auto* y) {
-          using T = std::remove_pointer_t<decltype(y)>;
-          T* at = y + (size_t)(m0 + begin) * P.ldy + n;
-          const bool inside = n < P.N;
-          drain_tile([&](int c, const uint32_t (&v)[16]) {
-            // (the address is kept from being formed for all sixteen at once, which takes 32 registers)
-            if (!inside) return;
-            if (c + 16 <= tokens) {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                *at = from_f32<T>(__uint_as_float(v[j]));
-                at += P.ldy;
-                asm volatile("" : "+l"(at));
-              }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                if (c + j < tokens) *at = from_f32<T>(__uint_as_float(v[j]));
-                at += P.ldy;
-                asm volatile("" : "+l"(at));
-              }
-            }
-          });
-        });
+        store_columns<(BN > 64)>(P, from, begin, end, m0, n);
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -564,6 +572,274 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
 }
 
+// ---------------------------------------------------------------------------------------------------------
+// Many tokens: a pair of CTAs shares a tile of 256 weight rows x BN tokens (cta_group::2).  Each brings its own 128 rows of the weights
+// and half of the tokens into its shared memory; the instruction reads both halves of the tokens for either CTA's rows.  So a CTA
+// writes and reads 16 KB + BN / 2 rows a stage where it alone would need BN rows: shared memory's bandwidth, what bounds
+// the kernel above, is enough (256 tokens: 128 bytes a clock).  Roles as above; the MMAs are issued by the pair's first CTA, the second
+// one's warp 1 tells it of its copies.  The tokens' scales are needed by both and lie in both CTAs' tensor memory.
+template <int BN>
+struct PairCfg {
+  static constexpr int kBStage = BN / 2 * kStageK / 2;
+  static constexpr int kStages = 6;
+  static constexpr int kScaleBytes = (kRows + BN) * 16;
+  static constexpr int kSfCols = Cfg<BN>::kSfCols, kSfbCols = Cfg<BN>::kSfbCols, kSfSlots = BN == 256 ? 5 : 2;
+  static constexpr int kDBuffers = 2 * BN + kSfSlots * kSfCols <= 512 ? 2 : 1;
+  static constexpr int kEpiHalves = 2;
+  static constexpr int kThreads = 32 * 15;
+  static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 512;
+  static_assert(kDBuffers * BN + kSfSlots * kSfCols <= 512 && kSmem <= 227 * 1024 && kSmem > 128 * 1024, "one CTA an SM");
+};
+
+__device__ __forceinline__ bool bar_try_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// bar_wait for barriers that the other CTA arrives at.
+__device__ __forceinline__ bool bar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (bar_try_cluster(bar, parity)) return true;
+  const unsigned long long t0 = timer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (bar_try_cluster(bar, parity)) return true;
+    if ((it & 255u) == 0) {
+      if (*abort_flag) return false;
+      if (timer_ns() - t0 > kWaitNs) { *abort_flag = 1; return false; }
+    }
+  }
+}
+// Arrives at the first CTA's barrier of the pair.  (No release at cluster scope: what it tells of, copies that have landed and tensor memory
+// that has been written or read, is ordered by the waits and fences before it; with it a stage took 0.9 us.)
+__device__ __forceinline__ void bar_arrive_first(uint32_t bar) {
+  asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %0, 0;\nmbarrier.arrive.shared::cluster.b64 _, [a];\n}" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma_mx_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %6, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+// At both CTAs' barriers, once the MMAs so far have finished.
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+
+template <int BN>
+__global__ void __launch_bounds__(PairCfg<BN>::kThreads, 1)
+mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+               const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const Args P) {
+  using C = PairCfg<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw_addr = (uint32_t)__cvta_generic_to_shared(smem_raw);
+  const uint32_t base = (raw_addr + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - raw_addr);
+  constexpr uint32_t kScaleAt = C::kStages * (kAStage + C::kBStage), kBarAt = kScaleAt + kScaleSlots * C::kScaleBytes;
+  const uint32_t a_base = base, b_base = base + C::kStages * kAStage, s_base = base + kScaleAt, bars = base + kBarAt;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (C::kStages + s); };
+  auto sc_full = [&](int s) { return bars + 8u * (2 * C::kStages + s); };
+  auto sc_empty = [&](int s) { return bars + 8u * (2 * C::kStages + kScaleSlots + s); };
+  constexpr int kB0 = 2 * C::kStages + 2 * kScaleSlots, kB1 = kB0 + 2 * C::kSfSlots;
+  auto ts_full = [&](int b) { return bars + 8u * (kB0 + b); };
+  auto ts_empty = [&](int b) { return bars + 8u * (kB0 + C::kSfSlots + b); };
+  auto d_full = [&](int b) { return bars + 8u * (kB1 + b); };
+  auto d_empty = [&](int b) { return bars + 8u * (kB1 + 2 + b); };
+  const uint32_t drain = bars + 8u * (kB1 + 4);
+  static_assert(8 * (kB1 + 5) + 8 <= 512, "barriers");
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + kBarAt + 8 * (kB1 + 5));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  uint32_t rank;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const bool first = rank == 0;
+  const int tile0 = blockIdx.x / 2, tile_step = gridDim.x / 2;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      bar_init(full(s), first ? 2 : 1);              // the first CTA's: its own copies, and word of the other's
+      bar_init(empty(s), 1);
+    }
+    for (int s = 0; s < kScaleSlots; ++s) {
+      bar_init(sc_full(s), 1);
+      bar_init(sc_empty(s), 4);
+    }
+    for (int b = 0; b < C::kSfSlots; ++b) {
+      bar_init(ts_full(b), 8);                       // both CTAs' warps
+      bar_init(ts_empty(b), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      bar_init(d_full(b), 1);
+      bar_init(d_empty(b), 2 * 4 * C::kEpiHalves);
+    }
+    bar_init(drain, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;"
+                 ::"r"((uint32_t)__cvta_generic_to_shared(tmem_holder)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");      // both CTAs' barriers and tensor memory are there
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *tmem_holder;
+  const uint32_t sf_tmem = tmem + C::kDBuffers * BN;
+
+  if (warp == 0 || warp == kScaleCopyWarp) {
+    const bool codes = warp == 0;
+    if (elect()) {
+      const int to = codes ? P.n_ks : P.n_ss, slots = codes ? C::kStages : kScaleSlots;
+      const uint32_t bytes = codes ? kAStage + C::kBStage : C::kScaleBytes;
+      auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
+      auto copy_w = [&](int s, int k, int row) {
+        if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full(s));
+        else copy_tile(s_base + s * C::kScaleBytes, &map_ws, k * 16, row, sc_full(s));
+      };
+      auto copy_x = [&](int s, int k, int row) {
+        if (codes) copy_tile(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), row + (int)rank * (BN / 2), full(s));
+        else copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, row, sc_full(s));
+      };
+      const int ahead = P.early && tile0 < P.n_tiles ? min(slots, to) : 0;
+      for (int i = 0; i < ahead; ++i) {
+        bar_expect_tx(full_of(i), bytes);
+        copy_w(i, i, tile0 / P.n_tiles_m * 2 * kRows + (int)rank * kRows);
+      }
+      begin_after_previous();
+      int it = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step) {
+        const int n0 = tile / P.n_tiles_m * 2 * kRows + (int)rank * kRows, m0 = tile % P.n_tiles_m * BN;
+        for (int k = 0; k < to; ++k, ++it) {
+          const int s = it % slots;
+          if (it >= ahead) {
+            ok = codes ? bar_wait_cluster(empty(s), ((it / slots) & 1u) ^ 1u, abort_flag) : bar_wait(sc_empty(s), ((it / slots) & 1u) ^ 1u, abort_flag);
+            if (!ok) break;
+            bar_expect_tx(full_of(s), bytes);
+            copy_w(s, k, n0);
+          }
+          copy_x(s, k, m0);
+        }
+      }
+      // nothing this thread issued may be in flight when the CTA exits
+      const int back = min(it, slots);
+      for (int i = 1; i <= back; ++i) bar_drain(full_of((it - i) % slots), ((it - i) / slots) & 1u);
+    }
+    __syncwarp();
+  } else if (warp == kMmaWarp) {
+    if (elect()) {
+      bool ok = true;
+      if (!first) {
+        // the other CTA's copies, stage by stage
+        uint32_t it = 0;
+        for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step)
+          for (int k = 0; k < P.n_ks; ++k, ++it) {
+            ok = bar_wait(full(it % C::kStages), (it / C::kStages) & 1u, abort_flag);
+            if (!ok) break;
+            bar_arrive_first(full(it % C::kStages));
+          }
+        bar_drain(drain, 0);
+      } else {
+        constexpr uint32_t kM = (uint32_t)(2 * kRows >> 4) << 24 ^ (uint32_t)(kRows >> 4) << 24;     // M = 256 in place of 128
+        constexpr uint32_t idesc[2] = {instr_desc(BN, 0) ^ kM, instr_desc(BN, 1) ^ kM};
+        const uint64_t a_desc0 = smem_desc(a_base), b_desc0 = smem_desc(b_base);
+        uint32_t it = 0, sit = 0, tl = 0;
+        for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+          const uint32_t buf = tl % C::kDBuffers;
+          ok = bar_wait_cluster(d_empty(buf), ((tl / C::kDBuffers) & 1u) ^ 1u, abort_flag);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t d = tmem + buf * BN;
+          for (int ss = 0; ss < P.n_ss && ok; ++ss, ++sit) {
+            const uint32_t sb = sit % C::kSfSlots;
+            ok = bar_wait_cluster(ts_full(sb), (sit / C::kSfSlots) & 1u, abort_flag);
+            if (!ok) break;
+            const uint32_t sfa = sf_tmem + sb * C::kSfCols, sfb = sfa + 16;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (2 * ss + h >= P.n_ks) break;
+              const uint32_t slot = it % C::kStages;
+              ok = bar_wait_cluster(full(slot), (it / C::kStages) & 1u, abort_flag);
+              if (!ok) break;
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              const uint64_t ad = a_desc0 + (uint64_t)(slot * kAStage >> 4), bd = b_desc0 + (uint64_t)(slot * C::kBStage >> 4);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                mma_mx_pair(d, ad + 2 * i, bd + 2 * i, idesc[i & 1], sfa + (2 * h + i / 2) * 4, sfb + (2 * h + i / 2) * C::kSfbCols,
+                            (uint32_t)(ss != 0 || h != 0 || i != 0));
+              mma_commit_pair(empty(slot));
+              ++it;
+            }
+            mma_commit_pair(ts_empty(sb));
+          }
+          if (ok) mma_commit_pair(d_full(buf));
+        }
+        // every MMA must have finished before tensor memory is released, the other CTA's too
+        mma_commit_pair(drain);
+        bar_drain(drain, 0);
+      }
+    }
+    __syncwarp();
+  } else if (warp < kFirstEpiWarp) {
+    const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16;
+    uint32_t sit = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step)
+      for (int ss = 0; ss < P.n_ss; ++ss, ++sit) {
+        const uint32_t slot = sit % kScaleSlots, sb = sit % C::kSfSlots;
+        ok = __all_sync(0xffffffffu, bar_wait(sc_full(slot), (sit / kScaleSlots) & 1u, abort_flag) &&
+                                         bar_wait_cluster(ts_empty(sb), ((sit / C::kSfSlots) & 1u) ^ 1u, abort_flag));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint8_t* rows = gen + kScaleAt + slot * C::kScaleBytes;
+        const uint32_t at = sf_tmem + sb * C::kSfCols + quarter;
+        scales_to_tmem<4, 4>(rows, at, lane);
+        scales_to_tmem<BN / 32, C::kSfbCols>(rows + kRows * 16, at + 16, lane);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          bar_arrive(sc_empty(slot));
+          bar_arrive_first(ts_full(sb));
+        }
+        __syncwarp();
+      }
+  } else {
+    const int quad = warp & 3;
+    const uint32_t quarter = (uint32_t)(32 * quad) << 16;
+    const int begin = warp > kScaleCopyWarp ? BN / 2 : 0;
+    uint32_t tl = 0;
+    bool ok = true;
+    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+      const uint32_t buf = tl % C::kDBuffers;
+      const int n = tile / P.n_tiles_m * 2 * kRows + (int)rank * kRows + 32 * quad + lane, m0 = tile % P.n_tiles_m * BN;
+      const int tokens = min(BN, P.M - m0);
+      ok = __all_sync(0xffffffffu, bar_wait_cluster(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      store_columns<true>(P, tmem + quarter + buf * BN, begin, begin ? tokens : min(tokens, BN / 2), m0, n);
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) bar_arrive_first(d_empty(buf));
+      __syncwarp();
+    }
+  }
+  // neither CTA leaves while the other may still read its shared memory or arrive at its barriers
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+  if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
+}
+
 bool encode_rows(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t rows, int64_t ld, int box_bytes, int box_rows, bool swizzled) {
   const EncodeTiledFn encode = encode_tiled();
   const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld};
@@ -573,30 +849,33 @@ bool encode_rows(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t rows
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a product is cut: the width of the token tiles and the CTAs that share a tile's columns.
-struct Plan { int width, split; };
+// How a product is cut: the width of the token tiles, whether a pair of CTAs shares one, or how many share its columns.
+struct Plan { int width, split; bool pair; };
 
-// Estimated in microseconds, from products timed alone on B200: 0.31 to 0.39 a stage (bound by shared memory's bandwidth: operands are
-// written once and read by the tensor core), an epilogue that only the widest tile cannot overlap with the next one's columns, and for a
-// shared tile the cluster's barrier and 1 us a 64 tokens to add up.  512 x 5120 x 5120: 192 tokens 12.2, 256 13.9, 128 17.8; 2048 x
-// 13824 x 5120: 68 with 256, 75 with 192; 333 x 5003 x 5001 14.7 with 128, 20.5 with 256; 1 x 4096 x 4096: 8.6 / 7.1 / 6.0 / 7.2
-// with 1 / 2 / 4 / 8 CTAs a tile, the last being more than one an SM.
+// Estimated in microseconds, from products timed alone on B200: 0.31 to 0.39 a stage, an epilogue that only the widest tile cannot
+// overlap with the next one's columns, for a shared tile the cluster's barrier and 1 us a 64 tokens to add up.  Pairs: 4096 x 8192 x
+// 8192 to bf16 96 us with 256 tokens, single CTAs 108; 2048 x 13824 x 5120 57 and 64 (192 tokens 64, in nine rounds); 2048 x 5120 x
+// 13824 58 with 192, single CTAs 62; 333 x 5003 x 5001 13.3 to 15.2, single CTAs of 128 tokens 13.3.  Single ones: 512 x 5120 x 5120
+// 12.2 with 192 tokens, 13.9 with 256, 17.8 with 128; 1 x 4096 x 4096 8.6 / 7.1 / 6.0 / 7.2 with 1 / 2 / 4 / 8 CTAs a tile, the last
+// being more than one an SM.
 Plan plan(int64_t M, int64_t N, int64_t n_ks) {
-  static constexpr struct { int width; double stage, epilogue; } kWidths[] = {
-      {16, 0.33, 0.1}, {32, 0.33, 0.2}, {64, 0.34, 0.4}, {128, 0.31, 0.4}, {192, 0.39, 0.2}, {256, 0.35, 2.9}};
+  static constexpr struct { int width; double stage, epilogue; bool pair; } kWidths[] = {
+      {16, 0.33, 0.1, false}, {32, 0.33, 0.2, false}, {64, 0.34, 0.4, false}, {128, 0.31, 0.4, false},
+      {192, 0.39, 0.2, false}, {256, 0.35, 2.9, false}, {192, 0.33, 0.1, true}, {256, 0.31, 2.6, true}};
   const int64_t sms = current_sm_count(), n_ss = (n_ks + 1) / 2;
-  Plan best = {256, 1};
+  Plan best = {256, 1, false};
   double least = 1e300;
   for (const auto& w : kWidths) {
     if (M > w.width && w.width < 128) continue;           // few tokens: one tile of them
-    const int64_t tiles = (M + w.width - 1) / w.width * ((N + kRows - 1) / kRows);
-    const int64_t waves = (tiles + sms - 1) / sms;
-    for (int s = 1; s <= kMostSplit && s <= n_ss && (s == 1 || tiles * s <= sms); ++s) {
+    const int64_t rows = w.pair ? 2 * kRows : kRows, tiles = (M + w.width - 1) / w.width * ((N + rows - 1) / rows);
+    const int64_t at_once = w.pair ? sms / 2 : sms, waves = (tiles + at_once - 1) / at_once;
+    for (int s = 1; s <= (w.pair ? 1 : kMostSplit) && s <= n_ss && (s == 1 || tiles * s <= sms); ++s) {
       if (s > 4 && (w.width >= 128 || tiles * s > sms / 2)) break;      // clusters of more than four do not fill the GPU
-      const double time = waves * (2 * w.stage * ((n_ss + s - 1) / s) + w.epilogue) + (s > 1 ? 2.0 + (M < w.width ? M : w.width) / (64.0 * s) : 0.0);
+      const double time = waves * (2 * w.stage * ((n_ss + s - 1) / s) + w.epilogue) + (w.pair ? 1.0 : 0.0) +
+                          (s > 1 ? 2.0 + (M < w.width ? M : w.width) / (64.0 * s) : 0.0);
       if (time < least) {
         least = time;
-        best = {w.width, s};
+        best = {w.width, s, w.pair};
       }
     }
     if (M <= w.width && w.width < 128) break;
@@ -656,6 +935,46 @@ lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* stat
   return LCD_OK;
 }
 
+template <int BN>
+lcd_status launch_pair(const MxProduct& p, bool early, int32_t* status, cudaStream_t s) {
+  using C = PairCfg<BN>;
+  auto kern = mx_pair_kernel<BN>;
+  static PerDeviceFlag attr_set;
+  int dev;
+  if (attr_set.first(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+    attr_set.done(dev);
+  }
+  const int64_t blocks = (p.K + kMxBlock - 1) / kMxBlock;
+  const int64_t n_tiles_m = (p.M + BN - 1) / BN, tiles = n_tiles_m * ((p.N + 2 * kRows - 1) / (2 * kRows));
+  if (tiles > 0x7fffffff) return LCD_ERR_UNSUPPORTED;
+  CUtensorMap w, x, ws, xs;
+  if (!encode_rows(&w, p.w_codes, blocks * 16, p.N, p.ldwc, kStageK / 2, kRows, true) ||
+      !encode_rows(&ws, p.w_scales, blocks, p.N, p.ldws, 16, kRows, false) ||
+      !encode_rows(&x, p.x_codes, blocks * 16, p.M, p.ldxc, kStageK / 2, BN / 2, true) ||
+      !encode_rows(&xs, p.x_scales, blocks, p.M, p.ldxs, 16, BN, false)) {
+    set_cuda_error((int)cudaErrorInvalidValue);
+    return LCD_ERR_CUDA;
+  }
+  Args a = {};
+  a.y = p.y;
+  a.ldy = p.ldy;
+  a.y_type = (int)p.y_type;
+  a.M = (int)p.M;
+  a.N = (int)p.N;
+  a.n_ks = (int)((blocks * kMxBlock + kStageK - 1) / kStageK);
+  a.n_ss = (a.n_ks + 1) / 2;
+  a.n_tiles_m = (int)n_tiles_m;
+  a.n_tiles = (int)tiles;
+  a.early = early;
+  a.status = status;
+  const int64_t pairs = current_sm_count() / 2;
+  const cudaError_t e = launch_overlapping(kern, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(C::kThreads), C::kSmem, 2u, s, w, x, ws, xs, a);
+  if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+  return LCD_OK;
+}
+
 }  // namespace
 
 // (4 x 8192 x 28672 35 us, 27 with two launches; 1 x 8192 x 28672 27.1 and 26.8; 4 x 4096 x 4096 6.7 and 6.6)
@@ -671,6 +990,7 @@ lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* st
       default: return launch_width<16, __nv_bfloat16>(p, w.split, false, status_word, s);
     }
   }
+  if (w.pair) return w.width == 192 ? launch_pair<192>(p, x_just_written, status_word, s) : launch_pair<256>(p, x_just_written, status_word, s);
   switch (w.width) {
     case 16: return launch_width<16>(p, w.split, x_just_written, status_word, s);
     case 32: return launch_width<32>(p, w.split, x_just_written, status_word, s);

@@ -60,6 +60,19 @@ def test_quantize_bit_exact(type, M, K, pitch, smooth):
     assert codes.shape == (M, 16 * -(-K // 32)) and scales.shape == (M, -(-K // 32)) and scales.stride(0) % 16 == 0
 
 
+@pytest.mark.parametrize("type", sorted(TYPES))
+@pytest.mark.parametrize("M,K,pitch", [(9600, 40, 0), (5000, 256, 0), (1300, 1100, 0), (1300, 1101, 0), (1237, 2050, 6), (700, 4097, 3)])
+def test_many_rows(type, M, K, pitch):
+    # several rows a thread, aligned and not, there and back
+    x = random_x(M + K, M, K, type, pitch)
+    codes, scales = check_quantize(x)
+    v = O.mx_values(codes.cpu().numpy(), scales.cpu().numpy(), K)
+    for out in sorted(TYPES):
+        room = torch.full((M + 1, K + pitch), 7.0, dtype=TYPES[out], device="cuda")
+        lcd.mx_dequantize(codes, scales, K, out=room[:M, :K])
+        assert torch.equal(room[:M, :K], torch.from_numpy(v).cuda().to(TYPES[out])) and (room[M] == 7).all() and (room[:, K:] == 7).all()
+
+
 @pytest.mark.parametrize("offset", range(8))
 def test_quantize_rows_at_every_offset(offset):
     room = random_x(7, 1, 3 * 300 + 8, "fp16")[0]
@@ -123,14 +136,14 @@ def test_dequantize_every_code_and_scale():
 
 
 # --------------------------------------------------------------------------------------------------------- the product
-def check_product(y, w, x):
+def check_product(y, w, x, product=None):
     """The error of binary32 sums.  Products of elements are exact; S is the sum of the products' magnitudes.  A tensor-core
     instruction adds the 64 columns of two blocks to the sum: it aligns their terms to the largest and keeps at least 24 bits of
     it, so each of the 64 + 1 terms loses less than 2^-23 of at most S: together, for K / 64 instructions, less than
     (K / 64) * 65 * 2^-23 * S if every term were as large as S.  Terms are S / 64 on average, and what is lost is a share of the
     largest term of an instruction or of the sum so far: (K / 32 + 8) * 2^-22 * S bounds it with room for the sums of K's parts.
     The rounding to y's type adds half a step, and its smallest subnormal half of itself."""
-    y64, size = O.mx_linear(w[2], w[3], x[2], x[3])
+    y64, size = O.mx_linear(w[2], w[3], x[2], x[3]) if product is None else product
     got = host(y)
     step = 0.0 if y.dtype == torch.float32 else torch.finfo(y.dtype).eps / 2
     blocks = w[3].shape[1]
@@ -147,6 +160,23 @@ SHAPES = [(1, 1, 1), (1, 8, 32), (3, 128, 64), (1, 130, 500), (2, 257, 1024), (5
 def test_product(M, N, K):
     w, x = random_mx(N * 7 + K, N, K), random_mx(M + K, M, K)
     check_product(lcd.mx_linear(w[0], w[1], x[0], x[1]), w, x)
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(577, 5003, 2049), (1537, 9001, 40), (1000, 14001, 3000), (2050, 2600, 777)])
+def test_product_of_many_tokens(M, N, K, type):
+    # several tiles a CTA, pairs of CTAs, the widest tiles, the last of them ragged (the oracle's product in float64 on the GPU)
+    w, x = random_mx(N * 7 + K, N, K), random_mx(M + K, M, K)
+    a, b = (torch.from_numpy(O.mx_values(t[2], t[3])).cuda() for t in (x, w))
+    product = (host(a @ b.t()), host(a.abs() @ b.abs().t()))
+    y = torch.full((M + 1, N), 7.0, dtype=TYPES[type], device="cuda")
+    lcd.mx_linear(w[0], w[1], x[0], x[1], y=y[:M])
+    check_product(y[:M], w, x, product)
+    assert (y[M] == 7).all()
+    again = torch.zeros_like(y[:M])
+    for _ in range(3):
+        lcd.mx_linear(w[0], w[1], x[0], x[1], y=again)
+        assert torch.equal(again, y[:M])
 
 
 @pytest.mark.parametrize("type", ["fp16", "bf16"])
