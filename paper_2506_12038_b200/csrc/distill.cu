@@ -9,9 +9,9 @@
 // for them makes 16 a clock and multiprocessor: 263 us of 4096 x 128000, of which the bytes take 320).  Two forms:
 //   distill_stream_kernel  a CTA per row and one after the other, copies running ahead through a ring in shared memory;
 //   distill_kernel         few long rows: a cluster per row, whose threads hold it in registers.
-// 4096 x 128000 bf16, k = 128, loss and gradient: 511 us = 4.1 TB/s of what has to move; loss of 4096 x 32000 54 us = 4.9 TB/s.  What
-// bounds them: neither bytes (DRAM 55 %) nor the exponentials' unit (50 to 60 % busy) but the latencies of a row's beginning and end
-// with 16 to 24 warps an SM; rows beyond the ring are read again from L2, which more CTAs' rows do not fit.
+// 4096 x 128000 bf16, k = 128, loss and gradient: 452 us alone, 4.6 TB/s of what has to move (5.5 with what is read again); loss of
+// 4440 x 32000 61 us, 4.7 TB/s (49 without the exponentials).  What bounds them: neither bytes nor the exponentials' unit, 55 to 67 and
+// 58 % busy, but the latencies of a row's beginning and end, which 16 to 24 warps an SM cover in part.
 #include <cfloat>
 #include <type_traits>
 
@@ -797,9 +797,10 @@ lcd_status launch_typed(Params p, int64_t rows, bool loss, bool grad, cudaStream
   const int64_t slots = (p.V + 2 * E - 2) / E;        // whatever the row's alignment
   const int64_t sms = current_sm_count();
   // Clusters take a few long rows: loss and gradient of 32 x 128000 bf16 11.5 us, a CTA a row 21; 74 x 128000 26 and 21; 32 x 32000
-  // 10.3 and 9.8.  CTAs of 256 threads where there are two rows a multiprocessor at most (148 x 32000 bf16, loss and gradient 10.0,
-  // 128 threads 13.5) and where many rows have a gradient (4096 x 128000: 511 and 545; 4096 x 32000 fp32: 188 and 264), unless rows
-  // are short (4096 x 4096: 74 and 41); else 128 (loss of 4096 x 32000: 54, 256 threads 74; 444 rows with gradient 18.7, 21.7).
+  // 10.3 and 9.8.  CTAs of 256 threads where there are two rows a multiprocessor at most (148 x 32000 bf16, loss and gradient 9.6,
+  // 128 threads 13.6) and where many rows have a gradient (4096 x 128000: 456 and 545; 4096 x 32000 fp32: 198 and 243), unless rows
+  // are short (4096 x 12000: 94 and 73); else 128 (loss of 4096 x 32000: 54, 256 threads 74; 444 rows with gradient 17.8, 21.3).
+  // CTAs of 64 threads are faster below 2000 columns only (4096 x 1000: 27, 128 threads 36).
   if (rows * 4 > sms || slots < 4096) {
     const bool wide = slots >= 2048 && (rows <= 2 * sms || (grad && rows >= 4 * sms));
     return wide ? launch_stream<T, 256>(p, rows, loss, grad, s) : launch_stream<T, 128>(p, rows, loss, grad, s);

@@ -11,6 +11,7 @@
 //   warp 1      owns tensor memory; one elected lane issues the MMAs
 //   warps 6-9, 11-14  epilogue: tensor memory -> y, coalesced along the weight rows; up to four tokens come as they are, then these warps
 //               quantise them into the stages first
+// Many tokens take pairs of CTAs (mx_pair_kernel below).
 // Where tiles are few the columns of a tile are cut among the CTAs of a cluster; their partial sums meet in distributed shared
 // memory and are added in the order of the ranks, so results do not depend on timing.
 // Every wait is bounded (status word LCD_ERR_TIMEOUT on expiry; then every role leaves its loop, copies and MMAs in flight are
