@@ -494,10 +494,15 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
   // backwards for the gradient, those first and the others copied again, the latest of them first, which are the likeliest to be in
   // L2.  So places are taken in one direction by a row's sum and in the other by its gradient and by the next row's sum.  (kDepth
   // is a power of two.)
+  // The gradient alone goes backwards too, over rows and within a row, against the order in which their sums were formed (loss, then
+  // gradient, of 2048 x 32000 bf16: 93.7 us forwards, 90.9 so; 777 x 50021 fp16 58.8 and 58.0).
   constexpr bool kTwice = LOSS && GRAD;
+  constexpr int64_t kNone = INT64_MIN;
+  const int64_t step = LOSS ? (int64_t)gridDim.x : -(int64_t)gridDim.x;
+  auto there = [&](int64_t t) { return (uint64_t)t < (uint64_t)rows; };
   uint32_t issued = 0, taken = 0;                    // copies asked for, and those that have been waited for
   int free_places = kDepth, copy_place = 0, copy_dir = 1;
-  int64_t copy_t = -1;             // the row that is being copied
+  int64_t copy_t = kNone;             // the row that is being copied
   Row copy_row = {};
   int copy_chunk = 0, copy_left = 0;                 // the next chunk, and how many there are of this pass
   bool copy_again = false;                           // in a row's first pass of two
@@ -515,9 +520,9 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       if (copy_t == t_next) return false;            // the row that is worked on, or the next one
       const bool begin = copy_t != t;
       copy_t = begin ? t : t_next;
-      if (copy_t < rows && (begin ? w_t : w_next) != 0.0f) {
+      if (there(copy_t) && (begin ? w_t : w_next) != 0.0f) {
         copy_row = row_of(copy_t);
-        copy_chunk = 0;
+        copy_chunk = LOSS ? 0 : copy_row.chunks - 1;
         copy_left = copy_row.chunks;
         copy_again = kTwice;
       }
@@ -548,7 +553,7 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    copy_chunk += kTwice && !copy_again ? -1 : 1;
+    copy_chunk += LOSS && (!GRAD || copy_again) ? 1 : -1;
     --copy_left;
     copy_place += copy_dir;
     --free_places;
@@ -563,7 +568,7 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
   uint32_t e_top = 0;
   T e_z = {};
   auto ask = [&](int64_t t) {
-    if (tid < P.k && t < rows) {
+    if (tid < P.k && there(t)) {
       if (P.idx_bytes == 4) e_idx.x = static_cast<const int32_t*>(P.idx)[t * P.ldi + tid];
       else e_idx = static_cast<const int2*>(P.idx)[t * P.ldi + tid];
       if (P.top_type == LCD_DTYPE_F32) e_top = static_cast<const uint32_t*>(P.top)[t * P.ldt + tid];
@@ -581,7 +586,7 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     const Entries n = entries(place);
     Pair top = {-FLT_MAX, 0.0f};
     const T* row = static_cast<const T*>(P.z) + t * P.ldz;
-    if (tid < P.k && t < rows) {
+    if (tid < P.k && there(t)) {
       const float v = teacher_in(e_top);
       const int i = v == -INFINITY ? -1 : index_in(e_idx);     // p = 0: as if it were absent
       n.idx[tid] = i;
@@ -611,24 +616,24 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     if (lane == 0) s_top[parity][warp] = top;
   };
 
-  int64_t t = blockIdx.x;
+  int64_t t = LOSS ? blockIdx.x : rows - 1 - blockIdx.x;
   float w = P.weight ? P.weight[t] : 1.0f;
-  int64_t t_next = t + gridDim.x;
-  float w_next = P.weight && t_next < rows ? P.weight[t_next] : 1.0f;
+  int64_t t_next = t + step;
+  float w_next = P.weight && there(t_next) ? P.weight[t_next] : 1.0f;
   float lse = P.lse ? P.lse[t] : 0.0f;
   ask(t);
   enter(t, 0, 0);
   __syncthreads();
   int place = 0;
-  for (int parity = 0; t < rows; parity ^= 1) {
+  for (int parity = 0; there(t); parity ^= 1) {
     const Entries n = entries(place);
     place = place == 2 ? 0 : place + 1;
     ask(t_next);
-    const int64_t t_then = t_next + gridDim.x;
-    const float w_then = P.weight && t_then < rows ? P.weight[t_then] : 1.0f;
+    const int64_t t_then = t_next + step;
+    const float w_then = P.weight && there(t_then) ? P.weight[t_then] : 1.0f;
     Pair all = {-FLT_MAX, 0.0f};
     if (!LOSS) all = {P.stats[2 * t], P.stats[2 * t + 1]};
-    const float lse_next = P.lse && t_next < rows ? P.lse[t_next] : 0.0f;
+    const float lse_next = P.lse && there(t_next) ? P.lse[t_next] : 0.0f;
     while (free_places > 0 && copy_one(t, w, t_next, w_next)) {}
     const Row row = row_of(t);
     const T* student = static_cast<const T*>(P.z) + t * P.ldz;
@@ -724,7 +729,7 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     if (GRAD && w != 0.0f) {
       const float wt = w * P.inv_tau, scale = wt * mass / all.s;
       for (int n_done = 0; n_done < row.chunks; ++n_done) {
-        const int c = kTwice ? row.chunks - 1 - n_done : n_done;
+        const int c = row.chunks - 1 - n_done;
         if (!kTwice || n_done >= kDepth) {
           copy_wait((int)(issued - taken - 1));
           ++taken;
