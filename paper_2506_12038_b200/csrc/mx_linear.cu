@@ -322,10 +322,13 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   if (warp == 0 || warp == kScaleCopyWarp) {
     // ---------------------------------------------------------------- TMA producers.  With P.early the kernel before this one wrote x's
     // codes and nothing else that is read here, and itself began when all before it was done: the weights' first copies do not wait.
-    const bool codes = warp == 0;
-    if (elect()) {
-      const int from = codes ? ks0 : ss0, to = codes ? ks1 : ss1, slots = codes ? C::kStages : kScaleSlots;
-      const uint32_t bytes = codes ? kAStage + (kReady ? C::kBStage : 0) : kReady ? C::kScaleBytes : kRows * 16;
+    // What this thread does a stage is on the critical path of narrow tiles: 16 x 11008 x 4096 8.4 us with a division by the ring's length,
+    // 7.9 without, 7.5 with a loop of its own for either kind of copies.
+    auto produce = [&](auto of_codes) {
+      constexpr bool codes = decltype(of_codes)::value;
+      constexpr int slots = codes ? C::kStages : kScaleSlots;
+      const int from = codes ? ks0 : ss0, to = codes ? ks1 : ss1;
+      constexpr uint32_t bytes = codes ? kAStage + (kReady ? C::kBStage : 0) : kReady ? C::kScaleBytes : kRows * 16;
       auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
       auto copy_w = [&](int s, int k, int row) {
         if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full(s));
@@ -341,24 +344,32 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         copy_w(i, from + i, tile0 / P.n_tiles_m * kRows);
       }
       begin_after_previous();
-      int it = 0;
+      int it = 0, s = 0;
+      uint32_t round = 1;          // the parity of a stage's barrier
       bool ok = true;
       for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step) {
         const int n0 = tile / P.n_tiles_m * kRows, m0 = tile % P.n_tiles_m * BN;
         for (int k = from; k < to; ++k, ++it) {
-          const int s = it % slots;
           if (it >= ahead) {
-            ok = bar_wait(codes ? empty(s) : sc_empty(s), ((it / slots) & 1u) ^ 1u, abort_flag);
+            ok = bar_wait(codes ? empty(s) : sc_empty(s), round, abort_flag);
             if (!ok) break;
             bar_expect_tx(full_of(s), bytes);
             copy_w(s, k, n0);
           }
           if (kReady) copy_x(s, k, m0);
+          if (++s == slots) {
+            s = 0;
+            round ^= 1u;
+          }
         }
       }
       // nothing this thread issued may be in flight when the CTA exits
       const int back = min(it, slots);
       for (int i = 1; i <= back; ++i) bar_drain(full_of((it - i) % slots), ((it - i) / slots) & 1u);
+    };
+    if (elect()) {
+      if (warp == 0) produce(std::true_type{});
+      else produce(std::false_type{});
     }
     __syncwarp();
   } else if (warp == kMmaWarp) {
@@ -692,10 +703,11 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   const uint32_t sf_tmem = tmem + C::kDBuffers * BN;
 
   if (warp == 0 || warp == kScaleCopyWarp) {
-    const bool codes = warp == 0;
-    if (elect()) {
-      const int to = codes ? P.n_ks : P.n_ss, slots = codes ? C::kStages : kScaleSlots;
-      const uint32_t bytes = codes ? kAStage + C::kBStage : C::kScaleBytes;
+    auto produce = [&](auto of_codes) {
+      constexpr bool codes = decltype(of_codes)::value;
+      constexpr int slots = codes ? C::kStages : kScaleSlots;
+      const int to = codes ? P.n_ks : P.n_ss;
+      constexpr uint32_t bytes = codes ? kAStage + C::kBStage : C::kScaleBytes;
       auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
       auto copy_w = [&](int s, int k, int row) {
         if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full(s));
@@ -711,24 +723,32 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         copy_w(i, i, tile0 / P.n_tiles_m * 2 * kRows + (int)rank * kRows);
       }
       begin_after_previous();
-      int it = 0;
+      int it = 0, s = 0;
+      uint32_t round = 1;          // the parity of a stage's barrier
       bool ok = true;
       for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step) {
         const int n0 = tile / P.n_tiles_m * 2 * kRows + (int)rank * kRows, m0 = tile % P.n_tiles_m * BN;
         for (int k = 0; k < to; ++k, ++it) {
-          const int s = it % slots;
           if (it >= ahead) {
-            ok = codes ? bar_wait_cluster(empty(s), ((it / slots) & 1u) ^ 1u, abort_flag) : bar_wait(sc_empty(s), ((it / slots) & 1u) ^ 1u, abort_flag);
+            ok = codes ? bar_wait_cluster(empty(s), round, abort_flag) : bar_wait(sc_empty(s), round, abort_flag);
             if (!ok) break;
             bar_expect_tx(full_of(s), bytes);
             copy_w(s, k, n0);
           }
           copy_x(s, k, m0);
+          if (++s == slots) {
+            s = 0;
+            round ^= 1u;
+          }
         }
       }
       // nothing this thread issued may be in flight when the CTA exits
       const int back = min(it, slots);
       for (int i = 1; i <= back; ++i) bar_drain(full_of((it - i) % slots), ((it - i) / slots) & 1u);
+    };
+    if (elect()) {
+      if (warp == 0) produce(std::true_type{});
+      else produce(std::false_type{});
     }
     __syncwarp();
   } else if (warp == kMmaWarp) {
