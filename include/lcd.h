@@ -423,6 +423,7 @@ lcd_status lcd_linear_host_batch(const lcd_host_problem* problems /* host */, in
  *   scales: uint8 [rows][lds], blocks bytes a row.
  * Both start on 16 bytes and ldc, lds are multiples of 16 (LCD_ERR_INVALID_ARG otherwise); bytes between a row's end and the
  * next row are neither read for their value nor written.
+ * lcd_mx_linear reads codes fastest when they and their rows start on 128 bytes.
  * Types of x, y and logits in this and the next section: lcd_dtype.
  * -------------------------------------------------------------------------------------------- */
 typedef enum {

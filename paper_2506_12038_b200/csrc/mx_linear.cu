@@ -873,12 +873,13 @@ bool encode_rows(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t rows
 // How a product is cut: the width of the token tiles, whether a pair of CTAs shares one, or how many share its columns.
 struct Plan { int width, split; bool pair; };
 
-// Estimated in microseconds, from products timed alone on B200: 0.31 to 0.39 a stage, an epilogue that only the widest tile cannot
-// overlap with the next one's columns, for a shared tile the cluster's barrier and 1 us a 64 tokens to add up.  Pairs: 4096 x 8192 x
-// 8192 to bf16 96 us with 256 tokens, single CTAs 108; 2048 x 13824 x 5120 57 and 64 (192 tokens 64, in nine rounds); 2048 x 5120 x
-// 13824 58 with 192, single CTAs 62; 333 x 5003 x 5001 13.3 to 15.2, single CTAs of 128 tokens 13.3.  Single ones: 512 x 5120 x 5120
-// 12.2 with 192 tokens, 13.9 with 256, 17.8 with 128; 1 x 4096 x 4096 8.6 / 7.1 / 6.0 / 7.2 with 1 / 2 / 4 / 8 CTAs a tile, the last
-// being more than one an SM.
+// Estimated in microseconds: a stage (upper values of what products timed alone on B200 show), an epilogue that only the widest tile
+// cannot overlap with the next one's columns, for a shared tile the cluster's barrier and 1 us a 64 tokens to add up.  Pairs to bf16:
+// 4096 x 8192 x 8192 97 us with 256 tokens, 100 with 192, single CTAs 107; 2048 x 13824 x 5120 58, 60 and 63; 1024 x 8192 x 8192
+// 27.9, 30.9 and 30.1.  To fp32: 2048 x 5120 x 13824 57 with pairs and 192 tokens, single CTAs 62; 333 x 5003 x 5001 13.8 with pairs,
+// single CTAs of 128 tokens 13.1, of 192 16; 512 x 5120 x 5120 10.8 with pairs and 192 tokens, single CTAs of 192 10.5, of 256 12.8,
+// of 128 14.2.  8 x 4096 x 4096 5.5 / 5.2 / 4.4 with 1 / 2 / 4 CTAs a tile, 16 x 4096 x 11008 12.9 / 10.3 / 8.5; eight a tile are more
+// than one an SM there and slower.
 Plan plan(int64_t M, int64_t N, int64_t n_ks) {
   static constexpr struct { int width; double stage, epilogue; bool pair; } kWidths[] = {
       {16, 0.33, 0.1, false}, {32, 0.33, 0.2, false}, {64, 0.34, 0.4, false}, {128, 0.31, 0.4, false},
