@@ -87,7 +87,8 @@ def distill(z, idx, top, tau=1.0, teacher_lse=None, weight=None):
         norm = a.max() + np.log(np.exp(a - a.max()).sum()) if teacher_lse is None else float(teacher_lse[t])
         p = np.exp(a - norm)
         at = idx[t, entries].astype(np.int64)
-        terms = p * ((a - norm) - logq[at])
+        with np.errstate(invalid="ignore"):
+            terms = np.where(p != 0, p * ((a - norm) - logq[at]), 0.0)       # p = 0 adds nothing, whatever q is
         loss[t], loss_size[t] = w * terms.sum(), abs(w) * (np.abs(terms) + p).sum()
         grad[t] = p.sum() * q
         grad_size[t] = p.sum() * q

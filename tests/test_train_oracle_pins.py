@@ -88,3 +88,11 @@ def test_tokens_without_entries_or_weight():
     top = np.array([[1.0, 2.0], [-np.inf, -np.inf], [1.0, 2.0]])
     loss, grad, stats, _, _ = O.distill(z, idx, top, weight=np.array([1.0, 1.0, 0.0]))
     assert not loss.any() and not grad.any() and np.isnan(stats[2]).all()
+
+
+def test_distill_entries_without_probability_add_nothing():
+    # the teacher rules out (p underflows to 0) what the student rules out too
+    z = np.array([[0.5, -np.inf, 1.0]])
+    loss, grad, *_ = O.distill(z, np.array([[0, 1, 2]]), np.array([[1.0, -65504.0, 2.0]]), 0.7)
+    short = O.distill(z[:, [0, 2]], np.array([[0, 1]]), np.array([[1.0, 2.0]]), 0.7)
+    assert np.array_equal(loss, short[0]) and np.array_equal(grad[:, [0, 2]], short[1]) and grad[0, 1] == 0
