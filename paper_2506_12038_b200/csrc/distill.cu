@@ -219,6 +219,28 @@ __device__ __forceinline__ V warp_sum(V v) {
   return v;
 }
 
+// Terms of a row's loss that some lanes add before the row's maximum is known, against a reference of their own: with r the largest
+// student's logit among THESE entries (not among other logits, which may all be masked), sum of p (log p - (z - r) / temperature).
+// Every z lies at or below r, and r below the row's maximum m, so that what a lane, a warp and the row add, (r' - r) / temperature
+// for the sum's p, is never negative: large parts do not cancel.
+struct Share { float r, part; };
+// Adds an entry to a share whose entries so far have p's sum `mass`.
+__device__ __forceinline__ void add_entry(Share& a, float mass, float p, float logp, float z, float inv_tau) {
+  if (p == 0.0f) return;
+  const float r = fmaxf(a.r, z);
+  if (mass != 0.0f) a.part += mass * ((r - a.r) * inv_tau);
+  a.part += p * (logp - (z - r) * inv_tau);
+  a.r = r;
+}
+// The lanes' shares together, in every lane.  `mass`: the lane's sum of p.
+__device__ __forceinline__ Share warp_share(Share a, float mass, float inv_tau) {
+  float r = a.r;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) r = fmaxf(r, __shfl_xor_sync(0xffffffffu, r, o));
+  if (mass != 0.0f) a.part += mass * ((r - a.r) * inv_tau);
+  return {r, warp_sum(a.part)};
+}
+
 // What the CTAs of a row tell one another: the pair of their logits, sum of p (log p - (z - m) / temperature) over the entries in
 // their slots with their own m, and sum of p over those.
 struct alignas(16) Word { float m, s, part, own; };
@@ -456,7 +478,8 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
   constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Pair s_top[2][kStreamWarps], s_row[2][kStreamWarps];
-  __shared__ float s_mass[2][kStreamWarps], s_part[2][kStreamWarps];
+  __shared__ float s_mass[2][kStreamWarps];
+  __shared__ Share s_share[2][kStreamWarps];
   begin_after_previous();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint4* ring = reinterpret_cast<uint4*>(smem) + tid;
@@ -679,8 +702,9 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       all = warp_pair(all, P.c);
       if (lane == 0) s_row[parity][warp] = all;
     }
-    // this row's p, its share of the loss with the warp's own maximum, the next row's entries, and one barrier for all reductions
-    float mass = 0.0f, part = 0.0f;                    // log p = (t - top.m) - norm
+    // this row's p, its entries' terms of the loss, the next row's entries, and one barrier for all reductions
+    float mass = 0.0f;                                 // log p = (t - top.m) - norm
+    Share share = {-FLT_MAX, 0.0f};
     if (warp * 32 < P.k) {
       const Pair top = pair_of<kStreamWarps>(s_top[parity], kLog2e);
       const float norm = P.lse ? lse - top.m : logf(top.s);
@@ -690,18 +714,18 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
         if (!LOSS && j == tid) n.z[j] = to_f32(e_z);
         if (LOSS && w != 0.0f && i >= 0) {
           const float z = to_f32(j == tid ? e_z : student[i]);
-          if (p != 0.0f) part += p * (logp - (z - all.m) * P.inv_tau);
+          add_entry(share, mass, p, logp, z, P.inv_tau);
           n.z[j] = z;
         }
         n.p[j] = p;
         mass += p;
       }
+      if (LOSS) share = warp_share(share, mass, P.inv_tau);
       mass = warp_sum(mass);
-      if (LOSS) part = warp_sum(part);
     }
     if (lane == 0) {
       s_mass[parity][warp] = mass;
-      s_part[parity][warp] = part;
+      if (LOSS) s_share[parity][warp] = share;
     }
     enter(t_next, place, parity ^ 1);
     __syncthreads();
@@ -710,12 +734,13 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       if (LOSS && w != 0.0f) all = pair_of<kStreamWarps>(s_row[parity], P.c);
     }
     if (LOSS && tid == 0) {
+      float sum = 0.0f;
       if (w != 0.0f) {
-        part = mass * logf(all.s);
+        sum = mass * logf(all.s);
         for (int i = 0; i < kStreamWarps; ++i)
-          if (s_mass[parity][i] != 0.0f) part += s_part[parity][i] + s_mass[parity][i] * ((all.m - s_row[parity][i].m) * P.inv_tau);
+          if (s_mass[parity][i] != 0.0f) sum += s_share[parity][i].part + s_mass[parity][i] * ((all.m - s_share[parity][i].r) * P.inv_tau);
       }
-      P.loss[t] = w == 0.0f || mass == 0.0f ? 0.0f : w * part;
+      P.loss[t] = w == 0.0f || mass == 0.0f ? 0.0f : w * sum;
       if (P.stats) {
         P.stats[2 * t] = w == 0.0f ? NAN : all.m;
         P.stats[2 * t + 1] = w == 0.0f ? NAN : all.s;

@@ -1,0 +1,71 @@
+"""The loss of a distillation call where a warp's teacher entries and the logits that it reads have nothing to do with each other:
+vocabularies shorter than a CTA's words, rows masked to a few columns.  Bounds as derived at check()."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_12038_b200 as lcd
+from test_distill_gpu import TYPES, check, every_path, host, make
+
+pytestmark = pytest.mark.gpu
+
+
+def every_loss(z, idx, top, **teacher):
+    """Both forms of the loss (alone, with a gradient) and the gradient, each against the oracle."""
+    loss, grad, stats = every_path(z, idx, top, **teacher)
+    args = teacher.get("temperature", 1.0), teacher.get("teacher_lse"), teacher.get("weight")
+    check(z, idx, top, *args, loss=loss, grad=grad, stats=stats)
+    check(z, idx, top, *args, loss=lcd.distill_loss(z, idx, top, **teacher))
+
+
+def whole_lse(teacher, tau):
+    high = teacher.max(axis=1, keepdims=True)
+    return torch.from_numpy(((high / tau)[:, 0] + np.log(np.exp((teacher - high) / tau).sum(axis=1))).astype(np.float32)).cuda()
+
+
+@pytest.mark.parametrize("type", sorted(TYPES))
+@pytest.mark.parametrize("tau", [0.7, 1.0, 2.0])
+@pytest.mark.parametrize("T,V,k", [(2, 33, 33), (3, 100, 64), (5, 256, 128), (40, 20, 20), (4, 300, 300), (64, 500, 40), (700, 256, 64), (3, 700, 700),
+                                   (1000, 130, 100)])
+def test_vocabularies_shorter_than_the_words_of_a_block(T, V, k, tau, type):
+    z, idx, top, teacher = make(T + V, T, V, k, type)
+    every_loss(z, idx, top, temperature=tau)
+    every_loss(z, idx, top, temperature=tau, teacher_lse=whole_lse(teacher, tau))
+
+
+@pytest.mark.parametrize("k", [33, 64, 128, 300])
+@pytest.mark.parametrize("left", [(0, 256), (31960, 32000), (17000, 17001)])
+@pytest.mark.parametrize("T,tau,type,low", [(1, 0.7, "bf16", False), (64, 1.0, "fp32", True), (64, 0.7, "fp16", False), (300, 0.7, "bf16", True),
+                                            (300, 2.0, "fp16", True), (1, 1.0, "fp32", True), (200, 0.7, "fp32", False)])
+def test_rows_masked_to_a_few_columns(T, tau, type, low, left, k):
+    # the teacher's entries lie among the columns that are left and take any place of the k; the others are absent, or the teacher
+    # has masked them too (by -infinity, or by its type's lowest value: p = 0)
+    V, n = 32000, left[1] - left[0]
+    rng = np.random.default_rng(k + n)
+    z = torch.full((T, V), torch.finfo(TYPES[type]).min if low else -float("inf"), dtype=TYPES[type], device="cuda")
+    z[:, left[0]:left[1]] = torch.from_numpy(rng.normal(size=(T, n)) * 2.5).to(z.dtype).cuda()
+    teacher = host(z[:, left[0]:left[1]]) + rng.normal(size=(T, n))
+    idx, top = np.full((T, k), -1, dtype=np.int64), np.zeros((T, k))
+    few = min(n, k)
+    for t in range(T):
+        place = rng.permutation(k)
+        best = np.argsort(-teacher[t])[:few]
+        idx[t, place[:few]], top[t, place[:few]] = left[0] + best, teacher[t, best]
+        masked = place[few:few + 9]
+        idx[t, masked], top[t, masked] = 1000 + np.arange(len(masked)), np.where(np.arange(len(masked)) % 2, -np.inf, -65504.0)
+    idx, top = torch.from_numpy(idx.astype(np.int32)).cuda(), torch.from_numpy(top).half().cuda()
+    every_loss(z, idx, top, temperature=tau)
+    every_loss(z, idx, top, temperature=tau, teacher_lse=whole_lse(teacher, tau))
+
+
+@pytest.mark.parametrize("T", [2, 64])
+def test_the_student_rules_out_what_the_teacher_holds_likely(T):
+    # at one entry of many, wherever in the row of entries it stands; and a token all of whose entries the student rules out
+    z, idx, top, _ = make(T, T, 260, 130)
+    for row, j in ((0, 0), (1, 129)):
+        z[row, idx[row, j].long()] = -float("inf")
+    loss, grad, _ = every_path(z, idx, top, temperature=0.7)
+    assert (loss[:2] == float("inf")).all() and torch.isfinite(loss[2:]).all() and torch.isfinite(grad).all()
+    z[0, idx[0].long()] = -float("inf")
+    loss, grad, _ = every_path(z, idx, top, temperature=0.7)
+    assert loss[0] == float("inf") and torch.isfinite(grad).all()
