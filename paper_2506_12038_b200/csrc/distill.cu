@@ -219,31 +219,65 @@ __device__ __forceinline__ V warp_sum(V v) {
   return v;
 }
 
-// Terms of a row's loss that some lanes add before the row's maximum is known, against a reference of their own: with r the largest
-// student's logit among THESE entries (not among other logits, which may all be masked), sum of p (log p - (z - r) / temperature).
-// Every z lies at or below r, and r below the row's maximum m, so that what a lane, a warp and the row add, (r' - r) / temperature
-// for the sum's p, is never negative: large parts do not cancel.
-struct Share { float r, part; };
+// Terms of a row's loss, added before the row's maximum m is known and against a reference of their own: of the entries added (p != 0)
+// the one with the largest student's logit, (v, r) with v = t / temperature.  part = sum of p ((v' - v) - (z' - r) / temperature).  Then
+//     loss = sum over shares of part + mass * ((v - log sum_j exp(v_j)) - (r - m) / temperature + log s),
+// the parentheses with what their roundings lose added at the end: log p and log q are each ten or more times the loss (256 x 32000 at
+// temperature 2 with teacher_lse, against 64 bits: 1.8e-7 relative, root mean square; 7.5e-7 with log p and log s summed apart).  The reference
+// is of THESE entries, not of other logits, which may all be masked: every z lies at or below r and r at or below m, so that what a
+// lane, a warp and the row add, (r' - r) / temperature for the sum's p, is never negative and large parts do not cancel.
+struct Share { float r, v, part; };
 // Adds an entry to a share whose entries so far have p's sum `mass`.
-__device__ __forceinline__ void add_entry(Share& a, float mass, float p, float logp, float z, float inv_tau) {
+__device__ __forceinline__ void add_entry(Share& a, float mass, float p, float v, float z, float inv_tau) {
   if (p == 0.0f) return;
   const float r = fmaxf(a.r, z);
-  if (mass != 0.0f) a.part += mass * ((r - a.r) * inv_tau);
-  a.part += p * (logp - (z - r) * inv_tau);
-  a.r = r;
+  if (mass == 0.0f || r > a.r) {
+    if (mass != 0.0f) a.part += mass * ((a.v - v) - (a.r - r) * inv_tau);
+    a.r = r;
+    a.v = v;
+  }
+  a.part += p * ((v - a.v) - (z - a.r) * inv_tau);
 }
 // The lanes' shares together, in every lane.  `mass`: the lane's sum of p.
 __device__ __forceinline__ Share warp_share(Share a, float mass, float inv_tau) {
-  float r = a.r;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) r = fmaxf(r, __shfl_xor_sync(0xffffffffu, r, o));
-  if (mass != 0.0f) a.part += mass * ((r - a.r) * inv_tau);
-  return {r, warp_sum(a.part)};
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(a.r));       // (five shuffles: 4440 x 32000, k = 128, 62.0 us, 61.2 so)
+  const unsigned at = __ballot_sync(0xffffffffu, mass != 0.0f && a.r == r);
+  const float v = __shfl_sync(0xffffffffu, a.v, at ? __ffs(at) - 1 : 0);
+  if (mass != 0.0f) a.part += mass * ((a.v - v) - (a.r - r) * inv_tau);
+  return {r, v, warp_sum(a.part)};
+}
+// A sum and what its rounding lost.
+__device__ __forceinline__ float two_sum(float a, float b, float& lost) {
+  const float s = __fadd_rn(a, b), t = __fsub_rn(s, a);
+  lost = __fadd_rn(__fsub_rn(a, __fsub_rn(s, t)), __fsub_rn(b, t));
+  return s;
+}
+// log s = whole * log 2 + rest, rest within [0, log 2] (s >= 1; but for rows without a finite logit, where rest is all of it).
+__device__ __forceinline__ void split_log(float s, float& whole, float& rest) {
+  const uint32_t bits = __float_as_uint(s);
+  const bool fine = s >= 1.0f && s <= FLT_MAX;
+  whole = fine ? (float)((int)(bits >> 23) - 127) : 0.0f;
+  rest = logf(fine ? __uint_as_float((bits & 0x007fffffu) | 0x3f800000u) : s);
+}
+// A share's part of the loss.  `all`: m and s of the row; the teacher's normalisation is *lse, or the pair of its logits.
+__device__ __forceinline__ float share_loss(float mass, const Share& a, const Pair& all, const Pair& teacher, const float* lse, float inv_tau) {
+  constexpr float kLog2Hi = 0.693145751953125f, kLog2Lo = 1.42860682030941723e-6f;       // 16 bits, so that their products are exact; the rest
+  float whole, rest, whole_t = 0.0f, rest_t = 0.0f, lost[4];
+  split_log(all.s, whole, rest);
+  if (!lse) split_log(teacher.s, whole_t, rest_t);
+  const float n = whole - whole_t;
+  const float log_p = two_sum(a.v, lse ? -*lse : -teacher.m, lost[0]);
+  const float below = two_sum(all.m, -a.r, lost[1]), scaled = below * inv_tau;
+  const float log_q = two_sum(scaled, n * kLog2Hi, lost[2]);
+  float sum = two_sum(log_p, log_q, lost[3]);
+  if (fabsf(sum) <= FLT_MAX) sum += ((lost[0] + lost[3]) + (lost[2] + (fmaf(below, inv_tau, -scaled) + lost[1] * inv_tau))) + n * kLog2Lo;
+  sum += rest - rest_t;
+  return mass == 0.0f ? 0.0f : a.part + mass * sum;
 }
 
-// What the CTAs of a row tell one another: the pair of their logits, sum of p (log p - (z - m) / temperature) over the entries in
-// their slots with their own m, and sum of p over those.
-struct alignas(16) Word { float m, s, part, own; };
+// What the CTAs of a row tell one another: the pair of their logits, the share of the entries in their slots, and the sum of p over those.
+struct alignas(16) Word { float m, s, own, r, v, part, unused[2]; };
 
 // LOSS: m, s and the loss (and the stats) are formed, by a cluster; otherwise they are read.  GRAD: the gradient is written.
 // ONCE: the row fits the registers of its CTAs.
@@ -341,17 +375,18 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
   mass = warp_sum(lane < warps ? s_mass[lane] : 0.0f);
   if (LOSS) {
     all = pair_of_warps(s_row, warps, P.c);
-    float part = 0.0f, own = 0.0f;
+    float own = 0.0f;
+    Share share = {-FLT_MAX, 0.0f, 0.0f};
     if (warp == 0) {
       for (int j = lane; j < P.k; j += 32) {
         const int i = s_idx[j];
         const float p = s_p[j];
         if (i >= 0 && p != 0.0f && i >= lo0 && i < lo0 + (int64_t)count * E) {
-          part += p * (((s_t[j] - top.m) - norm) - (s_z[j] - all.m) * P.inv_tau);
+          add_entry(share, own, p, s_t[j], s_z[j], P.inv_tau);
           own += p;
         }
       }
-      part = warp_sum(part);
+      share = warp_share(share, own, P.inv_tau);
       own = warp_sum(own);
     }
     if (P.parts > 1) {
@@ -360,21 +395,29 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
         const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&s_word[rank]);
         uint32_t at;
         asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(tid));
-        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(all.m), "f"(all.s), "f"(part), "f"(own) : "memory");
+        asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(all.m), "f"(all.s), "f"(own), "f"(share.r) : "memory");
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at + 16), "f"(share.v), "f"(share.part) : "memory");
       }
       asm volatile("barrier.cluster.arrive.release;" ::: "memory");
       asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
       all.m = s_word[0].m;
       for (int i = 1; i < P.parts; ++i) all.m = fmaxf(all.m, s_word[i].m);
-      all.s = part = 0.0f;
-      for (int i = 0; i < P.parts; ++i) {
-        const Word o = s_word[i];
-        all.s += o.s * exp2_fast((o.m - all.m) * P.c);
-        part += o.own == 0.0f ? 0.0f : o.part + o.own * ((all.m - o.m) * P.inv_tau);
+      all.s = 0.0f;
+      for (int i = 0; i < P.parts; ++i) all.s += s_word[i].s * exp2_fast((s_word[i].m - all.m) * P.c);
+    }
+    float sum = 0.0f;
+    if (rank == 0 && warp == 0) {          // a lane per CTA
+      if (P.parts > 1) {
+        const Word o = s_word[lane & (kMaxCluster - 1)];
+        own = lane < P.parts ? o.own : 0.0f;
+        share = {o.r, o.v, o.part};
       }
+      const float* lse = P.lse ? P.lse + t : nullptr;
+      sum = share_loss(own, share, all, top, lse, P.inv_tau);
+      if (P.parts > 1) sum = warp_sum(sum);
     }
     if (rank == 0 && tid == 0) {
-      P.loss[t] = mass == 0.0f ? 0.0f : w * (part + mass * logf(all.s));
+      P.loss[t] = mass == 0.0f ? 0.0f : w * sum;
       if (P.stats) {
         P.stats[2 * t] = all.m;
         P.stats[2 * t + 1] = all.s;
@@ -480,6 +523,8 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
   __shared__ Pair s_top[2][kStreamWarps], s_row[2][kStreamWarps];
   __shared__ float s_mass[2][kStreamWarps];
   __shared__ Share s_share[2][kStreamWarps];
+  __shared__ Pair s_teacher[2];
+  constexpr int kLossWarp = kStreamWarps - 1;        // has no entries unless there are many (4096 x 1000, k = 64: 19.1 us, by warp 0 20.7)
   begin_after_previous();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint4* ring = reinterpret_cast<uint4*>(smem) + tid;
@@ -703,18 +748,19 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       if (lane == 0) s_row[parity][warp] = all;
     }
     // this row's p, its entries' terms of the loss, the next row's entries, and one barrier for all reductions
-    float mass = 0.0f;                                 // log p = (t - top.m) - norm
-    Share share = {-FLT_MAX, 0.0f};
+    float mass = 0.0f;                                 // log p = (t / temperature - top.m) - norm
+    Share share = {-FLT_MAX, 0.0f, 0.0f};
     if (warp * 32 < P.k) {
       const Pair top = pair_of<kStreamWarps>(s_top[parity], kLog2e);
       const float norm = P.lse ? lse - top.m : logf(top.s);
+      if (LOSS && tid == 0) s_teacher[parity] = top;
       for (int j = tid; j < P.k; j += kStreamThreads) {
         const int i = n.idx[j];
-        const float logp = (n.p[j] - top.m) - norm, p = i >= 0 ? expf(logp) : 0.0f;
+        const float v = n.p[j], p = i >= 0 ? expf((v - top.m) - norm) : 0.0f;
         if (!LOSS && j == tid) n.z[j] = to_f32(e_z);
         if (LOSS && w != 0.0f && i >= 0) {
           const float z = to_f32(j == tid ? e_z : student[i]);
-          add_entry(share, mass, p, logp, z, P.inv_tau);
+          add_entry(share, mass, p, v, z, P.inv_tau);
           n.z[j] = z;
         }
         n.p[j] = p;
@@ -729,21 +775,24 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     }
     enter(t_next, place, parity ^ 1);
     __syncthreads();
-    if (GRAD || warp == 0) {
+    if (GRAD || warp == kLossWarp) {
       mass = sum_of<kStreamWarps>(s_mass[parity]);
       if (LOSS && w != 0.0f) all = pair_of<kStreamWarps>(s_row[parity], P.c);
     }
-    if (LOSS && tid == 0) {
+    if (LOSS && warp == kLossWarp) {
       float sum = 0.0f;
-      if (w != 0.0f) {
-        sum = mass * logf(all.s);
-        for (int i = 0; i < kStreamWarps; ++i)
-          if (s_mass[parity][i] != 0.0f) sum += s_share[parity][i].part + s_mass[parity][i] * ((all.m - s_share[parity][i].r) * P.inv_tau);
+      if (w != 0.0f) {               // a lane per warp
+        const int i = lane & (kStreamWarps - 1);
+        sum = share_loss(s_mass[parity][i], s_share[parity][i], all, s_teacher[parity], P.lse ? &lse : nullptr, P.inv_tau);
+#pragma unroll
+        for (int o = kStreamWarps / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
       }
-      P.loss[t] = w == 0.0f || mass == 0.0f ? 0.0f : w * sum;
-      if (P.stats) {
-        P.stats[2 * t] = w == 0.0f ? NAN : all.m;
-        P.stats[2 * t + 1] = w == 0.0f ? NAN : all.s;
+      if (lane == 0) {
+        P.loss[t] = w == 0.0f || mass == 0.0f ? 0.0f : w * sum;
+        if (P.stats) {
+          P.stats[2 * t] = w == 0.0f ? NAN : all.m;
+          P.stats[2 * t + 1] = w == 0.0f ? NAN : all.s;
+        }
       }
     }
     const bool none = w == 0.0f || mass == 0.0f;      // no gradient

@@ -69,3 +69,27 @@ def test_the_student_rules_out_what_the_teacher_holds_likely(T):
     z[0, idx[0].long()] = -float("inf")
     loss, grad, _ = every_path(z, idx, top, temperature=0.7)
     assert loss[0] == float("inf") and torch.isfinite(grad).all()
+
+
+@pytest.mark.parametrize("type", sorted(TYPES))
+@pytest.mark.parametrize("T,V,tau,whole", [(256, 32000, 2.0, True), (16, 33000, 2.0, True), (256, 5000, 2.0, True), (256, 32000, 1.0, False), (16, 33000, 1.0, True)])
+def test_digits_of_the_loss(T, V, tau, whole, type):
+    # log p and log q are each around ten times the loss: in 32 bits their roundings would be most of its error.  Held to the error of the
+    # formula in 32-bit tensor operations, where they are rounded once an entry and in no common way (over 256 rows, root mean square)
+    from oracle import train_oracle as O
+    errors = [], []
+    for seed in range(256 // T):
+        z, idx, top, teacher = make(seed, T, V, 64, type)
+        lse = whole_lse(teacher, tau) if whole else None
+        want = O.distill(host(z), idx.cpu().numpy(), host(top), tau, None if lse is None else host(lse))[0]
+        got = lcd.distill_loss(z, idx, top, temperature=tau, teacher_lse=lse)
+        a = top.float() / tau
+        logp = a - (torch.logsumexp(a, dim=1) if lse is None else lse)[:, None]
+        x = z.float() / tau
+        high = x.amax(dim=1, keepdim=True)
+        logq = (x.gather(1, idx.long()) - high) - torch.log(torch.exp(x - high).sum(dim=1, keepdim=True))
+        plain = (torch.exp(logp) * (logp - logq)).sum(dim=1)
+        for e, v in zip(errors, (got, plain)):
+            e.append((host(v) - want) / want)
+    own, plain = (np.sqrt(np.mean(np.concatenate(e) ** 2)) for e in errors)
+    assert own <= plain, (own, plain)
