@@ -588,8 +588,8 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 // Many tokens: a pair of CTAs shares a tile of 256 weight rows x BN tokens (cta_group::2).  Each brings its own 128 rows of the weights
 // and half of the tokens into its shared memory; the instruction reads both halves of the tokens for either CTA's rows.  So a CTA
 // writes and reads 16 KB + BN / 2 rows a stage where it alone would need BN rows: shared memory's bandwidth, what bounds
-// the kernel above, is enough (256 tokens: 128 bytes a clock).  Roles as above; the MMAs are issued by the pair's first CTA, the second
-// one's warp 1 tells it of its copies.  The tokens' scales are needed by both and lie in both CTAs' tensor memory.
+// the kernel above, is enough (256 tokens: 128 bytes a clock).  Roles as above; the MMAs are issued by the pair's first CTA, and the
+// copies of both CTAs' codes complete on its barriers.  The tokens' scales are needed by both and lie in both CTAs' tensor memory.
 template <int BN>
 struct PairCfg {
   static constexpr int kBStage = BN / 2 * kStageK / 2;
@@ -621,10 +621,22 @@ __device__ __forceinline__ bool bar_wait_cluster(uint32_t bar, uint32_t parity, 
     }
   }
 }
-// Arrives at the first CTA's barrier of the pair.  (No release at cluster scope: what it tells of, copies that have landed and tensor memory
-// that has been written or read, is ordered by the waits and fences before it; with it a stage took 0.9 us.)
+// An address of this CTA's shared memory, in the pair's CTA of that rank.
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+// Arrives at the first CTA's barrier of the pair.  What it tells of is tensor memory that has been written or read, which the tcgen05 fences
+// on both sides order around any signal; no other memory is handed over, so the signal itself is relaxed (with release at
+// cluster scope the call of 2048 x 13824 x 5120 takes 87 us, 67 so).
 __device__ __forceinline__ void bar_arrive_first(uint32_t bar) {
-  asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %0, 0;\nmbarrier.arrive.shared::cluster.b64 _, [a];\n}" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_cta(bar, 0)) : "memory");
+}
+// A tile into this CTA's shared memory that completes on a barrier of either CTA (an address in the cluster's window).
+__device__ __forceinline__ void copy_tile_pair(uint32_t dst, const CUtensorMap* map, int x, int row, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void mma_mx_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
   asm volatile(
@@ -659,9 +671,12 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   auto d_full = [&](int b) { return bars + 8u * (kB1 + b); };
   auto d_empty = [&](int b) { return bars + 8u * (kB1 + 2 + b); };
   const uint32_t drain = bars + 8u * (kB1 + 4);
-  static_assert(8 * (kB1 + 5) + 8 <= 512, "barriers");
+  static_assert(8 * (kB1 + 5) + 24 <= 512, "barriers");
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + kBarAt + 8 * (kB1 + 5));
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  // stages that this CTA has asked for copies of; the other CTA's flag and number, which it sends at its end
+  volatile int *asked = abort_flag + 1, *other_abort = abort_flag + 2, *other_asked = abort_flag + 3;
+  constexpr uint32_t kStageBytes = kAStage + C::kBStage;       // of one CTA
   uint32_t rank;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const bool first = rank == 0;
@@ -669,7 +684,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
-      bar_init(full(s), first ? 2 : 1);              // the first CTA's: its own copies, and word of the other's
+      bar_init(full(s), 1);                          // the first CTA's take both CTAs' copies, the other's are not used
       bar_init(empty(s), 1);
     }
     for (int s = 0; s < kScaleSlots; ++s) {
@@ -686,6 +701,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     }
     bar_init(drain, 1);
     *abort_flag = 0;
+    *asked = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -707,19 +723,24 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
       constexpr bool codes = decltype(of_codes)::value;
       constexpr int slots = codes ? C::kStages : kScaleSlots;
       const int to = codes ? P.n_ks : P.n_ss;
-      constexpr uint32_t bytes = codes ? kAStage + C::kBStage : C::kScaleBytes;
-      auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
+      // Codes: the first CTA's thread announces the bytes of both CTAs' copies (those of the other may have landed by then; its arrival is
+      // what the phase waits for).  The other is never a phase ahead: it waits for the MMAs that read what it overwrites.
+      const uint32_t full_first = in_cta(full(0), 0);
+      auto announce = [&](int s) {
+        if (!codes) bar_expect_tx(sc_full(s), C::kScaleBytes);
+        else if (first) bar_expect_tx(full(s), 2 * kStageBytes);
+      };
       auto copy_w = [&](int s, int k, int row) {
-        if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full(s));
+        if (codes) copy_tile_pair(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full_first + 8u * s);
         else copy_tile(s_base + s * C::kScaleBytes, &map_ws, k * 16, row, sc_full(s));
       };
       auto copy_x = [&](int s, int k, int row) {
-        if (codes) copy_tile(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), row + (int)rank * (BN / 2), full(s));
+        if (codes) copy_tile_pair(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), row + (int)rank * (BN / 2), full_first + 8u * s);
         else copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, row, sc_full(s));
       };
       const int ahead = P.early && tile0 < P.n_tiles ? min(slots, to) : 0;
       for (int i = 0; i < ahead; ++i) {
-        bar_expect_tx(full_of(i), bytes);
+        announce(i);
         copy_w(i, i, tile0 / P.n_tiles_m * 2 * kRows + (int)rank * kRows);
       }
       begin_after_previous();
@@ -732,7 +753,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
           if (it >= ahead) {
             ok = codes ? bar_wait_cluster(empty(s), round, abort_flag) : bar_wait(sc_empty(s), round, abort_flag);
             if (!ok) break;
-            bar_expect_tx(full_of(s), bytes);
+            announce(s);
             copy_w(s, k, n0);
           }
           copy_x(s, k, m0);
@@ -742,9 +763,14 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
           }
         }
       }
-      // nothing this thread issued may be in flight when the CTA exits
-      const int back = min(it, slots);
-      for (int i = 1; i <= back; ++i) bar_drain(full_of((it - i) % slots), ((it - i) / slots) & 1u);
+      // Nothing that this thread issued may be in flight when the CTA exits.  Codes have landed where every MMA has run; if not, see
+      // the end.
+      if (codes) {
+        *asked = it;
+      } else {
+        const int back = min(it, slots);
+        for (int i = 1; i <= back; ++i) bar_drain(sc_full((it - i) % slots), ((it - i) / slots) & 1u);
+      }
     };
     if (elect()) {
       if (warp == 0) produce(std::true_type{});
@@ -752,57 +778,45 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     }
     __syncwarp();
   } else if (warp == kMmaWarp) {
-    if (elect()) {
+    if (first && elect()) {
+      constexpr uint32_t kM = (uint32_t)(2 * kRows >> 4) << 24 ^ (uint32_t)(kRows >> 4) << 24;     // M = 256 in place of 128
+      constexpr uint32_t idesc[2] = {instr_desc(BN, 0) ^ kM, instr_desc(BN, 1) ^ kM};
+      const uint64_t a_desc0 = smem_desc(a_base), b_desc0 = smem_desc(b_base);
+      uint32_t it = 0, sit = 0, tl = 0;
       bool ok = true;
-      if (!first) {
-        // the other CTA's copies, stage by stage
-        uint32_t it = 0;
-        for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step)
-          for (int k = 0; k < P.n_ks; ++k, ++it) {
-            ok = bar_wait(full(it % C::kStages), (it / C::kStages) & 1u, abort_flag);
-            if (!ok) break;
-            bar_arrive_first(full(it % C::kStages));
-          }
-        bar_drain(drain, 0);
-      } else {
-        constexpr uint32_t kM = (uint32_t)(2 * kRows >> 4) << 24 ^ (uint32_t)(kRows >> 4) << 24;     // M = 256 in place of 128
-        constexpr uint32_t idesc[2] = {instr_desc(BN, 0) ^ kM, instr_desc(BN, 1) ^ kM};
-        const uint64_t a_desc0 = smem_desc(a_base), b_desc0 = smem_desc(b_base);
-        uint32_t it = 0, sit = 0, tl = 0;
-        for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
-          const uint32_t buf = tl % C::kDBuffers;
-          ok = bar_wait_cluster(d_empty(buf), ((tl / C::kDBuffers) & 1u) ^ 1u, abort_flag);
+      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+        const uint32_t buf = tl % C::kDBuffers;
+        ok = bar_wait_cluster(d_empty(buf), ((tl / C::kDBuffers) & 1u) ^ 1u, abort_flag);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + buf * BN;
+        for (int ss = 0; ss < P.n_ss && ok; ++ss, ++sit) {
+          const uint32_t sb = sit % C::kSfSlots;
+          ok = bar_wait_cluster(ts_full(sb), (sit / C::kSfSlots) & 1u, abort_flag);
           if (!ok) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t d = tmem + buf * BN;
-          for (int ss = 0; ss < P.n_ss && ok; ++ss, ++sit) {
-            const uint32_t sb = sit % C::kSfSlots;
-            ok = bar_wait_cluster(ts_full(sb), (sit / C::kSfSlots) & 1u, abort_flag);
+          const uint32_t sfa = sf_tmem + sb * C::kSfCols, sfb = sfa + 16;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (2 * ss + h >= P.n_ks) break;
+            const uint32_t slot = it % C::kStages;
+            ok = bar_wait_cluster(full(slot), (it / C::kStages) & 1u, abort_flag);
             if (!ok) break;
-            const uint32_t sfa = sf_tmem + sb * C::kSfCols, sfb = sfa + 16;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint64_t ad = a_desc0 + (uint64_t)(slot * kAStage >> 4), bd = b_desc0 + (uint64_t)(slot * C::kBStage >> 4);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (2 * ss + h >= P.n_ks) break;
-              const uint32_t slot = it % C::kStages;
-              ok = bar_wait_cluster(full(slot), (it / C::kStages) & 1u, abort_flag);
-              if (!ok) break;
-              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-              const uint64_t ad = a_desc0 + (uint64_t)(slot * kAStage >> 4), bd = b_desc0 + (uint64_t)(slot * C::kBStage >> 4);
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                mma_mx_pair(d, ad + 2 * i, bd + 2 * i, idesc[i & 1], sfa + (2 * h + i / 2) * 4, sfb + (2 * h + i / 2) * C::kSfbCols,
-                            (uint32_t)(ss != 0 || h != 0 || i != 0));
-              mma_commit_pair(empty(slot));
-              ++it;
-            }
-            mma_commit_pair(ts_empty(sb));
+            for (int i = 0; i < 4; ++i)
+              mma_mx_pair(d, ad + 2 * i, bd + 2 * i, idesc[i & 1], sfa + (2 * h + i / 2) * 4, sfb + (2 * h + i / 2) * C::kSfbCols,
+                          (uint32_t)(ss != 0 || h != 0 || i != 0));
+            mma_commit_pair(empty(slot));
+            ++it;
           }
-          if (ok) mma_commit_pair(d_full(buf));
+          mma_commit_pair(ts_empty(sb));
         }
-        // every MMA must have finished before tensor memory is released, the other CTA's too
-        mma_commit_pair(drain);
-        bar_drain(drain, 0);
+        if (ok) mma_commit_pair(d_full(buf));
       }
+      // every MMA must have finished before tensor memory is released, the other CTA's too
+      mma_commit_pair(drain);
+      bar_drain(drain, 0);
     }
     __syncwarp();
   } else if (warp < kFirstEpiWarp) {
@@ -852,8 +866,29 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   // neither CTA leaves while the other may still read its shared memory or arrive at its barriers
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if (!first && warp == kMmaWarp && elect()) bar_drain(drain, 0);      // the last of the signals that the first CTA's MMAs send here
+  if (threadIdx.x == 0) {
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(const_cast<int*>(other_abort));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(to, rank ^ 1u)), "r"(*abort_flag) : "memory");
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(to + 4, rank ^ 1u)), "r"(*asked) : "memory");
+  }
   asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  if (*abort_flag || *other_abort) {          // in both CTAs or in neither
+    if (first && threadIdx.x == 0) {
+      // Stages that one CTA alone has asked for: the other's part is announced, or taken back, so that their barriers complete when the
+      // copies have landed.
+      const int own = *asked, other = *other_asked, most = max(own, other);
+      for (int i = min(own, other); i < most; ++i) {
+        const uint32_t bar = full(i % C::kStages);
+        if (other > own) bar_expect_tx(bar, kStageBytes);
+        else asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(kStageBytes) : "memory");
+      }
+      for (int i = max(0, most - C::kStages); i < most; ++i) bar_drain(full(i % C::kStages), (i / C::kStages) & 1u);
+    }
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
