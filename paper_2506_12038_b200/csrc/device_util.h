@@ -58,10 +58,11 @@ inline cudaError_t launch_overlapping(void (*kern)(Params...), dim3 grid, dim3 b
   cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, static_cast<Params>(args)...);
 }
-// Waits for the kernels before this one and only then lets the next one begin: a kernel that has begun may take everything before
-// its direct predecessor for done.
+// Waits for the kernels before this one, and (the second) only then lets the next one begin: a kernel that has begun may take everything
+// before its direct predecessor for done.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void begin_after_previous() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  wait_for_previous();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 

@@ -39,5 +39,5 @@ def test_pairs_whose_weights_are_copied_ahead(M, N, K):
     for _ in range(10):
         for x, y in zip(xs, want):
             assert torch.equal(lcd.mx_linear_fused(w[0], w[1], x), y)
-    word = torch.full((1,), 7, dtype=torch.int32, device="cuda")
-    assert torch.equal(lcd.mx_linear_fused(w[0], w[1], xs[0], status_word=word), want[0]) and word.item() == 7
+    word = torch.full((1,), -5, dtype=torch.int32, device="cuda")
+    assert torch.equal(lcd.mx_linear_fused(w[0], w[1], xs[0], status_word=word), want[0]) and word.item() == -5
