@@ -91,10 +91,6 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t top_bits) {
 }
 // 2^(127 - byte), what a block's values are multiplied by before they are rounded (exact: at most 2^127, at least 2^-125).
 __device__ __forceinline__ float mx_inverse_scale(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
-// 2^(byte - 127); 255: NaN.
-__device__ __forceinline__ float mx_scale_value(uint32_t byte) {
-  return __uint_as_float(byte == 255u ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u);
-}
 // Eight values as eight codes, the first in the lowest nibble (nearest even, beyond 6: 6).
 __device__ __forceinline__ uint32_t mx_codes8(const float (&v)[8]) {
   uint32_t c;
@@ -107,38 +103,18 @@ __device__ __forceinline__ uint32_t mx_codes8(const float (&v)[8]) {
       : "=r"(c) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
   return c;
 }
-// What eight codes stand for, without their scale.
-__device__ __forceinline__ void mx_elements8(uint32_t c, float (&v)[8]) {
-  uint32_t h[4];
-  asm("{\n.reg .b8 b0, b1, b2, b3;\n"
-      "mov.b32 {b0, b1, b2, b3}, %4;\n"
-      "cvt.rn.f16x2.e2m1x2 %0, b0;\n"
-      "cvt.rn.f16x2.e2m1x2 %1, b1;\n"
-      "cvt.rn.f16x2.e2m1x2 %2, b2;\n"
-      "cvt.rn.f16x2.e2m1x2 %3, b3;\n}"
-      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(c));
+// What N codes under one scale byte stand for, the first in the lowest nibble.  A code's exponent and mantissa bits, put where a binary32
+// number has them, are its value times 2^-126 (a subnormal number for .5), so that one multiplication does up to scales of 2.  (Not by
+// cvt from .b8 parts of the word: where the word was a 16-bit load that way gave zeros from -O1 on, nvcc 12.9.86.)
+template <int N>
+__device__ __forceinline__ void mx_values(uint32_t c, uint32_t byte, float (&v)[N]) {
+  const float s = __uint_as_float((min(byte, 128u) + 126u) << 23);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-    v[2 * i] = f.x;
-    v[2 * i + 1] = f.y;
-  }
-}
-
-// What four codes stand for.  (Of its own: mx_elements8 of a word whose upper half the compiler knows to be zero came back as zeros in an
-// unrolled loop, nvcc 12.9.86.)
-__device__ __forceinline__ void mx_elements4(uint16_t c, float (&v)[4]) {
-  uint32_t h[2];
-  asm("{\n.reg .b8 b0, b1;\n"
-      "mov.b16 {b0, b1}, %2;\n"
-      "cvt.rn.f16x2.e2m1x2 %0, b0;\n"
-      "cvt.rn.f16x2.e2m1x2 %1, b1;\n}"
-      : "=r"(h[0]), "=r"(h[1]) : "h"(c));
+  for (int i = 0; i < N; ++i) v[i] = __fmul_rn(__uint_as_float((uint32_t)((int32_t)(c << (28 - 4 * i)) >> 6) & 0x81c00000u), s);
+  if (byte > 128u) {
+    const float more = __uint_as_float(byte == 255u ? 0x7fc00000u : (byte - 1u) << 23);
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-    v[2 * i] = f.x;
-    v[2 * i + 1] = f.y;
+    for (int i = 0; i < N; ++i) v[i] = __fmul_rn(v[i], more);
   }
 }
 
