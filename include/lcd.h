@@ -441,8 +441,9 @@ typedef enum {
 lcd_status lcd_mx_quantize(const void* x, lcd_dtype x_type, int64_t M, int64_t K, int64_t ldx, const float* inv_smooth,
                            uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, void* cuda_stream);
 
-/* What codes and scales stand for: out[m][k] = element * 2^(byte - 127), rounded once to the output type (fp32 holds every
- * value, bf16 all of them, fp16 overflows to infinity).  out: device, [M][ldo], ldo >= K. */
+/* What codes and scales stand for: out[m][k] = element * 2^(byte - 127), rounded once to the output type.  fp32 and bf16 hold every
+ * value below 2^128; those from there on (bytes 253 and 254 under 4 and 6 or 2 and more, which lcd_mx_quantize never writes) become
+ * infinity.  fp16 rounds, and overflows to infinity from 65520 on.  out: device, [M][ldo], ldo >= K. */
 lcd_status lcd_mx_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t* scales, int64_t lds, int64_t M, int64_t K,
                              void* out, lcd_dtype out_type, int64_t ldo, void* cuda_stream);
 
