@@ -1038,7 +1038,14 @@ lcd_status launch_pair(const MxProduct& p, bool early, int32_t* status, cudaStre
 
 }  // namespace
 
-// (4 x 8192 x 28672 35 us, 27 with two launches; 1 x 8192 x 28672 27.1 and 26.8; 4 x 4096 x 4096 6.7 and 6.6)
+// Device time, one launch and two, us (N x K: 1 / 2 / 3 / 4 tokens):
+//     1024 x 4096    4.1 4.9 / 4.3 4.9 / 4.7 5.0 / 4.8 5.2         11008 x 4096   6.6 7.6 / 7.8 7.6 / 8.1 7.8 / 8.7 7.6
+//     4096 x 4096    4.8 6.2 / 5.0 5.7 / 5.5 6.4 / 5.5 5.9         11008 x 8192   13.8 13.3 / 15.7 13.3 / 17.4 13.3 / 18.2 13.1
+//     4096 x 8192    5.7 6.9 / 6.2 7.1 / 6.7 7.1 / 7.0 7.0         28672 x 4096   12.9 16.2 / 13.3 14.8 / 14.2 17.5 / 14.2 14.9
+//     4096 x 14336   8.7 9.3 / 9.0 9.0 / 9.9 9.1 / 10.4 9.0        28672 x 8192   21.7 23.8 / 23.1 24.1 / 24.4 24.0 / 25.4 24.4
+//     4096 x 28672   15.1 15.4 / 16.5 15.4 / 17.7 15.4 / 18.4 15.4
+// One launch gains up to M * K of about 28672 where a tile's columns are cut or two CTAs share an SM, and on the host (5.4 us a call, 8.1);
+// with one CTA an SM and columns uncut (N of 9500 to 19000) only up to 8192.  The border goes by M and K alone, as the workspace does.
 bool mx_linear_quantizes(int64_t M, int64_t K) { return M <= kOwnTokens && M * K <= 28672; }
 
 lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* status_word, void* stream) {
