@@ -63,7 +63,7 @@ struct Slot {
   }
 };
 
-// A maximum and a sum of 2^((v - maximum) c) or exp(v - maximum).
+// A maximum and a sum of 2^((v - maximum) c).
 struct Pair { float m, s; };
 // Two binary32 numbers in a register pair: one instruction adds or multiplies both.
 __device__ __forceinline__ uint64_t pair2(float a, float b) {
@@ -178,24 +178,24 @@ struct Params {
   int64_t ldd;
 };
 
-// All lanes get the warp's pair.  `scale`: c, or log2(e) for natural exponentials.
-__device__ __forceinline__ Pair warp_pair(Pair a, float scale) {
+// All lanes get the warp's pair.
+__device__ __forceinline__ Pair warp_pair(Pair a, float c) {
   float m = a.m;
 #pragma unroll
   for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float s = a.s * exp2_fast((a.m - m) * scale);
+  float s = a.s * exp2_fast((a.m - m) * c);
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return {m, s};
 }
 // The same of WARPS warps' pairs and numbers (behind a barrier), a power of two.
 template <int WARPS>
-__device__ __forceinline__ Pair pair_of(const Pair* part, float scale) {
+__device__ __forceinline__ Pair pair_of(const Pair* part, float c) {
   const Pair a = part[threadIdx.x & (WARPS - 1)];
   float m = a.m;
 #pragma unroll
   for (int o = WARPS / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  float s = a.s * exp2_fast((a.m - m) * scale);
+  float s = a.s * exp2_fast((a.m - m) * c);
 #pragma unroll
   for (int o = WARPS / 2; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   return {m, s};
@@ -208,9 +208,9 @@ __device__ __forceinline__ float sum_of(const float* part) {
   return s;
 }
 // The same of any number of warps, in every warp.
-__device__ __forceinline__ Pair pair_of_warps(const Pair* part, int warps, float scale) {
+__device__ __forceinline__ Pair pair_of_warps(const Pair* part, int warps, float c) {
   const int lane = threadIdx.x & 31;
-  return warp_pair(lane < warps ? part[lane] : Pair{-FLT_MAX, 0.0f}, scale);
+  return warp_pair(lane < warps ? part[lane] : Pair{-FLT_MAX, 0.0f}, c);
 }
 template <typename V>
 __device__ __forceinline__ V warp_sum(V v) {
@@ -220,23 +220,23 @@ __device__ __forceinline__ V warp_sum(V v) {
 }
 
 // Terms of a row's loss, added before the row's maximum m is known and against a reference of their own: of the entries added (p != 0)
-// the one with the largest student's logit, (v, r) with v = t / temperature.  part = sum of p ((v' - v) - (z' - r) / temperature).  Then
-//     loss = sum over shares of part + mass * ((v - log sum_j exp(v_j)) - (r - m) / temperature + log s),
+// the one with the largest student's logit r; v is the teacher's there.  part = sum of p ((t - v) - (z - r)) / temperature.  Then
+//     loss = sum over shares of part + mass * ((v - r - t_max + m) / temperature - log sum_j exp((t_j - t_max) / temperature) + log s),
 // the parentheses with what their roundings lose added at the end: log p and log q are each ten or more times the loss (256 x 32000 at
 // temperature 2 with teacher_lse, against 64 bits: 1.8e-7 relative, root mean square; 7.5e-7 with log p and log s summed apart).  The reference
 // is of THESE entries, not of other logits, which may all be masked: every z lies at or below r and r at or below m, so that what a
 // lane, a warp and the row add, (r' - r) / temperature for the sum's p, is never negative and large parts do not cancel.
 struct Share { float r, v, part; };
 // Adds an entry to a share whose entries so far have p's sum `mass`.
-__device__ __forceinline__ void add_entry(Share& a, float mass, float p, float v, float z, float inv_tau) {
+__device__ __forceinline__ void add_entry(Share& a, float mass, float p, float t, float z, float inv_tau) {
   if (p == 0.0f) return;
   const float r = fmaxf(a.r, z);
   if (mass == 0.0f || r > a.r) {
-    if (mass != 0.0f) a.part += mass * ((a.v - v) - (a.r - r) * inv_tau);
+    if (mass != 0.0f) a.part += mass * (((a.v - t) - (a.r - r)) * inv_tau);
     a.r = r;
-    a.v = v;
+    a.v = t;
   }
-  a.part += p * ((v - a.v) - (z - a.r) * inv_tau);
+  a.part += p * (((t - a.v) - (z - a.r)) * inv_tau);
 }
 // The lanes' shares together, in every lane.  `mass`: the lane's sum of p.
 __device__ __forceinline__ Share warp_share(Share a, float mass, float inv_tau) {
@@ -244,7 +244,7 @@ __device__ __forceinline__ Share warp_share(Share a, float mass, float inv_tau) 
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(a.r));       // (five shuffles: 4440 x 32000, k = 128, 62.0 us, 61.2 so)
   const unsigned at = __ballot_sync(0xffffffffu, mass != 0.0f && a.r == r);
   const float v = __shfl_sync(0xffffffffu, a.v, at ? __ffs(at) - 1 : 0);
-  if (mass != 0.0f) a.part += mass * ((a.v - v) - (a.r - r) * inv_tau);
+  if (mass != 0.0f) a.part += mass * (((a.v - v) - (a.r - r)) * inv_tau);
   return {r, v, warp_sum(a.part)};
 }
 // A sum and what its rounding lost.
@@ -263,17 +263,26 @@ __device__ __forceinline__ void split_log(float s, float& whole, float& rest) {
 // A share's part of the loss.  `all`: m and s of the row; the teacher's normalisation is *lse, or the pair of its logits.
 __device__ __forceinline__ float share_loss(float mass, const Share& a, const Pair& all, const Pair& teacher, const float* lse, float inv_tau) {
   constexpr float kLog2Hi = 0.693145751953125f, kLog2Lo = 1.42860682030941723e-6f;       // 16 bits, so that their products are exact; the rest
-  float whole, rest, whole_t = 0.0f, rest_t = 0.0f, lost[4];
+  float whole, rest, whole_t = 0.0f, rest_t = 0.0f, lost[5];
   split_log(all.s, whole, rest);
   if (!lse) split_log(teacher.s, whole_t, rest_t);
   const float n = whole - whole_t;
-  const float log_p = two_sum(a.v, lse ? -*lse : -teacher.m, lost[0]);
-  const float below = two_sum(all.m, -a.r, lost[1]), scaled = below * inv_tau;
-  const float log_q = two_sum(scaled, n * kLog2Hi, lost[2]);
-  float sum = two_sum(log_p, log_q, lost[3]);
-  if (fabsf(sum) <= FLT_MAX) sum += ((lost[0] + lost[3]) + (lost[2] + (fmaf(below, inv_tau, -scaled) + lost[1] * inv_tau))) + n * kLog2Lo;
+  const float t = two_sum(a.v, lse ? 0.0f : -teacher.m, lost[0]), below = two_sum(all.m, -a.r, lost[1]);
+  const float both = two_sum(t, below, lost[2]), scaled = both * inv_tau;
+  const float logs = two_sum(n * kLog2Hi, lse ? -*lse : 0.0f, lost[3]);
+  float sum = two_sum(scaled, logs, lost[4]);
+  if (fabsf(sum) <= FLT_MAX) sum += ((lost[3] + lost[4]) + fmaf(lost[0] + (lost[1] + lost[2]), inv_tau, fmaf(both, inv_tau, -scaled))) + n * kLog2Lo;
   sum += rest - rest_t;
   return mass == 0.0f ? 0.0f : a.part + mass * sum;
+}
+// The teacher's probabilities are exp((t - from) / temperature - norm): differences of its logits, as large ones divided by the temperature
+// would not keep them; with teacher_lse from = 0 and norm is that.
+struct Teacher { float from, norm; };
+__device__ __forceinline__ Teacher teacher_of(const Pair& top, const float* lse) {
+  return lse ? Teacher{0.0f, *lse} : Teacher{top.m, logf(top.s)};
+}
+__device__ __forceinline__ float probability(float t, const Teacher& teacher, float inv_tau) {
+  return expf(fmaf(t - teacher.from, inv_tau, -teacher.norm));
 }
 
 // What the CTAs of a row tell one another: the pair of their logits, the share of the entries in their slots, and the sum of p over those.
@@ -325,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
   const int rounds = ONCE ? 1 : (count + kSlots * threads - 1) / (kSlots * threads);
   if (LOSS || ONCE) load(0);
 
-  // the teacher's entries: index (-1: absent or p = 0), t / temperature, and z of those in this CTA's slots
+  // the teacher's entries: index (-1: absent or p = 0), t, and z of those in this CTA's slots
   Pair top = {-FLT_MAX, 0.0f};
   for (int j = tid; j < P.k; j += threads) {
     const int64_t i = P.idx_bytes == 4 ? static_cast<const int32_t*>(P.idx)[t * P.ldi + j] : static_cast<const int64_t*>(P.idx)[t * P.ldi + j];
@@ -333,9 +342,9 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
     const int64_t at = t * P.ldt + j;
     float v = -INFINITY;
     if (there) {
-      v = P.inv_tau * (P.top_type == LCD_DTYPE_F32 ? static_cast<const float*>(P.top)[at]
-                       : P.top_type == LCD_DTYPE_F16 ? __half2float(static_cast<const __half*>(P.top)[at])
-                                                     : __bfloat162float(static_cast<const __nv_bfloat16*>(P.top)[at]));
+      v = P.top_type == LCD_DTYPE_F32 ? static_cast<const float*>(P.top)[at]
+          : P.top_type == LCD_DTYPE_F16 ? __half2float(static_cast<const __half*>(P.top)[at])
+                                        : __bfloat162float(static_cast<const __nv_bfloat16*>(P.top)[at]);
       there = v != -INFINITY;
     }
     s_idx[j] = there ? (int)i : -1;
@@ -343,18 +352,18 @@ __global__ void __launch_bounds__(kThreads, 2) distill_kernel(const Params P) {
     s_z[j] = there && i >= lo0 && i < lo0 + (int64_t)count * E ? to_f32(row[i]) : 0.0f;
     if (there) {
       const float m = fmaxf(top.m, v);
-      top.s = top.s * expf(top.m - m) + expf(v - m);
+      top.s = top.s * expf((top.m - m) * P.inv_tau) + expf((v - m) * P.inv_tau);
       top.m = m;
     }
   }
-  top = warp_pair(top, 1.4426950408889634f);
+  top = warp_pair(top, P.c);
   if (lane == 0) s_top[warp] = top;
   __syncthreads();
-  top = pair_of_warps(s_top, warps, 1.4426950408889634f);
-  const float norm = P.lse ? P.lse[t] - top.m : logf(top.s);          // log p = (v - top.m) - norm
+  top = pair_of_warps(s_top, warps, P.c);
+  const Teacher teacher = teacher_of(top, P.lse ? P.lse + t : nullptr);
   float mass = 0.0f;
   for (int j = tid; j < P.k; j += threads) {
-    const float p = s_idx[j] >= 0 ? expf((s_t[j] - top.m) - norm) : 0.0f;
+    const float p = s_idx[j] >= 0 ? probability(s_t[j], teacher, P.inv_tau) : 0.0f;
     s_p[j] = p;
     mass += p;
   }
@@ -474,7 +483,7 @@ __device__ __forceinline__ void copy_wait(int newer) {      // all copies but th
 
 struct Entries {         // of three rows in turn, k each: a row's are read until the last warp has left it
   int* idx;
-  float *p, *z;          // p holds t / temperature first
+  float *p, *z;          // p holds t first
 };
 // write(index, sum of its p, its logit) for every entry, k / warps of them a warp.  An index that comes twice has all of its p, in the
 // entries' order, and each of its entries writes the same.  Whether any does is seen by counting what is equal to a warp's
@@ -518,7 +527,6 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
   constexpr int kStreamThreads = THREADS, kStreamWarps = THREADS / 32;
   constexpr int kChunkSlots = THREADS * kStreamSlots, kChunkBytes = kChunkSlots * 16;
   constexpr int E = S::E;
-  constexpr float kLog2e = 1.4426950408889634f;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Pair s_top[2][kStreamWarps], s_row[2][kStreamWarps];
   __shared__ float s_mass[2][kStreamWarps];
@@ -647,8 +655,8 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
     return (P.idx_bytes == 4 || i.y == 0) && (unsigned)i.x < (unsigned)P.V ? i.x : -1;
   };
   auto teacher_in = [&](uint32_t x) {
-    return P.inv_tau * (P.top_type == LCD_DTYPE_F32 ? __uint_as_float(x) : P.top_type == LCD_DTYPE_F16 ? __half2float(__ushort_as_half((unsigned short)x))
-                                                                                                       : __uint_as_float(x << 16));
+    return P.top_type == LCD_DTYPE_F32 ? __uint_as_float(x) : P.top_type == LCD_DTYPE_F16 ? __half2float(__ushort_as_half((unsigned short)x))
+                                                                                          : __uint_as_float(x << 16);
   };
   auto enter = [&](int64_t t, int place, int parity) {   // row t's entries to shared memory, their pair; asks for the student's logits there
     const Entries n = entries(place);
@@ -675,12 +683,12 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
         n.p[j] = v2;
         if (i2 >= 0) {
           const float m = fmaxf(top.m, v2);
-          top = {m, top.s * exp2_fast((top.m - m) * kLog2e) + exp2_fast((v2 - m) * kLog2e)};
+          top = {m, top.s * exp2_fast((top.m - m) * P.c) + exp2_fast((v2 - m) * P.c)};
           if (!LOSS) n.z[j] = to_f32(row[i2]);
         }
       }
     }
-    if (warp * 32 < P.k) top = warp_pair(top, kLog2e);
+    if (warp * 32 < P.k) top = warp_pair(top, P.c);
     if (lane == 0) s_top[parity][warp] = top;
   };
 
@@ -748,15 +756,15 @@ __global__ void __launch_bounds__(THREADS, kStreamPerSm<THREADS>) distill_stream
       if (lane == 0) s_row[parity][warp] = all;
     }
     // this row's p, its entries' terms of the loss, the next row's entries, and one barrier for all reductions
-    float mass = 0.0f;                                 // log p = (t / temperature - top.m) - norm
+    float mass = 0.0f;
     Share share = {-FLT_MAX, 0.0f, 0.0f};
     if (warp * 32 < P.k) {
-      const Pair top = pair_of<kStreamWarps>(s_top[parity], kLog2e);
-      const float norm = P.lse ? lse - top.m : logf(top.s);
+      const Pair top = pair_of<kStreamWarps>(s_top[parity], P.c);
+      const Teacher teacher = teacher_of(top, P.lse ? &lse : nullptr);
       if (LOSS && tid == 0) s_teacher[parity] = top;
       for (int j = tid; j < P.k; j += kStreamThreads) {
         const int i = n.idx[j];
-        const float v = n.p[j], p = i >= 0 ? expf((v - top.m) - norm) : 0.0f;
+        const float v = n.p[j], p = i >= 0 ? probability(v, teacher, P.inv_tau) : 0.0f;
         if (!LOSS && j == tid) n.z[j] = to_f32(e_z);
         if (LOSS && w != 0.0f && i >= 0) {
           const float z = to_f32(j == tid ? e_z : student[i]);

@@ -93,3 +93,31 @@ def test_digits_of_the_loss(T, V, tau, whole, type):
             e.append((host(v) - want) / want)
     own, plain = (np.sqrt(np.mean(np.concatenate(e) ** 2)) for e in errors)
     assert own <= plain, (own, plain)
+
+
+@pytest.mark.parametrize("tau", [0.7, 1.3])
+@pytest.mark.parametrize("T,V,k", [(3, 3000, 10), (3, 40000, 300), (300, 700, 40)])
+def test_large_teacher_logits_keep_their_differences(T, V, k, tau):
+    # t / temperature is 11702 for t = 8192 and would be rounded to 2^-10
+    z, idx, top, _ = make(T + k, T, V, k)
+    top = (top.float() * 64).round() / 64 + 8192
+    every_loss(z, idx, top, temperature=tau)
+
+
+@pytest.mark.parametrize("type", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,V", [(3, 40000), (64, 700)])
+def test_teacher_logits_whose_quotients_overflow(T, V, type):
+    z, idx, top, _ = make(T, T, V, 40)
+    high, low = torch.finfo(TYPES[type]).max, torch.finfo(TYPES[type]).min
+    top = top.to(TYPES[type])
+    top[0] = low                          # all alike, however low: 1 / k each
+    top[1] = high
+    top[2, 5:] = low                      # five entries are left
+    loss, grad, stats = every_path(z, idx, top, temperature=0.5)
+    even = lcd.distill_loss(z[:2], idx[:2], torch.zeros_like(top[:2]), temperature=0.5)
+    # (the same formula on other numbers; 16 roundings of the loss's size)
+    assert torch.isfinite(loss).all() and ((even - loss[:2]).abs() <= 2.0 ** -20 * even).all()
+    short = lcd.distill_loss(z[2:3], idx[2:3, :5].contiguous(), top[2:3, :5].contiguous(), temperature=0.5)
+    assert ((short - loss[2]).abs() <= 2.0 ** -20 * short).all()
+    if T > 3:
+        check(z[3:], idx[3:], top[3:], 0.5, loss=loss[3:], grad=grad[3:], stats=stats[3:])
