@@ -380,7 +380,8 @@ def mx_quantize(x, inv_smooth=None, codes=None, scales=None, stream=None):
 
 
 def mx_dequantize(codes, scales, K=None, out=None, dtype=None, stream=None):
-    """What codes and scales stand for, as fp32 (or dtype, or in out) [M,K]; without K all 32 * blocks columns."""
+    """What codes and scales stand for, as fp32 (or dtype, or in out) [M,K]; without K all 32 * blocks columns.  Rows of codes and of
+    scales start on 16 bytes (mx_linear says how)."""
     r = (_host_calls or _calls()).mx_dequantize(codes, scales, K, out, dtype or _float32(), stream)
     if r.__class__ is int:
         _check(r, "lcd_mx_dequantize")
@@ -388,7 +389,9 @@ def mx_dequantize(codes, scales, K=None, out=None, dtype=None, stream=None):
 
 
 def mx_linear(w_codes, w_scales, x_codes, x_scales, y=None, dtype=None, status_word=None, stream=None):
-    """y[m][n] = sum_k x^[m][k] w^[n][k] of two microscaled matrices with the same K, fp32 sums; y: CUDA [M,N], fp32 or dtype."""
+    """y[m][n] = sum_k x^[m][k] w^[n][k] of two microscaled matrices with the same K, fp32 sums; y: CUDA [M,N], fp32 or dtype.
+    Rows of codes and of scales start on 16 bytes, as mx_quantize makes them; contiguous scales [N, blocks] of a checkpoint are
+    refused unless blocks is a multiple of 16: copy them into the first columns of a tensor with wider rows and pass that slice."""
     r = (_host_calls or _calls()).mx_linear(False, w_codes, w_scales, x_codes, x_scales, y, dtype or _float32(), None, status_word, stream)
     if r.__class__ is int:
         _check(r, "lcd_mx_linear")

@@ -14,7 +14,7 @@ constexpr int64_t kMostRows = 0x7fffffffLL, kMostColumns = 1LL << 30;
 int64_t blocks_of(int64_t K) { return (K + 31) / 32; }
 int64_t on_16(int64_t v) { return (v + 15) / 16 * 16; }
 // Bytes of a row of codes in a workspace.  Long rows begin on cache lines, which the product's copies of 128 bytes would straddle
-// otherwise (333 x 5003 x 5001 16.6 us, 14.5 so; 2048 x 5120 x 5024 41.9 and 37.7); for short ones that would be much more memory.
+// otherwise (333 x 5003 x 5001 16.6 us, 15.0 so; 2048 x 5120 x 5024 41.9 and 37.7); for short ones that would be much more memory.
 int64_t code_row(int64_t K) {
   const int64_t bytes = 16 * blocks_of(K);
   return bytes < 512 ? bytes : (bytes + 127) / 128 * 128;

@@ -249,9 +249,8 @@ __device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8
 
 // X: the type of x where the kernel quantises its tokens itself (few tokens), void where codes and scales come ready.  Then the
 // epilogue warps, which wait for the sums, take the stages in turn: a CTA needs its own columns of x only and blocks are complete in
-// them, so it can be done in every CTA, and a launch is saved: 1 x 11008 x 4096 9.7 us, 10.8
-// with two launches, 1 x 4096 x 4096 5.9 and 6.1, and 5.4 us on the host in place of 8.1; from eight tokens on it takes longer than the
-// weights' copies (8 x 4096 x 4096 8.4 and 6.9).
+// them, so it can be done in every CTA, and a launch is saved (times: mx_linear_quantizes); from eight tokens on it takes longer than the
+// weights' copies (8 x 4096 x 4096 8.4 us, 6.9 with two launches).
 template <int BN, typename X>
 __global__ void __launch_bounds__(Cfg<BN>::kThreads, Cfg<BN>::kPerSm)
 mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
