@@ -9,8 +9,8 @@
  *
  *      y[m][n] = s_q[m] * sum_k q[m][k] * cb[n][idx[n][k]]          (fp32)
  *
- * Beside it stand what makes such layers offline (smoothing search, centroid initialisation, distillation loss, reclassification) and
- * the product of layers in microscaled 4-bit floating point.
+ * Beside it stand what makes such layers offline (smoothing search, centroid initialisation, distillation loss, reclassification),
+ * the product of layers in microscaled 4-bit floating point, also of experts, and low-rank adapters beside such layers.
  *
  * Conventions for every function:
  *   - returns an lcd_status; never aborts, traps or throws;
@@ -464,6 +464,84 @@ lcd_status lcd_mx_linear_fused(const uint8_t* w_codes, int64_t ldwc, const uint8
                                const void* x, lcd_dtype x_type, int64_t ldx, const float* inv_smooth, int64_t M, void* y,
                                lcd_dtype y_type, int64_t ldy, void* workspace, size_t workspace_bytes,
                                int32_t* status_word_dev, void* cuda_stream);
+
+/* ----------------------------------------------------------------------------------------------
+ * Batches whose rows go to different weights: layers of experts, and low-rank adapters of several requests beside a shared layer.  The
+ * plan of a batch, made once for all calls that follow the same assignment, lists its rows by group:
+ *   order:   int32 [count], a permutation of the rows: those of group 0 in their order, those of group 1, ..., then the rows without a
+ *            group;
+ *   groups:  int32 [count], the group of every row of that list, -1: none;
+ *   offsets: int32 [G + 1]: where in the list every group begins; the rows without a group begin at offsets[G].
+ * 1 <= count <= 2^30 rows, 1 <= G <= 1024 groups (more: LCD_ERR_UNSUPPORTED).  The calls take a plan as lcd_group_rows writes it: what an
+ * entry of another one names outside its range is left out, but results are then unspecified.
+ * -------------------------------------------------------------------------------------------- */
+typedef struct {
+  const int32_t* order;   /* device */
+  const int32_t* groups;  /* device */
+  const int32_t* offsets; /* device */
+  int64_t count;
+} lcd_row_groups;
+
+/* group: device, int32 or int64 (idx_bytes 4 or 8) [count], a row's group; values outside [0, G): none.  order, groups, offsets:
+ * device out. */
+lcd_status lcd_group_rows(const void* group, int idx_bytes, int64_t count, int64_t G, int32_t* order, int32_t* groups, int32_t* offsets,
+                          void* cuda_stream);
+
+/* A layer of G experts in microscaled 4-bit floating point, from x to y: the count = T * k rows of the plan are pairs of a token and one of
+ * its k choices, row p belongs to token p / k, and
+ *     y[p][n] = sum over k of x^[p / k][k] * w^[group of p][n][k],
+ * x^ being what lcd_mx_quantize makes of x and inv_smooth; sums in fp32, rounded once to y's type.  Rows without a group: zeros.
+ *   w_codes:  device, [G] matrices as lcd_mx_linear takes them, N rows each, expert_codes bytes apart (a multiple of 16);  w_scales likewise;
+ *   x:        device, [T][ldx], ldx >= K, count a multiple of T;     inv_smooth: device fp32 [K] or NULL, for all experts;
+ *   y:        device out, [count][ldy], ldy >= N;     status_word_dev: as for lcd_lut_linear;
+ *   workspace: device scratch of lcd_mx_linear_grouped_workspace_bytes(count, K) bytes, 16-byte aligned, contents ignored; calls that may
+ *             overlap on the device need separate ones.
+ * The plan and x may come of the kernels before on the stream; the experts' matrices must be complete when the call is enqueued or come of
+ * kernels on the stream.  Results are reproducible from run to run. */
+lcd_status lcd_mx_linear_grouped_workspace_bytes(int64_t count, int64_t K, size_t* bytes);
+
+lcd_status lcd_mx_linear_grouped(const uint8_t* w_codes, int64_t ldwc, int64_t expert_codes, const uint8_t* w_scales, int64_t ldws,
+                                 int64_t expert_scales, int64_t G, int64_t N, int64_t K, const void* x, lcd_dtype x_type, int64_t T,
+                                 int64_t ldx, const float* inv_smooth, const lcd_row_groups* rows /* host struct */, void* y, lcd_dtype y_type,
+                                 int64_t ldy, void* workspace, size_t workspace_bytes, int32_t* status_word_dev, void* cuda_stream);
+
+/* G low-rank adapters of one layer.  1 <= rank <= 128 (more: LCD_ERR_UNSUPPORTED). */
+typedef struct {
+  const void* a;          /* device, [G][rank][K]: rows lda elements apart, adapters adapter_a elements apart */
+  const void* b;          /* device, [G][N][rank]: rows ldb elements apart, adapters adapter_b elements apart */
+  lcd_dtype type;         /* of a and b */
+  int64_t lda, adapter_a, ldb, adapter_b, G, rank, K, N;
+  const float* scale;     /* device fp32 [G], or NULL: all ones */
+} lcd_adapter_weights;
+
+/* What the adapters of a batch's rows add to what a shared layer gave (lcd_lut_linear, lcd_mx_linear, any other):
+ *     y[m] = base[m] + scale_g * (x[m] a_g^T) b_g^T, g the group of row m; rows without a group: y[m] = base[m].
+ * Sums and t = x a_g^T are fp32; the result is rounded once to y's type.
+ *   x:        device, [count][ldx], ldx >= K.  Types: x and the adapters alike, or either of them fp32 (else LCD_ERR_UNSUPPORTED);
+ *   base:     device, y's type, [count][ldbase], ldbase >= N, or NULL: zeros.  May be y itself (with ldbase = ldy);
+ *   y:        device out, [count][ldy], ldy >= N;
+ *   t:        device out, fp32 [count][ldt], ldt >= rank, or NULL: t, for lcd_adapters_grad (rows without a group: zeros);
+ *   workspace: device scratch of lcd_adapters_workspace_bytes(count, rank) bytes, 16-byte aligned, contents ignored; calls that may overlap on the
+ *             device need separate ones.
+ * Results are reproducible from run to run, but a row's last bits may differ with the rows beside it. */
+lcd_status lcd_adapters_workspace_bytes(int64_t count, int64_t rank, size_t* bytes);
+
+lcd_status lcd_adapters(const lcd_adapter_weights* weights /* host struct */, const void* x, lcd_dtype x_type, int64_t ldx,
+                        const lcd_row_groups* rows /* host struct */, const void* base, int64_t ldbase, void* y, lcd_dtype y_type, int64_t ldy,
+                        float* t, int64_t ldt, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The backward pass of lcd_adapters: with dt[m] = scale_g * dy[m] b_g (fp32),
+ *     dx[m] = base[m] + dt[m] a_g (rows without a group: base[m]),
+ *     da_g = sum over g's rows of dt[m]^T x[m],     db_g = scale_g * sum over g's rows of dy[m]^T t[m];  groups without rows: zeros.
+ *   dy:       device, [count][lddy], lddy >= N;   x: device, [count][ldx];   type: of dy, x, base and dx, types as for lcd_adapters;
+ *   t:        device, fp32 [count][ldt], as lcd_adapters gave it for this x (may be NULL without db);
+ *   base, dx: device, [count][ldbase], [count][lddx], as base and y of lcd_adapters; dx may be NULL: not wanted;
+ *   da, db:   device out, grad_type, dense [G][rank][K] and [G][N][rank]; either may be NULL: not wanted;
+ *   workspace: as for lcd_adapters. */
+lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights /* host struct */, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                             lcd_dtype type, const float* t, int64_t ldt, const lcd_row_groups* rows /* host struct */, const void* base,
+                             int64_t ldbase, void* dx, int64_t lddx, void* da, void* db, lcd_dtype grad_type, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream);
 
 /* ----------------------------------------------------------------------------------------------
  * Offline: distillation from a teacher's top logits (Section 3 trains the clustered weights against the full-precision

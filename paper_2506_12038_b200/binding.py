@@ -11,6 +11,7 @@ import ctypes
 import functools
 import os
 from ctypes import c_char_p, c_int, c_int64, c_size_t, c_void_p, POINTER, Structure, byref
+from typing import NamedTuple
 
 import numpy as np
 
@@ -33,7 +34,9 @@ EXPORTS = ["lcd_status_string", "lcd_last_cuda_error", "lcd_packed_weights_bytes
            "lcd_lut_linear_batch_act8", "lcd_linear_fused_batch_workspace_bytes", "lcd_linear_fused_batch",
            "lcd_smoothing_search_workspace_bytes", "lcd_smoothing_search", "lcd_reclassify",
            "lcd_dbci_workspace_bytes", "lcd_dbci", "lcd_mx_quantize", "lcd_mx_dequantize", "lcd_mx_linear",
-           "lcd_mx_linear_fused_workspace_bytes", "lcd_mx_linear_fused", "lcd_distill_loss", "lcd_distill_grad"]
+           "lcd_mx_linear_fused_workspace_bytes", "lcd_mx_linear_fused", "lcd_distill_loss", "lcd_distill_grad",
+           "lcd_group_rows", "lcd_mx_linear_grouped_workspace_bytes", "lcd_mx_linear_grouped", "lcd_adapters_workspace_bytes",
+           "lcd_adapters", "lcd_adapters_grad"]
 STATIC_SCRATCH_BYTES = 4 << 20
 
 
@@ -65,6 +68,17 @@ class LinearProblem(Structure):
     """lcd_linear_problem"""
     _fields_ = [("packed_weights_dev", c_void_p), ("header_host", c_void_p), ("act_idx", c_void_p),
                 ("act_scale", c_void_p), ("M", c_int64), ("y", c_void_p), ("ldy", c_int64)]
+
+
+class RowGroupsC(Structure):
+    """lcd_row_groups"""
+    _fields_ = [("order", c_void_p), ("groups", c_void_p), ("offsets", c_void_p), ("count", c_int64)]
+
+
+class AdapterWeights(Structure):
+    """lcd_adapter_weights"""
+    _fields_ = [("a", c_void_p), ("b", c_void_p), ("type", c_int), ("lda", c_int64), ("adapter_a", c_int64), ("ldb", c_int64),
+                ("adapter_b", c_int64), ("G", c_int64), ("rank", c_int64), ("K", c_int64), ("N", c_int64), ("scale", c_void_p)]
 
 
 class LcdError(RuntimeError):
@@ -125,6 +139,16 @@ def _load() -> ctypes.CDLL:
     distill = matrix + [c_int64, c_int64, c_int64, c_void_p, c_int, c_int64] + matrix + [c_int64, c_int64, ctypes.c_float, c_void_p, c_void_p]
     lib.lcd_distill_loss.argtypes = distill + [c_void_p, c_void_p, c_void_p, c_int64, c_void_p]
     lib.lcd_distill_grad.argtypes = distill + [c_void_p, c_void_p, c_int64, c_void_p]
+    rows, adapters = POINTER(RowGroupsC), POINTER(AdapterWeights)
+    lib.lcd_group_rows.argtypes = [c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.lcd_mx_linear_grouped_workspace_bytes.argtypes = [c_int64, c_int64, POINTER(c_size_t)]
+    lib.lcd_mx_linear_grouped.argtypes = [c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int64, c_int64] + matrix + [
+        c_int64, c_int64, c_void_p, rows] + matrix + [c_int64, c_void_p, c_size_t, c_void_p, c_void_p]
+    lib.lcd_adapters_workspace_bytes.argtypes = [c_int64, c_int64, POINTER(c_size_t)]
+    lib.lcd_adapters.argtypes = [adapters] + matrix + [c_int64, rows, c_void_p, c_int64] + matrix + [c_int64, c_void_p, c_int64, c_void_p, c_size_t,
+                                                                                                 c_void_p]
+    lib.lcd_adapters_grad.argtypes = [adapters, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, rows, c_void_p, c_int64, c_void_p, c_int64,
+                                      c_void_p, c_void_p, c_int, c_void_p, c_size_t, c_void_p]
     for name in EXPORTS:
         if name not in ("lcd_status_string", "lcd_last_cuda_error"):
             getattr(lib, name).restype = c_int
@@ -445,6 +469,72 @@ def distill_grad(logits, teacher_idx, teacher_logits, stats, temperature: float 
     if r.__class__ is int:
         _check(r, "lcd_distill_grad")
     return r[2]
+
+
+# --------------------------------------------------------------------- rows of one batch that go to different weights
+class RowGroups(NamedTuple):
+    """The plan of a batch (lcd_row_groups): order int32 [rows], the rows sorted by group; groups int32 [rows], the group at every
+    place of that list, -1: none; offsets int32 [G + 1], where the groups begin in it.  Made once for all calls on the same rows."""
+    order: object
+    groups: object
+    offsets: object
+
+
+def group_rows(group, G: int, order=None, groups=None, offsets=None, stream=None) -> RowGroups:
+    """group: CUDA int32 or int64, one for every row (any shape, contiguous): the row's group, or anything outside [0, G) for none."""
+    r = (_host_calls or _calls()).group_rows(group, G, order, groups, offsets, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_group_rows")
+    return RowGroups(*r)
+
+
+def mx_linear_grouped(w_codes, w_scales, x, rows: RowGroups, inv_smooth=None, y=None, dtype=None, workspace=None, status_word=None, stream=None):
+    """A layer of G experts in microscaled 4-bit floating point.  w_codes: CUDA uint8 [G, N, 16 * blocks], w_scales uint8 [G, N, blocks], rows of
+    both on 16 bytes as for mx_linear; x: fp32, fp16 or bf16 [T, K].  rows: the plan of the T * k pairs of a token and its choices (row p
+    is token p // k), group_rows(choices [T, k], G).  y: CUDA [T * k, N], fp32 or dtype; rows without an expert are zeros.  workspace: CUDA
+    scratch of at least mx_linear_grouped_workspace_bytes(T * k, K) bytes (allocated here if absent)."""
+    r = (_host_calls or _calls()).mx_linear_grouped(w_codes, w_scales, x, *rows, inv_smooth, y, dtype or _float32(), workspace, status_word, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_mx_linear_grouped")
+    return r
+
+
+def mx_linear_grouped_workspace_bytes(count: int, K: int) -> int:
+    out = c_size_t(0)
+    _check(lib.lcd_mx_linear_grouped_workspace_bytes(count, K, byref(out)), "lcd_mx_linear_grouped_workspace_bytes")
+    return out.value
+
+
+def adapters(x, a, b, rows: RowGroups, base=None, y=None, scale=None, dtype=None, want_t=False, t=None, workspace=None, stream=None):
+    """y[m] = base[m] + scale[g] * (x[m] @ a[g].T) @ b[g].T, g the adapter of row m; rows without one keep base (zeros without base).
+    x: CUDA fp32, fp16 or bf16 [rows, K]; a [G, rank, K] and b [G, N, rank] of x's type or fp32 (any type if x is fp32); scale: fp32 [G];
+    base: [rows, N], y's type; y: may be base itself.  Without base y has dtype, or x's type.  Returns y, and with want_t (or t given) also
+    t = x a^T, fp32 [rows, rank], for adapters_grad.  workspace: CUDA scratch of at least adapters_workspace_bytes(rows, rank) bytes
+    (allocated here if absent)."""
+    r = (_host_calls or _calls()).adapters(x, a, b, *rows, base, y, scale, dtype, t if t is not None else True if want_t else None, workspace, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_adapters")
+    return r[0] if r[1] is None else r
+
+
+def adapters_grad(dy, x, a, b, t, rows: RowGroups, base=None, dx=None, scale=None, da=None, db=None, grad_dtype=None, want_dx=True, want_weights=True,
+                  workspace=None, stream=None):
+    """The backward pass of adapters: (dx, da, db).  With dt[m] = scale[g] * dy[m] @ b[g]: dx[m] = base[m] + dt[m] @ a[g] (base: the shared
+    layer's part of the gradient, dx may be base itself), da[g] = dt^T x and db[g] = scale[g] dy^T t over g's rows, in grad_dtype (a's type);
+    adapters without rows get zeros.  dy and x have one type, which is dx's.  t: as adapters gave it.  want_dx, want_weights: False leaves
+    that part out (None in its place)."""
+    r = (_host_calls or _calls()).adapters_grad(dy, x, a, b, t, *rows, base, scale, (True if dx is None else dx) if want_dx else None,
+                                                (True if da is None else da) if want_weights else None,
+                                                (True if db is None else db) if want_weights else None, grad_dtype, workspace, stream)
+    if r.__class__ is int:
+        _check(r, "lcd_adapters_grad")
+    return r
+
+
+def adapters_workspace_bytes(count: int, rank: int) -> int:
+    out = c_size_t(0)
+    _check(lib.lcd_adapters_workspace_bytes(count, rank, byref(out)), "lcd_adapters_workspace_bytes")
+    return out.value
 
 
 def resolve_batch_algo(weights_and_tokens, algo: int = ALGO_AUTO) -> int:

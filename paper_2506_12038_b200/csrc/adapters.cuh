@@ -1,0 +1,164 @@
+// Low-rank adapters beside a shared layer: what the three kernels have in common (adapters_down.cu: x a^T and dy b, adapters_up.cu: t b^T
+// and dt a, added to what is there, adapters_outer.cu: the adapters' gradients).
+//
+// All three are bound by the one pass over x, y, dy or dx (a rank of 64 needs 64 FLOP a byte of 16-bit activations), so operands go
+// from memory to registers in the fragment order of mma.sync and nothing is staged: a sum does not care for the order of its terms, so
+// a lane takes 16 consecutive bytes of its row for the slots that the instruction gives it, and both operands use the same order.
+// (A tcgen05 product would have to bring the gathered rows of x to shared memory first.)
+//
+// Arithmetic.  Two 16-bit operands of one type: their products are exact, sums are fp32.  The products with t or dt, which are fp32: with
+// bf16 beside them as two bf16 terms (16 bits, relative error 2^-16 where the result is rounded to 16-bit types) or three (24 bits, for
+// fp32 results), else as two tf32 terms (22 bits; fp32 beside them likewise in two).
+#ifndef LCD_ADAPTERS_CUH_
+#define LCD_ADAPTERS_CUH_
+
+#include <type_traits>
+
+#include "common.h"
+#include "device_util.h"
+#include "mx.cuh"
+
+namespace lcd {
+
+template <typename T> constexpr bool kIs16 = sizeof(T) == 2;
+
+// D (16 x 8) += A (16 x 16) B (16 x 8) of 16-bit values, pairs in a word.
+template <typename T>
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (std::is_same<T, __half>::value)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// D (16 x 8) += A (16 x 8) B (8 x 8) of tf32 values.
+__device__ __forceinline__ void mma_tf32(float (&d)[4], float a0, float a1, float a2, float a3, float b0, float b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(__float_as_uint(a0)), "r"(__float_as_uint(a1)), "r"(__float_as_uint(a2)), "r"(__float_as_uint(a3)),
+                 "r"(__float_as_uint(b0)), "r"(__float_as_uint(b1)));
+}
+
+// v = upper + rest.  The upper part is v cut off (never rounded up, which could overflow), the rest exact; an infinity has no rest.
+__device__ __forceinline__ float upper_tf32(float v) { return __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
+__device__ __forceinline__ float upper_bf16(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
+__device__ __forceinline__ float rest_of(float v, float upper) { return (__float_as_uint(v) & 0x7fffffffu) == 0x7f800000u ? 0.0f : v - upper; }
+// Two values as a word of bf16: their upper parts, or rounded.
+__device__ __forceinline__ uint32_t pair_upper(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
+__device__ __forceinline__ uint32_t pair_rounded(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// N consecutive values of a row as words, zeros where `have` ends.  WIDE: they lie on N * sizeof(T) bytes (16 at most) and are all there or
+// none is.
+template <typename T, int N>
+struct Words {
+  static constexpr int kCount = N * (int)sizeof(T) / 4;
+  uint32_t w[kCount];
+};
+template <typename T, int N>
+__device__ __forceinline__ void load_words(Words<T, N>& out, const T* p, int have, bool wide) {
+  constexpr int kCount = Words<T, N>::kCount;
+  if (wide) {
+    if (have > 0) {
+      if constexpr (kCount >= 4) {
+#pragma unroll
+        for (int i = 0; i < kCount; i += 4) {
+          const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i);
+          out.w[i] = v.x; out.w[i + 1] = v.y; out.w[i + 2] = v.z; out.w[i + 3] = v.w;
+        }
+      } else if constexpr (kCount == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        out.w[0] = v.x; out.w[1] = v.y;
+      } else {
+        out.w[0] = *reinterpret_cast<const uint32_t*>(p);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) out.w[i] = 0u;
+    }
+    return;
+  }
+  if constexpr (kIs16<T>) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const uint32_t lo = i < have ? q[i] : 0u, hi = i + 1 < have ? q[i + 1] : 0u;
+      out.w[i / 2] = lo | hi << 16;
+    }
+  } else {
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) out.w[i] = i < have ? q[i] : 0u;
+  }
+}
+// Value i of them.
+template <typename T, int N>
+__device__ __forceinline__ float value_of(const Words<T, N>& v, int i) {
+  if constexpr (std::is_same<T, float>::value) {
+    return __uint_as_float(v.w[i]);
+  } else if constexpr (std::is_same<T, __half>::value) {
+    const __half2 h = *reinterpret_cast<const __half2*>(&v.w[i / 2]);
+    return i % 2 ? __high2float(h) : __low2float(h);
+  } else {
+    return __uint_as_float(i % 2 ? v.w[i / 2] & 0xffff0000u : v.w[i / 2] << 16);
+  }
+}
+// Value i of two rows as a word of 16-bit values.
+template <typename T, int N>
+__device__ __forceinline__ uint32_t pair_of(const Words<T, N>& a, const Words<T, N>& b, int i) {
+  return __byte_perm(a.w[i / 2], b.w[i / 2], i % 2 ? 0x7632 : 0x5410);
+}
+
+// The plan of the rows and the adapters, as the kernels see them.
+struct AdapterArgs {
+  const int32_t *order, *groups, *offsets;
+  int rows, G;
+  int r;                       // the rank
+  long long K;                 // columns of the long side of this launch's adapter matrix
+  const void* w;               // adapter matrix: a [G][r][K] or b [G][K][r]
+  long long ldw, sw;           // its rows' and adapters' pitch
+  const float* scale;          // [G] or null
+  int wide_w, wide_x;
+};
+
+__device__ __forceinline__ int row_of(const int32_t* order, int at, int rows) {
+  const int row = order[at];
+  return (unsigned)row < (unsigned)rows ? row : -1;
+}
+
+// RT for a rank: 16 * RT is the rank padded.
+constexpr int rank_tiles(int64_t r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }
+constexpr int kMostRank = 128;
+
+template <typename F>
+lcd_status by_rank(int64_t r, F&& f) {
+  switch (rank_tiles(r)) {
+    case 1: return f(std::integral_constant<int, 1>{});
+    case 2: return f(std::integral_constant<int, 2>{});
+    case 4: return f(std::integral_constant<int, 4>{});
+    default: return f(std::integral_constant<int, 8>{});
+  }
+}
+template <typename T> struct TypeTag { using type = T; };
+template <typename F>
+lcd_status by_dtype(lcd_dtype t, F&& f) {
+  switch (t) {
+    case LCD_DTYPE_F32: return f(TypeTag<float>{});
+    case LCD_DTYPE_F16: return f(TypeTag<__half>{});
+    default: return f(TypeTag<__nv_bfloat16>{});
+  }
+}
+// Whether pieces of `bytes` bytes of rows with that pitch (elements) and, over several adapters, that distance can be loaded whole.
+inline bool on_bytes(const void* p, int64_t pitch, int64_t distance, int64_t size, int64_t bytes) {
+  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && pitch * size % bytes == 0 && distance * size % bytes == 0;
+}
+inline lcd_status adapter_launched(cudaError_t e) {
+  if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+  return LCD_OK;
+}
+
+}  // namespace lcd
+#endif

@@ -1,0 +1,47 @@
+// The launches of the adapters' kernels (arguments are checked and laid out by api_groups.cu).
+#ifndef LCD_ADAPTERS_LAUNCH_H_
+#define LCD_ADAPTERS_LAUNCH_H_
+
+#include "adapters.cuh"
+
+namespace lcd {
+
+struct UpArgs {
+  AdapterArgs a;
+  const float* t;              // by place, 16 * RT values a row
+  const void* base;            // or null
+  void* y;
+  long long ldbase, ldy;
+  int window, wide_base, wide_y, in_place;
+  int early;                   // the kernel before this one wrote t and nothing else that is read here, and began when all before it was done
+};
+lcd_status launch_adapters_up(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s);
+
+struct DownArgs;
+lcd_status launch_adapters_down_f32(const DownArgs& P, lcd_dtype w_type, bool backward, cudaStream_t s);
+lcd_status launch_adapters_down_f16(const DownArgs& P, lcd_dtype w_type, bool backward, cudaStream_t s);
+lcd_status launch_adapters_down_bf16(const DownArgs& P, lcd_dtype w_type, bool backward, cudaStream_t s);
+
+// The gradient of one adapter matrix: [r] x columns of z's, sums over an adapter's rows of u (r values a row, fp32) times z.
+struct OuterSide {
+  const float* u;              // [rows][ldu], by place or by row
+  long long ldu;
+  int u_by_place, wide_u;
+  const void* z;               // [rows][ldz]
+  long long ldz;
+  int wide_z;
+  long long columns;
+  const float* scale;          // [G] or null
+  void* out;                   // [G][r][columns], or [G][columns][r]
+  int by_column;
+};
+struct OuterArgs {
+  const int32_t *order, *offsets;
+  int rows, G, r, out_type, sides;
+  OuterSide side[2];
+  long long slabs[2];
+};
+lcd_status launch_adapters_outer(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s);
+
+}  // namespace lcd
+#endif

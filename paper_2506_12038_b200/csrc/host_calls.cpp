@@ -589,6 +589,275 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- rows that go to different weights
+// The plan's three tensors: int32, contiguous, on one device.
+bool plan_of(PyObject* const* a, const at::Device& device, int64_t* G, lcd_row_groups* out) {
+  const at::Tensor *order = tensor_of(a[0], "order"), *groups = order ? tensor_of(a[1], "groups") : nullptr;
+  const at::Tensor* offsets = groups ? tensor_of(a[2], "offsets") : nullptr;
+  if (!offsets) return false;
+  for (const at::Tensor* t : {order, groups, offsets})
+    if (!require(t->device() == device && t->scalar_type() == at::kInt && t->dim() == 1 && t->is_contiguous(),
+                 "rows: int32 order, groups and offsets, contiguous, on the same device as the other arguments"))
+      return false;
+  if (!require(groups->size(0) == order->size(0) && offsets->size(0) >= 2, "rows: as many groups as rows, an offset more than groups")) return false;
+  *G = offsets->size(0) - 1;
+  *out = {static_cast<const int32_t*>(order->data_ptr()), static_cast<const int32_t*>(groups->data_ptr()),
+          static_cast<const int32_t*>(offsets->data_ptr()), order->size(0)};
+  return true;
+}
+// A given workspace (contiguous, on the device) or a new one.
+bool workspace_of(PyObject* o, size_t need, const at::Device& device, at::Tensor* space, size_t* have) {
+  if (o == Py_None) {
+    *space = fresh({(int64_t)need}, at::kByte, device);
+  } else {
+    const at::Tensor* t = tensor_of(o, "workspace");
+    if (!t || !require(t->device() == device && t->is_contiguous(), "workspace: contiguous, on the same device")) return false;
+    *space = *t;
+  }
+  *have = (size_t)space->numel() * space->element_size();
+  return true;
+}
+
+// (group, G, order, groups, offsets, stream) -> (order, groups, offsets) or a status
+PyObject* group_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 6)) return nullptr;
+  const at::Tensor* group = tensor_of(a[0], "group");
+  if (!group || !require(group->is_cuda() && group->is_contiguous() && (group->scalar_type() == at::kInt || group->scalar_type() == at::kLong),
+                         "group: contiguous CUDA int32 or int64"))
+    return nullptr;
+  const int64_t G = PyLong_AsLongLong(a[1]), count = group->numel();
+  if (PyErr_Occurred()) return nullptr;
+  const at::Device device = group->device();
+  const c10::cuda::CUDAGuard on(device);
+  const CallStream stream(a[5]);
+  if (!stream.ok()) return nullptr;
+  if (count < 1 || G < 1) return PyLong_FromLong((long)LCD_ERR_INVALID_ARG);
+  if (G > 1024 || count > (1ll << 30)) return PyLong_FromLong((long)(G > 1024 ? LCD_ERR_UNSUPPORTED : LCD_ERR_INVALID_ARG));
+  at::Tensor order, groups, offsets;
+  if (!output_of(a[2], "order", {count}, at::kInt, device, "order: int32 [rows] on group's device", &order) ||
+      !output_of(a[3], "groups", {count}, at::kInt, device, "groups: int32 [rows] on group's device", &groups) ||
+      !output_of(a[4], "offsets", {G + 1}, at::kInt, device, "offsets: int32 [G + 1] on group's device", &offsets) ||
+      !require(order.is_contiguous() && groups.is_contiguous() && offsets.is_contiguous(), "order, groups, offsets: contiguous"))
+    return nullptr;
+  const lcd_status st = without_gil([&] {
+    return lcd_group_rows(group->data_ptr(), group->scalar_type() == at::kInt ? 4 : 8, count, G, static_cast<int32_t*>(order.data_ptr()),
+                          static_cast<int32_t*>(groups.data_ptr()), static_cast<int32_t*>(offsets.data_ptr()), stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return pack({returned(stream, a[2], order), returned(stream, a[3], groups), returned(stream, a[4], offsets)});
+  END_HANDLE_TH_ERRORS
+}
+
+// (w_codes, w_scales, x, order, groups, offsets, inv_smooth, y, dtype, workspace, status_word, stream) -> y or a status
+PyObject* mx_linear_grouped(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 12)) return nullptr;
+  const at::Tensor *wc = tensor_of(a[0], "w_codes"), *ws = wc ? tensor_of(a[1], "w_scales") : nullptr, *x = ws ? tensor_of(a[2], "x") : nullptr;
+  if (!x || !require(wc->is_cuda() && wc->scalar_type() == at::kByte && wc->dim() == 3 && wc->size(2) % 16 == 0 && wc->size(2) > 0 && wc->stride(2) == 1,
+                     "w_codes: CUDA uint8 [G, N, 16 * blocks]"))
+    return nullptr;
+  const at::Device device = wc->device();
+  const int64_t G = wc->size(0), N = wc->size(1), blocks = wc->size(2) / 16;
+  if (!require(ws->device() == device && ws->scalar_type() == at::kByte && ws->dim() == 3 && ws->size(0) == G && ws->size(1) == N &&
+                   ws->size(2) == blocks && (ws->stride(2) == 1 || blocks == 1),
+               "w_scales: uint8 [G, N, blocks] on the codes' device"))
+    return nullptr;
+  lcd_dtype x_type, y_type;
+  if (!require(dense(*x, &x_type) && x->device() == device, "x: fp32, fp16 or bf16 [T, K] with unit column stride on the weights' device")) return nullptr;
+  const int64_t T = x->size(0), K = x->size(1);
+  int64_t groups;
+  lcd_row_groups rows;
+  const float* inv;
+  int32_t* word;
+  at::ScalarType type;
+  if (!require((K + 31) / 32 == blocks, "x: [T, K], K being 32 * blocks of the weights, or up to 31 less") || !plan_of(a + 3, device, &groups, &rows) ||
+      !require(groups == G, "rows: a plan of as many groups as there are experts") ||
+      !require(T > 0 && rows.count % T == 0, "rows: a multiple of x's rows") ||
+      !vector_of(a[6], "inv_smooth", device, K, "inv_smooth: fp32 [K] on x's device", &inv) || !dtype_of(a[8], &type) ||
+      !status_word_of(a[10], device, &word))
+    return nullptr;
+  const c10::cuda::CUDAGuard on(device);
+  const CallStream stream(a[11]);
+  if (!stream.ok()) return nullptr;
+  if (a[7] != Py_None) {
+    const at::Tensor* t = tensor_of(a[7], "y");
+    if (!t) return nullptr;
+    type = t->scalar_type();
+  }
+  size_t need = 0, have = 0;
+  const lcd_status sized = lcd_mx_linear_grouped_workspace_bytes(rows.count, K, &need);
+  if (sized != LCD_OK) return PyLong_FromLong((long)sized);
+  at::Tensor y, space;
+  if (!require(type_of(type, &y_type), "y: fp32, fp16 or bf16") ||
+      !output_of(a[7], "y", {rows.count, N}, type, device, "y: [rows, N] with unit column stride on the weights' device", &y) ||
+      !workspace_of(a[9], need, device, &space, &have))
+    return nullptr;
+  const lcd_status st = without_gil([&] {
+    const int64_t ldc = N > 1 ? wc->stride(1) : 16 * blocks, lds = N > 1 ? ws->stride(1) : (blocks + 15) / 16 * 16;
+    return lcd_mx_linear_grouped(static_cast<const uint8_t*>(wc->data_ptr()), ldc, wc->stride(0), static_cast<const uint8_t*>(ws->data_ptr()), lds,
+                                 ws->stride(0), G, N, K, x->data_ptr(), x_type, T, row_stride(*x), inv, &rows, y.data_ptr(), y_type, row_stride(y),
+                                 have ? space.data_ptr() : nullptr, have, word, stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return returned(stream, a[7], y);
+  END_HANDLE_TH_ERRORS
+}
+
+// The adapters' matrices and factors.
+bool adapters_of(PyObject* a, PyObject* b, PyObject* scale, lcd_adapter_weights* w, at::Device* device) {
+  const at::Tensor *ta = tensor_of(a, "a"), *tb = ta ? tensor_of(b, "b") : nullptr;
+  if (!tb || !require(ta->is_cuda() && ta->dim() == 3 && type_of(ta->scalar_type(), &w->type) && (ta->stride(2) == 1 || ta->size(2) == 1),
+                      "a: CUDA fp32, fp16 or bf16 [G, rank, K] with unit column stride") ||
+      !require(tb->device() == ta->device() && tb->dim() == 3 && tb->scalar_type() == ta->scalar_type() && (tb->stride(2) == 1 || tb->size(2) == 1) &&
+                   tb->size(0) == ta->size(0) && tb->size(2) == ta->size(1),
+               "b: [G, N, rank] of a's type, with unit column stride, on a's device"))
+    return false;
+  *device = ta->device();
+  w->a = ta->data_ptr();
+  w->b = tb->data_ptr();
+  w->G = ta->size(0);
+  w->rank = ta->size(1);
+  w->K = ta->size(2);
+  w->N = tb->size(1);
+  w->lda = w->rank > 1 ? ta->stride(1) : w->K;
+  w->ldb = w->N > 1 ? tb->stride(1) : w->rank;
+  w->adapter_a = ta->stride(0);
+  w->adapter_b = tb->stride(0);
+  return vector_of(scale, "scale", *device, w->G, "scale: fp32 [G] on the adapters' device", &w->scale);
+}
+bool rows_of_x(const at::Tensor* x, const at::Device& device, int64_t count, int64_t columns, lcd_dtype* type, const char* expected) {
+  return x && require(dense(*x, type) && x->device() == device && x->size(0) == count && x->size(1) == columns, expected);
+}
+
+// (x, a, b, order, groups, offsets, base, y, scale, dtype or None, t (None, True: a new one), workspace, stream) -> (y, t or None) or a status
+PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 13)) return nullptr;
+  lcd_adapter_weights w = {};
+  at::Device device(at::kCPU);
+  int64_t groups;
+  lcd_row_groups rows;
+  lcd_dtype x_type, y_type, base_type;
+  if (!adapters_of(a[1], a[2], a[8], &w, &device) || !plan_of(a + 3, device, &groups, &rows) ||
+      !require(groups == w.G, "rows: a plan of as many groups as there are adapters"))
+    return nullptr;
+  const at::Tensor *x = tensor_of(a[0], "x"), *base = nullptr;
+  if (!rows_of_x(x, device, rows.count, w.K, &x_type, "x: fp32, fp16 or bf16 [rows, K] with unit column stride on the adapters' device")) return nullptr;
+  at::ScalarType type = x->scalar_type();
+  if (a[9] != Py_None && !dtype_of(a[9], &type)) return nullptr;
+  if (a[6] != Py_None) {
+    base = tensor_of(a[6], "base");
+    if (!rows_of_x(base, device, rows.count, w.N, &base_type, "base: fp32, fp16 or bf16 [rows, N] with unit column stride on the adapters' device") ||
+        !require(a[9] == Py_None || base->scalar_type() == type, "dtype: base's"))
+      return nullptr;
+    type = base->scalar_type();
+  } else if (a[7] != Py_None && a[9] == Py_None) {
+    const at::Tensor* t = tensor_of(a[7], "y");
+    if (!t) return nullptr;
+    type = t->scalar_type();
+  }
+  const c10::cuda::CUDAGuard on(device);
+  const CallStream stream(a[12]);
+  if (!stream.ok()) return nullptr;
+  size_t need = 0, have = 0;
+  const lcd_status sized = lcd_adapters_workspace_bytes(rows.count, w.rank, &need);
+  if (sized != LCD_OK) return PyLong_FromLong((long)sized);
+  PyObject* want_t = a[10] == Py_True ? Py_None : a[10];
+  const bool has_t = a[10] != Py_None;
+  at::Tensor y, t, space;
+  if (!require(type_of(type, &y_type), "y: fp32, fp16 or bf16") ||
+      !output_of(a[7], "y", {rows.count, w.N}, type, device, "y: [rows, N] of base's type, with unit column stride, on the adapters' device", &y) ||
+      (has_t && !output_of(want_t, "t", {rows.count, w.rank}, at::kFloat, device, "t: fp32 [rows, rank] with unit column stride on the adapters' device", &t)) ||
+      !workspace_of(a[11], need, device, &space, &have))
+    return nullptr;
+  const lcd_status st = without_gil([&] {
+    return lcd_adapters(&w, x->data_ptr(), x_type, row_stride(*x), &rows, base ? base->data_ptr() : nullptr, base ? row_stride(*base) : 0, y.data_ptr(),
+                        y_type, row_stride(y), has_t ? static_cast<float*>(t.data_ptr()) : nullptr, has_t ? row_stride(t) : 0,
+                        have ? space.data_ptr() : nullptr, have, stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return pack({returned(stream, a[7], y), has_t ? returned(stream, want_t, t) : Py_NewRef(Py_None)});
+  END_HANDLE_TH_ERRORS
+}
+
+// (dy, x or None, a, b, t or None, order, groups, offsets, base, scale, dx, da, db (each None: not wanted, True: a new one), grad dtype or None,
+//  workspace, stream) -> (dx, da, db), None where not wanted, or a status
+PyObject* adapters_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (!count_args(n, 16)) return nullptr;
+  lcd_adapter_weights w = {};
+  at::Device device(at::kCPU);
+  int64_t groups;
+  lcd_row_groups rows;
+  lcd_dtype type, other, grad_type = LCD_DTYPE_F32;
+  if (!adapters_of(a[2], a[3], a[9], &w, &device) || !plan_of(a + 5, device, &groups, &rows) ||
+      !require(groups == w.G, "rows: a plan of as many groups as there are adapters"))
+    return nullptr;
+  const at::Tensor *dy = tensor_of(a[0], "dy"), *x = nullptr, *t = nullptr, *base = nullptr;
+  if (!rows_of_x(dy, device, rows.count, w.N, &type, "dy: fp32, fp16 or bf16 [rows, N] with unit column stride on the adapters' device")) return nullptr;
+  if (a[1] != Py_None) {
+    x = tensor_of(a[1], "x");
+    if (!rows_of_x(x, device, rows.count, w.K, &other, "x: [rows, K] of dy's type, with unit column stride, on the adapters' device") ||
+        !require(other == type, "x: dy's type"))
+      return nullptr;
+  }
+  if (a[4] != Py_None) {
+    t = tensor_of(a[4], "t");
+    if (!rows_of_x(t, device, rows.count, w.rank, &other, "t: fp32 [rows, rank] with unit column stride on the adapters' device") ||
+        !require(other == LCD_DTYPE_F32, "t: fp32"))
+      return nullptr;
+  }
+  if (a[8] != Py_None) {
+    base = tensor_of(a[8], "base");
+    if (!rows_of_x(base, device, rows.count, w.K, &other, "base: [rows, K] of dy's type, with unit column stride, on the adapters' device") ||
+        !require(other == type, "base: dy's type"))
+      return nullptr;
+  }
+  PyObject* want[3];
+  bool has[3];
+  for (int i = 0; i < 3; ++i) {
+    has[i] = a[10 + i] != Py_None;
+    want[i] = a[10 + i] == Py_True ? Py_None : a[10 + i];
+  }
+  at::ScalarType kind = tensor_of(a[2], "a")->scalar_type();
+  if (a[13] != Py_None && !dtype_of(a[13], &kind)) return nullptr;
+  if (a[13] == Py_None)
+    for (int i = 1; i < 3; ++i)
+      if (has[i] && want[i] != Py_None) {
+        const at::Tensor* given = tensor_of(want[i], "da, db");
+        if (!given) return nullptr;
+        kind = given->scalar_type();
+        break;
+      }
+  if (!require(type_of(kind, &grad_type), "da, db: fp32, fp16 or bf16") || !require(x || !has[1], "da: needs x") || !require(t || !has[2], "db: needs t")) return nullptr;
+  const c10::cuda::CUDAGuard on(device);
+  const CallStream stream(a[15]);
+  if (!stream.ok()) return nullptr;
+  size_t need = 0, have = 0;
+  const lcd_status sized = lcd_adapters_workspace_bytes(rows.count, w.rank, &need);
+  if (sized != LCD_OK) return PyLong_FromLong((long)sized);
+  at::Tensor dx, da, db, space;
+  if ((has[0] && !output_of(want[0], "dx", {rows.count, w.K}, dy->scalar_type(), device, "dx: [rows, K] of dy's type, with unit column stride, on the adapters' device", &dx)) ||
+      (has[1] && (!output_of(want[1], "da", {w.G, w.rank, w.K}, kind, device, "da: [G, rank, K] on the adapters' device", &da) ||
+                  !require(da.is_contiguous(), "da: contiguous"))) ||
+      (has[2] && (!output_of(want[2], "db", {w.G, w.N, w.rank}, kind, device, "db: [G, N, rank] of da's type on the adapters' device", &db) ||
+                  !require(db.is_contiguous(), "db: contiguous"))) ||
+      !workspace_of(a[14], need, device, &space, &have))
+    return nullptr;
+  const lcd_status st = without_gil([&] {
+    return lcd_adapters_grad(&w, dy->data_ptr(), row_stride(*dy), x ? x->data_ptr() : nullptr, x ? row_stride(*x) : 0, type,
+                             t ? static_cast<const float*>(t->data_ptr()) : nullptr, t ? row_stride(*t) : 0, &rows, base ? base->data_ptr() : nullptr,
+                             base ? row_stride(*base) : 0, has[0] ? dx.data_ptr() : nullptr, has[0] ? row_stride(dx) : 0,
+                             has[1] ? da.data_ptr() : nullptr, has[2] ? db.data_ptr() : nullptr, grad_type, have ? space.data_ptr() : nullptr, have,
+                             stream.raw());
+  });
+  if (st != LCD_OK) return PyLong_FromLong((long)st);
+  return pack({has[0] ? returned(stream, want[0], dx) : Py_NewRef(Py_None), has[1] ? returned(stream, want[1], da) : Py_NewRef(Py_None),
+               has[2] ? returned(stream, want[2], db) : Py_NewRef(Py_None)});
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef kMethods[] = {
     {"smooth_quantize_act", reinterpret_cast<PyCFunction>(smooth_quantize_act), METH_FASTCALL, nullptr},
     {"lut_linear", reinterpret_cast<PyCFunction>(lut_linear), METH_FASTCALL, nullptr},
@@ -600,6 +869,10 @@ PyMethodDef kMethods[] = {
     {"mx_dequantize", reinterpret_cast<PyCFunction>(mx_dequantize), METH_FASTCALL, nullptr},
     {"mx_linear", reinterpret_cast<PyCFunction>(mx_linear), METH_FASTCALL, nullptr},
     {"distill", reinterpret_cast<PyCFunction>(distill), METH_FASTCALL, nullptr},
+    {"group_rows", reinterpret_cast<PyCFunction>(group_rows), METH_FASTCALL, nullptr},
+    {"mx_linear_grouped", reinterpret_cast<PyCFunction>(mx_linear_grouped), METH_FASTCALL, nullptr},
+    {"adapters", reinterpret_cast<PyCFunction>(adapters), METH_FASTCALL, nullptr},
+    {"adapters_grad", reinterpret_cast<PyCFunction>(adapters_grad), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

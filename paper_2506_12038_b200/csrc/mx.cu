@@ -32,12 +32,28 @@ __device__ __forceinline__ Place place() {
   return {blockIdx.y * blockDim.x + threadIdx.x, (int64_t)blockIdx.x * EACH * blockDim.y + threadIdx.y};
 }
 
+// Rows by a plan: row i of the codes is row order[i] / each of x; rows from *end on are not needed.
+struct Gather {
+  const int32_t *order, *end;
+  int each;
+};
+
 // VEC: rows of x start on 16 bytes.
-template <typename T, bool VEC, int EACH>
+template <typename T, bool VEC, int EACH, bool GATHER>
 __global__ void __launch_bounds__(kMxThreads)
 mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc, uint8_t* scales,
-                   int64_t lds, uint32_t units) {
+                   int64_t lds, uint32_t units, Gather gather) {
   begin_after_previous();       // (no __restrict__: loads of what the kernel before wrote are coherent ones)
+  const int64_t rows = M;
+  if (GATHER) {
+    M = min(M, (int64_t)*gather.end);
+    if ((int64_t)blockIdx.x * EACH * blockDim.y >= M) return;
+  }
+  auto row_at = [&](int64_t row) {
+    if (!GATHER) return row;
+    const uint32_t from = (uint32_t)gather.order[row];
+    return from < (uint64_t)rows ? (int64_t)(from / (uint32_t)gather.each) : (int64_t)0;
+  };
   __shared__ __align__(16) T s_x[VEC ? 1 : EACH * kMxThreads * 8];
   const Place at = place<EACH>();
   const int64_t k0 = (int64_t)at.unit * 8;
@@ -46,7 +62,7 @@ mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* i
   Raw8<T> raw[EACH];
   if (whole) {
 #pragma unroll
-    for (int u = 0; u < EACH; ++u) raw[u] = load8(x + min(at.row0 + u * blockDim.y, M - 1) * ldx + k0);
+    for (int u = 0; u < EACH; ++u) raw[u] = load8(x + row_at(min(at.row0 + u * blockDim.y, M - 1)) * ldx + k0);
   }
   if (inv) {
     if (k0 + 8 <= K && (reinterpret_cast<uintptr_t>(inv) & 15) == 0) {
@@ -61,11 +77,11 @@ mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* i
     const int64_t from = (int64_t)blockIdx.y * n + threadIdx.x;
 #pragma unroll
     for (int u = 0; u < EACH; ++u) {
-      const int64_t row = at.row0 + u * blockDim.y;
+      const int64_t row = at.row0 + u * blockDim.y, from_row = row < M ? row_at(row) : 0;
       T* line = s_x + (u * blockDim.y + threadIdx.y) * n + threadIdx.x;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        line[i * blockDim.x] = row < M && from + i * blockDim.x < K ? x[row * ldx + from + i * blockDim.x] : from_f32<T>(0.0f);
+        line[i * blockDim.x] = row < M && from + i * blockDim.x < K ? x[from_row * ldx + from + i * blockDim.x] : from_f32<T>(0.0f);
     }
     __syncthreads();
   }
@@ -76,7 +92,7 @@ mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* i
       values8(raw[u], t);
     } else if (VEC) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t[i] = row < M && k0 + i < K ? to_f32(x[row * ldx + k0 + i]) : 0.0f;
+      for (int i = 0; i < 8; ++i) t[i] = row < M && k0 + i < K ? to_f32(x[row_at(row) * ldx + k0 + i]) : 0.0f;
     } else {
       const T* line = s_x + (u * blockDim.y + threadIdx.y) * blockDim.x * 8;
       values8(load8(line + threadIdx.x * 8), t);
@@ -181,17 +197,17 @@ Shape shape_of(int64_t rows, uint32_t units, uint32_t threads) {
   return {dim3((unsigned)((rows + per - 1) / per), columns), dim3(x, y), each};
 }
 
-template <typename T>
+template <typename T, bool GATHER = false>
 lcd_status quantize_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc,
-                         uint8_t* scales, int64_t lds, cudaStream_t s) {
+                         uint8_t* scales, int64_t lds, cudaStream_t s, const Gather& gather = {}) {
   const uint32_t units = (uint32_t)((K + kMxBlock - 1) / kMxBlock * 4);
-  const bool vec = on16(x, ldx, sizeof(T), M);
+  const bool vec = on16(x, ldx, sizeof(T), GATHER ? M / gather.each : M);
   // (2048 x 5120 bf16: 128 threads 7.8 us, 256 8.9; through shared memory, 333 x 5001, 5.1 and 4.2)
   const Shape q = shape_of(M, units, vec ? kMxThreads / 2 : kMxThreads);
   if (q.grid.y > 65535) return LCD_ERR_UNSUPPORTED;
-  auto kern = vec ? (q.each ? mx_quantize_kernel<T, true, kRowsEach> : mx_quantize_kernel<T, true, 1>)
-                  : (q.each ? mx_quantize_kernel<T, false, kRowsEach> : mx_quantize_kernel<T, false, 1>);
-  return launched(launch_overlapping(kern, q.grid, q.block, 0, 1, s, static_cast<const T*>(x), M, K, ldx, inv, codes, ldc, scales, lds, units));
+  auto kern = vec ? (q.each ? mx_quantize_kernel<T, true, kRowsEach, GATHER> : mx_quantize_kernel<T, true, 1, GATHER>)
+                  : (q.each ? mx_quantize_kernel<T, false, kRowsEach, GATHER> : mx_quantize_kernel<T, false, 1, GATHER>);
+  return launched(launch_overlapping(kern, q.grid, q.block, 0, 1, s, static_cast<const T*>(x), M, K, ldx, inv, codes, ldc, scales, lds, units, gather));
 }
 
 template <typename T>
@@ -216,6 +232,17 @@ lcd_status launch_mx_quantize(const void* x, lcd_dtype type, int64_t M, int64_t 
     case LCD_DTYPE_F32: return quantize_rows<float>(x, M, K, ldx, inv, codes, ldc, scales, lds, s);
     case LCD_DTYPE_F16: return quantize_rows<__half>(x, M, K, ldx, inv, codes, ldc, scales, lds, s);
     default: return quantize_rows<__nv_bfloat16>(x, M, K, ldx, inv, codes, ldc, scales, lds, s);
+  }
+}
+
+lcd_status launch_mx_quantize_rows(const void* x, lcd_dtype type, int64_t T, int64_t K, int64_t ldx, const float* inv, const lcd_row_groups& rows,
+                                   int64_t G, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, void* stream) {
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const Gather gather = {rows.order, rows.offsets + G, (int)(rows.count / T)};
+  switch (type) {
+    case LCD_DTYPE_F32: return quantize_rows<float, true>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+    case LCD_DTYPE_F16: return quantize_rows<__half, true>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+    default: return quantize_rows<__nv_bfloat16, true>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
   }
 }
 

@@ -12,12 +12,15 @@
 //   warps 6-9, 11-14  epilogue: tensor memory -> y, coalesced along the weight rows; up to four tokens come as they are, then these warps
 //               quantise them into the stages first
 // Many tokens take pairs of CTAs (mx_pair_kernel below).
+// Products grouped by expert (lcd_mx_linear_grouped) are the same kernel with another list of tiles: the tokens' codes lie sorted by
+// expert, a tile is a piece of one expert's tokens, and y's rows are scattered to where the plan says they come from.
 // Where tiles are few the columns of a tile are cut among the CTAs of a cluster; their partial sums meet in distributed shared
 // memory and are added in the order of the ranks, so results do not depend on timing.
 // Every wait is bounded (status word LCD_ERR_TIMEOUT on expiry; then every role leaves its loop, copies and MMAs in flight are
 // drained, tensor memory is released).
 #include <cuda.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include "common.h"
@@ -35,6 +38,7 @@ constexpr int kScaleSlots = 3;
 constexpr int kMostSplit = 8;                  // a cluster's CTAs
 constexpr int kOwnTokens = 4;                  // tokens that the kernel quantises itself
 constexpr int kMmaWarp = 1, kFirstEpiWarp = 6, kScaleCopyWarp = 10;
+
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
 template <int BN>
@@ -69,6 +73,33 @@ struct Args {
   long long ldx;
   const float* inv;
   int K, x_wide;
+  const int32_t *order, *offsets;    // grouped: the plan of the M rows, and the number of experts
+  int G;
+};
+
+// A tile's first weight row, first token, number of tokens and, grouped, expert.
+struct Spot { int n0, m0, tokens, expert; };
+
+// The tiles in order: along the weight rows, a weight tile's token tiles one after the other; grouped, one expert after the other.
+// first: the token tiles before every expert, and of all (shared memory).  Tiles are asked for in ascending order.
+template <int BN, bool GROUPED>
+struct Tiles {
+  const Args& P;
+  const int* first;
+  int expert = 0;
+  __device__ __forceinline__ Spot at(int tile) {
+    if constexpr (GROUPED) {
+      const int nt = (P.N + kRows - 1) / kRows;
+      while (expert + 1 < P.G && (long long)first[expert + 1] * nt <= tile) ++expert;
+      const int local = tile - first[expert] * nt, mt = max(1, first[expert + 1] - first[expert]);
+      const int begin = min(max(P.offsets[expert], 0), P.M), end = min(max(P.offsets[expert + 1], begin), P.M);
+      const int m0 = begin + local % mt * BN;
+      return {local / mt * kRows, m0, min(BN, end - m0), expert};
+    } else {
+      const int m0 = tile % P.n_tiles_m * BN;
+      return {tile / P.n_tiles_m * kRows, m0, min(BN, P.M - m0), 0};
+    }
+  }
 };
 
 __device__ __forceinline__ unsigned long long timer_ns() {
@@ -116,6 +147,10 @@ __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, int x, int row, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void copy_tile_of(uint32_t dst, const CUtensorMap* map, int x, int row, int expert, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(expert), "r"(bar) : "memory");
 }
 // Shared-memory matrix descriptor: K-major, 128-byte swizzle, 8-row groups 1024 bytes apart.
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
@@ -235,6 +270,28 @@ __device__ __forceinline__ void store_columns(const Args& P, uint32_t from, int 
   });
 }
 
+// The same with the tokens' rows of y from the plan: lane j % 16 has the row of column c + j, asked for sixteen columns ahead.
+__device__ __forceinline__ int planned_row(const Args& P, int place) {
+  const int row = place < P.M ? P.order[place] : -1;
+  return (unsigned)row < (unsigned)P.M ? row : -1;
+}
+template <bool AHEAD>
+__device__ __forceinline__ void scatter_columns(const Args& P, uint32_t from, int begin, int end, int m0, int n, int first_row) {
+  by_type(P, [&](auto* y) {
+    using T = std::remove_pointer_t<decltype(y)>;
+    int next = first_row;
+    drain_columns<AHEAD>(from, begin, end, [&](int c, const uint32_t (&v)[16]) {
+      const int row = next, ahead = c + 16 + (threadIdx.x & 15);
+      next = ahead < end ? planned_row(P, m0 + ahead) : -1;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        const int r = __shfl_sync(0xffffffffu, row, j);
+        if (r >= 0 && n < P.N) y[(size_t)r * P.ldy + n] = from_f32<T>(__uint_as_float(v[j]));
+      }
+    });
+  });
+}
+
 // Eight columns of a token from k on, zeros beyond K.  `raw` holds them where they lie on 16 bytes inside the row.
 template <typename X>
 __device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8<X>& raw, float (&t)[8]) {
@@ -251,7 +308,7 @@ __device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8
 // epilogue warps, which wait for the sums, take the stages in turn: a CTA needs its own columns of x only and blocks are complete in
 // them, so it can be done in every CTA, and a launch is saved (times: mx_linear_quantizes); from eight tokens on it takes longer than the
 // weights' copies (8 x 4096 x 4096 8.4 us, 6.9 with two launches).
-template <int BN, typename X>
+template <int BN, typename X, bool GROUPED>
 __global__ void __launch_bounds__(Cfg<BN>::kThreads, Cfg<BN>::kPerSm)
 mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                  const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const Args P) {
@@ -284,6 +341,8 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   const int ks0 = 2 * ss0, ks1 = min(P.n_ks, 2 * ss1);
   const int tile0 = blockIdx.x / split, tile_step = gridDim.x / split;
   constexpr bool kReady = std::is_same<X, void>::value;
+  static_assert(kReady || !GROUPED, "grouped tokens' codes come ready");
+  int* first = reinterpret_cast<int*>(gen + kBarAt + 256);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
@@ -312,9 +371,32 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                  ::"r"((uint32_t)__cvta_generic_to_shared(tmem_holder)), "r"((uint32_t)C::kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (GROUPED && warp == 2) {
+    // The plan was there when the kernel before this one began (P.early).
+    int sum = 0;
+    for (int e0 = 0; e0 < P.G; e0 += 32) {
+      const int e = e0 + lane;
+      int tiles = 0;
+      if (e < P.G) {
+        const int begin = min(max(P.offsets[e], 0), P.M), end = min(max(P.offsets[e + 1], begin), P.M);
+        tiles = (end - begin + BN - 1) / BN;
+      }
+      int upto = tiles;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int v = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += v;
+      }
+      if (e < P.G) first[e] = sum + upto - tiles;
+      sum += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    if (lane == 0) first[P.G] = sum;
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const int n_tiles = GROUPED ? min(P.n_tiles, first[P.G] * ((P.N + kRows - 1) / kRows)) : P.n_tiles;
+  Tiles<BN, GROUPED> tiles{P, first};
   const uint32_t tmem = *tmem_holder;
   const uint32_t sf_tmem = tmem + C::kDBuffers * BN;
   // The kernel before may run on for long: no other role starts the time of a wait before it has ended.  (The copying threads wait for it
@@ -332,33 +414,37 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       const int from = codes ? ks0 : ss0, to = codes ? ks1 : ss1;
       constexpr uint32_t bytes = codes ? kAStage + (kReady ? C::kBStage : 0) : kReady ? C::kScaleBytes : kRows * 16;
       auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
-      auto copy_w = [&](int s, int k, int row) {
-        if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full(s));
-        else copy_tile(s_base + s * C::kScaleBytes, &map_ws, k * 16, row, sc_full(s));
+      auto copy_w = [&](int s, int k, const Spot& q) {
+        if (GROUPED) copy_tile_of(codes ? a_base + s * kAStage : s_base + s * C::kScaleBytes, codes ? &map_w : &map_ws, k * (codes ? kStageK / 2 : 16), q.n0, q.expert, full_of(s));
+        else if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), q.n0, full(s));
+        else copy_tile(s_base + s * C::kScaleBytes, &map_ws, k * 16, q.n0, sc_full(s));
       };
       auto copy_x = [&](int s, int k, int row) {
         if (codes) copy_tile(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), row, full(s));
         else copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, row, sc_full(s));
       };
-      const int ahead = P.early && tile0 < P.n_tiles ? min(slots, to - from) : 0;
-      for (int i = 0; i < ahead; ++i) {
-        bar_expect_tx(full_of(i), bytes);
-        copy_w(i, from + i, tile0 / P.n_tiles_m * kRows);
+      const int ahead = P.early && tile0 < n_tiles ? min(slots, to - from) : 0;
+      if (ahead > 0) {
+        const Spot q = tiles.at(tile0);
+        for (int i = 0; i < ahead; ++i) {
+          bar_expect_tx(full_of(i), bytes);
+          copy_w(i, from + i, q);
+        }
       }
       begin_after_previous();
       int it = 0, s = 0;
       uint32_t round = 1;          // the parity of a stage's barrier
       bool ok = true;
-      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step) {
-        const int n0 = tile / P.n_tiles_m * kRows, m0 = tile % P.n_tiles_m * BN;
+      for (int tile = tile0; tile < n_tiles && ok; tile += tile_step) {
+        const Spot q = tiles.at(tile);
         for (int k = from; k < to; ++k, ++it) {
           if (it >= ahead) {
             ok = bar_wait(codes ? empty(s) : sc_empty(s), round, abort_flag);
             if (!ok) break;
             bar_expect_tx(full_of(s), bytes);
-            copy_w(s, k, n0);
+            copy_w(s, k, q);
           }
-          if (kReady) copy_x(s, k, m0);
+          if (kReady) copy_x(s, k, q.m0);
           if (++s == slots) {
             s = 0;
             round ^= 1u;
@@ -380,7 +466,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       const uint64_t a_desc0 = smem_desc(a_base), b_desc0 = smem_desc(b_base);
       uint32_t it = 0, sit = 0, tl = 0;
       bool ok = true;
-      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+      for (int tile = tile0; tile < n_tiles && ok; tile += tile_step, ++tl) {
         const uint32_t buf = tl % C::kDBuffers;
         ok = bar_wait(d_empty(buf), ((tl / C::kDBuffers) & 1u) ^ 1u, abort_flag);
         if (!ok) break;
@@ -420,7 +506,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16;
     uint32_t sit = 0;
     bool ok = true;
-    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step)
+    for (int tile = tile0; tile < n_tiles && ok; tile += tile_step)
       for (int ss = ss0; ss < ss1; ++ss, ++sit) {
         const uint32_t slot = sit % kScaleSlots, sb = sit % C::kSfSlots;
         ok = __all_sync(0xffffffffu, bar_wait(sc_full(slot), (sit / kScaleSlots) & 1u, abort_flag) &&
@@ -446,7 +532,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const uint32_t quarter = (uint32_t)(32 * quad) << 16;
     uint32_t tl = 0;
     bool ok = true;
-    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+    for (int tile = tile0; tile < n_tiles && ok; tile += tile_step, ++tl) {
       if constexpr (!kReady) {
         if (tl == 0) begin_after_previous();
         // Stage i of the CTA's belongs to warp i % 4: a lane has eight columns, four lanes a block, of one token after the other.  The
@@ -517,19 +603,23 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         if (!ok) break;
       }
       const uint32_t buf = tl % C::kDBuffers;
-      const int n = tile / P.n_tiles_m * kRows + 32 * quad + lane, m0 = tile % P.n_tiles_m * BN;
-      const int tokens = min(BN, P.M - m0);
+      const Spot q = tiles.at(tile);
+      const int n = q.n0 + 32 * quad + lane, m0 = q.m0, tokens = q.tokens;
+      const int half = warp > kScaleCopyWarp ? BN / 2 : 0;
+      const int row = GROUPED && half + (lane & 15) < tokens ? planned_row(P, m0 + half + (lane & 15)) : -1;
       ok = __all_sync(0xffffffffu, bar_wait(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t from = tmem + quarter + buf * BN;
-      const int begin = warp > kScaleCopyWarp ? BN / 2 : 0, end = C::kEpiHalves == 2 && !begin ? min(tokens, BN / 2) : tokens;
+      const int begin = half, end = C::kEpiHalves == 2 && !begin ? min(tokens, BN / 2) : tokens;
       if (split > 1) {            // every copy into the stages has landed and been read: they hold the partial sums
         float* part = reinterpret_cast<float*>(gen) + 32 * quad + lane;
         drain_columns<(BN > 64)>(from, begin, end, [&](int c, const uint32_t (&v)[16]) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) part[(c + j) * kRows] = __uint_as_float(v[j]);
         });
+      } else if constexpr (GROUPED) {
+        scatter_columns<(BN > 64)>(P, from, begin, end, m0, n, row);
       } else {
         store_columns<(BN > 64)>(P, from, begin, end, m0, n);
       }
@@ -538,13 +628,24 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       if (lane == 0) bar_arrive(d_empty(buf));
       __syncwarp();
     }
+    if constexpr (GROUPED) {           // rows without an expert: zeros
+      const int thread = (warp > kScaleCopyWarp ? warp - 1 : warp) * 32 + lane - 32 * kFirstEpiWarp;
+      by_type(P, [&](auto* y) {
+        using T = std::remove_pointer_t<decltype(y)>;
+        for (long long i = (long long)max(P.offsets[P.G], 0) + blockIdx.x; i < P.M; i += gridDim.x) {
+          const int r = planned_row(P, (int)i);
+          if (r < 0) continue;
+          for (int n = thread; n < P.N; n += 128 * C::kEpiHalves) y[(size_t)r * P.ldy + n] = from_f32<T>(0.0f);
+        }
+      });
+    }
   }
   if (split > 1) {
     // Token t of the tile is added up by rank t % split, a warp for 32 rows; the loads from all ranks are on their way together.
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-    const int n0 = tile0 / P.n_tiles_m * kRows, m0 = tile0 % P.n_tiles_m * BN;
-    const int tokens = min(BN, P.M - m0);
+    const Spot q = !GROUPED || tile0 < n_tiles ? Tiles<BN, GROUPED>{P, first}.at(tile0) : Spot{0, 0, 0, 0};
+    const int n0 = q.n0, m0 = q.m0, tokens = q.tokens;
     constexpr int kBatch = BN == 16 ? 1 : 4;           // groups of 32 rows that a warp adds at a time
     for (int item = warp;; item += C::kThreads / 32) {
       const int t = rank + split * (item * kBatch / 4), row = item * kBatch % 4 * 32 + lane;
@@ -568,10 +669,11 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       }
       by_type(P, [&](auto* y) {
         using T = std::remove_pointer_t<decltype(y)>;
-        T* to = y + (size_t)(m0 + t) * P.ldy + n0 + row;
+        const int y_row = GROUPED ? planned_row(P, m0 + t) : m0 + t;
+        T* to = y + (size_t)max(y_row, 0) * P.ldy + n0 + row;
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
-          if (n0 + row + 32 * j < P.N) to[32 * j] = from_f32<T>(v[0][j]);
+          if (n0 + row + 32 * j < P.N && (!GROUPED || y_row >= 0)) to[32 * j] = from_f32<T>(v[0][j]);
       });
     }
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
@@ -943,10 +1045,35 @@ Plan plan(int64_t M, int64_t N, int64_t n_ks) {
   return best;
 }
 
+// The width and the cut of a product grouped by expert.  How many rows an expert has is not known here; from the mean m over the experts
+// that can occur, taken for exponentially distributed, an expert has 1 / (1 - exp(-w / m)) tiles of w tokens.  Times as above.
+Plan plan_grouped(int64_t rows, int64_t G, int64_t N, int64_t n_ks) {
+  static constexpr struct { int width; double stage, epilogue; } kWidths[] = {{16, 0.33, 0.1}, {32, 0.33, 0.2}, {64, 0.34, 0.4},
+                                                                               {128, 0.31, 0.4}, {192, 0.39, 0.2}, {256, 0.35, 2.9}};
+  const double experts = (double)(G < rows ? G : rows), mean = (double)rows / experts, sms = current_sm_count();
+  const int64_t n_tiles_n = (N + kRows - 1) / kRows, n_ss = (n_ks + 1) / 2;
+  Plan best = {256, 1, false};
+  double least = 1e300;
+  for (const auto& w : kWidths) {
+    const double tiles = experts * n_tiles_n / (1.0 - exp(-w.width / mean));
+    const int64_t bound = (rows / w.width + (int64_t)experts) * n_tiles_n;
+    for (int s = 1; s <= kMostSplit && s <= n_ss && (s == 1 || bound * s <= (int64_t)sms); s *= 2) {
+      if (s > 4 && (w.width >= 128 || bound * s > (int64_t)sms / 2)) break;
+      const double waves = tiles < sms ? 1.0 : tiles / sms;
+      const double time = waves * (2 * w.stage * ((n_ss + s - 1) / s) + w.epilogue) + (s > 1 ? 2.0 + fmin(mean, w.width) / (64.0 * s) : 0.0);
+      if (time < least) {
+        least = time;
+        best = {w.width, s, false};
+      }
+    }
+  }
+  return best;
+}
+
 template <int BN, typename X = void>
 lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* status, cudaStream_t s) {
   using C = Cfg<BN>;
-  auto kern = mx_linear_kernel<BN, X>;
+  auto kern = mx_linear_kernel<BN, X, false>;
   static PerDeviceFlag attr_set;
   int dev;
   if (attr_set.first(&dev)) {
@@ -991,6 +1118,63 @@ lcd_status launch_width(const MxProduct& p, int split, bool early, int32_t* stat
   const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
   const unsigned grid = (unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room);
   const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(C::kThreads), C::kSmem, (unsigned)split, s, w, x, ws, xs, a);
+  if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+  return LCD_OK;
+}
+
+// The matrices of all experts: the third coordinate is the expert.
+bool encode_experts(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t rows, int64_t ld, int64_t experts, int64_t distance, int box_bytes,
+                    bool swizzled) {
+  const EncodeTiledFn encode = encode_tiled();
+  const cuuint64_t dims[3] = {(cuuint64_t)bytes, (cuuint64_t)rows, (cuuint64_t)experts}, strides[2] = {(cuuint64_t)ld, (cuuint64_t)distance};
+  const cuuint32_t box[3] = {(cuuint32_t)box_bytes, (cuuint32_t)kRows, 1}, one[3] = {1, 1, 1};
+  return encode && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<uint8_t*>(p), dims, strides, box, one,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, swizzled ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN>
+lcd_status launch_grouped(const MxGrouped& p, int split, int32_t* status, cudaStream_t s) {
+  using C = Cfg<BN>;
+  constexpr int kSmem = C::kSmem + 4 * (kMostGroups + 1);
+  static_assert(kSmem <= 227 * 1024 && C::kPerSm * (kSmem + 1024) <= 228 * 1024, "shared memory");
+  auto kern = mx_linear_kernel<BN, void, true>;
+  static PerDeviceFlag attr_set;
+  int dev;
+  if (attr_set.first(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+    attr_set.done(dev);
+  }
+  const int64_t blocks = (p.K + kMxBlock - 1) / kMxBlock, n_tiles_n = (p.N + kRows - 1) / kRows;
+  // at most: every expert's last tile may hold one token
+  const int64_t tiles = (p.rows.count / BN + (p.G < p.rows.count ? p.G : p.rows.count)) * n_tiles_n;
+  if (tiles * split > 0x7fffffff) return LCD_ERR_UNSUPPORTED;
+  CUtensorMap w, x, ws, xs;
+  if (!encode_experts(&w, p.w_codes, blocks * 16, p.N, p.ldwc, p.G, p.dwc, kStageK / 2, true) ||
+      !encode_experts(&ws, p.w_scales, blocks, p.N, p.ldws, p.G, p.dws, 16, false) ||
+      !encode_rows(&x, p.x_codes, blocks * 16, p.rows.count, p.ldxc, kStageK / 2, BN, true) ||
+      !encode_rows(&xs, p.x_scales, blocks, p.rows.count, p.ldxs, 16, BN, false)) {
+    set_cuda_error((int)cudaErrorInvalidValue);
+    return LCD_ERR_CUDA;
+  }
+  Args a = {};
+  a.y = p.y;
+  a.ldy = p.ldy;
+  a.y_type = (int)p.y_type;
+  a.M = (int)p.rows.count;
+  a.N = (int)p.N;
+  a.n_ks = (int)((blocks * kMxBlock + kStageK - 1) / kStageK);
+  a.n_ss = (a.n_ks + 1) / 2;
+  a.n_tiles = (int)tiles;
+  a.early = 1;
+  a.status = status;
+  a.order = p.rows.order;
+  a.offsets = p.rows.offsets;
+  a.G = (int)p.G;
+  const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
+  const unsigned grid = (unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room);
+  const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(C::kThreads), kSmem, (unsigned)split, s, w, x, ws, xs, a);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
@@ -1065,6 +1249,20 @@ lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* st
     case 128: return launch_width<128>(p, w.split, x_just_written, status_word, s);
     case 192: return launch_width<192>(p, w.split, x_just_written, status_word, s);
     default: return launch_width<256>(p, w.split, x_just_written, status_word, s);
+  }
+}
+
+lcd_status launch_mx_grouped(const MxGrouped& p, int32_t* status_word, void* stream) {
+  if (p.G > kMostGroups) return LCD_ERR_UNSUPPORTED;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const Plan w = plan_grouped(p.rows.count, p.G, p.N, ((p.K + kMxBlock - 1) / kMxBlock * kMxBlock + kStageK - 1) / kStageK);
+  switch (w.width) {
+    case 16: return launch_grouped<16>(p, w.split, status_word, s);
+    case 32: return launch_grouped<32>(p, w.split, status_word, s);
+    case 64: return launch_grouped<64>(p, w.split, status_word, s);
+    case 128: return launch_grouped<128>(p, w.split, status_word, s);
+    case 192: return launch_grouped<192>(p, w.split, status_word, s);
+    default: return launch_grouped<256>(p, w.split, status_word, s);
   }
 }
 
