@@ -491,6 +491,7 @@ lcd_status lcd_group_rows(const void* group, int idx_bytes, int64_t count, int64
  * its k choices, row p belongs to token p / k, and
  *     y[p][n] = sum over k of x^[p / k][k] * w^[group of p][n][k],
  * x^ being what lcd_mx_quantize makes of x and inv_smooth; sums in fp32, rounded once to y's type.  Rows without a group: zeros.
+ *   1 <= G <= 512 (more: LCD_ERR_UNSUPPORTED);
  *   w_codes:  device, [G] matrices as lcd_mx_linear takes them, N rows each, expert_codes bytes apart (a multiple of 16);  w_scales likewise;
  *   x:        device, [T][ldx], ldx >= K, count a multiple of T;     inv_smooth: device fp32 [K] or NULL, for all experts;
  *   y:        device out, [count][ldy], ldy >= N;     status_word_dev: as for lcd_lut_linear;

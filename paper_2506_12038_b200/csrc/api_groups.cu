@@ -94,7 +94,7 @@ extern "C" lcd_status lcd_mx_linear_grouped(const uint8_t* w_codes, int64_t ldwc
       !aligned(status_word_dev, 4) || lcd_mx_linear_grouped_workspace_bytes(rows->count, K, &need) != LCD_OK)
     return LCD_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < need) return LCD_ERR_BUFFER_TOO_SMALL;
-  if (G > kMostGroups) return LCD_ERR_UNSUPPORTED;
+  if (G > kMostExperts) return LCD_ERR_UNSUPPORTED;
   const int64_t ldc = code_row(K), lds = on(blocks_of(K), 16);
   uint8_t* codes = static_cast<uint8_t*>(workspace);
   uint8_t* scales = codes + rows->count * ldc;

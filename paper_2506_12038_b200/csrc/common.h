@@ -120,7 +120,7 @@ lcd_status launch_mx_dequantize(const uint8_t* codes, int64_t ldc, const uint8_t
                                 lcd_dtype type, int64_t ldo, void* stream);
 // x_just_written: x's codes come of the kernel launched directly before, which lets this one start early (launch_mx_quantize).
 lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* status_word, void* stream);
-constexpr int kMostGroups = 1024;
+constexpr int kMostGroups = 1024, kMostExperts = 512;
 // The rows of one batch that go to different weights (arguments are checked by api_groups.cu).
 lcd_status launch_group_rows(const void* group, int idx_bytes, int64_t rows, int64_t G, int32_t* order, int32_t* groups, int32_t* offsets,
                              void* stream);

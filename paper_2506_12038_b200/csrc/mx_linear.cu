@@ -41,10 +41,10 @@ constexpr int kMmaWarp = 1, kFirstEpiWarp = 6, kScaleCopyWarp = 10;
 
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
-template <int BN>
+template <int BN, bool GROUPED = false>
 struct Cfg {
   static constexpr int kBStage = BN * kStageK / 2;
-  static constexpr int kStages = BN <= 32 ? 5 : BN == 256 ? 4 : BN == 192 ? 5 : BN == 128 ? 6 : 4;
+  static constexpr int kStages = BN == 32 && GROUPED ? 4 : BN <= 32 ? 5 : BN == 256 ? 4 : BN == 192 ? 5 : BN == 128 ? 6 : 4;
   static constexpr int kScaleBytes = (kRows + BN) * 16;
   static constexpr int kSfbCols = (BN + 127) / 128 * 4;                   // tensor-memory columns of the tokens' scales, per 128 columns
   static constexpr int kSfCols = 4 * (4 + kSfbCols);                     // of a scale slot: 512 columns
@@ -52,9 +52,11 @@ struct Cfg {
   static constexpr int kSfSlots = 2;                                     // (four were no faster)
   static constexpr int kUsed = kDBuffers * BN + kSfSlots * kSfCols;
   static constexpr int kTmemCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
-  static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 256;
   static constexpr int kPerSm = BN <= 64 ? 2 : 1;
-  static constexpr int kEpiHalves = kDBuffers == 1 ? 2 : 1;              // the one accumulator is drained by twice the warps
+  static constexpr int kEpiHalves = kDBuffers == 1 || (GROUPED && BN == 192) ? 2 : 1;   // the one accumulator is drained by twice the warps
+  // grouped: the token tiles before every expert and where its tokens begin, and for every epilogue warp where its columns go
+  static constexpr int kPlanBytes = 8 * (kMostExperts + 1), kPlacesBytes = 4 * BN * 8;
+  static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 256 + (GROUPED ? kPlanBytes + kPlacesBytes : 0);
   static constexpr int kThreads = 32 * (11 + 4 * (kEpiHalves - 1));
   // Whatever shares an SM has tensor memory enough, so that no CTA of a cluster waits for columns while another CTA of it holds some:
   // two of the narrow tiles fit, and beside a wide one nothing does (shared memory).
@@ -81,20 +83,27 @@ struct Args {
 struct Spot { int n0, m0, tokens, expert; };
 
 // The tiles in order: along the weight rows, a weight tile's token tiles one after the other; grouped, one expert after the other.
-// first: the token tiles before every expert, and of all (shared memory).  Tiles are asked for in ascending order.
+// first: the token tiles before every expert, and of all; begins: where the experts' tokens begin (shared memory).  Tiles are asked for in
+// ascending order.
 template <int BN, bool GROUPED>
 struct Tiles {
   const Args& P;
-  const int* first;
+  const int *first, *begins;
   int expert = 0;
   __device__ __forceinline__ Spot at(int tile) {
     if constexpr (GROUPED) {
       const int nt = (P.N + kRows - 1) / kRows;
-      while (expert + 1 < P.G && (long long)first[expert + 1] * nt <= tile) ++expert;
+      if (expert + 1 < P.G && first[expert + 1] * nt <= tile) {
+        int high = P.G - 1;                      // the last expert that begins at this tile or before
+        while (expert < high) {
+          const int middle = (expert + high + 1) / 2;
+          if (first[middle] * nt <= tile) expert = middle;
+          else high = middle - 1;
+        }
+      }
       const int local = tile - first[expert] * nt, mt = max(1, first[expert + 1] - first[expert]);
-      const int begin = min(max(P.offsets[expert], 0), P.M), end = min(max(P.offsets[expert + 1], begin), P.M);
-      const int m0 = begin + local % mt * BN;
-      return {local / mt * kRows, m0, min(BN, end - m0), expert};
+      const int m0 = begins[expert] + local % mt * BN;
+      return {local / mt * kRows, m0, min(BN, begins[expert + 1] - m0), expert};
     } else {
       const int m0 = tile % P.n_tiles_m * BN;
       return {tile / P.n_tiles_m * kRows, m0, min(BN, P.M - m0), 0};
@@ -270,23 +279,29 @@ __device__ __forceinline__ void store_columns(const Args& P, uint32_t from, int 
   });
 }
 
-// The same with the tokens' rows of y from the plan: lane j % 16 has the row of column c + j, asked for sixteen columns ahead.
+// The row of y of a place of the plan, or -1.
 __device__ __forceinline__ int planned_row(const Args& P, int place) {
   const int row = place < P.M ? P.order[place] : -1;
   return (unsigned)row < (unsigned)P.M ? row : -1;
 }
+// store_columns with the tokens' rows from the plan: places[c - begin] is the first element of column c's row in y, or negative.
 template <bool AHEAD>
-__device__ __forceinline__ void scatter_columns(const Args& P, uint32_t from, int begin, int end, int m0, int n, int first_row) {
+__device__ __forceinline__ void scatter_columns(const Args& P, uint32_t from, int begin, int end, uint32_t places, int n) {
   by_type(P, [&](auto* y) {
     using T = std::remove_pointer_t<decltype(y)>;
-    int next = first_row;
+    y += n;
+    const bool inside = n < P.N;
     drain_columns<AHEAD>(from, begin, end, [&](int c, const uint32_t (&v)[16]) {
-      const int row = next, ahead = c + 16 + (threadIdx.x & 15);
-      next = ahead < end ? planned_row(P, m0 + ahead) : -1;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        const int r = __shfl_sync(0xffffffffu, row, j);
-        if (r >= 0 && n < P.N) y[(size_t)r * P.ldy + n] = from_f32<T>(__uint_as_float(v[j]));
+      for (int half = 0; half < 16; half += 8) {
+        // (asked for together: behind a store the compiler would wait for that)
+        long long at[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2)
+          asm volatile("ld.shared.v2.s64 {%0, %1}, [%2];" : "=l"(at[j]), "=l"(at[j + 1]) : "r"(places + 8 * (c - begin + half + j)));
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (inside && at[j] >= 0) y[at[j]] = from_f32<T>(__uint_as_float(v[half + j]));
       }
     });
   });
@@ -309,10 +324,10 @@ __device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8
 // them, so it can be done in every CTA, and a launch is saved (times: mx_linear_quantizes); from eight tokens on it takes longer than the
 // weights' copies (8 x 4096 x 4096 8.4 us, 6.9 with two launches).
 template <int BN, typename X, bool GROUPED>
-__global__ void __launch_bounds__(Cfg<BN>::kThreads, Cfg<BN>::kPerSm)
+__global__ void __launch_bounds__(Cfg<BN, GROUPED>::kThreads, Cfg<BN, GROUPED>::kPerSm)
 mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                  const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const Args P) {
-  using C = Cfg<BN>;
+  using C = Cfg<BN, GROUPED>;
   extern __shared__ uint8_t smem_raw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw_addr = (uint32_t)__cvta_generic_to_shared(smem_raw);
@@ -342,7 +357,9 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   const int tile0 = blockIdx.x / split, tile_step = gridDim.x / split;
   constexpr bool kReady = std::is_same<X, void>::value;
   static_assert(kReady || !GROUPED, "grouped tokens' codes come ready");
-  int* first = reinterpret_cast<int*>(gen + kBarAt + 256);
+  long long* places = reinterpret_cast<long long*>(gen + kBarAt + 256);          // grouped
+  int* first = reinterpret_cast<int*>(gen + kBarAt + 256 + C::kPlacesBytes);
+  int* begins = first + kMostExperts + 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
@@ -380,6 +397,8 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       if (e < P.G) {
         const int begin = min(max(P.offsets[e], 0), P.M), end = min(max(P.offsets[e + 1], begin), P.M);
         tiles = (end - begin + BN - 1) / BN;
+        begins[e] = begin;
+        if (e == P.G - 1) begins[P.G] = end;
       }
       int upto = tiles;
 #pragma unroll
@@ -396,7 +415,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const int n_tiles = GROUPED ? min(P.n_tiles, first[P.G] * ((P.N + kRows - 1) / kRows)) : P.n_tiles;
-  Tiles<BN, GROUPED> tiles{P, first};
+  Tiles<BN, GROUPED> tiles{P, first, begins};
   const uint32_t tmem = *tmem_holder;
   const uint32_t sf_tmem = tmem + C::kDBuffers * BN;
   // The kernel before may run on for long: no other role starts the time of a wait before it has ended.  (The copying threads wait for it
@@ -606,7 +625,15 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       const Spot q = tiles.at(tile);
       const int n = q.n0 + 32 * quad + lane, m0 = q.m0, tokens = q.tokens;
       const int half = warp > kScaleCopyWarp ? BN / 2 : 0;
-      const int row = GROUPED && half + (lane & 15) < tokens ? planned_row(P, m0 + half + (lane & 15)) : -1;
+      long long* mine = places + (warp > kScaleCopyWarp ? warp - kFirstEpiWarp - 1 : warp - kFirstEpiWarp) * (BN / C::kEpiHalves);
+      if constexpr (GROUPED) {
+        __syncwarp();
+        for (int i = lane; i < BN / C::kEpiHalves; i += 32) {
+          const int row = half + i < tokens ? planned_row(P, m0 + half + i) : -1;
+          mine[i] = row < 0 ? -1 : row * P.ldy;
+        }
+        __syncwarp();
+      }
       ok = __all_sync(0xffffffffu, bar_wait(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -619,7 +646,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
           for (int j = 0; j < 16; ++j) part[(c + j) * kRows] = __uint_as_float(v[j]);
         });
       } else if constexpr (GROUPED) {
-        scatter_columns<(BN > 64)>(P, from, begin, end, m0, n, row);
+        scatter_columns<(BN > 64)>(P, from, begin, end, (uint32_t)__cvta_generic_to_shared(mine), n);
       } else {
         store_columns<(BN > 64)>(P, from, begin, end, m0, n);
       }
@@ -644,7 +671,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     // Token t of the tile is added up by rank t % split, a warp for 32 rows; the loads from all ranks are on their way together.
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-    const Spot q = !GROUPED || tile0 < n_tiles ? Tiles<BN, GROUPED>{P, first}.at(tile0) : Spot{0, 0, 0, 0};
+    const Spot q = !GROUPED || tile0 < n_tiles ? Tiles<BN, GROUPED>{P, first, begins}.at(tile0) : Spot{0, 0, 0, 0};
     const int n0 = q.n0, m0 = q.m0, tokens = q.tokens;
     constexpr int kBatch = BN == 16 ? 1 : 4;           // groups of 32 rows that a warp adds at a time
     for (int item = warp;; item += C::kThreads / 32) {
@@ -1135,14 +1162,12 @@ bool encode_experts(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t r
 
 template <int BN>
 lcd_status launch_grouped(const MxGrouped& p, int split, int32_t* status, cudaStream_t s) {
-  using C = Cfg<BN>;
-  constexpr int kSmem = C::kSmem + 4 * (kMostGroups + 1);
-  static_assert(kSmem <= 227 * 1024 && C::kPerSm * (kSmem + 1024) <= 228 * 1024, "shared memory");
+  using C = Cfg<BN, true>;
   auto kern = mx_linear_kernel<BN, void, true>;
   static PerDeviceFlag attr_set;
   int dev;
   if (attr_set.first(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
     if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
     attr_set.done(dev);
   }
@@ -1174,7 +1199,7 @@ lcd_status launch_grouped(const MxGrouped& p, int split, int32_t* status, cudaSt
   a.G = (int)p.G;
   const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
   const unsigned grid = (unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room);
-  const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(C::kThreads), kSmem, (unsigned)split, s, w, x, ws, xs, a);
+  const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(C::kThreads), C::kSmem, (unsigned)split, s, w, x, ws, xs, a);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
@@ -1253,7 +1278,7 @@ lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* st
 }
 
 lcd_status launch_mx_grouped(const MxGrouped& p, int32_t* status_word, void* stream) {
-  if (p.G > kMostGroups) return LCD_ERR_UNSUPPORTED;
+  if (p.G > kMostExperts) return LCD_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Plan w = plan_grouped(p.rows.count, p.G, p.N, ((p.K + kMxBlock - 1) / kMxBlock * kMxBlock + kStageK - 1) / kStageK);
   switch (w.width) {

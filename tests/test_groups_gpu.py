@@ -130,7 +130,7 @@ def test_every_width_of_tiles():
 
 def test_more_experts_than_a_warp_and_than_rows():
     check_experts(50, 2, 200, 40, 96)
-    check_experts(2, 2, 1024, 16, 64)
+    check_experts(2, 2, 512, 16, 64)
 
 
 def test_many_tiles_a_cta():

@@ -66,7 +66,7 @@ def test_invalid_arguments(call, bad):
 
 
 def test_unsupported_and_short_workspaces():
-    assert group(G=1025) == 2 and experts(G=1025) == 2
+    assert group(G=1025) == 2 and experts(G=513) == 2
     assert adapters(w=weights(rank=129, lda=64, adapter_a=64 * 129, ldb=129, adapter_b=1290)) == 2
     assert adapters(w=weights(type=2)) == 2 and grad(w=weights(type=2)) == 2              # fp16 beside bf16
     assert adapters(w=weights(G=1025)) == 2 and grad(w=weights(G=1025)) == 2
