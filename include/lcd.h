@@ -523,13 +523,14 @@ typedef struct {
  *   y:        device out, [count][ldy], ldy >= N;
  *   t:        device out, fp32 [count][ldt], ldt >= rank, or NULL: t, for lcd_adapters_grad (rows without a group: zeros);
  *   workspace: device scratch of lcd_adapters_workspace_bytes(count, rank) bytes, 16-byte aligned, contents ignored; calls that may overlap on the
- *             device need separate ones.
+ *             device need separate ones;
+ *   status_word_dev: as for lcd_lut_linear.
  * Results are reproducible from run to run, but a row's last bits may differ with the rows beside it. */
 lcd_status lcd_adapters_workspace_bytes(int64_t count, int64_t rank, size_t* bytes);
 
 lcd_status lcd_adapters(const lcd_adapter_weights* weights /* host struct */, const void* x, lcd_dtype x_type, int64_t ldx,
                         const lcd_row_groups* rows /* host struct */, const void* base, int64_t ldbase, void* y, lcd_dtype y_type, int64_t ldy,
-                        float* t, int64_t ldt, void* workspace, size_t workspace_bytes, void* cuda_stream);
+                        float* t, int64_t ldt, void* workspace, size_t workspace_bytes, int32_t* status_word_dev, void* cuda_stream);
 
 /* The backward pass of lcd_adapters: with dt[m] = scale_g * dy[m] b_g (fp32),
  *     dx[m] = base[m] + dt[m] a_g (rows without a group: base[m]),
@@ -538,11 +539,11 @@ lcd_status lcd_adapters(const lcd_adapter_weights* weights /* host struct */, co
  *   t:        device, fp32 [count][ldt], as lcd_adapters gave it for this x (may be NULL without db);
  *   base, dx: device, [count][ldbase], [count][lddx], as base and y of lcd_adapters; dx may be NULL: not wanted;
  *   da, db:   device out, grad_type, dense [G][rank][K] and [G][N][rank]; either may be NULL: not wanted;
- *   workspace: as for lcd_adapters. */
+ *   workspace, status_word_dev: as for lcd_adapters. */
 lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights /* host struct */, const void* dy, int64_t lddy, const void* x, int64_t ldx,
                              lcd_dtype type, const float* t, int64_t ldt, const lcd_row_groups* rows /* host struct */, const void* base,
                              int64_t ldbase, void* dx, int64_t lddx, void* da, void* db, lcd_dtype grad_type, void* workspace,
-                             size_t workspace_bytes, void* cuda_stream);
+                             size_t workspace_bytes, int32_t* status_word_dev, void* cuda_stream);
 
 /* ----------------------------------------------------------------------------------------------
  * Offline: distillation from a teacher's top logits (Section 3 trains the clustered weights against the full-precision

@@ -146,9 +146,9 @@ def _load() -> ctypes.CDLL:
         c_int64, c_int64, c_void_p, rows] + matrix + [c_int64, c_void_p, c_size_t, c_void_p, c_void_p]
     lib.lcd_adapters_workspace_bytes.argtypes = [c_int64, c_int64, POINTER(c_size_t)]
     lib.lcd_adapters.argtypes = [adapters] + matrix + [c_int64, rows, c_void_p, c_int64] + matrix + [c_int64, c_void_p, c_int64, c_void_p, c_size_t,
-                                                                                                 c_void_p]
+                                                                                                 c_void_p, c_void_p]
     lib.lcd_adapters_grad.argtypes = [adapters, c_void_p, c_int64, c_void_p, c_int64, c_int, c_void_p, c_int64, rows, c_void_p, c_int64, c_void_p, c_int64,
-                                      c_void_p, c_void_p, c_int, c_void_p, c_size_t, c_void_p]
+                                      c_void_p, c_void_p, c_int, c_void_p, c_size_t, c_void_p, c_void_p]
     for name in EXPORTS:
         if name not in ("lcd_status_string", "lcd_last_cuda_error"):
             getattr(lib, name).restype = c_int
@@ -505,27 +505,29 @@ def mx_linear_grouped_workspace_bytes(count: int, K: int) -> int:
     return out.value
 
 
-def adapters(x, a, b, rows: RowGroups, base=None, y=None, scale=None, dtype=None, want_t=False, t=None, workspace=None, stream=None):
+def adapters(x, a, b, rows: RowGroups, base=None, y=None, scale=None, dtype=None, want_t=False, t=None, workspace=None, status_word=None,
+             stream=None):
     """y[m] = base[m] + scale[g] * (x[m] @ a[g].T) @ b[g].T, g the adapter of row m; rows without one keep base (zeros without base).
     x: CUDA fp32, fp16 or bf16 [rows, K]; a [G, rank, K] and b [G, N, rank] of x's type or fp32 (any type if x is fp32); scale: fp32 [G];
     base: [rows, N], y's type; y: may be base itself.  Without base y has dtype, or x's type.  Returns y, and with want_t (or t given) also
     t = x a^T, fp32 [rows, rank], for adapters_grad.  workspace: CUDA scratch of at least adapters_workspace_bytes(rows, rank) bytes
     (allocated here if absent)."""
-    r = (_host_calls or _calls()).adapters(x, a, b, *rows, base, y, scale, dtype, t if t is not None else True if want_t else None, workspace, stream)
+    r = (_host_calls or _calls()).adapters(x, a, b, *rows, base, y, scale, dtype, t if t is not None else True if want_t else None, workspace,
+                                           status_word, stream)
     if r.__class__ is int:
         _check(r, "lcd_adapters")
     return r[0] if r[1] is None else r
 
 
 def adapters_grad(dy, x, a, b, t, rows: RowGroups, base=None, dx=None, scale=None, da=None, db=None, grad_dtype=None, want_dx=True, want_weights=True,
-                  workspace=None, stream=None):
+                  workspace=None, status_word=None, stream=None):
     """The backward pass of adapters: (dx, da, db).  With dt[m] = scale[g] * dy[m] @ b[g]: dx[m] = base[m] + dt[m] @ a[g] (base: the shared
     layer's part of the gradient, dx may be base itself), da[g] = dt^T x and db[g] = scale[g] dy^T t over g's rows, in grad_dtype (a's type);
     adapters without rows get zeros.  dy and x have one type, which is dx's.  t: as adapters gave it.  want_dx, want_weights: False leaves
     that part out (None in its place)."""
     r = (_host_calls or _calls()).adapters_grad(dy, x, a, b, t, *rows, base, scale, (True if dx is None else dx) if want_dx else None,
                                                 (True if da is None else da) if want_weights else None,
-                                                (True if db is None else db) if want_weights else None, grad_dtype, workspace, stream)
+                                                (True if db is None else db) if want_weights else None, grad_dtype, workspace, status_word, stream)
     if r.__class__ is int:
         _check(r, "lcd_adapters_grad")
     return r

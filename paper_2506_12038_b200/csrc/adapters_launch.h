@@ -13,9 +13,14 @@ struct UpArgs {
   void* y;
   long long ldbase, ldy;
   int window, wide_base, wide_y, in_place;
+  int32_t* status;
   int early;                   // the kernel before this one wrote t and nothing else that is read here, and began when all before it was done
 };
 lcd_status launch_adapters_up(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s);
+
+// The same on tcgen05, where there are many rows and their pieces start on 16 bytes.
+bool adapters_up_tc_takes(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type);
+lcd_status launch_adapters_up_tc(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s);
 
 struct DownArgs;
 lcd_status launch_adapters_down_f32(const DownArgs& P, lcd_dtype w_type, bool backward, cudaStream_t s);

@@ -1,0 +1,340 @@
+// adapters_up.cu's products for many rows: y = base + s t b^T, dx = base + dt a.
+//
+// A tile is 128 rows of one adapter by NC columns.  Rows of base come in by bulk copies, one a row, which follow the plan at no cost, and
+// rows of y leave the same way; the product, t's parts times the adapter matrix's, waits in tensor memory meanwhile.  A CTA has consecutive
+// tiles of the list (columns, rows), so that the adapter's part stays in shared memory from tile to tile.
+//
+// Roles (14 warps): warp 0 copies base in; warp 1 owns tensor memory, one elected lane issues the MMAs; warps 2-5 bring t and, where it
+// changes, the adapter matrix, split into bf16 parts; warps 6-13 add: a thread has a row and half of the columns, reads the base's from
+// shared memory (rows 16 bytes longer than their columns: no bank conflicts), writes the sums there and sends them off itself.
+// Two tiles are in flight: while one is added up and leaves, the next one's base comes in.
+#include "adapters_launch.h"
+#include "adapters_tc.cuh"
+
+namespace lcd {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 14 * 32, kFirstLoadWarp = 2, kFirstEpiWarp = 6;
+constexpr int kMostSmem = 227 * 1024;
+
+template <typename W, typename Y, int R, bool TRANSPOSED>
+struct Shape {
+  // (a third part of the matrix is smaller than what two parts of t leave out)
+  static constexpr int kParts_t = sizeof(Y) == 4 ? 3 : 2, kParts_w = kParts<W> < kParts_t ? kParts<W> : kParts_t, kSteps = R / 16;
+  // t: [128 rows][parts][R], in blocks of 64 columns
+  static constexpr int kT = (kParts_t * R + 63) / 64 * 128 * 128;
+  static constexpr int w_bytes(int nc) { return TRANSPOSED ? nc / 64 * kParts_w * R * 128 : (kParts_w * R + 63) / 64 * nc * 128; }
+  static constexpr int pitch(int nc) { return nc * (int)sizeof(Y) + 16; }
+  static constexpr int smem(int nc) { return 1024 + kT + w_bytes(nc) + 2 * 128 * pitch(nc) + Plan::kBytes + 256; }
+  static constexpr int kNC = sizeof(Y) == 2 && smem(256) <= kMostSmem ? 256 : smem(128) <= kMostSmem ? 128 : 64;
+  static constexpr int kSmem = smem(kNC), kPitch = pitch(kNC), kW = w_bytes(kNC), kTmem = 2 * kNC;
+  // whatever shares an SM has tensor memory enough
+  static constexpr int kPerSm = 228 * 1024 / (kSmem + 1024);
+  static_assert(kSmem <= kMostSmem && kPerSm * kTmem <= 512, "shared and tensor memory");
+};
+
+template <typename W, typename Y, int R, bool TRANSPOSED>
+__global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArgs P) {
+  using S = Shape<W, Y, R, TRANSPOSED>;
+  constexpr int NC = S::kNC;
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw_addr = (uint32_t)__cvta_generic_to_shared(smem_raw);
+  const uint32_t at_t = (raw_addr + 1023u) & ~1023u, at_w = at_t + S::kT, at_y = at_w + S::kW, at_plan = at_y + 2 * 128 * S::kPitch;
+  const uint32_t bars = at_plan + Plan::kBytes;
+  uint8_t* gen = smem_raw - raw_addr;                       // gen + a shared address
+  const Plan plan = {reinterpret_cast<int*>(gen + at_plan), reinterpret_cast<int*>(gen + at_plan) + kMostGroups + 2};
+  auto y_full = [&](int b) { return bars + 8u * b; };
+  auto y_empty = [&](int b) { return bars + 16u + 8u * b; };
+  auto d_full = [&](int b) { return bars + 32u + 8u * b; };
+  auto d_empty = [&](int b) { return bars + 48u + 8u * b; };
+  const uint32_t t_full = bars + 64u, t_empty = bars + 72u, drain = bars + 80u;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + bars + 88u);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + bars + 92u);
+  if (!P.early) wait_for_previous();
+  if (threadIdx.x == 0) {
+    for (int b = 0; b < 2; ++b) {
+      bar_init(y_full(b), 1);
+      bar_init(y_empty(b), 8);
+      bar_init(d_full(b), 1);
+      bar_init(d_empty(b), 8);
+    }
+    bar_init(t_full, 128);
+    bar_init(t_empty, 1);
+    bar_init(drain, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (warp == 1) tmem_alloc((uint32_t)__cvta_generic_to_shared(tmem_holder), S::kTmem);
+  if (warp == 2) plan.make(P.a, lane, kPlaces);
+  before_sync();
+  __syncthreads();
+  after_sync();
+  const uint32_t tmem = *tmem_holder;
+  const int G = P.a.G, row_tiles = plan.first[P.in_place ? G : G + 1];
+  const long long tiles = (long long)row_tiles * ((P.a.K + NC - 1) / NC);
+  const int tile0 = (int)(tiles * blockIdx.x / gridDim.x), tile1 = (int)(tiles * (blockIdx.x + 1) / gridDim.x);
+  auto columns_of = [&](long long c0) { return (int)min((long long)NC, P.a.K - c0); };
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------------------------------ rows of base
+    bool ok = true;
+    uint32_t it = 0;
+    if (P.base) {
+      for (int tile = tile0; tile < tile1 && ok; ++tile, ++it) {
+        const Plan::Spot q = plan.at(tile % row_tiles, G, kPlaces);
+        const long long c0 = (long long)(tile / row_tiles) * NC;
+        const uint32_t b = it & 1u, bytes = (uint32_t)columns_of(c0) * sizeof(Y);
+        int row[4], valid = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          row[i] = 32 * i + lane < q.count ? row_of(P.a.order, q.place + 32 * i + lane, P.a.rows) : -1;
+          valid += __popc(__ballot_sync(0xffffffffu, row[i] >= 0));
+        }
+        ok = __all_sync(0xffffffffu, bar_wait(y_empty(b), ((it >> 1) & 1u) ^ 1u, abort_flag));
+        if (!ok) break;
+        if (lane == 0) bar_expect_tx(y_full(b), bytes * valid);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (row[i] >= 0)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                         ::"r"(at_y + (b * 128 + 32 * i + lane) * S::kPitch), "l"(static_cast<const Y*>(P.base) + row[i] * P.ldbase + c0), "r"(bytes),
+                           "r"(y_full(b)) : "memory");
+        __syncwarp();
+      }
+      // nothing this warp issued may be in flight when the CTA exits
+      for (uint32_t i = 1; i <= 2 && i <= it; ++i) bar_drain(y_full((it - i) & 1u), ((it - i) >> 1) & 1u);
+    }
+    begin_after_previous();
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------------------------------ MMAs
+    begin_after_previous();
+    if (elect()) {
+      constexpr uint32_t idesc = instr_desc(NC, true, false, TRANSPOSED);
+      const uint64_t t_desc = tile_desc(at_t, 0), w_desc = tile_desc(at_w, TRANSPOSED ? S::kParts_w * R * 128 : 0);
+      uint32_t it = 0;
+      bool ok = true;
+      for (int tile = tile0; tile < tile1 && ok; ++tile) {
+        if (plan.at(tile % row_tiles, G, kPlaces).group >= G) continue;
+        const uint32_t b = it & 1u;
+        ok = bar_wait(d_empty(b), ((it >> 1) & 1u) ^ 1u, abort_flag) && bar_wait(t_full, it & 1u, abort_flag);
+        if (!ok) break;
+        after_sync();
+        uint32_t more = 0;
+#pragma unroll
+        for (int pt = 0; pt < S::kParts_t; ++pt)
+#pragma unroll
+          for (int pw = 0; pw < S::kParts_w; ++pw) {
+            if (pt + pw >= S::kParts_t) continue;         // smaller than what the parts leave out
+#pragma unroll
+            for (int k = 0; k < S::kSteps; ++k) {
+              const int kt = pt * S::kSteps + k, kw = pw * S::kSteps + k;
+              const uint32_t w_off = TRANSPOSED ? kw * 2048 : kw / 4 * NC * 128 + kw % 4 * 32;
+              mma(tmem + b * NC, t_desc + ((kt / 4 * 128 * 128 + kt % 4 * 32) >> 4), w_desc + (w_off >> 4), idesc, more);
+              more = 1;
+            }
+          }
+        mma_commit(t_empty);
+        mma_commit(d_full(b));
+        ++it;
+      }
+      mma_commit(drain);
+      bar_drain(drain, 0);
+    }
+    __syncwarp();
+  } else if (warp < kFirstEpiWarp) {
+    // ------------------------------------------------------------------------------------------ t and the adapter matrix, in parts
+    const int thread = threadIdx.x - 32 * kFirstLoadWarp;
+    bool waited = false, ok = true;
+    uint32_t it = 0;
+    int group = -1;
+    long long columns = -1;
+    for (int tile = tile0; tile < tile1 && ok; ++tile) {
+      const Plan::Spot q = plan.at(tile % row_tiles, G, kPlaces);
+      if (q.group >= G) continue;
+      const long long c0 = (long long)(tile / row_tiles) * NC;
+      ok = __all_sync(0xffffffffu, bar_wait(t_empty, (it & 1u) ^ 1u, abort_flag));
+      if (!ok) break;
+      if (q.group != group || c0 != columns) {
+        group = q.group;
+        columns = c0;
+        const W* w = static_cast<const W*>(P.a.w) + group * P.a.sw;
+        constexpr int kRowsW = TRANSPOSED ? R : NC, kUnits = TRANSPOSED ? NC / 8 : R / 8;
+#pragma unroll 2
+        for (int u = thread; u < kRowsW * kUnits; u += 128) {
+          const int row = u / kUnits, unit = u % kUnits;
+          const long long at_row = TRANSPOSED ? row : c0 + row, at_col = TRANSPOSED ? c0 + unit * 8 : unit * 8;
+          const long long rows = TRANSPOSED ? P.a.r : P.a.K, cols = TRANSPOSED ? P.a.K : P.a.r;
+          const int have = at_row < rows ? (int)max(0ll, min(8ll, cols - at_col)) : 0;
+          Words<W, 8> in;
+          load_words(in, w + at_row * P.a.ldw + at_col, have, P.a.wide_w && (have <= 0 || have >= 8));
+          uint4 out[S::kParts_w];
+          if constexpr (S::kParts_w == 1) {
+            out[0] = make_uint4(in.w[0], in.w[1], in.w[2], in.w[3]);
+          } else {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = value_of(in, i);
+            parts_of<S::kParts_w>(v, out);
+          }
+#pragma unroll
+          for (int p = 0; p < S::kParts_w; ++p) {
+            if (TRANSPOSED) {
+              store16(at_w + unit / 8 * (S::kParts_w * R * 128) + piece_at(p * R + row, unit % 8), out[p]);
+            } else {
+              const int k = p * S::kSteps + unit / 2;
+              store16(at_w + k / 4 * (NC * 128) + piece_at(row, k % 4 * 2 + unit % 2), out[p]);
+            }
+          }
+        }
+      }
+      if (!waited) {
+        begin_after_previous();
+        waited = true;
+      }
+#pragma unroll 4
+      for (int u = thread; u < 128 * (R / 8); u += 128) {
+        const int row = u / (R / 8), unit = u % (R / 8);
+        float v[8];
+        if (row < q.count) {
+          values8(load8(P.t + (long long)(q.place + row) * R + unit * 8), v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        }
+        uint4 out[S::kParts_t];
+        parts_of<S::kParts_t>(v, out);
+#pragma unroll
+        for (int p = 0; p < S::kParts_t; ++p) {
+          const int k = p * S::kSteps + unit / 2;
+          store16(at_t + k / 4 * (128 * 128) + piece_at(row, k % 4 * 2 + unit % 2), out[p]);
+        }
+      }
+      fence_async();
+      bar_arrive(t_full);
+      ++it;
+    }
+    if (!waited) begin_after_previous();
+  } else {
+    // ------------------------------------------------------------------------------------------ sums, and rows of y
+    begin_after_previous();
+    const int quad = warp & 3, half = (warp - kFirstEpiWarp) / 4, mine = 32 * quad + lane;
+    constexpr int kHalf = NC / 2;
+    bool ok = true;
+    uint32_t it = 0, dt = 0;
+    for (int tile = tile0; tile < tile1 && ok; ++tile, ++it) {
+      const Plan::Spot q = plan.at(tile % row_tiles, G, kPlaces);
+      const long long c0 = (long long)(tile / row_tiles) * NC;
+      const int columns = columns_of(c0) - half * kHalf;
+      const uint32_t b = it & 1u, db = dt & 1u;
+      const int row = mine < q.count ? row_of(P.a.order, q.place + mine, P.a.rows) : -1;
+      const float factor = P.a.scale && q.group < G ? P.a.scale[q.group] : 1.0f;
+      // the tile before has left its buffer: the next one's base may come in
+      asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+      __syncwarp();
+      if (it > 0 && lane == 0) bar_arrive(y_empty(b ^ 1u));
+      if (P.base) ok = __all_sync(0xffffffffu, bar_wait(y_full(b), (it >> 1) & 1u, abort_flag));
+      if (ok && q.group < G) ok = __all_sync(0xffffffffu, bar_wait(d_full(db), (dt >> 1) & 1u, abort_flag));
+      if (!ok) break;
+      after_sync();
+      const uint32_t at = at_y + (b * 128 + mine) * S::kPitch + half * kHalf * (int)sizeof(Y);
+      Y* own = reinterpret_cast<Y*>(gen + at);
+      if (q.group < G) {
+        const uint32_t from = tmem + ((uint32_t)(32 * quad) << 16) + db * NC + half * kHalf;
+#pragma unroll 2
+        for (int c = 0; c < kHalf; c += 16) {
+          uint32_t d[16];
+          tmem_ld16(from + c, d);
+          Raw8<Y> raw[2];
+          if (P.base) {
+            raw[0] = load8(own + c);
+            raw[1] = load8(own + c + 8);
+          }
+          tmem_wait_ld();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float v[8];
+            if (P.base) {
+              values8(raw[h], v);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __fmaf_rn(factor, __uint_as_float(d[8 * h + i]), v[i]);
+            store8(own + c + 8 * h, v);
+          }
+        }
+        before_sync();
+        __syncwarp();
+        if (lane == 0) bar_arrive(d_empty(db));
+        ++dt;
+      } else if (!P.base) {
+        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        for (int c = 0; c < kHalf; c += 8) store8(own + c, zero);
+      }
+      fence_async();
+      if (row >= 0 && columns > 0)
+        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                     ::"l"(static_cast<Y*>(P.y) + row * P.ldy + c0 + half * kHalf), "r"(at), "r"((uint32_t)(min(columns, kHalf) * sizeof(Y))) : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      __syncwarp();
+    }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+  }
+  before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    after_sync();
+    tmem_free(tmem, S::kTmem);
+  }
+  if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
+}
+
+template <typename W, typename Y, int R, bool TRANSPOSED>
+lcd_status launch_shape(UpArgs P, cudaStream_t s) {
+  using S = Shape<W, Y, R, TRANSPOSED>;
+  auto kern = adapters_up_tc_kernel<W, Y, R, TRANSPOSED>;
+  static PerDeviceFlag attr_set;
+  int dev;
+  if (attr_set.first(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+    attr_set.done(dev);
+  }
+  P.a.wide_w = on_bytes(P.a.w, P.a.ldw, P.a.sw, sizeof(W), 16);
+  const long long most = ((long long)P.a.rows / kPlaces + (P.a.G + 1 < P.a.rows ? P.a.G + 1 : P.a.rows)) * ((P.a.K + S::kNC - 1) / S::kNC);
+  const long long room = (long long)current_sm_count() * S::kPerSm;
+  return adapter_launched(launch_overlapping(kern, dim3((unsigned)(most < room ? most : room)), dim3(kThreads), S::kSmem, 1, s, P));
+}
+
+}  // namespace
+
+bool adapters_up_tc_takes(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type) {
+  const int64_t size = y_type == LCD_DTYPE_F32 ? 4 : 2;
+  if (!on_bytes(P.y, P.ldy, P.a.K, size, 16) || (P.base && !on_bytes(P.base, P.ldbase, 0, size, 16))) return false;
+  if (P.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return false;      // the parts do not fit
+  return P.a.rows >= 512 && ((long long)P.a.rows / kPlaces + P.a.G + 1) * ((P.a.K + 63) / 64) <= 0x7fffffff;
+}
+
+lcd_status launch_adapters_up_tc(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s) {
+  return by_dtype(w_type, [&](auto w) {
+    return by_dtype(y_type, [&](auto y) {
+      using W = typename decltype(w)::type;
+      using Y = typename decltype(y)::type;
+      return by_rank(P.a.r, [&](auto rt) {
+        constexpr int R = 16 * decltype(rt)::value;
+        if constexpr (R <= 64 || (std::is_same<W, __nv_bfloat16>::value && sizeof(Y) == 2))
+          return transposed ? launch_shape<W, Y, R, true>(P, s) : launch_shape<W, Y, R, false>(P, s);
+        return (lcd_status)LCD_ERR_UNSUPPORTED;
+      });
+    });
+  });
+}
+
+}  // namespace lcd

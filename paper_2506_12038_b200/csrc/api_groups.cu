@@ -115,10 +115,10 @@ extern "C" lcd_status lcd_adapters_workspace_bytes(int64_t count, int64_t rank, 
 
 extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const void* x, lcd_dtype x_type, int64_t ldx, const lcd_row_groups* rows,
                                    const void* base, int64_t ldbase, void* y, lcd_dtype y_type, int64_t ldy, float* t, int64_t ldt, void* workspace,
-                                   size_t workspace_bytes, void* cuda_stream) {
+                                   size_t workspace_bytes, int32_t* status_word_dev, void* cuda_stream) {
   if (!planned(rows) || !adapters_there(weights) || !dense_rows(x, x_type, weights->K, ldx) || !dense_rows(y, y_type, weights->N, ldy) ||
       (base && !dense_rows(base, y_type, weights->N, ldbase)) || (base == y && ldbase != ldy && rows->count > 1) ||
-      (t && (ldt < weights->rank || !aligned(t, 4))) || !aligned(workspace, 16))
+      (t && (ldt < weights->rank || !aligned(t, 4))) || !aligned(workspace, 16) || !aligned(status_word_dev, 4))
     return LCD_ERR_INVALID_ARG;
   if (weights->rank > kMostRank || weights->G > kMostGroups || !types_go(x_type, weights->type)) return LCD_ERR_UNSUPPORTED;
   size_t need = 0;
@@ -143,18 +143,20 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   u.ldbase = ldbase;
   u.ldy = ldy;
   u.early = 1;
+  u.status = status_word_dev;
   return launch_adapters_up(u, weights->type, y_type, false, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, const void* dy, int64_t lddy, const void* x, int64_t ldx, lcd_dtype type,
                                         const float* t, int64_t ldt, const lcd_row_groups* rows, const void* base, int64_t ldbase, void* dx,
                                         int64_t lddx, void* da, void* db, lcd_dtype grad_type, void* workspace, size_t workspace_bytes,
-                                        void* cuda_stream) {
+                                        int32_t* status_word_dev, void* cuda_stream) {
   if (!planned(rows) || !adapters_there(weights) || !dense_rows(dy, type, weights->N, lddy) || (!dx && !da && !db) ||
       (da && !dense_rows(x, type, weights->K, ldx)) || (db && (!t || ldt < weights->rank || !aligned(t, 4))) ||
       (dx && (!dense_rows(dx, type, weights->K, lddx) || (base && !dense_rows(base, type, weights->K, ldbase)) ||
               (base == dx && ldbase != lddx && rows->count > 1))) ||
-      ((da || db) && (!known(grad_type) || !aligned(da, size_of(grad_type)) || !aligned(db, size_of(grad_type)))) || !aligned(workspace, 16))
+      ((da || db) && (!known(grad_type) || !aligned(da, size_of(grad_type)) || !aligned(db, size_of(grad_type)))) || !aligned(workspace, 16) ||
+      !aligned(status_word_dev, 4))
     return LCD_ERR_INVALID_ARG;
   if (weights->rank > kMostRank || weights->G > kMostGroups || !types_go(type, weights->type)) return LCD_ERR_UNSUPPORTED;
   size_t need = 0;
@@ -182,6 +184,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
     u.ldbase = ldbase;
     u.ldy = lddx;
     u.early = 1;
+    u.status = status_word_dev;
     st = launch_adapters_up(u, weights->type, type, true, s);
     if (st != LCD_OK) return st;
   }

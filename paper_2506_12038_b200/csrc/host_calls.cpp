@@ -730,16 +730,17 @@ bool rows_of_x(const at::Tensor* x, const at::Device& device, int64_t count, int
   return x && require(dense(*x, type) && x->device() == device && x->size(0) == count && x->size(1) == columns, expected);
 }
 
-// (x, a, b, order, groups, offsets, base, y, scale, dtype or None, t (None, True: a new one), workspace, stream) -> (y, t or None) or a status
+// (x, a, b, order, groups, offsets, base, y, scale, dtype or None, t (None, True: a new one), workspace, status_word, stream) -> (y, t or None) or a status
 PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (!count_args(n, 13)) return nullptr;
+  if (!count_args(n, 14)) return nullptr;
   lcd_adapter_weights w = {};
+  int32_t* word;
   at::Device device(at::kCPU);
   int64_t groups;
   lcd_row_groups rows;
   lcd_dtype x_type, y_type, base_type;
-  if (!adapters_of(a[1], a[2], a[8], &w, &device) || !plan_of(a + 3, device, &groups, &rows) ||
+  if (!adapters_of(a[1], a[2], a[8], &w, &device) || !plan_of(a + 3, device, &groups, &rows) || !status_word_of(a[12], device, &word) ||
       !require(groups == w.G, "rows: a plan of as many groups as there are adapters"))
     return nullptr;
   const at::Tensor *x = tensor_of(a[0], "x"), *base = nullptr;
@@ -758,7 +759,7 @@ PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
     type = t->scalar_type();
   }
   const c10::cuda::CUDAGuard on(device);
-  const CallStream stream(a[12]);
+  const CallStream stream(a[13]);
   if (!stream.ok()) return nullptr;
   size_t need = 0, have = 0;
   const lcd_status sized = lcd_adapters_workspace_bytes(rows.count, w.rank, &need);
@@ -774,7 +775,7 @@ PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const lcd_status st = without_gil([&] {
     return lcd_adapters(&w, x->data_ptr(), x_type, row_stride(*x), &rows, base ? base->data_ptr() : nullptr, base ? row_stride(*base) : 0, y.data_ptr(),
                         y_type, row_stride(y), has_t ? static_cast<float*>(t.data_ptr()) : nullptr, has_t ? row_stride(t) : 0,
-                        have ? space.data_ptr() : nullptr, have, stream.raw());
+                        have ? space.data_ptr() : nullptr, have, word, stream.raw());
   });
   if (st != LCD_OK) return PyLong_FromLong((long)st);
   return pack({returned(stream, a[7], y), has_t ? returned(stream, want_t, t) : Py_NewRef(Py_None)});
@@ -782,16 +783,17 @@ PyObject* adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // (dy, x or None, a, b, t or None, order, groups, offsets, base, scale, dx, da, db (each None: not wanted, True: a new one), grad dtype or None,
-//  workspace, stream) -> (dx, da, db), None where not wanted, or a status
+//  workspace, status_word, stream) -> (dx, da, db), None where not wanted, or a status
 PyObject* adapters_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  if (!count_args(n, 16)) return nullptr;
+  if (!count_args(n, 17)) return nullptr;
   lcd_adapter_weights w = {};
+  int32_t* word;
   at::Device device(at::kCPU);
   int64_t groups;
   lcd_row_groups rows;
   lcd_dtype type, other, grad_type = LCD_DTYPE_F32;
-  if (!adapters_of(a[2], a[3], a[9], &w, &device) || !plan_of(a + 5, device, &groups, &rows) ||
+  if (!adapters_of(a[2], a[3], a[9], &w, &device) || !plan_of(a + 5, device, &groups, &rows) || !status_word_of(a[15], device, &word) ||
       !require(groups == w.G, "rows: a plan of as many groups as there are adapters"))
     return nullptr;
   const at::Tensor *dy = tensor_of(a[0], "dy"), *x = nullptr, *t = nullptr, *base = nullptr;
@@ -832,7 +834,7 @@ PyObject* adapters_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
   if (!require(type_of(kind, &grad_type), "da, db: fp32, fp16 or bf16") || !require(x || !has[1], "da: needs x") || !require(t || !has[2], "db: needs t")) return nullptr;
   const c10::cuda::CUDAGuard on(device);
-  const CallStream stream(a[15]);
+  const CallStream stream(a[16]);
   if (!stream.ok()) return nullptr;
   size_t need = 0, have = 0;
   const lcd_status sized = lcd_adapters_workspace_bytes(rows.count, w.rank, &need);
@@ -850,7 +852,7 @@ PyObject* adapters_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
                              t ? static_cast<const float*>(t->data_ptr()) : nullptr, t ? row_stride(*t) : 0, &rows, base ? base->data_ptr() : nullptr,
                              base ? row_stride(*base) : 0, has[0] ? dx.data_ptr() : nullptr, has[0] ? row_stride(dx) : 0,
                              has[1] ? da.data_ptr() : nullptr, has[2] ? db.data_ptr() : nullptr, grad_type, have ? space.data_ptr() : nullptr, have,
-                             stream.raw());
+                             word, stream.raw());
   });
   if (st != LCD_OK) return PyLong_FromLong((long)st);
   return pack({has[0] ? returned(stream, want[0], dx) : Py_NewRef(Py_None), has[1] ? returned(stream, want[1], da) : Py_NewRef(Py_None),

@@ -264,6 +264,32 @@ def test_adapters_ragged(sizes):
         check_adapters(make_adapters(3, len(group), len(sizes), 20, 130, 150, "fp16", "fp16", "fp32", group=group, scale=False), ("fp16",))
 
 
+MANY = [(512, 1, 16, 96, 64), (700, 3, 8, 96, 264), (1500, 9, 33, 64, 128), (513, 2, 64, 64, 520), (640, 4, 128, 64, 200), (600, 700, 12, 32, 48)]
+
+
+@pytest.mark.parametrize("x,w", PAIRS)
+@pytest.mark.parametrize("M,G,r,K,N", MANY)
+def test_adapters_of_many_rows(x, w, M, G, r, K, N):
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    c = make_adapters(M + r, M, G, r, K, N, x, w)
+    check_adapters(c, (x, w), status_word=word)
+    whole = make_adapters(M + r, M, G, r, K, N, x, w, "fp32", whole=True, pitch=8)
+    check_adapters(whole, exact=True, status_word=word)
+    assert word.item() == 0
+
+
+def test_adapters_of_many_rows_without_base_and_in_place():
+    for group in (None, np.full(600, -1), np.arange(600) % 3 - 1):
+        c = make_adapters(13, 600, 2, 16, 64, 136, "bf16", "bf16", base=False, group=group)
+        check_adapters(c, ("bf16",))
+        c["base"] = torch.randn(600, 136, device="cuda").bfloat16()
+        y, _ = check_adapters(c, ("bf16",))
+        room = torch.full((601, 144), 7.0, dtype=torch.bfloat16, device="cuda")
+        room[:600, :136] = c["base"]
+        got = lcd.adapters(c["x"], c["a"], c["b"], c["rows"], room[:600, :136], y=room[:600, :136], scale=c["scale"])
+        assert torch.equal(got, y) and (room[600] == 7).all() and (room[:, 136:] == 7).all()
+
+
 def test_adapters_in_place_and_beyond_their_rows():
     c = make_adapters(5, 20, 3, 16, 64, 72, "bf16", "bf16")
     y, _ = check_adapters(c, ("bf16",))
@@ -277,9 +303,10 @@ def test_adapters_in_place_and_beyond_their_rows():
     assert torch.equal(got[none], c["base"][none]) and (t[none] == 0).all()
 
 
+@pytest.mark.parametrize("times", [4, 120])
 @pytest.mark.parametrize("x,w", [("bf16", "bf16"), ("fp16", "fp16"), ("fp32", "fp32")])
-def test_adapters_keep_what_is_not_finite_in_its_row_and_adapter(x, w):
-    c = make_adapters(9, 24, 4, 16, 96, 80, x, w, group=[0, 1, 2, 3, -1, 0] * 4)
+def test_adapters_keep_what_is_not_finite_in_its_row_and_adapter(x, w, times):
+    c = make_adapters(9, 6 * times, 4, 16, 96, 80, x, w, group=[0, 1, 2, 3, -1, 0] * times)
     for key, at in (("x", (0, 5)), ("x", (4, 6)), ("a", (1, 3, 7)), ("b", (2, 9, 1))):
         c[key][at] = float("nan")
     c["x"][9, 1] = float("inf")
@@ -335,6 +362,18 @@ def check_grad(c, x, types=(), exact=False, grad_dtype=None, base=True, seed=0, 
                                              (64, 64, 16, 64, 64, 0), (100, 3, 64, 333, 129, 0), (70, 2, 100, 96, 90, 1), (600, 2, 8, 72, 520, 0)])
 def test_grad(x, w, M, G, r, K, N, pitch):
     check_grad(make_adapters(M + r, M, G, r, K, N, x, w, pitch=pitch), x, (x, w))
+
+
+@pytest.mark.parametrize("x,w", PAIRS)
+@pytest.mark.parametrize("M,G,r,K,N", MANY)
+def test_grad_of_many_rows(x, w, M, G, r, K, N):
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    c = make_adapters(M + r, M, G, r, N, K, x, w)
+    check_grad(c, x, (x, w), status_word=word)
+    check_grad(c, x, (x, w), status_word=word, grad_dtype=torch.float32, base=False)
+    whole = make_adapters(M + r, M, G, r, N, K, x, w, whole=True, pitch=8)
+    check_grad(whole, x, whole=True, exact=x == "fp32", grad_dtype=torch.float32, types=(x, w), status_word=word)
+    assert word.item() == 0
 
 
 @pytest.mark.parametrize("x,w", PAIRS)

@@ -32,15 +32,15 @@ def experts(wc=A, ldwc=32, dwc=32 * 5, ws=A, ldws=16, dws=16 * 5, G=3, N=5, K=64
                                      space, bytes, word, None)
 
 
-def adapters(w=None, x=A, x_type=1, ldx=64, rows=None, base=A, ldbase=10, y=ODD, y_type=0, ldy=10, t=None, ldt=0, space=A, bytes=1 << 20):
+def adapters(w=None, x=A, x_type=1, ldx=64, rows=None, base=A, ldbase=10, y=ODD, y_type=0, ldy=10, t=None, ldt=0, space=A, bytes=1 << 20, word=None):
     return lib.lcd_adapters(weights() if w is None else w, x, x_type, ldx, plan() if rows is None else rows, base, ldbase, y, y_type, ldy, t, ldt,
-                            space, bytes, None)
+                            space, bytes, word, None)
 
 
 def grad(w=None, dy=A, lddy=10, x=A, ldx=64, type=1, t=A, ldt=4, rows=None, base=A, ldbase=64, dx=ODD, lddx=64, da=A, db=A, grad_type=0, space=A,
-         bytes=1 << 20):
+         bytes=1 << 20, word=None):
     return lib.lcd_adapters_grad(weights() if w is None else w, dy, lddy, x, ldx, type, t, ldt, plan() if rows is None else rows, base, ldbase, dx,
-                                 lddx, da, db, grad_type, space, bytes, None)
+                                 lddx, da, db, grad_type, space, bytes, word, None)
 
 
 PLANS = [dict(rows=plan(order=None)), dict(rows=plan(groups=None)), dict(rows=plan(offsets=None)), dict(rows=plan(count=0)), dict(rows=plan(count=-1)),
@@ -56,10 +56,10 @@ WEIGHTS = [dict(w=weights(**kw)) for kw in (dict(a=None), dict(b=None), dict(typ
                        dict(dwc=32 * 5 - 16), dict(dwc=32 * 5 + 8), dict(dws=16 * 4), dict(G=0), dict(N=0), dict(K=0), dict(K=65), dict(T=0), dict(T=4),
                        dict(T=12), dict(ldx=63), dict(ldy=4), dict(x_type=3), dict(y_type=-1), dict(inv=TWO), dict(space=ODD), dict(word=TWO), dict(y=TWO)]),
     (adapters, PLANS + WEIGHTS + [dict(x=None), dict(x_type=5), dict(ldx=63), dict(x=ctypes.c_void_p(1)), dict(y=None), dict(ldy=9), dict(y_type=3),
-                                  dict(base=TWO), dict(ldbase=9), dict(y=A, ldy=12), dict(t=A, ldt=3), dict(t=TWO, ldt=4), dict(space=ODD)]),
+                                  dict(base=TWO), dict(ldbase=9), dict(y=A, ldy=12), dict(t=A, ldt=3), dict(t=TWO, ldt=4), dict(space=ODD), dict(word=TWO)]),
     (grad, PLANS + WEIGHTS + [dict(dy=None), dict(lddy=9), dict(x=None), dict(ldx=63), dict(type=3), dict(t=None), dict(ldt=3), dict(t=TWO),
                               dict(base=ctypes.c_void_p(1)), dict(ldbase=63), dict(lddx=63), dict(dx=A, lddx=70), dict(dx=None, da=None, db=None),
-                              dict(grad_type=3), dict(da=TWO), dict(space=ODD)])])
+                              dict(grad_type=3), dict(da=TWO), dict(space=ODD), dict(word=TWO)])])
 def test_invalid_arguments(call, bad):
     for kw in bad:
         assert call(**kw) == 1, kw
