@@ -20,6 +20,7 @@ struct DownArgs {
   int window;
   float *t, *t_rows;           // by place, 16 * RT values a row; by row (may be null)
   long long ldt_rows;
+  int32_t* status;
 };
 
 constexpr int kDownWarps = 8;

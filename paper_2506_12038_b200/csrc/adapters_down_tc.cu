@@ -1,0 +1,242 @@
+// adapters_down.cuh's products for many rows: x a^T and dy b, where x and the adapters have one 16-bit type.
+//
+// A tile is 128 rows of one adapter by the whole rank; a cluster's CTAs share its columns and add their sums up in distributed shared
+// memory, in the order of the ranks.  Rows of x follow the plan through 16-byte cp.async copies, 64 columns a stage; what bounds it is that
+// one pass over x.
+// Roles (5 warps): warps 0-3 copy, then read the sums from tensor memory; warp 4 owns tensor memory, one elected lane issues the MMAs.
+// TRANSPOSED: the adapter matrix is b [K][r], the MN-major operand as it lies.
+#include "adapters_down.cuh"
+#include "adapters_launch.h"
+#include "adapters_tc.cuh"
+
+namespace lcd {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 5 * 32, kCopyThreads = 128;
+
+template <int R, bool TRANSPOSED>
+struct Shape {
+  static constexpr int kX = 128 * 128, kW = TRANSPOSED ? (R + 63) / 64 * 64 * 128 : R * 128, kStage = kX + kW;
+  static constexpr int kStages = R == 128 ? 5 : 4;                                // (two CTAs an SM but at rank 128)
+  static constexpr int kPitch = R + 4;                                            // of the sums, fp32
+  static constexpr int kSmem = 1024 + kStages * kStage + Plan::kBytes + 128;
+  static constexpr int kTmem = R < 32 ? 32 : R;
+  static_assert(128 * kPitch * 4 <= kStages * kStage && kSmem <= 227 * 1024, "sums lie in the stages");
+};
+
+template <typename X, int R, bool TRANSPOSED>
+__global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const DownArgs P) {
+  using S = Shape<R, TRANSPOSED>;
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw_addr = (uint32_t)__cvta_generic_to_shared(smem_raw);
+  const uint32_t base = (raw_addr + 1023u) & ~1023u, at_plan = base + S::kStages * S::kStage, bars = at_plan + Plan::kBytes;
+  uint8_t* gen = smem_raw - raw_addr;
+  const Plan plan = {reinterpret_cast<int*>(gen + at_plan), reinterpret_cast<int*>(gen + at_plan) + kMostGroups + 2};
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (S::kStages + s); };
+  const uint32_t d_full = bars + 8u * 2 * S::kStages;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + d_full + 8u);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + d_full + 12u);
+  uint32_t rank, split;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+  begin_after_previous();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      bar_init(full(s), kCopyThreads);
+      bar_init(empty(s), 1);
+    }
+    bar_init(d_full, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (warp == 4) tmem_alloc((uint32_t)__cvta_generic_to_shared(tmem_holder), S::kTmem);
+  if (warp == 0) plan.make(P.a, lane, kPlaces);
+  before_sync();
+  __syncthreads();
+  after_sync();
+  const uint32_t tmem = *tmem_holder;
+  const int tile = blockIdx.x / split, G = P.a.G;
+  const Plan::Spot q = tile < plan.first[G + 1] ? plan.at(tile, G, kPlaces) : Plan::Spot{G, 0, 0};
+  const bool real = q.group < G;                         // the same in all CTAs of the cluster
+  const int stages = (int)((P.a.K + 63) / 64);
+  const int k0 = (int)((long long)stages * rank / split), k1 = real ? (int)((long long)stages * (rank + 1) / split) : k0;
+  bool ok = true;
+
+  if (warp == 4) {
+    if (elect()) {
+      constexpr uint32_t idesc = instr_desc(R, std::is_same<X, __nv_bfloat16>::value, false, TRANSPOSED);
+      for (int k = k0; k < k1 && ok; ++k) {
+        const int it = k - k0, s = it % S::kStages;
+        ok = bar_wait(full(s), (it / S::kStages) & 1u, abort_flag);
+        if (!ok) break;
+        after_sync();
+        const uint64_t xd = tile_desc(base + s * S::kStage, 0), wd = tile_desc(base + s * S::kStage + S::kX, TRANSPOSED ? 64 * 128 : 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma(tmem, xd + 2 * i, wd + (TRANSPOSED ? 128 * i : 2 * i), idesc, (uint32_t)(it != 0 || i != 0));
+        mma_commit(empty(s));
+      }
+      mma_commit(d_full);
+      bar_drain(d_full, 0);            // every MMA has finished before this CTA leaves, whatever the others wait for
+    }
+    __syncwarp();
+  } else {
+    // A row's eight pieces belong to eight neighbouring threads, 16 rows to a pass.
+    const int thread = threadIdx.x, piece = thread & 7;
+    const X* x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int at = thread / 8 + 16 * i, row = at < q.count ? row_of(P.a.order, q.place + at, P.a.rows) : -1;
+      x[i] = row >= 0 ? static_cast<const X*>(P.x) + row * P.ldx : nullptr;
+    }
+    const X* w = static_cast<const X*>(P.a.w) + (real ? q.group : 0) * P.a.sw;
+    auto arrive = [&](int it) {
+      fence_async();
+      bar_arrive(full(it % S::kStages));
+    };
+    constexpr int kBehind = S::kStages - 1;               // stages on their way before the first of them is handed over
+    for (int k = k0; k < k1 && ok; ++k) {
+      const int it = k - k0, s = it % S::kStages;
+      ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
+      if (!ok) break;
+      const long long c = (long long)k * 64 + piece * 8;
+      const int have = (int)max(0ll, min(8ll, P.a.K - c)) * 2;
+      const uint32_t to_x = base + s * S::kStage, to_w = to_x + S::kX;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int there = x[i] ? have : 0;
+        copy16(to_x + piece_at(thread / 8 + 16 * i, piece), there ? static_cast<const void*>(x[i] + c) : P.x, there);
+      }
+      if (TRANSPOSED) {
+        constexpr int kPieces = R / 8 < 8 ? R / 8 : 8;     // of a row of 64 ranks
+#pragma unroll
+        for (int u = thread; u < (R + 63) / 64 * 64 * kPieces; u += kCopyThreads) {
+          const int p = u % kPieces, row = u / kPieces % 64, block = u / kPieces / 64;
+          const long long n = (long long)k * 64 + row;
+          const int r = block * 64 + p * 8, there = n < P.a.K ? max(0, min(8, P.a.r - r)) * 2 : 0;
+          copy16(to_w + block * 64 * 128 + piece_at(row, p), there ? static_cast<const void*>(w + n * P.a.ldw + r) : P.a.w, there);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < R / 16; ++i) {
+          const int r = thread / 8 + 16 * i, there = r < P.a.r ? have : 0;
+          copy16(to_w + piece_at(r, piece), there ? static_cast<const void*>(w + r * P.a.ldw + c) : P.a.w, there);
+        }
+      }
+      copies_commit();
+      if (it >= kBehind) {
+        copies_wait<kBehind>();
+        arrive(it - kBehind);
+      }
+    }
+    copies_wait<0>();
+    if (ok)
+      for (int it = max(0, k1 - k0 - kBehind); it < k1 - k0; ++it) arrive(it);
+    ok = __all_sync(0xffffffffu, ok && bar_wait(d_full, 0, abort_flag));
+    after_sync();
+    // the stages are done with: they hold the sums
+    float* sum = reinterpret_cast<float*>(gen + base) + thread * S::kPitch;
+#pragma unroll
+    for (int c = 0; c < R; c += 16) {
+      uint32_t v[16];
+      if (k1 > k0) {
+        tmem_ld16(tmem + ((uint32_t)(32 * warp) << 16) + c, v);
+        tmem_wait_ld();
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(sum + c + i) = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+    }
+    before_sync();
+  }
+  if (split > 1) {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+  const float factor = P.a.scale && real ? P.a.scale[q.group] : 1.0f;
+  for (int e = rank * kThreads + threadIdx.x; e < q.count * R; e += split * kThreads) {
+    const int at = e / R, r = e % R;
+    float sum = 0.0f;
+    if (real) {
+      const uint32_t from = base + (at * S::kPitch + r) * 4;
+      float v[kDownSplit];
+#pragma unroll
+      for (int i = 0; i < kDownSplit; ++i) {
+        v[i] = 0.0f;
+        if (i < (int)split) {
+          uint32_t there;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(from), "r"(i));
+          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(there) : "memory");
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kDownSplit; ++i) sum += v[i];
+      sum = r < P.a.r ? sum * factor : 0.0f;
+    }
+    P.t[(long long)q.place * R + e] = sum;
+    if (P.t_rows && r < P.a.r) {
+      const int row = row_of(P.a.order, q.place + at, P.a.rows);
+      if (row >= 0) P.t_rows[row * P.ldt_rows + r] = sum;
+    }
+  }
+  if (split > 1) {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
+  before_sync();
+  __syncthreads();
+  if (warp == 4) {
+    after_sync();
+    tmem_free(tmem, S::kTmem);
+  }
+  if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
+}
+
+template <typename X, int R, bool TRANSPOSED>
+lcd_status launch_shape(const DownArgs& P, cudaStream_t s) {
+  using S = Shape<R, TRANSPOSED>;
+  auto kern = adapters_down_tc_kernel<X, R, TRANSPOSED>;
+  static PerDeviceFlag attr_set;
+  int dev;
+  if (attr_set.first(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+    attr_set.done(dev);
+  }
+  // at most that many tiles; those that hold rows are about half of the groups fewer
+  const long long tiles = P.a.rows / kPlaces + (P.a.G + 1 < P.a.rows ? P.a.G + 1 : P.a.rows);
+  const int sms = current_sm_count();
+  unsigned split = 1;
+  while (split < kDownSplit && (P.a.rows / kPlaces + 1) * 2ll * split <= 2 * sms && (P.a.K + 63) / 64 >= 8ll * split) split *= 2;
+  return adapter_launched(launch_overlapping(kern, dim3((unsigned)(tiles * split)), dim3(kThreads), S::kSmem, split, s, P));
+}
+
+template <typename X>
+lcd_status launch_type(const DownArgs& P, bool backward, cudaStream_t s) {
+  return by_rank(P.a.r, [&](auto rt) {
+    constexpr int R = 16 * decltype(rt)::value;
+    return backward ? launch_shape<X, R, true>(P, s) : launch_shape<X, R, false>(P, s);
+  });
+}
+
+}  // namespace
+
+bool adapters_down_tc_takes(const DownArgs& P, lcd_dtype x_type, lcd_dtype w_type) {
+  return x_type == w_type && x_type != LCD_DTYPE_F32 && P.a.rows >= 512 && on_bytes(P.x, P.ldx, 0, 2, 16) && on_bytes(P.a.w, P.a.ldw, P.a.sw, 2, 16);
+}
+
+lcd_status launch_adapters_down_tc(const DownArgs& P, lcd_dtype type, bool backward, cudaStream_t s) {
+  return type == LCD_DTYPE_F16 ? launch_type<__half>(P, backward, s) : launch_type<__nv_bfloat16>(P, backward, s);
+}
+
+}  // namespace lcd

@@ -27,6 +27,9 @@ lcd_status launch_adapters_down_f32(const DownArgs& P, lcd_dtype w_type, bool ba
 lcd_status launch_adapters_down_f16(const DownArgs& P, lcd_dtype w_type, bool backward, cudaStream_t s);
 lcd_status launch_adapters_down_bf16(const DownArgs& P, lcd_dtype w_type, bool backward, cudaStream_t s);
 
+bool adapters_down_tc_takes(const DownArgs& P, lcd_dtype x_type, lcd_dtype w_type);
+lcd_status launch_adapters_down_tc(const DownArgs& P, lcd_dtype type, bool backward, cudaStream_t s);
+
 // The gradient of one adapter matrix: [r] x columns of z's, sums over an adapter's rows of u (r values a row, fp32) times z.
 struct OuterSide {
   const float* u;              // [rows][ldu], by place or by row
@@ -45,8 +48,11 @@ struct OuterArgs {
   int rows, G, r, out_type, sides;
   OuterSide side[2];
   long long slabs[2];
+  int32_t* status;
 };
 lcd_status launch_adapters_outer(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s);
+bool adapters_outer_tc_takes(const OuterArgs& P, lcd_dtype z_type);
+lcd_status launch_adapters_outer_tc(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s);
 
 }  // namespace lcd
 #endif

@@ -1,0 +1,321 @@
+// adapters_outer.cu's gradients for many rows: da = sum over an adapter's rows of dt^T x, db = s sum of dy^T t.
+//
+// A tile is 128 columns of z (x or dy) by the whole rank of one adapter; the sum runs over its rows, 64 a stage, so both operands are
+// MN-major as they lie.  Rows of z follow the plan through 16-byte copies (bf16 as it is; fp16 and fp32 through registers, in two or three bf16
+// parts), those of t or dt are split into parts on their way.  A cluster's CTAs share an adapter's rows where there are few tiles and
+// add their sums up in distributed shared memory, in the order of the ranks.  Reading z bounds it.
+// Roles (9 warps): warps 0-3 bring z, then read the sums from tensor memory; warps 4-7 bring t or dt; warp 8 owns tensor memory, one
+// elected lane issues the MMAs.
+#include "adapters_launch.h"
+#include "adapters_tc.cuh"
+
+namespace lcd {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kThreads = 9 * 32, kStageRows = 64, kOuterSplit = 8;
+
+template <typename Z, typename O, int R>
+struct Shape {
+  static constexpr int kParts_u = kPartsFor<Z, O>, kParts_z = kParts<Z> < kParts_u ? kParts<Z> : kParts_u;
+  static constexpr int kZPart = 2 * kStageRows * 128, kUPart = (R + 63) / 64 * kStageRows * 128;
+  static constexpr int kStage = kParts_z * kZPart + kParts_u * kUPart;
+  static constexpr int kStages = 5 * kStage <= 110 * 1024 ? 5 : 4 * kStage <= 220 * 1024 ? 4 : 3;
+  static constexpr int kPitch = R + 1;                                            // of the sums, fp32
+  static constexpr int kSmem = 1024 + kStages * kStage + 128;
+  static constexpr int kTmem = R < 32 ? 32 : R;
+  static_assert(128 * kPitch * 4 <= kStages * kStage && kSmem <= 227 * 1024, "sums lie in the stages");
+};
+
+template <typename Z, typename O, int R>
+__global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __grid_constant__ OuterArgs P) {
+  using S = Shape<Z, O, R>;
+  constexpr bool kCopied = S::kParts_z == 1;
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t raw_addr = (uint32_t)__cvta_generic_to_shared(smem_raw);
+  const uint32_t base = (raw_addr + 1023u) & ~1023u, bars = base + S::kStages * S::kStage;
+  uint8_t* gen = smem_raw - raw_addr;
+  auto full = [&](int s) { return bars + 8u * s; };
+  auto empty = [&](int s) { return bars + 8u * (S::kStages + s); };
+  const uint32_t d_full = bars + 8u * 2 * S::kStages;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(gen + d_full + 8u);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + d_full + 12u);
+  uint32_t rank, split;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+  begin_after_previous();
+  const int group = blockIdx.y;
+  long long slab = blockIdx.x / split;
+  const int side = slab >= P.slabs[0];
+  if (side) slab -= P.slabs[0];
+  const OuterSide& E = P.side[side];
+  const long long col0 = slab * 128;
+  const int from = max(0, min(P.rows, P.offsets[group])), to = max(from, min(P.rows, P.offsets[group + 1]));
+  O* out = static_cast<O*>(E.out);
+  if (to == from) {                                  // in all CTAs of the cluster: zeros
+    for (int e = rank * kThreads + threadIdx.x; e < 128 * P.r; e += split * kThreads) {
+      const int r = E.by_column ? e % P.r : e / 128, c = E.by_column ? e / P.r : e % 128;
+      if (col0 + c < E.columns)
+        out[E.by_column ? ((long long)group * E.columns + col0 + c) * P.r + r : ((long long)group * P.r + r) * E.columns + col0 + c] = from_f32<O>(0.0f);
+    }
+    return;
+  }
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < S::kStages; ++s) {
+      bar_init(full(s), 256);
+      bar_init(empty(s), 1);
+    }
+    bar_init(d_full, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async();
+  }
+  if (warp == 8) tmem_alloc((uint32_t)__cvta_generic_to_shared(tmem_holder), S::kTmem);
+  before_sync();
+  __syncthreads();
+  after_sync();
+  const uint32_t tmem = *tmem_holder;
+  const int stages = (to - from + kStageRows - 1) / kStageRows;
+  const int k0 = (int)((long long)stages * rank / split), n = (int)((long long)stages * (rank + 1) / split) - k0;
+  bool ok = true;
+
+  if (warp == 8) {
+    if (elect()) {
+      constexpr uint32_t idesc = instr_desc(R, true, true, true);
+      uint32_t more = 0;
+      for (int it = 0; it < n && ok; ++it) {
+        const int s = it % S::kStages;
+        ok = bar_wait(full(s), (it / S::kStages) & 1u, abort_flag);
+        if (!ok) break;
+        after_sync();
+        const uint64_t zd = tile_desc(base + s * S::kStage, kStageRows * 128), ud = tile_desc(base + s * S::kStage + S::kParts_z * S::kZPart, kStageRows * 128);
+#pragma unroll
+        for (int pz = 0; pz < S::kParts_z; ++pz)
+#pragma unroll
+          for (int pu = 0; pu < S::kParts_u; ++pu) {
+            if (pz + pu >= S::kParts_u) continue;        // smaller than what the parts leave out
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              mma(tmem, zd + ((pz * S::kZPart + 2048 * i) >> 4), ud + ((pu * S::kUPart + 2048 * i) >> 4), idesc, more);
+              more = 1;
+            }
+          }
+        mma_commit(empty(s));
+      }
+      mma_commit(d_full);
+      bar_drain(d_full, 0);            // every MMA has finished before this CTA leaves, whatever the others wait for
+    }
+    __syncwarp();
+  } else if (warp < 4) {
+    // A row's sixteen pieces belong to sixteen neighbouring threads, eight rows to a pass.
+    const int thread = threadIdx.x, piece = thread & 15;
+    const long long c = col0 + piece * 8;
+    const int have = (int)max(0ll, min(8ll, E.columns - c));
+    const uint32_t at_piece = (uint32_t)(piece / 8 * kStageRows * 128);
+    const Z* z = static_cast<const Z*>(E.z) + c;
+    auto row_at = [&](int it, int i) {
+      const int place = from + (k0 + it) * kStageRows + thread / 16 + 8 * i;
+      return place < to ? row_of(P.order, place, P.rows) : -1;
+    };
+    int row[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) row[i] = row_at(0, i);
+    if constexpr (kCopied) {
+      constexpr int kBehind = S::kStages - 1;
+      for (int it = 0; it < n && ok; ++it) {
+        const int s = it % S::kStages;
+        ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int there = row[i] >= 0 ? have * 2 : 0;
+          copy16(base + s * S::kStage + at_piece + piece_at(thread / 16 + 8 * i, piece % 8), there ? static_cast<const void*>(z + row[i] * E.ldz) : E.z, there);
+        }
+        copies_commit();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row[i] = it + 1 < n ? row_at(it + 1, i) : -1;
+        if (it >= kBehind) {
+          copies_wait<kBehind>();
+          fence_async();
+          bar_arrive(full((it - kBehind) % S::kStages));
+        }
+      }
+      copies_wait<0>();
+      if (ok) {
+        fence_async();
+        for (int it = max(0, n - kBehind); it < n; ++it) bar_arrive(full(it % S::kStages));
+      }
+    } else {
+      Words<Z, 8> in[8];
+      auto load = [&] {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) load_words(in[i], z + (row[i] >= 0 ? row[i] * E.ldz : 0), row[i] >= 0 ? have : 0, E.wide_z && (have <= 0 || have >= 8));
+      };
+      load();
+      for (int it = 0; it < n && ok; ++it) {
+        const int s = it % S::kStages;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) row[i] = it + 1 < n ? row_at(it + 1, i) : -1;
+        ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = value_of(in[i], e);
+          uint4 parts[S::kParts_z];
+          parts_of<S::kParts_z>(v, parts);
+#pragma unroll
+          for (int p = 0; p < S::kParts_z; ++p) store16(base + s * S::kStage + p * S::kZPart + at_piece + piece_at(thread / 16 + 8 * i, piece % 8), parts[p]);
+        }
+        fence_async();
+        bar_arrive(full(s));
+        if (it + 1 < n) load();
+      }
+    }
+    ok = __all_sync(0xffffffffu, ok && bar_wait(d_full, 0, abort_flag));
+    after_sync();
+    float* sum = reinterpret_cast<float*>(gen + base) + thread * S::kPitch;      // the stages are done with
+#pragma unroll
+    for (int c2 = 0; c2 < R; c2 += 16) {
+      uint32_t v[16];
+      if (n > 0) {
+        tmem_ld16(tmem + ((uint32_t)(32 * warp) << 16) + c2, v);
+        tmem_wait_ld();
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sum[c2 + i] = __uint_as_float(v[i]);
+    }
+    before_sync();
+  } else {
+    // t or dt: a thread has eight ranks of R / 16 rows
+    const int thread = threadIdx.x - 128;
+    constexpr int kUnits = R / 8, kEach = kStageRows * kUnits / 128;
+    Words<float, 8> in[kEach];
+    auto load = [&](int it) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int u = thread + 128 * i, unit = u % kUnits, place = from + (k0 + it) * kStageRows + u / kUnits;
+        const int row = place < to ? row_of(P.order, place, P.rows) : -1, have = row >= 0 ? max(0, min(8, P.r - unit * 8)) : 0;
+        load_words(in[i], E.u + (E.u_by_place ? (long long)(row >= 0 ? place : 0) : (long long)(row >= 0 ? row : 0)) * E.ldu + unit * 8, have,
+                   E.wide_u && (have <= 0 || have >= 8));
+      }
+    };
+    if (n > 0) load(0);
+    for (int it = 0; it < n && ok; ++it) {
+      const int s = it % S::kStages;
+      ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
+      if (!ok) break;
+      const uint32_t to_u = base + s * S::kStage + S::kParts_z * S::kZPart;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int u = thread + 128 * i, unit = u % kUnits, at = u / kUnits;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = value_of(in[i], e);
+        uint4 parts[S::kParts_u];
+        parts_of<S::kParts_u>(v, parts);
+#pragma unroll
+        for (int p = 0; p < S::kParts_u; ++p) store16(to_u + p * S::kUPart + unit / 8 * kStageRows * 128 + piece_at(at, unit % 8), parts[p]);
+      }
+      fence_async();
+      bar_arrive(full(s));
+      if (it + 1 < n) load(it + 1);
+    }
+  }
+  if (split > 1) {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+  const float factor = E.scale ? E.scale[group] : 1.0f;
+  for (int e = rank * kThreads + threadIdx.x; e < 128 * P.r; e += split * kThreads) {
+    // consecutive threads: consecutive places of the output
+    const int r = E.by_column ? e % P.r : e / 128, c = E.by_column ? e / P.r : e % 128;
+    if (col0 + c >= E.columns) continue;
+    const uint32_t at = base + (c * S::kPitch + r) * 4;
+    float v[kOuterSplit], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kOuterSplit; ++i) {
+      v[i] = 0.0f;
+      if (i < (int)split) {
+        uint32_t there;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(i));
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(there) : "memory");
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kOuterSplit; ++i) sum += v[i];
+    out[E.by_column ? ((long long)group * E.columns + col0 + c) * P.r + r : ((long long)group * P.r + r) * E.columns + col0 + c] = from_f32<O>(sum * factor);
+  }
+  if (split > 1) {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  }
+  before_sync();
+  __syncthreads();
+  if (warp == 8) {
+    after_sync();
+    tmem_free(tmem, S::kTmem);
+  }
+  if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
+}
+
+template <typename Z, typename O, int R>
+lcd_status launch_shape(OuterArgs P, cudaStream_t s) {
+  using S = Shape<Z, O, R>;
+  auto kern = adapters_outer_tc_kernel<Z, O, R>;
+  static PerDeviceFlag attr_set;
+  int dev;
+  if (attr_set.first(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+    attr_set.done(dev);
+  }
+  long long slabs = 0;
+  for (int i = 0; i < 2; ++i) {
+    P.slabs[i] = i < P.sides ? (P.side[i].columns + 127) / 128 : 0;
+    slabs += P.slabs[i];
+    P.side[i].wide_z = on_bytes(P.side[i].z, P.side[i].ldz, 0, sizeof(Z), 16);
+    P.side[i].wide_u = on_bytes(P.side[i].u, P.side[i].ldu, 0, 4, 16);
+  }
+  // CTAs that share an adapter's rows: until there are two for every SM, while each has four stages of an average adapter
+  const int sms = current_sm_count(), mean = P.rows / (P.G < P.rows ? P.G : P.rows);
+  unsigned split = 1;
+  while (split < kOuterSplit && slabs * P.G * split < 2 * sms && mean > 4 * kStageRows * (int)split) split *= 2;
+  return adapter_launched(launch_overlapping(kern, dim3((unsigned)(slabs * split), (unsigned)P.G), dim3(kThreads), S::kSmem, split, s, P));
+}
+
+}  // namespace
+
+bool adapters_outer_tc_takes(const OuterArgs& P, lcd_dtype z_type) {
+  long long slabs = 0;
+  for (int i = 0; i < P.sides; ++i) {
+    if (z_type == LCD_DTYPE_BF16 && !on_bytes(P.side[i].z, P.side[i].ldz, 0, 2, 16)) return false;
+    slabs += (P.side[i].columns + 127) / 128;
+  }
+  return P.rows >= 512 && P.r <= 64 && slabs <= 0x7fffffff / kOuterSplit;
+}
+
+lcd_status launch_adapters_outer_tc(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s) {
+  return by_dtype(z_type, [&](auto z) {
+    return by_dtype((lcd_dtype)P.out_type, [&](auto o) {
+      using Z = typename decltype(z)::type;
+      using O = typename decltype(o)::type;
+      switch (rank_tiles(P.r)) {
+        case 1: return launch_shape<Z, O, 16>(P, s);
+        case 2: return launch_shape<Z, O, 32>(P, s);
+        default: return launch_shape<Z, O, 64>(P, s);
+      }
+    });
+  });
+}
+
+}  // namespace lcd

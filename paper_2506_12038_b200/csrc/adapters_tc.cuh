@@ -122,6 +122,10 @@ __device__ __forceinline__ void parts_of(float (&v)[8], uint4 (&out)[PARTS]) {
 // The parts that a type's values take: bf16 is one, fp16 two (11 bits), fp32 three.
 template <typename T> constexpr int kParts = std::is_same<T, __nv_bfloat16>::value ? 1 : std::is_same<T, __half>::value ? 2 : 3;
 
+// The parts of t and dt beside an operand of type T for a result of type O: two where both are bf16 (2^-16 of a term is left out, half a step
+// of the result is 2^-9), else three.
+template <typename T, typename O> constexpr int kPartsFor = std::is_same<T, __nv_bfloat16>::value && std::is_same<O, __nv_bfloat16>::value ? 2 : 3;
+
 // The plan's tiles of 128 places, each of one group, in shared memory: first[g] tiles lie before group g, begins[g] places; group G stands
 // for the rows without one.
 constexpr int kPlaces = 128;

@@ -56,6 +56,7 @@ AdapterArgs args_of(const lcd_adapter_weights& w, const lcd_row_groups& rows, bo
 }
 lcd_status down(const DownArgs& d, lcd_dtype x_type, lcd_dtype w_type, bool backward, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (adapters_down_tc_takes(d, x_type, w_type)) return launch_adapters_down_tc(d, x_type, backward, s);
   switch (x_type) {
     case LCD_DTYPE_F32: return launch_adapters_down_f32(d, w_type, backward, s);
     case LCD_DTYPE_F16: return launch_adapters_down_f16(d, w_type, backward, s);
@@ -132,6 +133,7 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   d.t = static_cast<float*>(workspace);
   d.t_rows = t;
   d.ldt_rows = ldt;
+  d.status = status_word_dev;
   st = down(d, x_type, weights->type, false, cuda_stream);
   if (st != LCD_OK) return st;
   UpArgs u = {};
@@ -172,6 +174,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
     d.x = dy;
     d.ldx = lddy;
     d.t = dt;
+    d.status = status_word_dev;
     st = down(d, type, weights->type, true, cuda_stream);
     if (st != LCD_OK) return st;
   }
@@ -196,6 +199,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
   o.G = (int)weights->G;
   o.r = (int)weights->rank;
   o.out_type = (int)grad_type;
+  o.status = status_word_dev;
   if (da) o.side[o.sides++] = {dt, padded_rank(weights->rank), 1, 0, x, ldx, 0, weights->K, nullptr, da, 0};
   if (db) o.side[o.sides++] = {t, ldt, 0, 0, dy, lddy, 0, weights->N, weights->scale, db, 1};
   return launch_adapters_outer(o, type, s);
