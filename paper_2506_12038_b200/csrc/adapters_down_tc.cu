@@ -214,10 +214,8 @@ lcd_status launch_shape(const DownArgs& P, cudaStream_t s) {
     attr_set.done(dev);
   }
   // at most that many tiles; those that hold rows are about half of the groups fewer
-  const long long tiles = P.a.rows / kPlaces + (P.a.G + 1 < P.a.rows ? P.a.G + 1 : P.a.rows);
-  const int sms = current_sm_count();
-  unsigned split = 1;
-  while (split < kDownSplit && (P.a.rows / kPlaces + 1) * 2ll * split <= 2 * sms && (P.a.K + 63) / 64 >= 8ll * split) split *= 2;
+  const long long tiles = P.a.rows / kPlaces + (P.a.G + 1 < P.a.rows ? P.a.G + 1 : P.a.rows), likely = P.a.rows / kPlaces + (P.a.G + 1) / 2;
+  const unsigned split = split_of(likely, (P.a.K + 63) / 64, (long long)current_sm_count() * (228 * 1024 / (S::kSmem + 1024)), kDownSplit);
   return adapter_launched(launch_overlapping(kern, dim3((unsigned)(tiles * split)), dim3(kThreads), S::kSmem, split, s, P));
 }
 

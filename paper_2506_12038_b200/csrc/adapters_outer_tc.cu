@@ -4,8 +4,8 @@
 // MN-major as they lie.  Rows of z follow the plan through 16-byte copies (bf16 as it is; fp16 and fp32 through registers, in two or three bf16
 // parts), those of t or dt are split into parts on their way.  A cluster's CTAs share an adapter's rows where there are few tiles and
 // add their sums up in distributed shared memory, in the order of the ranks.  Reading z bounds it.
-// Roles (9 warps): warps 0-3 bring z, then read the sums from tensor memory; warps 4-7 bring t or dt; warp 8 owns tensor memory, one
-// elected lane issues the MMAs.
+// Roles (9 warps, 13 at ranks above 32): warps 0-3 bring z, then read the sums from tensor memory; the last one owns tensor memory, one elected
+// lane issues the MMAs; those between bring t or dt, each (or a pair) every fourth stage, so that its loads have four stages' time.
 #include "adapters_launch.h"
 #include "adapters_tc.cuh"
 
@@ -15,14 +15,17 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 9 * 32, kStageRows = 64, kOuterSplit = 8;
+constexpr int kStageRows = 64, kOuterSplit = 8;
 
 template <typename Z, typename O, int R>
 struct Shape {
   static constexpr int kParts_u = kPartsFor<Z, O>, kParts_z = kParts<Z> < kParts_u ? kParts<Z> : kParts_u;
   static constexpr int kZPart = 2 * kStageRows * 128, kUPart = (R + 63) / 64 * kStageRows * 128;
   static constexpr int kStage = kParts_z * kZPart + kParts_u * kUPart;
-  static constexpr int kStages = 5 * kStage <= 110 * 1024 ? 5 : 4 * kStage <= 220 * 1024 ? 4 : 3;
+  // two CTAs an SM where they have three stages each
+  static constexpr int kStages = 4 * kStage <= 110 * 1024 ? 4 : 3 * kStage <= 110 * 1024 ? 3 : 4 * kStage <= 220 * 1024 ? 4 : 3;
+  static constexpr int kPer = R == 64 ? 2 : 1;                                    // warps that bring a stage of t
+  static constexpr int kMmaWarp = 4 + 4 * kPer, kThreads = 32 * (kMmaWarp + 1);
   static constexpr int kPitch = R + 1;                                            // of the sums, fp32
   static constexpr int kSmem = 1024 + kStages * kStage + 128;
   static constexpr int kTmem = R < 32 ? 32 : R;
@@ -30,7 +33,7 @@ struct Shape {
 };
 
 template <typename Z, typename O, int R>
-__global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __grid_constant__ OuterArgs P) {
+__global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc_kernel(const __grid_constant__ OuterArgs P) {
   using S = Shape<Z, O, R>;
   constexpr bool kCopied = S::kParts_z == 1;
   extern __shared__ uint8_t smem_raw[];
@@ -56,7 +59,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
   const int from = max(0, min(P.rows, P.offsets[group])), to = max(from, min(P.rows, P.offsets[group + 1]));
   O* out = static_cast<O*>(E.out);
   if (to == from) {                                  // in all CTAs of the cluster: zeros
-    for (int e = rank * kThreads + threadIdx.x; e < 128 * P.r; e += split * kThreads) {
+    for (int e = rank * S::kThreads + threadIdx.x; e < 128 * P.r; e += split * S::kThreads) {
       const int r = E.by_column ? e % P.r : e / 128, c = E.by_column ? e / P.r : e % 128;
       if (col0 + c < E.columns)
         out[E.by_column ? ((long long)group * E.columns + col0 + c) * P.r + r : ((long long)group * P.r + r) * E.columns + col0 + c] = from_f32<O>(0.0f);
@@ -65,7 +68,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) {
-      bar_init(full(s), 256);
+      bar_init(full(s), 128 + 32 * S::kPer);
       bar_init(empty(s), 1);
     }
     bar_init(d_full, 1);
@@ -73,7 +76,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
   }
-  if (warp == 8) tmem_alloc((uint32_t)__cvta_generic_to_shared(tmem_holder), S::kTmem);
+  if (warp == S::kMmaWarp) tmem_alloc((uint32_t)__cvta_generic_to_shared(tmem_holder), S::kTmem);
   before_sync();
   __syncthreads();
   after_sync();
@@ -82,7 +85,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
   const int k0 = (int)((long long)stages * rank / split), n = (int)((long long)stages * (rank + 1) / split) - k0;
   bool ok = true;
 
-  if (warp == 8) {
+  if (warp == S::kMmaWarp) {
     if (elect()) {
       constexpr uint32_t idesc = instr_desc(R, true, true, true);
       uint32_t more = 0;
@@ -120,9 +123,19 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
       const int place = from + (k0 + it) * kStageRows + thread / 16 + 8 * i;
       return place < to ? row_of(P.order, place, P.rows) : -1;
     };
-    int row[8];
+    int row[8], then[8];                                // of this stage and the next
 #pragma unroll
-    for (int i = 0; i < 8; ++i) row[i] = row_at(0, i);
+    for (int i = 0; i < 8; ++i) {
+      row[i] = row_at(0, i);
+      then[i] = 1 < n ? row_at(1, i) : -1;
+    }
+    auto next_rows = [&](int it) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        row[i] = then[i];
+        then[i] = it + 2 < n ? row_at(it + 2, i) : -1;
+      }
+    };
     if constexpr (kCopied) {
       constexpr int kBehind = S::kStages - 1;
       for (int it = 0; it < n && ok; ++it) {
@@ -135,8 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
           copy16(base + s * S::kStage + at_piece + piece_at(thread / 16 + 8 * i, piece % 8), there ? static_cast<const void*>(z + row[i] * E.ldz) : E.z, there);
         }
         copies_commit();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) row[i] = it + 1 < n ? row_at(it + 1, i) : -1;
+        next_rows(it);
         if (it >= kBehind) {
           copies_wait<kBehind>();
           fence_async();
@@ -157,8 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
       load();
       for (int it = 0; it < n && ok; ++it) {
         const int s = it % S::kStages;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) row[i] = it + 1 < n ? row_at(it + 1, i) : -1;
+        next_rows(it);
         ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
         if (!ok) break;
 #pragma unroll
@@ -194,28 +205,36 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
     }
     before_sync();
   } else {
-    // t or dt: a thread has eight ranks of R / 16 rows
-    const int thread = threadIdx.x - 128;
-    constexpr int kUnits = R / 8, kEach = kStageRows * kUnits / 128;
+    // t or dt: pieces of eight ranks
+    const int mine = (warp - 4) / S::kPer, first = (warp - 4) % S::kPer * 32 + lane;
+    constexpr int kUnits = R / 8, kEach = kStageRows * kUnits / (32 * S::kPer);
     Words<float, 8> in[kEach];
-    auto load = [&](int it) {
+    int row[kEach];
+    auto find = [&](int it) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int u = thread + 128 * i, unit = u % kUnits, place = from + (k0 + it) * kStageRows + u / kUnits;
-        const int row = place < to ? row_of(P.order, place, P.rows) : -1, have = row >= 0 ? max(0, min(8, P.r - unit * 8)) : 0;
-        load_words(in[i], E.u + (E.u_by_place ? (long long)(row >= 0 ? place : 0) : (long long)(row >= 0 ? row : 0)) * E.ldu + unit * 8, have,
-                   E.wide_u && (have <= 0 || have >= 8));
+        const int place = from + (k0 + it) * kStageRows + (first + 32 * S::kPer * i) / kUnits;
+        row[i] = it < n && place < to ? (E.u_by_place ? place : row_of(P.order, place, P.rows)) : -1;
       }
     };
-    if (n > 0) load(0);
-    for (int it = 0; it < n && ok; ++it) {
+    auto load = [&] {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int unit = (first + 32 * S::kPer * i) % kUnits, have = row[i] >= 0 ? max(0, min(8, P.r - unit * 8)) : 0;
+        load_words(in[i], E.u + (long long)max(row[i], 0) * E.ldu + unit * 8, have, E.wide_u && (have <= 0 || have >= 8));
+      }
+    };
+    find(mine);
+    load();
+    find(mine + 4);
+    for (int it = mine; it < n && ok; it += 4) {
       const int s = it % S::kStages;
-      ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
+      ok = __all_sync(0xffffffffu, bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag));
       if (!ok) break;
       const uint32_t to_u = base + s * S::kStage + S::kParts_z * S::kZPart;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int u = thread + 128 * i, unit = u % kUnits, at = u / kUnits;
+        const int u = first + 32 * S::kPer * i, unit = u % kUnits, at = u / kUnits;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = value_of(in[i], e);
@@ -226,7 +245,8 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
       }
       fence_async();
       bar_arrive(full(s));
-      if (it + 1 < n) load(it + 1);
+      load();
+      find(it + 8);
     }
   }
   if (split > 1) {
@@ -236,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
     __syncthreads();
   }
   const float factor = E.scale ? E.scale[group] : 1.0f;
-  for (int e = rank * kThreads + threadIdx.x; e < 128 * P.r; e += split * kThreads) {
+  for (int e = rank * S::kThreads + threadIdx.x; e < 128 * P.r; e += split * S::kThreads) {
     // consecutive threads: consecutive places of the output
     const int r = E.by_column ? e % P.r : e / 128, c = E.by_column ? e / P.r : e % 128;
     if (col0 + c >= E.columns) continue;
@@ -261,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_outer_tc_kernel(const __
   }
   before_sync();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == S::kMmaWarp) {
     after_sync();
     tmem_free(tmem, S::kTmem);
   }
@@ -286,11 +306,9 @@ lcd_status launch_shape(OuterArgs P, cudaStream_t s) {
     P.side[i].wide_z = on_bytes(P.side[i].z, P.side[i].ldz, 0, sizeof(Z), 16);
     P.side[i].wide_u = on_bytes(P.side[i].u, P.side[i].ldu, 0, 4, 16);
   }
-  // CTAs that share an adapter's rows: until there are two for every SM, while each has four stages of an average adapter
-  const int sms = current_sm_count(), mean = P.rows / (P.G < P.rows ? P.G : P.rows);
-  unsigned split = 1;
-  while (split < kOuterSplit && slabs * P.G * split < 2 * sms && mean > 4 * kStageRows * (int)split) split *= 2;
-  return adapter_launched(launch_overlapping(kern, dim3((unsigned)(slabs * split), (unsigned)P.G), dim3(kThreads), S::kSmem, split, s, P));
+  const long long stages = P.rows / (P.G < P.rows ? P.G : P.rows) / kStageRows + 1;
+  const unsigned split = split_of(slabs * P.G, stages, (long long)current_sm_count() * (228 * 1024 / (S::kSmem + 1024)), kOuterSplit);
+  return adapter_launched(launch_overlapping(kern, dim3((unsigned)(slabs * split), (unsigned)P.G), dim3(S::kThreads), S::kSmem, split, s, P));
 }
 
 }  // namespace

@@ -126,6 +126,21 @@ template <typename T> constexpr int kParts = std::is_same<T, __nv_bfloat16>::val
 // of the result is 2^-9), else three.
 template <typename T, typename O> constexpr int kPartsFor = std::is_same<T, __nv_bfloat16>::value && std::is_same<O, __nv_bfloat16>::value ? 2 : 3;
 
+// How many CTAs of a cluster share the stages of a sum, when `tiles` sums of `stages` stages each run on `slots` places at a time: what takes least
+// time if starting and joining takes as long as six stages.
+inline unsigned split_of(long long tiles, long long stages, long long slots, unsigned most) {
+  unsigned best = 1;
+  long long least = 0;
+  for (unsigned s = 1; s <= most && s <= stages; s *= 2) {
+    const long long time = (tiles * s + slots - 1) / slots * ((stages + s - 1) / s + 6);
+    if (s == 1 || time < least) {
+      least = time;
+      best = s;
+    }
+  }
+  return best;
+}
+
 // The plan's tiles of 128 places, each of one group, in shared memory: first[g] tiles lie before group g, begins[g] places; group G stands
 // for the rows without one.
 constexpr int kPlaces = 128;

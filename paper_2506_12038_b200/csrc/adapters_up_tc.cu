@@ -149,14 +149,42 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
     __syncwarp();
   } else if (warp < kFirstEpiWarp) {
     // ------------------------------------------------------------------------------------------ t and the adapter matrix, in parts
+    // The next tile's t is on its way while this one is multiplied: it waits in registers.
     const int thread = threadIdx.x - 32 * kFirstLoadWarp;
+    constexpr int kEach = R / 8, kAhead = kEach < 8 ? kEach : 8;         // pieces of eight ranks a thread, and how many of them wait
+    auto unit_of = [&](int i) { return thread + 128 * i; };
+    auto load_t = [&](const Plan::Spot& q, int i) {
+      const int row = unit_of(i) / kEach, unit = unit_of(i) % kEach;
+      Raw8<float> v = {};
+      if (row < q.count) v = load8(P.t + (long long)(q.place + row) * R + unit * 8);
+      return v;
+    };
+    auto place_t = [&](const Raw8<float>& raw, int i) {
+      const int row = unit_of(i) / kEach, unit = unit_of(i) % kEach;
+      float v[8];
+      values8(raw, v);
+      uint4 out[S::kParts_t];
+      parts_of<S::kParts_t>(v, out);
+#pragma unroll
+      for (int p = 0; p < S::kParts_t; ++p) {
+        const int k = p * S::kSteps + unit / 2;
+        store16(at_t + k / 4 * (128 * 128) + piece_at(row, k % 4 * 2 + unit % 2), out[p]);
+      }
+    };
     bool waited = false, ok = true;
     uint32_t it = 0;
     int group = -1;
     long long columns = -1;
-    for (int tile = tile0; tile < tile1 && ok; ++tile) {
-      const Plan::Spot q = plan.at(tile % row_tiles, G, kPlaces);
-      if (q.group >= G) continue;
+    Raw8<float> ahead[kAhead];
+    Plan::Spot q = {};
+    auto find = [&](int tile) {                  // the next tile of an adapter, or tile1
+      for (; tile < tile1; ++tile) {
+        q = plan.at(tile % row_tiles, G, kPlaces);
+        if (q.group < G) break;
+      }
+      return tile;
+    };
+    for (int tile = find(tile0); tile < tile1 && ok;) {
       const long long c0 = (long long)(tile / row_tiles) * NC;
       ok = __all_sync(0xffffffffu, bar_wait(t_empty, (it & 1u) ^ 1u, abort_flag));
       if (!ok) break;
@@ -164,31 +192,39 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
         group = q.group;
         columns = c0;
         const W* w = static_cast<const W*>(P.a.w) + group * P.a.sw;
-        constexpr int kRowsW = TRANSPOSED ? R : NC, kUnits = TRANSPOSED ? NC / 8 : R / 8;
-#pragma unroll 2
-        for (int u = thread; u < kRowsW * kUnits; u += 128) {
-          const int row = u / kUnits, unit = u % kUnits;
-          const long long at_row = TRANSPOSED ? row : c0 + row, at_col = TRANSPOSED ? c0 + unit * 8 : unit * 8;
-          const long long rows = TRANSPOSED ? P.a.r : P.a.K, cols = TRANSPOSED ? P.a.K : P.a.r;
-          const int have = at_row < rows ? (int)max(0ll, min(8ll, cols - at_col)) : 0;
-          Words<W, 8> in;
-          load_words(in, w + at_row * P.a.ldw + at_col, have, P.a.wide_w && (have <= 0 || have >= 8));
-          uint4 out[S::kParts_w];
-          if constexpr (S::kParts_w == 1) {
-            out[0] = make_uint4(in.w[0], in.w[1], in.w[2], in.w[3]);
-          } else {
-            float v[8];
+        constexpr int kRowsW = TRANSPOSED ? R : NC, kUnits = TRANSPOSED ? NC / 8 : R / 8, kEachW = kRowsW * kUnits / 128, kMostBatch = S::kParts_w == 1 ? 8 : 4,
+                      kBatch = kEachW < kMostBatch ? kEachW : kMostBatch;
+#pragma unroll 1
+        for (int u0 = thread; u0 < kRowsW * kUnits; u0 += 128 * kBatch) {
+          Words<W, 8> in[kBatch];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = value_of(in, i);
-            parts_of<S::kParts_w>(v, out);
+          for (int i = 0; i < kBatch; ++i) {
+            const int row = (u0 + 128 * i) / kUnits, unit = (u0 + 128 * i) % kUnits;
+            const long long at_row = TRANSPOSED ? row : c0 + row, at_col = TRANSPOSED ? c0 + unit * 8 : unit * 8;
+            const long long rows = TRANSPOSED ? P.a.r : P.a.K, cols = TRANSPOSED ? P.a.K : P.a.r;
+            const int have = at_row < rows ? (int)max(0ll, min(8ll, cols - at_col)) : 0;
+            load_words(in[i], w + at_row * P.a.ldw + at_col, have, P.a.wide_w && (have <= 0 || have >= 8));
           }
 #pragma unroll
-          for (int p = 0; p < S::kParts_w; ++p) {
-            if (TRANSPOSED) {
-              store16(at_w + unit / 8 * (S::kParts_w * R * 128) + piece_at(p * R + row, unit % 8), out[p]);
+          for (int i = 0; i < kBatch; ++i) {
+            const int row = (u0 + 128 * i) / kUnits, unit = (u0 + 128 * i) % kUnits;
+            uint4 out[S::kParts_w];
+            if constexpr (S::kParts_w == 1) {
+              out[0] = make_uint4(in[i].w[0], in[i].w[1], in[i].w[2], in[i].w[3]);
             } else {
-              const int k = p * S::kSteps + unit / 2;
-              store16(at_w + k / 4 * (NC * 128) + piece_at(row, k % 4 * 2 + unit % 2), out[p]);
+              float v[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] = value_of(in[i], e);
+              parts_of<S::kParts_w>(v, out);
+            }
+#pragma unroll
+            for (int p = 0; p < S::kParts_w; ++p) {
+              if (TRANSPOSED) {
+                store16(at_w + unit / 8 * (S::kParts_w * R * 128) + piece_at(p * R + row, unit % 8), out[p]);
+              } else {
+                const int k = p * S::kSteps + unit / 2;
+                store16(at_w + k / 4 * (NC * 128) + piece_at(row, k % 4 * 2 + unit % 2), out[p]);
+              }
             }
           }
         }
@@ -196,28 +232,25 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
       if (!waited) {
         begin_after_previous();
         waited = true;
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ahead[i] = load_t(q, i);
       }
-#pragma unroll 4
-      for (int u = thread; u < 128 * (R / 8); u += 128) {
-        const int row = u / (R / 8), unit = u % (R / 8);
-        float v[8];
-        if (row < q.count) {
-          values8(load8(P.t + (long long)(q.place + row) * R + unit * 8), v);
-        } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-        }
-        uint4 out[S::kParts_t];
-        parts_of<S::kParts_t>(v, out);
+      for (int i = 0; i < kAhead; ++i) place_t(ahead[i], i);
+      if constexpr (kEach > kAhead) {
 #pragma unroll
-        for (int p = 0; p < S::kParts_t; ++p) {
-          const int k = p * S::kSteps + unit / 2;
-          store16(at_t + k / 4 * (128 * 128) + piece_at(row, k % 4 * 2 + unit % 2), out[p]);
-        }
+        for (int i = kAhead; i < kEach; ++i) ahead[i - kAhead] = load_t(q, i);
+#pragma unroll
+        for (int i = kAhead; i < kEach; ++i) place_t(ahead[i - kAhead], i);
       }
       fence_async();
       bar_arrive(t_full);
       ++it;
+      tile = find(tile + 1);
+      if (tile < tile1) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ahead[i] = load_t(q, i);
+      }
     }
     if (!waited) begin_after_previous();
   } else {
