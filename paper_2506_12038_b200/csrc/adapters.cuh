@@ -43,7 +43,7 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], float a0, float a1, floa
 // v = upper + rest.  The upper part is v cut off (never rounded up, which could overflow), the rest exact; an infinity has no rest.
 __device__ __forceinline__ float upper_tf32(float v) { return __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
 __device__ __forceinline__ float upper_bf16(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
-__device__ __forceinline__ float rest_of(float v, float upper) { return (__float_as_uint(v) & 0x7fffffffu) == 0x7f800000u ? 0.0f : v - upper; }
+__device__ __forceinline__ float rest_of(float v, float upper) { return v == upper ? 0.0f : v - upper; }
 // Two values as a word of bf16: their upper parts, or rounded.
 __device__ __forceinline__ uint32_t pair_upper(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
 __device__ __forceinline__ uint32_t pair_rounded(float lo, float hi) {

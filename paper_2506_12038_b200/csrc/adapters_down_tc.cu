@@ -164,31 +164,19 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
     __syncthreads();
   }
   const float factor = P.a.scale && real ? P.a.scale[q.group] : 1.0f;
-  for (int e = rank * kThreads + threadIdx.x; e < q.count * R; e += split * kThreads) {
-    const int at = e / R, r = e % R;
-    float sum = 0.0f;
-    if (real) {
-      const uint32_t from = base + (at * S::kPitch + r) * 4;
-      float v[kDownSplit];
-#pragma unroll
-      for (int i = 0; i < kDownSplit; ++i) {
-        v[i] = 0.0f;
-        if (i < (int)split) {
-          uint32_t there;
-          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(from), "r"(i));
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(there) : "memory");
-        }
+  by_split(split, [&](auto ranks) {
+    constexpr int kRanks = decltype(ranks)::value;
+#pragma unroll 4
+    for (int e = rank * kThreads + threadIdx.x; e < q.count * R; e += kRanks * kThreads) {
+      const int at = e / R, r = e % R;
+      const float sum = real && r < P.a.r ? sum_of_ranks<kRanks>(base + (at * S::kPitch + r) * 4) * factor : 0.0f;
+      P.t[(long long)q.place * R + e] = sum;
+      if (P.t_rows && r < P.a.r) {
+        const int row = row_of(P.a.order, q.place + at, P.a.rows);
+        if (row >= 0) P.t_rows[row * P.ldt_rows + r] = sum;
       }
-#pragma unroll
-      for (int i = 0; i < kDownSplit; ++i) sum += v[i];
-      sum = r < P.a.r ? sum * factor : 0.0f;
     }
-    P.t[(long long)q.place * R + e] = sum;
-    if (P.t_rows && r < P.a.r) {
-      const int row = row_of(P.a.order, q.place + at, P.a.rows);
-      if (row >= 0) P.t_rows[row * P.ldt_rows + r] = sum;
-    }
-  }
+  });
   if (split > 1) {
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");

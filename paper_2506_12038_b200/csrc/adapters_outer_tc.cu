@@ -29,11 +29,12 @@ struct Shape {
   static constexpr int kPitch = R + 1;                                            // of the sums, fp32
   static constexpr int kSmem = 1024 + kStages * kStage + 128;
   static constexpr int kTmem = R < 32 ? 32 : R;
+  static constexpr int kPerSm = 2 * (kSmem + 1024) <= 228 * 1024 ? 2 : 1;
   static_assert(128 * kPitch * 4 <= kStages * kStage && kSmem <= 227 * 1024, "sums lie in the stages");
 };
 
 template <typename Z, typename O, int R>
-__global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc_kernel(const __grid_constant__ OuterArgs P) {
+__global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPerSm) adapters_outer_tc_kernel(const __grid_constant__ OuterArgs P) {
   using S = Shape<Z, O, R>;
   constexpr bool kCopied = S::kParts_z == 1;
   extern __shared__ uint8_t smem_raw[];
@@ -58,11 +59,13 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
   const long long col0 = slab * 128;
   const int from = max(0, min(P.rows, P.offsets[group])), to = max(from, min(P.rows, P.offsets[group + 1]));
   O* out = static_cast<O*>(E.out);
+  auto place_of = [&](int r, int c) {
+    return E.by_column ? ((long long)group * E.columns + col0 + c) * P.r + r : ((long long)group * P.r + r) * E.columns + col0 + c;
+  };
   if (to == from) {                                  // in all CTAs of the cluster: zeros
-    for (int e = rank * S::kThreads + threadIdx.x; e < 128 * P.r; e += split * S::kThreads) {
-      const int r = E.by_column ? e % P.r : e / 128, c = E.by_column ? e / P.r : e % 128;
-      if (col0 + c < E.columns)
-        out[E.by_column ? ((long long)group * E.columns + col0 + c) * P.r + r : ((long long)group * P.r + r) * E.columns + col0 + c] = from_f32<O>(0.0f);
+    for (int e = rank * S::kThreads + threadIdx.x; e < 128 * R; e += split * S::kThreads) {
+      const int r = E.by_column ? e % R : e / 128, c = E.by_column ? e / R : e % 128;
+      if (r < P.r && col0 + c < E.columns) out[place_of(r, c)] = from_f32<O>(0.0f);
     }
     return;
   }
@@ -256,25 +259,16 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
     __syncthreads();
   }
   const float factor = E.scale ? E.scale[group] : 1.0f;
-  for (int e = rank * S::kThreads + threadIdx.x; e < 128 * P.r; e += split * S::kThreads) {
-    // consecutive threads: consecutive places of the output
-    const int r = E.by_column ? e % P.r : e / 128, c = E.by_column ? e / P.r : e % 128;
-    if (col0 + c >= E.columns) continue;
-    const uint32_t at = base + (c * S::kPitch + r) * 4;
-    float v[kOuterSplit], sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kOuterSplit; ++i) {
-      v[i] = 0.0f;
-      if (i < (int)split) {
-        uint32_t there;
-        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(i));
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(there) : "memory");
-      }
+  by_split(split, [&](auto ranks) {
+    constexpr int kRanks = decltype(ranks)::value;
+#pragma unroll 4
+    for (int e = rank * S::kThreads + threadIdx.x; e < 128 * R; e += kRanks * S::kThreads) {
+      // consecutive threads: consecutive places of the output
+      const int r = E.by_column ? e % R : e / 128, c = E.by_column ? e / R : e % 128;
+      if (r >= P.r || col0 + c >= E.columns) continue;
+      out[place_of(r, c)] = from_f32<O>(sum_of_ranks<kRanks>(base + (c * S::kPitch + r) * 4) * factor);
     }
-#pragma unroll
-    for (int i = 0; i < kOuterSplit; ++i) sum += v[i];
-    out[E.by_column ? ((long long)group * E.columns + col0 + c) * P.r + r : ((long long)group * P.r + r) * E.columns + col0 + c] = from_f32<O>(sum * factor);
-  }
+  });
   if (split > 1) {
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
@@ -307,7 +301,7 @@ lcd_status launch_shape(OuterArgs P, cudaStream_t s) {
     P.side[i].wide_u = on_bytes(P.side[i].u, P.side[i].ldu, 0, 4, 16);
   }
   const long long stages = P.rows / (P.G < P.rows ? P.G : P.rows) / kStageRows + 1;
-  const unsigned split = split_of(slabs * P.G, stages, (long long)current_sm_count() * (228 * 1024 / (S::kSmem + 1024)), kOuterSplit);
+  const unsigned split = split_of(slabs * P.G, stages, (long long)current_sm_count() * S::kPerSm, kOuterSplit);
   return adapter_launched(launch_overlapping(kern, dim3((unsigned)(slabs * split), (unsigned)P.G), dim3(S::kThreads), S::kSmem, split, s, P));
 }
 

@@ -141,6 +141,61 @@ inline unsigned split_of(long long tiles, long long stages, long long slots, uns
   return best;
 }
 
+// The sum over a cluster's CTAs, in their order, of what lies at this shared address in each.
+template <int SPLIT>
+__device__ __forceinline__ float sum_of_ranks(uint32_t at) {
+  float v[SPLIT];
+#pragma unroll
+  for (int i = 0; i < SPLIT; ++i) {
+    if constexpr (SPLIT == 1) {
+      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[i]) : "r"(at) : "memory");
+    } else {
+      uint32_t there;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(i));
+      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(there) : "memory");
+    }
+  }
+  float sum = v[0];
+#pragma unroll
+  for (int i = 1; i < SPLIT; ++i) sum += v[i];
+  return sum;
+}
+// f(std::integral_constant<int, split>) for a split of 1, 2, 4 or 8.
+template <typename F>
+__device__ __forceinline__ void by_split(uint32_t split, F&& f) {
+  if (split == 1) f(std::integral_constant<int, 1>{});
+  else if (split == 2) f(std::integral_constant<int, 2>{});
+  else if (split == 4) f(std::integral_constant<int, 4>{});
+  else f(std::integral_constant<int, 8>{});
+}
+// Sixteen values of a row from an address on 16 bytes, or, wide, on 32.
+template <typename Y>
+__device__ __forceinline__ void store16_values(Y* p, const float (&v)[16], bool wide) {
+  uint32_t w[sizeof(Y) == 4 ? 16 : 8];
+  if constexpr (sizeof(Y) == 4) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[i]);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float part[8] = {v[8 * h], v[8 * h + 1], v[8 * h + 2], v[8 * h + 3], v[8 * h + 4], v[8 * h + 5], v[8 * h + 6], v[8 * h + 7]};
+      const uint4 q = pack8<Y>(part);
+      w[4 * h] = q.x; w[4 * h + 1] = q.y; w[4 * h + 2] = q.z; w[4 * h + 3] = q.w;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < (sizeof(Y) == 4 ? 16 : 8); i += 8) {
+    uint32_t* to = reinterpret_cast<uint32_t*>(p) + i;
+    if (wide) {
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                   ::"l"(to), "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7]) : "memory");
+    } else {
+      *reinterpret_cast<uint4*>(to) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+      *reinterpret_cast<uint4*>(to + 4) = make_uint4(w[i + 4], w[i + 5], w[i + 6], w[i + 7]);
+    }
+  }
+}
+
 // The plan's tiles of 128 places, each of one group, in shared memory: first[g] tiles lie before group g, begins[g] places; group G stands
 // for the rows without one.
 constexpr int kPlaces = 128;

@@ -1,13 +1,13 @@
 // adapters_up.cu's products for many rows: y = base + s t b^T, dx = base + dt a.
 //
-// A tile is 128 rows of one adapter by NC columns.  Rows of base come in by bulk copies, one a row, which follow the plan at no cost, and
-// rows of y leave the same way; the product, t's parts times the adapter matrix's, waits in tensor memory meanwhile.  A CTA has consecutive
+// A tile is 128 rows of one adapter by NC columns.  Rows of base come in by bulk copies, one a row, which follow the plan at no cost; the
+// product, t's parts times the adapter matrix's, waits in tensor memory meanwhile.  A CTA has consecutive
 // tiles of the list (columns, rows), so that the adapter's part stays in shared memory from tile to tile.
 //
 // Roles (14 warps): warp 0 copies base in; warp 1 owns tensor memory, one elected lane issues the MMAs; warps 2-5 bring t and, where it
 // changes, the adapter matrix, split into bf16 parts; warps 6-13 add: a thread has a row and half of the columns, reads the base's from
-// shared memory (rows 16 bytes longer than their columns: no bank conflicts), writes the sums there and sends them off itself.
-// Two tiles are in flight: while one is added up and leaves, the next one's base comes in.
+// shared memory (rows 16 bytes longer than their columns: no bank conflicts) and stores 32 bytes at a time, whole sectors.
+// Two tiles are in flight: while one is added up, the next one's base comes in.
 #include "adapters_launch.h"
 #include "adapters_tc.cuh"
 
@@ -260,65 +260,71 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
     constexpr int kHalf = NC / 2;
     bool ok = true;
     uint32_t it = 0, dt = 0;
+    // of the next tile: asked for while this one is added up
+    Plan::Spot q = {};
+    int row = -1;
+    float factor = 1.0f;
+    auto look = [&](int tile) {
+      if (tile >= tile1) return;
+      q = plan.at(tile % row_tiles, G, kPlaces);
+      row = mine < q.count ? row_of(P.a.order, q.place + mine, P.a.rows) : -1;
+      factor = P.a.scale && q.group < G ? P.a.scale[q.group] : 1.0f;
+    };
+    look(tile0);
     for (int tile = tile0; tile < tile1 && ok; ++tile, ++it) {
-      const Plan::Spot q = plan.at(tile % row_tiles, G, kPlaces);
-      const long long c0 = (long long)(tile / row_tiles) * NC;
-      const int columns = columns_of(c0) - half * kHalf;
+      const long long c0 = (long long)(tile / row_tiles) * NC + half * kHalf;
+      const int columns = (int)min((long long)kHalf, P.a.K - c0), to_row = row;
+      const float s = factor;
+      const bool real = q.group < G;
       const uint32_t b = it & 1u, db = dt & 1u;
-      const int row = mine < q.count ? row_of(P.a.order, q.place + mine, P.a.rows) : -1;
-      const float factor = P.a.scale && q.group < G ? P.a.scale[q.group] : 1.0f;
-      // the tile before has left its buffer: the next one's base may come in
-      asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-      __syncwarp();
-      if (it > 0 && lane == 0) bar_arrive(y_empty(b ^ 1u));
+      look(tile + 1);
       if (P.base) ok = __all_sync(0xffffffffu, bar_wait(y_full(b), (it >> 1) & 1u, abort_flag));
-      if (ok && q.group < G) ok = __all_sync(0xffffffffu, bar_wait(d_full(db), (dt >> 1) & 1u, abort_flag));
+      if (ok && real) ok = __all_sync(0xffffffffu, bar_wait(d_full(db), (dt >> 1) & 1u, abort_flag));
       if (!ok) break;
       after_sync();
-      const uint32_t at = at_y + (b * 128 + mine) * S::kPitch + half * kHalf * (int)sizeof(Y);
-      Y* own = reinterpret_cast<Y*>(gen + at);
-      if (q.group < G) {
-        const uint32_t from = tmem + ((uint32_t)(32 * quad) << 16) + db * NC + half * kHalf;
-#pragma unroll 2
-        for (int c = 0; c < kHalf; c += 16) {
-          uint32_t d[16];
-          tmem_ld16(from + c, d);
-          Raw8<Y> raw[2];
-          if (P.base) {
-            raw[0] = load8(own + c);
-            raw[1] = load8(own + c + 8);
-          }
-          tmem_wait_ld();
+      const Y* own = reinterpret_cast<const Y*>(gen + at_y + (b * 128 + mine) * S::kPitch) + half * kHalf;
+      Y* y = static_cast<Y*>(P.y) + max(to_row, 0) * P.ldy + c0;
+      const uint32_t from = tmem + ((uint32_t)(32 * quad) << 16) + db * NC + half * kHalf;
+      uint32_t d[2][16];
+      if (real) tmem_ld16(from, d[0]);
+#pragma unroll
+      for (int c = 0; c < kHalf; c += 16) {
+        float v[16];
+        if (P.base) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            float v[8];
-            if (P.base) {
-              values8(raw[h], v);
-            } else {
+            float part[8];
+            values8(load8(own + c + 8 * h), part);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __fmaf_rn(factor, __uint_as_float(d[8 * h + i]), v[i]);
-            store8(own + c + 8 * h, v);
+            for (int i = 0; i < 8; ++i) v[8 * h + i] = part[i];
           }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = 0.0f;
         }
-        before_sync();
-        __syncwarp();
-        if (lane == 0) bar_arrive(d_empty(db));
-        ++dt;
-      } else if (!P.base) {
-        const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        for (int c = 0; c < kHalf; c += 8) store8(own + c, zero);
+        if (real) {
+          tmem_wait_ld();
+          if (c + 16 < kHalf) tmem_ld16(from + c + 16, d[(c / 16 + 1) & 1]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = __fmaf_rn(s, __uint_as_float(d[(c / 16) & 1][i]), v[i]);
+        }
+        if (to_row < 0 || c >= columns) continue;
+        if (c + 16 <= columns) {
+          store16_values(y + c, v, P.wide_y);
+        } else {                                              // the row ends after four or eight, or twelve
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (c + i < columns) y[c + i] = from_f32<Y>(v[i]);
+        }
       }
-      fence_async();
-      if (row >= 0 && columns > 0)
-        asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
-                     ::"l"(static_cast<Y*>(P.y) + row * P.ldy + c0 + half * kHalf), "r"(at), "r"((uint32_t)(min(columns, kHalf) * sizeof(Y))) : "memory");
-      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      before_sync();
       __syncwarp();
+      if (lane == 0) {
+        bar_arrive(y_empty(b));
+        if (real) bar_arrive(d_empty(db));
+      }
+      if (real) ++dt;
     }
-    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   before_sync();
   __syncthreads();
@@ -341,6 +347,7 @@ lcd_status launch_shape(UpArgs P, cudaStream_t s) {
     attr_set.done(dev);
   }
   P.a.wide_w = on_bytes(P.a.w, P.a.ldw, P.a.sw, sizeof(W), 16);
+  P.wide_y = on_bytes(P.y, P.ldy, 0, sizeof(Y), 32);
   const long long most = ((long long)P.a.rows / kPlaces + (P.a.G + 1 < P.a.rows ? P.a.G + 1 : P.a.rows)) * ((P.a.K + S::kNC - 1) / S::kNC);
   const long long room = (long long)current_sm_count() * S::kPerSm;
   return adapter_launched(launch_overlapping(kern, dim3((unsigned)(most < room ? most : room)), dim3(kThreads), S::kSmem, 1, s, P));
