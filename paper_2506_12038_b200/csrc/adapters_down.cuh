@@ -20,8 +20,22 @@ struct DownArgs {
   int window;
   float *t, *t_rows;           // by place, 16 * RT values a row; by row (may be null)
   long long ldt_rows;
+  void* t_parts;               // by place, [rows][parts][16 * RT] bf16 (may be null)
+  int parts;
   int32_t* status;
 };
+
+// One value of t, with its bf16 parts: all but the last cut off, that one rounded.
+__device__ __forceinline__ void store_t(const DownArgs& P, int R, long long place, int r, float v) {
+  P.t[place * R + r] = v;
+  if (!P.t_parts) return;
+  __nv_bfloat16* to = static_cast<__nv_bfloat16*>(P.t_parts) + place * P.parts * R + r;
+  for (int p = 0; p < P.parts; ++p) {
+    const float upper = p + 1 < P.parts ? upper_bf16(v) : v;
+    to[p * R] = from_f32<__nv_bfloat16>(upper);
+    v = rest_of(v, upper);
+  }
+}
 
 constexpr int kDownWarps = 8;
 template <int RT> constexpr int kDownTokens = RT == 8 ? 2 : 4;              // groups of eight rows in the widest window
@@ -205,7 +219,7 @@ __global__ void __launch_bounds__(32 * kDownWarps, 1) adapters_down_kernel(const
     const int at = e / R, r = e % R, group = s_group[at];
     if (P.a.scale && group >= 0) sum *= P.a.scale[group];
     if (r >= P.a.r) sum = 0.0f;
-    P.t[(long long)place0 * R + e] = sum;
+    store_t(P, R, place0 + at, r, sum);
     if (P.t_rows && r < P.a.r && s_row[at] >= 0) P.t_rows[(long long)s_row[at] * P.ldt_rows + r] = sum;
   }
   if (split > 1) {

@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
     for (int e = rank * kThreads + threadIdx.x; e < q.count * R; e += kRanks * kThreads) {
       const int at = e / R, r = e % R;
       const float sum = real && r < P.a.r ? sum_of_ranks<kRanks>(base + (at * S::kPitch + r) * 4) * factor : 0.0f;
-      P.t[(long long)q.place * R + e] = sum;
+      store_t(P, R, q.place + at, r, sum);
       if (P.t_rows && r < P.a.r) {
         const int row = row_of(P.a.order, q.place + at, P.a.rows);
         if (row >= 0) P.t_rows[row * P.ldt_rows + r] = sum;

@@ -9,6 +9,7 @@ namespace lcd {
 struct UpArgs {
   AdapterArgs a;
   const float* t;              // by place, 16 * RT values a row
+  const void* t_parts;         // the same as bf16 parts, [rows][parts][16 * RT], where adapters_up_tc_parts says so
   const void* base;            // or null
   void* y;
   long long ldbase, ldy;
@@ -19,7 +20,8 @@ struct UpArgs {
 lcd_status launch_adapters_up(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s);
 
 // The same on tcgen05, where there are many rows and their pieces start on 16 bytes.
-bool adapters_up_tc_takes(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type);
+// The parts of t that it needs, 0 where the other kernel runs.
+int adapters_up_tc_parts(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type);
 lcd_status launch_adapters_up_tc(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s);
 
 struct DownArgs;

@@ -252,7 +252,7 @@ lcd_status launch_types(UpArgs P, cudaStream_t s) {
 }  // namespace
 
 lcd_status launch_adapters_up(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s) {
-  if (adapters_up_tc_takes(P, w_type, y_type)) return launch_adapters_up_tc(P, w_type, y_type, transposed, s);
+  if (P.t_parts) return launch_adapters_up_tc(P, w_type, y_type, transposed, s);
   return by_dtype(w_type, [&](auto w) {
     return by_dtype(y_type, [&](auto y) {
       using W = typename decltype(w)::type;

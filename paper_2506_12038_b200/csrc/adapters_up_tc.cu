@@ -1,11 +1,12 @@
 // adapters_up.cu's products for many rows: y = base + s t b^T, dx = base + dt a.
 //
-// A tile is 128 rows of one adapter by NC columns.  Rows of base come in by bulk copies, one a row, which follow the plan at no cost; the
-// product, t's parts times the adapter matrix's, waits in tensor memory meanwhile.  A CTA has consecutive
-// tiles of the list (columns, rows), so that the adapter's part stays in shared memory from tile to tile.
+// A tile is 128 rows of one adapter by NC columns.  Rows of base follow the plan through 16-byte cp.async copies, whole rows side by side (one bulk
+// copy a row takes a thread some 120 clocks, 128 of them three times as long as their bytes need); the product, t's parts times the adapter
+// matrix's, waits in tensor memory meanwhile.  A CTA has consecutive tiles of the list (columns, rows), so that the adapter's part stays
+// in shared memory from tile to tile.
 //
-// Roles (14 warps): warp 0 copies base in; warp 1 owns tensor memory, one elected lane issues the MMAs; warps 2-5 bring t and, where it
-// changes, the adapter matrix, split into bf16 parts; warps 6-13 add: a thread has a row and half of the columns, reads the base's from
+// Roles (17 warps): warps 0-3 copy base in; warp 4 owns tensor memory, one elected lane issues the MMAs; warps 5-8 bring t and, where it
+// changes, the adapter matrix, split into bf16 parts; warps 9-16 add: a thread has a row and half of the columns, reads the base's from
 // shared memory (rows 16 bytes longer than their columns: no bank conflicts) and stores 32 bytes at a time, whole sectors.
 // Two tiles are in flight: while one is added up, the next one's base comes in.
 #include "adapters_launch.h"
@@ -17,7 +18,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 14 * 32, kFirstLoadWarp = 2, kFirstEpiWarp = 6;
+constexpr int kMmaWarp = 4, kFirstLoadWarp = 5, kFirstEpiWarp = 9, kThreads = 17 * 32;
 constexpr int kMostSmem = 227 * 1024;
 
 template <typename W, typename Y, int R, bool TRANSPOSED>
@@ -57,7 +58,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
   if (!P.early) wait_for_previous();
   if (threadIdx.x == 0) {
     for (int b = 0; b < 2; ++b) {
-      bar_init(y_full(b), 1);
+      bar_init(y_full(b), 128);
       bar_init(y_empty(b), 8);
       bar_init(d_full(b), 1);
       bar_init(d_empty(b), 8);
@@ -69,8 +70,8 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async();
   }
-  if (warp == 1) tmem_alloc((uint32_t)__cvta_generic_to_shared(tmem_holder), S::kTmem);
-  if (warp == 2) plan.make(P.a, lane, kPlaces);
+  if (warp == kMmaWarp) tmem_alloc((uint32_t)__cvta_generic_to_shared(tmem_holder), S::kTmem);
+  if (warp == 0) plan.make(P.a, lane, kPlaces);
   before_sync();
   __syncthreads();
   after_sync();
@@ -80,38 +81,41 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
   const int tile0 = (int)(tiles * blockIdx.x / gridDim.x), tile1 = (int)(tiles * (blockIdx.x + 1) / gridDim.x);
   auto columns_of = [&](long long c0) { return (int)min((long long)NC, P.a.K - c0); };
 
-  if (warp == 0) {
+  if (warp < kMmaWarp) {
     // ------------------------------------------------------------------------------------------ rows of base
-    bool ok = true;
-    uint32_t it = 0;
     if (P.base) {
-      for (int tile = tile0; tile < tile1 && ok; ++tile, ++it) {
+      constexpr int kPieces = NC * (int)sizeof(Y) / 16, kRowsEach = 32 / kPieces;     // 16-byte pieces of a row; rows of a warp's copy
+      const int piece = lane % kPieces;
+      bool ok = true;
+      uint32_t it = 0;
+      int next = -1;                             // lane l: row l of the warp's 32 of the next tile
+      auto look = [&](int tile) {
+        if (tile >= tile1) return;
         const Plan::Spot q = plan.at(tile % row_tiles, G, kPlaces);
+        next = 32 * warp + lane < q.count ? row_of(P.a.order, q.place + 32 * warp + lane, P.a.rows) : -1;
+      };
+      look(tile0);
+      for (int tile = tile0; tile < tile1 && ok; ++tile, ++it) {
         const long long c0 = (long long)(tile / row_tiles) * NC;
-        const uint32_t b = it & 1u, bytes = (uint32_t)columns_of(c0) * sizeof(Y);
-        int row[4], valid = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          row[i] = 32 * i + lane < q.count ? row_of(P.a.order, q.place + 32 * i + lane, P.a.rows) : -1;
-          valid += __popc(__ballot_sync(0xffffffffu, row[i] >= 0));
-        }
+        const uint32_t b = it & 1u;
+        const int row = next;
+        const bool inside = piece * 16 < columns_of(c0) * (int)sizeof(Y);
+        const Y* from = static_cast<const Y*>(P.base) + c0 + piece * (16 / (int)sizeof(Y));
+        look(tile + 1);
         ok = __all_sync(0xffffffffu, bar_wait(y_empty(b), ((it >> 1) & 1u) ^ 1u, abort_flag));
         if (!ok) break;
-        if (lane == 0) bar_expect_tx(y_full(b), bytes * valid);
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (row[i] >= 0)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                         ::"r"(at_y + (b * 128 + 32 * i + lane) * S::kPitch), "l"(static_cast<const Y*>(P.base) + row[i] * P.ldbase + c0), "r"(bytes),
-                           "r"(y_full(b)) : "memory");
-        __syncwarp();
+        const uint32_t to = at_y + (b * 128 + 32 * warp + lane / kPieces) * S::kPitch + piece * 16;
+#pragma unroll 8
+        for (int i = 0; i < 32; i += kRowsEach) {
+          const int r = __shfl_sync(0xffffffffu, row, i + lane / kPieces);
+          if (r >= 0 && inside) copy16(to + i * S::kPitch, from + r * P.ldbase, 16);
+        }
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(y_full(b)) : "memory");
       }
-      // nothing this warp issued may be in flight when the CTA exits
-      for (uint32_t i = 1; i <= 2 && i <= it; ++i) bar_drain(y_full((it - i) & 1u), ((it - i) >> 1) & 1u);
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
     begin_after_previous();
-  } else if (warp == 1) {
+  } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------------------------------------ MMAs
     begin_after_previous();
     if (elect()) {
@@ -149,33 +153,11 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
     __syncwarp();
   } else if (warp < kFirstEpiWarp) {
     // ------------------------------------------------------------------------------------------ t and the adapter matrix, in parts
-    // The next tile's t is on its way while this one is multiplied: it waits in registers.
     const int thread = threadIdx.x - 32 * kFirstLoadWarp;
-    constexpr int kEach = R / 8, kAhead = kEach < 8 ? kEach : 8;         // pieces of eight ranks a thread, and how many of them wait
-    auto unit_of = [&](int i) { return thread + 128 * i; };
-    auto load_t = [&](const Plan::Spot& q, int i) {
-      const int row = unit_of(i) / kEach, unit = unit_of(i) % kEach;
-      Raw8<float> v = {};
-      if (row < q.count) v = load8(P.t + (long long)(q.place + row) * R + unit * 8);
-      return v;
-    };
-    auto place_t = [&](const Raw8<float>& raw, int i) {
-      const int row = unit_of(i) / kEach, unit = unit_of(i) % kEach;
-      float v[8];
-      values8(raw, v);
-      uint4 out[S::kParts_t];
-      parts_of<S::kParts_t>(v, out);
-#pragma unroll
-      for (int p = 0; p < S::kParts_t; ++p) {
-        const int k = p * S::kSteps + unit / 2;
-        store16(at_t + k / 4 * (128 * 128) + piece_at(row, k % 4 * 2 + unit % 2), out[p]);
-      }
-    };
     bool waited = false, ok = true;
     uint32_t it = 0;
     int group = -1;
     long long columns = -1;
-    Raw8<float> ahead[kAhead];
     Plan::Spot q = {};
     auto find = [&](int tile) {                  // the next tile of an adapter, or tile1
       for (; tile < tile1; ++tile) {
@@ -232,25 +214,20 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
       if (!waited) {
         begin_after_previous();
         waited = true;
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) ahead[i] = load_t(q, i);
       }
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) place_t(ahead[i], i);
-      if constexpr (kEach > kAhead) {
-#pragma unroll
-        for (int i = kAhead; i < kEach; ++i) ahead[i - kAhead] = load_t(q, i);
-#pragma unroll
-        for (int i = kAhead; i < kEach; ++i) place_t(ahead[i - kAhead], i);
+      constexpr int kUnits = S::kParts_t * (R / 8);               // pieces of eight ranks of a row
+      const __nv_bfloat16* t = static_cast<const __nv_bfloat16*>(P.t_parts) + (long long)q.place * (S::kParts_t * R);
+#pragma unroll 8
+      for (int u = thread; u < 128 * kUnits; u += 128) {
+        const int row = u / kUnits, unit = u % kUnits;
+        // part after part, steps of 16 ranks four to a block
+        copy16(at_t + unit / 8 * (128 * 128) + piece_at(row, unit % 8), row < q.count ? t + (long long)u * 8 : P.t_parts, row < q.count ? 16 : 0);
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
       fence_async();
       bar_arrive(t_full);
       ++it;
       tile = find(tile + 1);
-      if (tile < tile1) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) ahead[i] = load_t(q, i);
-      }
     }
     if (!waited) begin_after_previous();
   } else {
@@ -328,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
   }
   before_sync();
   __syncthreads();
-  if (warp == 1) {
+  if (warp == kMmaWarp) {
     after_sync();
     tmem_free(tmem, S::kTmem);
   }
@@ -355,11 +332,12 @@ lcd_status launch_shape(UpArgs P, cudaStream_t s) {
 
 }  // namespace
 
-bool adapters_up_tc_takes(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type) {
+int adapters_up_tc_parts(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type) {
   const int64_t size = y_type == LCD_DTYPE_F32 ? 4 : 2;
-  if (!on_bytes(P.y, P.ldy, P.a.K, size, 16) || (P.base && !on_bytes(P.base, P.ldbase, 0, size, 16))) return false;
-  if (P.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return false;      // the parts do not fit
-  return P.a.rows >= 512 && ((long long)P.a.rows / kPlaces + P.a.G + 1) * ((P.a.K + 63) / 64) <= 0x7fffffff;
+  if (P.a.rows < 512 || ((long long)P.a.rows / kPlaces + P.a.G + 1) * ((P.a.K + 63) / 64) > 0x7fffffff) return 0;
+  if (!on_bytes(P.y, P.ldy, P.a.K, size, 16) || (P.base && !on_bytes(P.base, P.ldbase, 0, size, 16))) return 0;
+  if (P.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return 0;      // the parts do not fit
+  return w_type == LCD_DTYPE_BF16 && y_type == LCD_DTYPE_BF16 ? 2 : 3;
 }
 
 lcd_status launch_adapters_up_tc(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s) {

@@ -110,7 +110,8 @@ extern "C" lcd_status lcd_mx_linear_grouped(const uint8_t* w_codes, int64_t ldwc
 extern "C" lcd_status lcd_adapters_workspace_bytes(int64_t count, int64_t rank, size_t* bytes) {
   if (!bytes || !counted(count) || rank < 1) return LCD_ERR_INVALID_ARG;
   if (rank > kMostRank) return LCD_ERR_UNSUPPORTED;
-  *bytes = (size_t)count * (size_t)padded_rank(rank) * 4;
+  // t or dt, and for many rows its bf16 parts
+  *bytes = (size_t)count * (size_t)padded_rank(rank) * (count >= 512 ? 10 : 4);
   return LCD_OK;
 }
 
@@ -134,8 +135,6 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   d.t_rows = t;
   d.ldt_rows = ldt;
   d.status = status_word_dev;
-  st = down(d, x_type, weights->type, false, cuda_stream);
-  if (st != LCD_OK) return st;
   UpArgs u = {};
   u.a = args_of(*weights, *rows, true);
   u.a.scale = weights->scale;
@@ -146,6 +145,10 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   u.ldy = ldy;
   u.early = 1;
   u.status = status_word_dev;
+  d.parts = adapters_up_tc_parts(u, weights->type, y_type);
+  u.t_parts = d.t_parts = d.parts ? d.t + rows->count * padded_rank(weights->rank) : nullptr;
+  st = down(d, x_type, weights->type, false, cuda_stream);
+  if (st != LCD_OK) return st;
   return launch_adapters_up(u, weights->type, y_type, false, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -167,19 +170,8 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
   if (!workspace || workspace_bytes < need) return LCD_ERR_BUFFER_TOO_SMALL;
   float* dt = static_cast<float*>(workspace);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (dx || da) {
-    DownArgs d = {};
-    d.a = args_of(*weights, *rows, true);
-    d.a.scale = weights->scale;
-    d.x = dy;
-    d.ldx = lddy;
-    d.t = dt;
-    d.status = status_word_dev;
-    st = down(d, type, weights->type, true, cuda_stream);
-    if (st != LCD_OK) return st;
-  }
+  UpArgs u = {};
   if (dx) {
-    UpArgs u = {};
     u.a = args_of(*weights, *rows, false);
     u.t = dt;
     u.base = base;
@@ -188,6 +180,21 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
     u.ldy = lddx;
     u.early = 1;
     u.status = status_word_dev;
+  }
+  if (dx || da) {
+    DownArgs d = {};
+    d.a = args_of(*weights, *rows, true);
+    d.a.scale = weights->scale;
+    d.x = dy;
+    d.ldx = lddy;
+    d.t = dt;
+    d.status = status_word_dev;
+    d.parts = dx ? adapters_up_tc_parts(u, weights->type, type) : 0;
+    u.t_parts = d.t_parts = d.parts ? dt + rows->count * padded_rank(weights->rank) : nullptr;
+    st = down(d, type, weights->type, true, cuda_stream);
+    if (st != LCD_OK) return st;
+  }
+  if (dx) {
     st = launch_adapters_up(u, weights->type, type, true, s);
     if (st != LCD_OK) return st;
   }

@@ -76,7 +76,7 @@ def test_unsupported_and_short_workspaces():
     assert lib.lcd_adapters_workspace_bytes(6, 129, ctypes.byref(need)) == 2 and lib.lcd_adapters_workspace_bytes(0, 4, ctypes.byref(need)) == 1
     assert lib.lcd_adapters_workspace_bytes(6, 4, None) == 1 and lib.lcd_mx_linear_grouped_workspace_bytes(6, 0, ctypes.byref(need)) == 1
     for rank, padded in ((1, 16), (16, 16), (17, 32), (33, 64), (65, 128), (128, 128)):
-        assert lcd.adapters_workspace_bytes(7, rank) == 7 * padded * 4
+        assert lcd.adapters_workspace_bytes(511, rank) == 511 * padded * 4 and lcd.adapters_workspace_bytes(512, rank) == 512 * padded * 10
     assert lcd.mx_linear_grouped_workspace_bytes(6, 64) == 6 * 48
 
 
