@@ -124,10 +124,9 @@ struct AdapterArgs {
   int wide_w, wide_x;
 };
 
-__device__ __forceinline__ int row_of(const int32_t* order, int at, int rows) {
-  const int row = order[at];
-  return (unsigned)row < (unsigned)rows ? row : -1;
-}
+// A row that the plan names, -1 where it is none.  (Where the plan is read ahead, the check waits until the row is used.)
+__device__ __forceinline__ int checked_row(int row, int rows) { return (unsigned)row < (unsigned)rows ? row : -1; }
+__device__ __forceinline__ int row_of(const int32_t* order, int at, int rows) { return checked_row(order[at], rows); }
 
 // RT for a rank: 16 * RT is the rank padded.
 constexpr int rank_tiles(int64_t r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }

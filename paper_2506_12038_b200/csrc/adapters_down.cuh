@@ -25,15 +25,17 @@ struct DownArgs {
   int32_t* status;
 };
 
-// One value of t, with its bf16 parts: all but the last cut off, that one rounded.
-__device__ __forceinline__ void store_t(const DownArgs& P, int R, long long place, int r, float v) {
-  P.t[place * R + r] = v;
+// Four values of t, with their bf16 parts: all but the last cut off, that one rounded.
+__device__ __forceinline__ void store_t4(const DownArgs& P, int R, long long place, int r, const float (&v)[4]) {
+  *reinterpret_cast<float4*>(P.t + place * R + r) = make_float4(v[0], v[1], v[2], v[3]);
   if (!P.t_parts) return;
-  __nv_bfloat16* to = static_cast<__nv_bfloat16*>(P.t_parts) + place * P.parts * R + r;
+  uint2* to = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.t_parts) + place * P.parts * R + r);
+  float w[4] = {v[0], v[1], v[2], v[3]};
   for (int p = 0; p < P.parts; ++p) {
-    const float upper = p + 1 < P.parts ? upper_bf16(v) : v;
-    to[p * R] = from_f32<__nv_bfloat16>(upper);
-    v = rest_of(v, upper);
+    const bool last = p + 1 == P.parts;
+    to[p * R / 4] = last ? make_uint2(pair_rounded(w[0], w[1]), pair_rounded(w[2], w[3])) : make_uint2(pair_upper(w[0], w[1]), pair_upper(w[2], w[3]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = rest_of(w[i], upper_bf16(w[i]));
   }
 }
 
@@ -197,30 +199,41 @@ __global__ void __launch_bounds__(32 * kDownWarps, 1) adapters_down_kernel(const
   } else {
     __syncthreads();
   }
-  for (int e = rank * blockDim.x + threadIdx.x; e < count * R; e += split * blockDim.x) {
-    float sum = 0.0f;
+  for (int e = 4 * (rank * blockDim.x + threadIdx.x); e < count * R; e += 4 * split * blockDim.x) {
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (split > 1) {
       const uint32_t at = (uint32_t)__cvta_generic_to_shared(s_sum + e);
-      float v[kDownSplit];
+      float4 part[kDownSplit];
 #pragma unroll
       for (int i = 0; i < kDownSplit; ++i) {
-        v[i] = 0.0f;
+        part[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (i < (int)split) {
           uint32_t there;
           asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(i));
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(there) : "memory");
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(part[i].x), "=f"(part[i].y), "=f"(part[i].z), "=f"(part[i].w) : "r"(there));
         }
       }
 #pragma unroll
-      for (int i = 0; i < kDownSplit; ++i) sum += v[i];
+      for (int i = 0; i < kDownSplit; ++i) {
+        v[0] += part[i].x;
+        v[1] += part[i].y;
+        v[2] += part[i].z;
+        v[3] += part[i].w;
+      }
     } else {
-      sum = s_sum[e];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = s_sum[e + i];
     }
     const int at = e / R, r = e % R, group = s_group[at];
-    if (P.a.scale && group >= 0) sum *= P.a.scale[group];
-    if (r >= P.a.r) sum = 0.0f;
-    store_t(P, R, place0 + at, r, sum);
-    if (P.t_rows && r < P.a.r && s_row[at] >= 0) P.t_rows[(long long)s_row[at] * P.ldt_rows + r] = sum;
+    const float factor = P.a.scale && group >= 0 ? P.a.scale[group] : 1.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = r + i < P.a.r ? v[i] * factor : 0.0f;
+    store_t4(P, R, place0 + at, r, v);
+    if (P.t_rows && s_row[at] >= 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r + i < P.a.r) P.t_rows[(long long)s_row[at] * P.ldt_rows + r + i] = v[i];
+    }
   }
   if (split > 1) {
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");

@@ -166,14 +166,18 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
   const float factor = P.a.scale && real ? P.a.scale[q.group] : 1.0f;
   by_split(split, [&](auto ranks) {
     constexpr int kRanks = decltype(ranks)::value;
-#pragma unroll 4
-    for (int e = rank * kThreads + threadIdx.x; e < q.count * R; e += kRanks * kThreads) {
-      const int at = e / R, r = e % R;
-      const float sum = real && r < P.a.r ? sum_of_ranks<kRanks>(base + (at * S::kPitch + r) * 4) * factor : 0.0f;
-      store_t(P, R, q.place + at, r, sum);
-      if (P.t_rows && r < P.a.r) {
+    for (int e = rank * kThreads + threadIdx.x; e < q.count * (R / 4); e += kRanks * kThreads) {
+      const int at = e / (R / 4), r = e % (R / 4) * 4;
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (real) sum = sums_of_ranks<kRanks>(base + (at * S::kPitch + r) * 4);
+      const float v[4] = {r < P.a.r ? sum.x * factor : 0.0f, r + 1 < P.a.r ? sum.y * factor : 0.0f, r + 2 < P.a.r ? sum.z * factor : 0.0f,
+                          r + 3 < P.a.r ? sum.w * factor : 0.0f};
+      store_t4(P, R, q.place + at, r, v);
+      if (P.t_rows) {
         const int row = row_of(P.a.order, q.place + at, P.a.rows);
-        if (row >= 0) P.t_rows[row * P.ldt_rows + r] = sum;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (row >= 0 && r + i < P.a.r) P.t_rows[row * P.ldt_rows + r + i] = v[i];
       }
     }
   });

@@ -26,7 +26,7 @@ struct Shape {
   static constexpr int kStages = 4 * kStage <= 110 * 1024 ? 4 : 3 * kStage <= 110 * 1024 ? 3 : 4 * kStage <= 220 * 1024 ? 4 : 3;
   static constexpr int kPer = R == 64 ? 2 : 1;                                    // warps that bring a stage of t
   static constexpr int kMmaWarp = 4 + 4 * kPer, kThreads = 32 * (kMmaWarp + 1);
-  static constexpr int kPitch = R + 1;                                            // of the sums, fp32
+  static constexpr int kPitch = R + 4;                                            // of the sums, fp32
   static constexpr int kSmem = 1024 + kStages * kStage + 128;
   static constexpr int kTmem = R < 32 ? 32 : R;
   static constexpr int kPerSm = 2 * (kSmem + 1024) <= 228 * 1024 ? 2 : 1;
@@ -124,18 +124,18 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
     const Z* z = static_cast<const Z*>(E.z) + c;
     auto row_at = [&](int it, int i) {
       const int place = from + (k0 + it) * kStageRows + thread / 16 + 8 * i;
-      return place < to ? row_of(P.order, place, P.rows) : -1;
+      return place < to ? P.order[place] : -1;
     };
     int row[8], then[8];                                // of this stage and the next
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      row[i] = row_at(0, i);
+      row[i] = checked_row(row_at(0, i), P.rows);
       then[i] = 1 < n ? row_at(1, i) : -1;
     }
     auto next_rows = [&](int it) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        row[i] = then[i];
+        row[i] = checked_row(then[i], P.rows);
         then[i] = it + 2 < n ? row_at(it + 2, i) : -1;
       }
     };
@@ -204,7 +204,8 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
         for (int i = 0; i < 16; ++i) v[i] = 0u;
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[c2 + i] = __uint_as_float(v[i]);
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(sum + c2 + i) = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
     }
     before_sync();
   } else {
@@ -217,14 +218,14 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
         const int place = from + (k0 + it) * kStageRows + (first + 32 * S::kPer * i) / kUnits;
-        row[i] = it < n && place < to ? (E.u_by_place ? place : row_of(P.order, place, P.rows)) : -1;
+        row[i] = it < n && place < to ? (E.u_by_place ? place : P.order[place]) : -1;
       }
     };
     auto load = [&] {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
-        const int unit = (first + 32 * S::kPer * i) % kUnits, have = row[i] >= 0 ? max(0, min(8, P.r - unit * 8)) : 0;
-        load_words(in[i], E.u + (long long)max(row[i], 0) * E.ldu + unit * 8, have, E.wide_u && (have <= 0 || have >= 8));
+        const int at = checked_row(row[i], P.rows), unit = (first + 32 * S::kPer * i) % kUnits, have = at >= 0 ? max(0, min(8, P.r - unit * 8)) : 0;
+        load_words(in[i], E.u + (long long)max(at, 0) * E.ldu + unit * 8, have, E.wide_u && (have <= 0 || have >= 8));
       }
     };
     find(mine);
@@ -261,12 +262,16 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
   const float factor = E.scale ? E.scale[group] : 1.0f;
   by_split(split, [&](auto ranks) {
     constexpr int kRanks = decltype(ranks)::value;
-#pragma unroll 4
-    for (int e = rank * S::kThreads + threadIdx.x; e < 128 * R; e += kRanks * S::kThreads) {
-      // consecutive threads: consecutive places of the output
-      const int r = E.by_column ? e % R : e / 128, c = E.by_column ? e / R : e % 128;
+#pragma unroll 2
+    for (int e = rank * S::kThreads + threadIdx.x; e < 128 * R / 4; e += kRanks * S::kThreads) {
+      // four ranks of a column; consecutive threads: consecutive places of the output
+      const int r = E.by_column ? e % (R / 4) * 4 : e / 128 * 4, c = E.by_column ? e / (R / 4) : e % 128;
       if (r >= P.r || col0 + c >= E.columns) continue;
-      out[place_of(r, c)] = from_f32<O>(sum_of_ranks<kRanks>(base + (c * S::kPitch + r) * 4) * factor);
+      const float4 sum = sums_of_ranks<kRanks>(base + (c * S::kPitch + r) * 4);
+      const float v[4] = {sum.x * factor, sum.y * factor, sum.z * factor, sum.w * factor};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (r + i < P.r) out[place_of(r + i, c)] = from_f32<O>(v[i]);
     }
   });
   if (split > 1) {

@@ -131,7 +131,7 @@ template <typename T, typename O> constexpr int kPartsFor = std::is_same<T, __nv
 inline unsigned split_of(long long tiles, long long stages, long long slots, unsigned most) {
   unsigned best = 1;
   long long least = 0;
-  for (unsigned s = 1; s <= most && s <= stages; s *= 2) {
+  for (unsigned s = 1; s <= most && s <= stages; ++s) {
     const long long time = (tiles * s + slots - 1) / slots * ((stages + s - 1) / s + 6);
     if (s == 1 || time < least) {
       least = time;
@@ -141,32 +141,43 @@ inline unsigned split_of(long long tiles, long long stages, long long slots, uns
   return best;
 }
 
-// The sum over a cluster's CTAs, in their order, of what lies at this shared address in each.
+// The sums over a cluster's CTAs, in their order, of the four values that lie at this shared address in each.
 template <int SPLIT>
-__device__ __forceinline__ float sum_of_ranks(uint32_t at) {
-  float v[SPLIT];
+__device__ __forceinline__ float4 sums_of_ranks(uint32_t at) {
+  float4 v[SPLIT];
 #pragma unroll
   for (int i = 0; i < SPLIT; ++i) {
     if constexpr (SPLIT == 1) {
-      asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[i]) : "r"(at) : "memory");
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i].x), "=f"(v[i].y), "=f"(v[i].z), "=f"(v[i].w) : "r"(at));
     } else {
       uint32_t there;
       asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(i));
-      asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(there) : "memory");
+      asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[i].x), "=f"(v[i].y), "=f"(v[i].z), "=f"(v[i].w) : "r"(there));
     }
   }
-  float sum = v[0];
+  float4 sum = v[0];
 #pragma unroll
-  for (int i = 1; i < SPLIT; ++i) sum += v[i];
+  for (int i = 1; i < SPLIT; ++i) {
+    sum.x += v[i].x;
+    sum.y += v[i].y;
+    sum.z += v[i].z;
+    sum.w += v[i].w;
+  }
   return sum;
 }
-// f(std::integral_constant<int, split>) for a split of 1, 2, 4 or 8.
+// f(std::integral_constant<int, split>) for a split of 1 to 8.
 template <typename F>
 __device__ __forceinline__ void by_split(uint32_t split, F&& f) {
-  if (split == 1) f(std::integral_constant<int, 1>{});
-  else if (split == 2) f(std::integral_constant<int, 2>{});
-  else if (split == 4) f(std::integral_constant<int, 4>{});
-  else f(std::integral_constant<int, 8>{});
+  switch (split) {
+    case 1: f(std::integral_constant<int, 1>{}); break;
+    case 2: f(std::integral_constant<int, 2>{}); break;
+    case 3: f(std::integral_constant<int, 3>{}); break;
+    case 4: f(std::integral_constant<int, 4>{}); break;
+    case 5: f(std::integral_constant<int, 5>{}); break;
+    case 6: f(std::integral_constant<int, 6>{}); break;
+    case 7: f(std::integral_constant<int, 7>{}); break;
+    default: f(std::integral_constant<int, 8>{});
+  }
 }
 // Sixteen values of a row from an address on 16 bytes, or, wide, on 32.
 template <typename Y>

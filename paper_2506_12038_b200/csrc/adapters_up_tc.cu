@@ -92,13 +92,13 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
       auto look = [&](int tile) {
         if (tile >= tile1) return;
         const Plan::Spot q = plan.at(tile % row_tiles, G, kPlaces);
-        next = 32 * warp + lane < q.count ? row_of(P.a.order, q.place + 32 * warp + lane, P.a.rows) : -1;
+        next = 32 * warp + lane < q.count ? P.a.order[q.place + 32 * warp + lane] : -1;
       };
       look(tile0);
       for (int tile = tile0; tile < tile1 && ok; ++tile, ++it) {
         const long long c0 = (long long)(tile / row_tiles) * NC;
         const uint32_t b = it & 1u;
-        const int row = next;
+        const int row = checked_row(next, P.a.rows);
         const bool inside = piece * 16 < columns_of(c0) * (int)sizeof(Y);
         const Y* from = static_cast<const Y*>(P.base) + c0 + piece * (16 / (int)sizeof(Y));
         look(tile + 1);
@@ -174,10 +174,22 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
         group = q.group;
         columns = c0;
         const W* w = static_cast<const W*>(P.a.w) + group * P.a.sw;
-        constexpr int kRowsW = TRANSPOSED ? R : NC, kUnits = TRANSPOSED ? NC / 8 : R / 8, kEachW = kRowsW * kUnits / 128, kMostBatch = S::kParts_w == 1 ? 8 : 4,
+        constexpr int kRowsW = TRANSPOSED ? R : NC, kUnits = TRANSPOSED ? NC / 8 : R / 8, kEachW = kRowsW * kUnits / 128, kMostBatch = sizeof(W) == 2 ? 8 : 4,
                       kBatch = kEachW < kMostBatch ? kEachW : kMostBatch;
+        const bool copied = S::kParts_w == 1 && P.a.wide_w;          // as it lies, all pieces on their way together
+        if (copied) {
+#pragma unroll 8
+          for (int u = thread; u < kRowsW * kUnits; u += 128) {
+            const int row = u / kUnits, unit = u % kUnits;
+            const long long at_row = TRANSPOSED ? row : c0 + row, at_col = TRANSPOSED ? c0 + unit * 8 : unit * 8;
+            const long long rows = TRANSPOSED ? P.a.r : P.a.K, cols = TRANSPOSED ? P.a.K : P.a.r;
+            const int have = at_row < rows ? (int)max(0ll, min(8ll, cols - at_col)) * 2 : 0;
+            const uint32_t to = TRANSPOSED ? unit / 8 * (S::kParts_w * R * 128) + piece_at(row, unit % 8) : unit / 8 * (NC * 128) + piece_at(row, unit % 8);
+            copy16(at_w + to, have ? static_cast<const void*>(w + at_row * P.a.ldw + at_col) : P.a.w, have);
+          }
+        }
 #pragma unroll 1
-        for (int u0 = thread; u0 < kRowsW * kUnits; u0 += 128 * kBatch) {
+        for (int u0 = copied ? kRowsW * kUnits : thread; u0 < kRowsW * kUnits; u0 += 128 * kBatch) {
           Words<W, 8> in[kBatch];
 #pragma unroll
           for (int i = 0; i < kBatch; ++i) {
@@ -244,13 +256,13 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
     auto look = [&](int tile) {
       if (tile >= tile1) return;
       q = plan.at(tile % row_tiles, G, kPlaces);
-      row = mine < q.count ? row_of(P.a.order, q.place + mine, P.a.rows) : -1;
+      row = mine < q.count ? P.a.order[q.place + mine] : -1;
       factor = P.a.scale && q.group < G ? P.a.scale[q.group] : 1.0f;
     };
     look(tile0);
     for (int tile = tile0; tile < tile1 && ok; ++tile, ++it) {
       const long long c0 = (long long)(tile / row_tiles) * NC + half * kHalf;
-      const int columns = (int)min((long long)kHalf, P.a.K - c0), to_row = row;
+      const int columns = (int)min((long long)kHalf, P.a.K - c0), to_row = checked_row(row, P.a.rows);
       const float s = factor;
       const bool real = q.group < G;
       const uint32_t b = it & 1u, db = dt & 1u;
