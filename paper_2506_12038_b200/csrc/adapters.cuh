@@ -8,7 +8,7 @@
 //
 // Arithmetic.  Two 16-bit operands of one type: their products are exact, sums are fp32.  The products with t or dt, which are fp32: with
 // bf16 beside them as two bf16 terms (16 bits, relative error 2^-16 where the result is rounded to 16-bit types) or three (24 bits, for
-// fp32 results), else as two tf32 terms (22 bits; fp32 beside them likewise in two).
+// fp32 results), else as two tf32 terms (22 bits and their rounding; fp32 beside them likewise in two).
 #ifndef LCD_ADAPTERS_CUH_
 #define LCD_ADAPTERS_CUH_
 
@@ -40,10 +40,21 @@ __device__ __forceinline__ void mma_tf32(float (&d)[4], float a0, float a1, floa
                  "r"(__float_as_uint(b0)), "r"(__float_as_uint(b1)));
 }
 
-// v = upper + rest.  The upper part is v cut off (never rounded up, which could overflow), the rest exact; an infinity has no rest.
-__device__ __forceinline__ float upper_tf32(float v) { return __uint_as_float(__float_as_uint(v) & 0xffffe000u); }
+// v = upper + rest.  The upper part is never rounded up to an infinity (tf32: to the nearest, cut off where that would overflow; bf16: cut off),
+// the rest is exact; an infinity has no rest.
+__device__ __forceinline__ float nearest_tf32(float v) {
+  uint32_t r;
+  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(v));
+  return __uint_as_float(r);
+}
+__device__ __forceinline__ float upper_tf32(float v) {
+  const float r = nearest_tf32(v);
+  return fabsf(r) == __uint_as_float(0x7f800000u) ? __uint_as_float(__float_as_uint(v) & 0xffffe000u) : r;
+}
 __device__ __forceinline__ float upper_bf16(float v) { return __uint_as_float(__float_as_uint(v) & 0xffff0000u); }
 __device__ __forceinline__ float rest_of(float v, float upper) { return v == upper ? 0.0f : v - upper; }
+// The same rounded to tf32, which the instruction would cut off.
+__device__ __forceinline__ float rest_tf32(float v, float upper) { return nearest_tf32(rest_of(v, upper)); }
 // Two values as a word of bf16: their upper parts, or rounded.
 __device__ __forceinline__ uint32_t pair_upper(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
 __device__ __forceinline__ uint32_t pair_rounded(float lo, float hi) {
@@ -51,13 +62,41 @@ __device__ __forceinline__ uint32_t pair_rounded(float lo, float hi) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// N consecutive values of a row as words, zeros where `have` ends.  WIDE: they lie on N * sizeof(T) bytes (16 at most) and are all there or
-// none is.
+// N consecutive values of a row as words.
 template <typename T, int N>
 struct Words {
   static constexpr int kCount = N * (int)sizeof(T) / 4;
   uint32_t w[kCount];
 };
+// The same at any alignment: the aligned words around them, then shifted (apart, so that several rows' loads are on their way together).
+// Sixteen bytes of the row on either side are there.
+template <typename T, int N>
+struct Around {
+  static constexpr int kCount = (Words<T, N>::kCount + 3) / 4 * 4 + 4;
+  uint32_t w[kCount];
+};
+template <typename T, int N>
+__device__ __forceinline__ void load_around(Around<T, N>& out, const T* p, bool there) {
+  const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+#pragma unroll
+  for (int i = 0; i < Around<T, N>::kCount; i += 4) {
+    const uint4 v = there ? q[i / 4] : make_uint4(0u, 0u, 0u, 0u);
+    out.w[i] = v.x; out.w[i + 1] = v.y; out.w[i + 2] = v.z; out.w[i + 3] = v.w;
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void shift_words(Words<T, N>& out, const Around<T, N>& in, const T* p) {
+  constexpr int kCount = Words<T, N>::kCount;
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u);
+  uint32_t w[kCount + 2], u[kCount + 1];
+#pragma unroll
+  for (int i = 0; i < kCount + 2; ++i) w[i] = off & 8u ? in.w[i + 2] : in.w[i];
+#pragma unroll
+  for (int i = 0; i < kCount + 1; ++i) u[i] = off & 4u ? w[i + 1] : w[i];
+#pragma unroll
+  for (int i = 0; i < kCount; ++i) out.w[i] = kIs16<T> ? __byte_perm(u[i], u[i + 1], off & 2u ? 0x5432 : 0x3210) : u[i];
+}
+// Zeros where `have` ends.  wide: they lie on N * sizeof(T) bytes (16 at most) and are all there or none is.
 template <typename T, int N>
 __device__ __forceinline__ void load_words(Words<T, N>& out, const T* p, int have, bool wide) {
   constexpr int kCount = Words<T, N>::kCount;

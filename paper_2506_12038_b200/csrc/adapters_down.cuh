@@ -43,9 +43,10 @@ constexpr int kDownWarps = 8;
 template <int RT> constexpr int kDownTokens = RT == 8 ? 2 : 4;              // groups of eight rows in the widest window
 constexpr int kDownSplit = 8;                                       // most CTAs that share the columns
 
-template <typename X, typename W, int RT, bool TRANSPOSED>
-__global__ void __launch_bounds__(32 * kDownWarps, 1) adapters_down_kernel(const DownArgs P) {
-  constexpr int NT = kDownTokens<RT>, R = 16 * RT;
+// NT: groups of eight rows of the widest window; one for windows of up to eight rows, whose many CTAs then have registers to share an SM.
+template <typename X, typename W, int RT, int NT, bool TRANSPOSED>
+__global__ void __launch_bounds__(32 * kDownWarps, NT == 1 && RT * sizeof(W) <= 4 ? 3 : NT == 1 && RT * sizeof(W) <= 8 ? 2 : 1) adapters_down_kernel(const DownArgs P) {
+  constexpr int R = 16 * RT;
   constexpr bool kNative = kIs16<X> && std::is_same<X, W>::value;
   using WWords = Words<W, TRANSPOSED ? 2 * RT : 8>;
   constexpr int kW = TRANSPOSED ? 8 : 2 * RT;
@@ -98,18 +99,42 @@ __global__ void __launch_bounds__(32 * kDownWarps, 1) adapters_down_kernel(const
     auto load = [&](Frag& f, int c) {
       const long long k = (long long)c * 32;
       const int have = (int)min((long long)8, P.a.K - k - 8 * t);
+      // chunks with another on either side: rows at any alignment in aligned words, four rows' loads at a time
+      const bool within = k >= 32 && k + 64 <= P.a.K;
+      if (!TRANSPOSED && !P.a.wide_w && within) {
 #pragma unroll
-      for (int i = 0; i < kW; ++i) {
-        if (TRANSPOSED) {
-          const int ranks = min(2 * RT, P.a.r - g * 2 * RT);
-          load_words(f.w[i], w + (k + i) * P.a.ldw, i < have ? ranks : 0, P.a.wide_w && (ranks <= 0 || ranks >= 2 * RT));
-        } else {
-          load_words(f.w[i], w + 8 * i * P.a.ldw + k, 8 * i + g < P.a.r ? have : 0, P.a.wide_w && (have <= 0 || have >= 8));
+        for (int i0 = 0; i0 < kW; i0 += 4) {
+          constexpr int kBatch = kW < 4 ? kW : 4;
+          Around<W, TRANSPOSED ? 2 * RT : 8> around[kBatch];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) load_around(around[i], w + 8 * (i0 + i) * P.a.ldw + k, 8 * (i0 + i) + g < P.a.r);
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) shift_words(f.w[i0 + i], around[i], w + 8 * (i0 + i) * P.a.ldw + k);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+          if (TRANSPOSED) {
+            const int ranks = min(2 * RT, P.a.r - g * 2 * RT);
+            load_words(f.w[i], w + (k + i) * P.a.ldw, i < have ? ranks : 0, P.a.wide_w && (ranks <= 0 || ranks >= 2 * RT));
+          } else {
+            load_words(f.w[i], w + 8 * i * P.a.ldw + k, 8 * i + g < P.a.r ? have : 0, P.a.wide_w && (have <= 0 || have >= 8));
+          }
         }
       }
+      if (!P.a.wide_x && within) {
+        Around<X, 8> around[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-        if (8 * n < i1 && 8 * n + 8 > i0) load_words(f.x[n], xrow[n] + k, mine[n] ? have : 0, P.a.wide_x && (have <= 0 || have >= 8));
+        for (int n = 0; n < NT; ++n)
+          if (8 * n < i1 && 8 * n + 8 > i0) load_around(around[n], xrow[n] + k, mine[n]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          if (8 * n < i1 && 8 * n + 8 > i0) shift_words(f.x[n], around[n], xrow[n] + k);
+      } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+          if (8 * n < i1 && 8 * n + 8 > i0) load_words(f.x[n], xrow[n] + k, mine[n] ? have : 0, P.a.wide_x && (have <= 0 || have >= 8));
+      }
     };
     // value e (column 8 t + e of the chunk) of the lane's rank q: row 8 q + g, or g * 2 RT + q
     auto value_w = [&](const Frag& f, int q, int e) { return TRANSPOSED ? value_of(f.w[TRANSPOSED ? e : 0], q) : value_of(f.w[TRANSPOSED ? 0 : q], e); };
@@ -134,14 +159,15 @@ __global__ void __launch_bounds__(32 * kDownWarps, 1) adapters_down_kernel(const
       } else {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          float b[NT][2], b_rest[NT][2];
+          float b[NT][2], b_rest[NT][2], b_finite[NT][2];         // (an infinite x has its say in the first product alone, which keeps its sign)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
               const float v = value_of(f.x[n], 2 * s + j);
               b[n][j] = kIs16<X> ? v : upper_tf32(v);
-              b_rest[n][j] = kIs16<X> ? 0.0f : rest_of(v, b[n][j]);
+              b_rest[n][j] = kIs16<X> ? 0.0f : rest_tf32(v, b[n][j]);
+              b_finite[n][j] = kIs16<W> || fabsf(b[n][j]) != __uint_as_float(0x7f800000u) ? b[n][j] : 0.0f;
             }
 #pragma unroll
           for (int i = 0; i < RT; ++i) {
@@ -150,14 +176,14 @@ __global__ void __launch_bounds__(32 * kDownWarps, 1) adapters_down_kernel(const
             for (int j = 0; j < 4; ++j) {
               const float v = value_w(f, 2 * i + j % 2, 2 * s + j / 2);
               a[j] = kIs16<W> ? v : upper_tf32(v);
-              a_rest[j] = kIs16<W> ? 0.0f : rest_of(v, a[j]);
+              a_rest[j] = kIs16<W> ? 0.0f : rest_tf32(v, a[j]);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
               if (8 * n < i1 && 8 * n + 8 > i0) {
                 mma_tf32(acc[i][n], a[0], a[1], a[2], a[3], b[n][0], b[n][1]);
                 if constexpr (!kIs16<X>) mma_tf32(acc[i][n], a[0], a[1], a[2], a[3], b_rest[n][0], b_rest[n][1]);
-                if constexpr (!kIs16<W>) mma_tf32(acc[i][n], a_rest[0], a_rest[1], a_rest[2], a_rest[3], b[n][0], b[n][1]);
+                if constexpr (!kIs16<W>) mma_tf32(acc[i][n], a_rest[0], a_rest[1], a_rest[2], a_rest[3], b_finite[n][0], b_finite[n][1]);
               }
           }
         }
@@ -245,26 +271,30 @@ template <typename X, typename W, bool TRANSPOSED>
 lcd_status launch_down_types(DownArgs P, cudaStream_t s) {
   P.a.wide_x = on_bytes(P.x, P.ldx, 0, sizeof(X), 16);
   return by_rank(P.a.r, [&](auto rt) {
-    constexpr int RT = decltype(rt)::value, NT = kDownTokens<RT>, kMostSmem = kDownWarps * 8 * NT * 16 * RT * 4;
+    constexpr int RT = decltype(rt)::value, MOST = kDownTokens<RT>;
     constexpr int kWide = TRANSPOSED && 2 * RT * (int)sizeof(W) < 16 ? 2 * RT * (int)sizeof(W) : 16;
     P.a.wide_w = on_bytes(P.a.w, P.a.ldw, P.a.sw, sizeof(W), kWide);
-    auto kern = adapters_down_kernel<X, W, RT, TRANSPOSED>;
-    static PerDeviceFlag attr_set;
-    int dev;
-    if (attr_set.first(&dev)) {
-      const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
-      if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
-      attr_set.done(dev);
-    }
     // Rows of a window: as many as a group has on average if all groups occur, so that few windows have rows of several.  CTAs that share its
-    // columns: until there are two for every SM, while each warp has a chunk.
-    const int mean = P.a.rows / (P.a.G < P.a.rows ? P.a.G : P.a.rows);
-    P.window = mean < 2 ? 1 : mean < 4 ? 2 : mean < 8 ? 4 : mean < 16 ? 8 : mean < 32 || NT == 2 ? 16 : 8 * NT;
-    const int windows = (P.a.rows + P.window - 1) / P.window, sms = current_sm_count();
+    // columns: until there are two for every SM (four of the small ones), while each warp has a chunk.
+    const int mean = P.a.rows / (P.a.G < P.a.rows ? P.a.G : P.a.rows), sms = current_sm_count();
+    P.window = mean < 2 ? 1 : mean < 4 ? 2 : mean < 8 ? 4 : mean < 16 ? 8 : mean < 32 || MOST == 2 ? 16 : 8 * MOST;
+    const int windows = (P.a.rows + P.window - 1) / P.window;
     unsigned split = 1;
-    while (split < kDownSplit && (long long)windows * split < 2 * sms && (P.a.K + 31) / 32 > (long long)split * kDownWarps) split *= 2;
-    return adapter_launched(launch_overlapping(kern, dim3((unsigned)windows * split), dim3(32 * kDownWarps),
-                                               (size_t)kDownWarps * P.window * 16 * RT * 4, split, s, P));
+    while (split < kDownSplit && (long long)windows * split < (P.window <= 8 ? 3 : 2) * sms && (P.a.K + 31) / 32 > (long long)split * kDownWarps) split *= 2;
+    auto go = [&](auto nt) {
+      constexpr int NT = decltype(nt)::value, kMostSmem = kDownWarps * 8 * NT * 16 * RT * 4;
+      auto kern = adapters_down_kernel<X, W, RT, NT, TRANSPOSED>;
+      static PerDeviceFlag attr_set;
+      int dev;
+      if (attr_set.first(&dev)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
+        if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+        attr_set.done(dev);
+      }
+      return adapter_launched(launch_overlapping(kern, dim3((unsigned)windows * split), dim3(32 * kDownWarps),
+                                                 (size_t)kDownWarps * P.window * 16 * RT * 4, split, s, P));
+    };
+    return P.window <= 8 ? go(std::integral_constant<int, 1>{}) : go(std::integral_constant<int, MOST>{});
   });
 }
 

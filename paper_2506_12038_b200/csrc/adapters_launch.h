@@ -17,7 +17,9 @@ struct UpArgs {
   int32_t* status;
   int early;                   // the kernel before this one wrote t and nothing else that is read here, and began when all before it was done
 };
-lcd_status launch_adapters_up(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s);
+lcd_status launch_adapters_up_f32(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
+lcd_status launch_adapters_up_f16(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
+lcd_status launch_adapters_up_bf16(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
 
 // The same on tcgen05, where there are many rows and their pieces start on 16 bytes.
 // The parts of t that it needs, 0 where the other kernel runs.

@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(32 * kOuterWarps) adapters_outer_kernel(const 
           for (int q = 0; q < 4; ++q) {
             const float x = value_of(f.u[2 * s + q / 2], 2 * i + q % 2);
             a[i][q] = upper_tf32(x);
-            a_rest[i][q] = rest_of(x, a[i][q]);
+            a_rest[i][q] = rest_tf32(x, a[i][q]);
           }
 #pragma unroll
         for (int j = 0; j < CT; ++j) {
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(32 * kOuterWarps) adapters_outer_kernel(const 
           for (int q = 0; q < 2; ++q) {
             const float x = value_of(f.z[2 * s + q], j);
             b[q] = kIs16<Z> ? x : upper_tf32(x);
-            b_rest[q] = kIs16<Z> ? 0.0f : rest_of(x, b[q]);
+            b_rest[q] = kIs16<Z> ? 0.0f : rest_tf32(x, b[q]);
           }
 #pragma unroll
           for (int i = 0; i < RT; ++i) {

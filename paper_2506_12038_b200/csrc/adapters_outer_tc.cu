@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
     const int have = (int)max(0ll, min(8ll, E.columns - c));
     const uint32_t at_piece = (uint32_t)(piece / 8 * kStageRows * 128);
     const Z* z = static_cast<const Z*>(E.z) + c;
+    const bool inside = have >= 8 && c >= 16 / (int)sizeof(Z) && c + 8 + 16 / (int)sizeof(Z) <= E.columns;
     auto row_at = [&](int it, int i) {
       const int place = from + (k0 + it) * kStageRows + thread / 16 + 8 * i;
       return place < to ? P.order[place] : -1;
@@ -166,6 +167,17 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
     } else {
       Words<Z, 8> in[8];
       auto load = [&] {
+        if (!E.wide_z && inside) {
+#pragma unroll
+          for (int i0 = 0; i0 < 8; i0 += 4) {
+            Around<Z, 8> around[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_around(around[i], z + max(row[i0 + i], 0) * E.ldz, row[i0 + i] >= 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) shift_words(in[i0 + i], around[i], z + max(row[i0 + i], 0) * E.ldz);
+          }
+          return;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) load_words(in[i], z + (row[i] >= 0 ? row[i] * E.ldz : 0), row[i] >= 0 ? have : 0, E.wide_z && (have <= 0 || have >= 8));
       };

@@ -64,6 +64,16 @@ lcd_status down(const DownArgs& d, lcd_dtype x_type, lcd_dtype w_type, bool back
   }
 }
 
+lcd_status up(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type, bool transposed, void* stream) {
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (u.t_parts) return launch_adapters_up_tc(u, w_type, y_type, transposed, s);
+  switch (w_type) {
+    case LCD_DTYPE_F32: return launch_adapters_up_f32(u, y_type, transposed, s);
+    case LCD_DTYPE_F16: return launch_adapters_up_f16(u, y_type, transposed, s);
+    default: return launch_adapters_up_bf16(u, y_type, transposed, s);
+  }
+}
+
 }  // namespace
 
 }  // namespace lcd
@@ -149,7 +159,7 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   u.t_parts = d.t_parts = d.parts ? d.t + rows->count * padded_rank(weights->rank) : nullptr;
   st = down(d, x_type, weights->type, false, cuda_stream);
   if (st != LCD_OK) return st;
-  return launch_adapters_up(u, weights->type, y_type, false, static_cast<cudaStream_t>(cuda_stream));
+  return up(u, weights->type, y_type, false, cuda_stream);
 }
 
 extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, const void* dy, int64_t lddy, const void* x, int64_t ldx, lcd_dtype type,
@@ -195,7 +205,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
     if (st != LCD_OK) return st;
   }
   if (dx) {
-    st = launch_adapters_up(u, weights->type, type, true, s);
+    st = up(u, weights->type, type, true, cuda_stream);
     if (st != LCD_OK) return st;
   }
   if (!da && !db) return LCD_OK;
