@@ -170,6 +170,8 @@ __device__ __forceinline__ int row_of(const int32_t* order, int at, int rows) { 
 // RT for a rank: 16 * RT is the rank padded.
 constexpr int rank_tiles(int64_t r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }
 constexpr int kMostRank = 128;
+// From this many rows on the products run on tcgen05 (adapters_tc.cuh).
+constexpr int kManyRows = 512;
 
 template <typename F>
 lcd_status by_rank(int64_t r, F&& f) {

@@ -99,17 +99,22 @@ __global__ void __launch_bounds__(32 * kDownWarps, NT == 1 && RT * sizeof(W) <= 
     auto load = [&](Frag& f, int c) {
       const long long k = (long long)c * 32;
       const int have = (int)min((long long)8, P.a.K - k - 8 * t);
-      // chunks with another on either side: rows at any alignment in aligned words, four rows' loads at a time
-      const bool within = k >= 32 && k + 64 <= P.a.K;
-      if (!TRANSPOSED && !P.a.wide_w && within) {
+      // chunks with another on either side: rows at any alignment in aligned words, all rows' loads on their way together (of large ranks
+      // four rows' at a time)
+      const bool within = k >= 32 && k + 64 <= P.a.K, shift_w = !TRANSPOSED && !P.a.wide_w && within, shift_x = !P.a.wide_x && within;
+      constexpr int kBatch = kW <= 4 ? kW : 4;
+      Around<W, TRANSPOSED ? 2 * RT : 8> around_w[kBatch];
+      Around<X, 8> around_x[NT];
+      auto row_w = [&](int i) { return w + 8 * i * P.a.ldw + k; };
+      if (shift_w) {
 #pragma unroll
-        for (int i0 = 0; i0 < kW; i0 += 4) {
-          constexpr int kBatch = kW < 4 ? kW : 4;
-          Around<W, TRANSPOSED ? 2 * RT : 8> around[kBatch];
+        for (int i0 = 0; i0 < kW; i0 += kBatch) {
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) load_around(around[i], w + 8 * (i0 + i) * P.a.ldw + k, 8 * (i0 + i) + g < P.a.r);
+          for (int i = 0; i < kBatch; ++i) load_around(around_w[i], row_w(i0 + i), 8 * (i0 + i) + g < P.a.r);
+          if (kW > kBatch) {
 #pragma unroll
-          for (int i = 0; i < kBatch; ++i) shift_words(f.w[i0 + i], around[i], w + 8 * (i0 + i) * P.a.ldw + k);
+            for (int i = 0; i < kBatch; ++i) shift_words(f.w[i0 + i], around_w[i], row_w(i0 + i));
+          }
         }
       } else {
 #pragma unroll
@@ -118,22 +123,25 @@ __global__ void __launch_bounds__(32 * kDownWarps, NT == 1 && RT * sizeof(W) <= 
             const int ranks = min(2 * RT, P.a.r - g * 2 * RT);
             load_words(f.w[i], w + (k + i) * P.a.ldw, i < have ? ranks : 0, P.a.wide_w && (ranks <= 0 || ranks >= 2 * RT));
           } else {
-            load_words(f.w[i], w + 8 * i * P.a.ldw + k, 8 * i + g < P.a.r ? have : 0, P.a.wide_w && (have <= 0 || have >= 8));
+            load_words(f.w[i], row_w(i), 8 * i + g < P.a.r ? have : 0, P.a.wide_w && (have <= 0 || have >= 8));
           }
         }
       }
-      if (!P.a.wide_x && within) {
-        Around<X, 8> around[NT];
+      if (shift_x) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          if (8 * n < i1 && 8 * n + 8 > i0) load_around(around[n], xrow[n] + k, mine[n]);
+          if (8 * n < i1 && 8 * n + 8 > i0) load_around(around_x[n], xrow[n] + k, mine[n]);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
-          if (8 * n < i1 && 8 * n + 8 > i0) shift_words(f.x[n], around[n], xrow[n] + k);
+          if (8 * n < i1 && 8 * n + 8 > i0) shift_words(f.x[n], around_x[n], xrow[n] + k);
       } else {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
           if (8 * n < i1 && 8 * n + 8 > i0) load_words(f.x[n], xrow[n] + k, mine[n] ? have : 0, P.a.wide_x && (have <= 0 || have >= 8));
+      }
+      if (shift_w && kW <= kBatch) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) shift_words(f.w[i], around_w[i], row_w(i));
       }
     };
     // value e (column 8 t + e of the chunk) of the lane's rank q: row 8 q + g, or g * 2 RT + q

@@ -27,7 +27,8 @@ struct Shape {
   static_assert(128 * kPitch * 4 <= kStages * kStage && kSmem <= 227 * 1024, "sums lie in the stages");
 };
 
-template <typename X, int R, bool TRANSPOSED>
+// COPIED: rows of x and of the adapter matrix start on 16 bytes.
+template <typename X, int R, bool TRANSPOSED, bool COPIED>
 __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const DownArgs P) {
   using S = Shape<R, TRANSPOSED>;
   extern __shared__ uint8_t smem_raw[];
@@ -100,7 +101,55 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
       bar_arrive(full(it % S::kStages));
     };
     constexpr int kBehind = S::kStages - 1;               // stages on their way before the first of them is handed over
-    for (int k = k0; k < k1 && ok; ++k) {
+    // Rows that do not start on 16 bytes: through registers, a stage at a time.
+    for (int k = k0; k < k1 && ok && !COPIED; ++k) {
+      const int it = k - k0, s = it % S::kStages;
+      const long long c = (long long)k * 64 + piece * 8;
+      const int have = (int)max(0ll, min(8ll, P.a.K - c));
+      const bool within = c >= 8 && c + 16 <= P.a.K;
+      const uint32_t to_x = base + s * S::kStage, to_w = to_x + S::kX;
+      bool free = false;
+#pragma unroll
+      for (int i0 = 0; i0 < 8; i0 += 4) {
+        Words<X, 8> in[4];
+        if (within && !P.a.wide_x) {
+          Around<X, 8> around[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load_around(around[i], x[i0 + i] ? x[i0 + i] + c : static_cast<const X*>(P.x), x[i0 + i] != nullptr);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) shift_words(in[i], around[i], x[i0 + i] + c);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load_words(in[i], x[i0 + i] + c, x[i0 + i] ? have : 0, P.a.wide_x && (have <= 0 || have >= 8));
+        }
+        if (!free) ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
+        free = true;
+        if (!ok) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store16(to_x + piece_at(thread / 8 + 16 * (i0 + i), piece), make_uint4(in[i].w[0], in[i].w[1], in[i].w[2], in[i].w[3]));
+      }
+      if (!ok) break;
+      constexpr int kRowsW = TRANSPOSED ? (R + 63) / 64 * 64 : R, kPieces = TRANSPOSED && R < 64 ? R / 8 : 8;
+#pragma unroll 4
+      for (int u = thread; u < kRowsW * kPieces; u += kCopyThreads) {
+        const int p = u % kPieces, row = u / kPieces % (TRANSPOSED ? 64 : R), block = TRANSPOSED ? u / kPieces / 64 : 0;
+        const long long at_row = TRANSPOSED ? (long long)k * 64 + row : row, at = TRANSPOSED ? block * 64 + p * 8 : (long long)k * 64 + p * 8;
+        const long long rows = TRANSPOSED ? P.a.K : P.a.r, columns = TRANSPOSED ? P.a.r : P.a.K;
+        const int there = at_row < rows ? (int)max(0ll, min(8ll, columns - at)) : 0;
+        const X* from = w + at_row * P.a.ldw + at;
+        Words<X, 8> in;
+        if (!P.a.wide_w && there == 8 && at >= 8 && at + 16 <= columns) {
+          Around<X, 8> around;
+          load_around(around, from, true);
+          shift_words(in, around, from);
+        } else {
+          load_words(in, from, there, P.a.wide_w && (there <= 0 || there >= 8));
+        }
+        store16(to_w + block * 64 * 128 + piece_at(row, p), make_uint4(in.w[0], in.w[1], in.w[2], in.w[3]));
+      }
+      arrive(it);
+    }
+    for (int k = k0; k < k1 && ok && COPIED; ++k) {
       const int it = k - k0, s = it % S::kStages;
       ok = bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag);
       if (!ok) break;
@@ -135,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
       }
     }
     copies_wait<0>();
-    if (ok)
+    if (ok && COPIED)
       for (int it = max(0, k1 - k0 - kBehind); it < k1 - k0; ++it) arrive(it);
     ok = __all_sync(0xffffffffu, ok && bar_wait(d_full, 0, abort_flag));
     after_sync();
@@ -194,10 +243,10 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
   if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
 }
 
-template <typename X, int R, bool TRANSPOSED>
+template <typename X, int R, bool TRANSPOSED, bool COPIED>
 lcd_status launch_shape(const DownArgs& P, cudaStream_t s) {
   using S = Shape<R, TRANSPOSED>;
-  auto kern = adapters_down_tc_kernel<X, R, TRANSPOSED>;
+  auto kern = adapters_down_tc_kernel<X, R, TRANSPOSED, COPIED>;
   static PerDeviceFlag attr_set;
   int dev;
   if (attr_set.first(&dev)) {
@@ -212,17 +261,21 @@ lcd_status launch_shape(const DownArgs& P, cudaStream_t s) {
 }
 
 template <typename X>
-lcd_status launch_type(const DownArgs& P, bool backward, cudaStream_t s) {
+lcd_status launch_type(DownArgs P, bool backward, cudaStream_t s) {
+  P.a.wide_x = on_bytes(P.x, P.ldx, 0, sizeof(X), 16);
+  P.a.wide_w = on_bytes(P.a.w, P.a.ldw, P.a.sw, sizeof(X), 16);
+  const bool copied = P.a.wide_x && P.a.wide_w;
   return by_rank(P.a.r, [&](auto rt) {
     constexpr int R = 16 * decltype(rt)::value;
-    return backward ? launch_shape<X, R, true>(P, s) : launch_shape<X, R, false>(P, s);
+    if (copied) return backward ? launch_shape<X, R, true, true>(P, s) : launch_shape<X, R, false, true>(P, s);
+    return backward ? launch_shape<X, R, true, false>(P, s) : launch_shape<X, R, false, false>(P, s);
   });
 }
 
 }  // namespace
 
 bool adapters_down_tc_takes(const DownArgs& P, lcd_dtype x_type, lcd_dtype w_type) {
-  return x_type == w_type && x_type != LCD_DTYPE_F32 && P.a.rows >= 512 && on_bytes(P.x, P.ldx, 0, 2, 16) && on_bytes(P.a.w, P.a.ldw, P.a.sw, 2, 16);
+  return x_type == w_type && x_type != LCD_DTYPE_F32 && P.a.rows >= kManyRows;
 }
 
 lcd_status launch_adapters_down_tc(const DownArgs& P, lcd_dtype type, bool backward, cudaStream_t s) {

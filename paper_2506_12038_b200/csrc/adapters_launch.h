@@ -21,10 +21,10 @@ lcd_status launch_adapters_up_f32(const UpArgs& P, lcd_dtype y_type, bool transp
 lcd_status launch_adapters_up_f16(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
 lcd_status launch_adapters_up_bf16(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
 
-// The same on tcgen05, where there are many rows and their pieces start on 16 bytes.
-// The parts of t that it needs, 0 where the other kernel runs.
-int adapters_up_tc_parts(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type);
-lcd_status launch_adapters_up_tc(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s);
+// The same on tcgen05, for many rows, from t_parts.
+lcd_status launch_adapters_up_tc_f32(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
+lcd_status launch_adapters_up_tc_f16(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
+lcd_status launch_adapters_up_tc_bf16(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s);
 
 struct DownArgs;
 lcd_status launch_adapters_down_f32(const DownArgs& P, lcd_dtype w_type, bool backward, cudaStream_t s);

@@ -1,11 +1,12 @@
 // adapters_outer.cu's gradients for many rows: da = sum over an adapter's rows of dt^T x, db = s sum of dy^T t.
 //
 // A tile is 128 columns of z (x or dy) by the whole rank of one adapter; the sum runs over its rows, 64 a stage, so both operands are
-// MN-major as they lie.  Rows of z follow the plan through 16-byte copies (bf16 as it is; fp16 and fp32 through registers, in two or three bf16
-// parts), those of t or dt are split into parts on their way.  A cluster's CTAs share an adapter's rows where there are few tiles and
+// MN-major as they lie.  Rows of z follow the plan through 16-byte copies (bf16 as it is where rows start on 16 bytes; else, and fp16 and fp32, through
+// registers, in one to three bf16 parts), those of t or dt are split into parts on their way.  A cluster's CTAs share an adapter's rows where there are few tiles and
 // add their sums up in distributed shared memory, in the order of the ranks.  Reading z bounds it.
-// Roles (9 warps, 13 at ranks above 32): warps 0-3 bring z, then read the sums from tensor memory; the last one owns tensor memory, one elected
-// lane issues the MMAs; those between bring t or dt, each (or a pair) every fourth stage, so that its loads have four stages' time.
+// Roles (8 to 13 warps): warps 0-3 bring z, then read the sums from tensor memory; the last one owns tensor memory, one elected lane issues
+// the MMAs; those between bring t or dt, one of them (two at ranks above 32) for every stage's place, so that its loads have the time of
+// all stages.
 #include "adapters_launch.h"
 #include "adapters_tc.cuh"
 
@@ -24,8 +25,10 @@ struct Shape {
   static constexpr int kStage = kParts_z * kZPart + kParts_u * kUPart;
   // two CTAs an SM where they have three stages each
   static constexpr int kStages = 4 * kStage <= 110 * 1024 ? 4 : 3 * kStage <= 110 * 1024 ? 3 : 4 * kStage <= 220 * 1024 ? 4 : 3;
-  static constexpr int kPer = R == 64 ? 2 : 1;                                    // warps that bring a stage of t
-  static constexpr int kMmaWarp = 4 + 4 * kPer, kThreads = 32 * (kMmaWarp + 1);
+  // Warps that bring a stage of t.  A stage's place belongs to the same ones every time: a wait for a parity passes two phases early, so whoever
+  // fills a place has to have filled it the time before.
+  static constexpr int kPer = R == 64 ? 2 : 1;
+  static constexpr int kMmaWarp = 4 + kStages * kPer, kThreads = 32 * (kMmaWarp + 1);
   static constexpr int kPitch = R + 4;                                            // of the sums, fp32
   static constexpr int kSmem = 1024 + kStages * kStage + 128;
   static constexpr int kTmem = R < 32 ? 32 : R;
@@ -140,7 +143,7 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
         then[i] = it + 2 < n ? row_at(it + 2, i) : -1;
       }
     };
-    if constexpr (kCopied) {
+    if (kCopied && E.wide_z) {
       constexpr int kBehind = S::kStages - 1;
       for (int it = 0; it < n && ok; ++it) {
         const int s = it % S::kStages;
@@ -242,9 +245,9 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
     };
     find(mine);
     load();
-    find(mine + 4);
-    for (int it = mine; it < n && ok; it += 4) {
-      const int s = it % S::kStages;
+    find(mine + S::kStages);
+    for (int it = mine; it < n && ok; it += S::kStages) {
+      const int s = mine;
       ok = __all_sync(0xffffffffu, bar_wait(empty(s), ((it / S::kStages) & 1u) ^ 1u, abort_flag));
       if (!ok) break;
       const uint32_t to_u = base + s * S::kStage + S::kParts_z * S::kZPart;
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, Shape<Z, O, R>::kPer
       fence_async();
       bar_arrive(full(s));
       load();
-      find(it + 8);
+      find(it + 2 * S::kStages);
     }
   }
   if (split > 1) {
@@ -327,10 +330,9 @@ lcd_status launch_shape(OuterArgs P, cudaStream_t s) {
 bool adapters_outer_tc_takes(const OuterArgs& P, lcd_dtype z_type) {
   long long slabs = 0;
   for (int i = 0; i < P.sides; ++i) {
-    if (z_type == LCD_DTYPE_BF16 && !on_bytes(P.side[i].z, P.side[i].ldz, 0, 2, 16)) return false;
     slabs += (P.side[i].columns + 127) / 128;
   }
-  return P.rows >= 512 && P.r <= 64 && slabs <= 0x7fffffff / kOuterSplit;
+  return P.rows >= kManyRows && P.r <= 64 && slabs <= 0x7fffffff / kOuterSplit;
 }
 
 lcd_status launch_adapters_outer_tc(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s) {

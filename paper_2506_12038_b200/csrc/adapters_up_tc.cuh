@@ -9,6 +9,9 @@
 // changes, the adapter matrix, split into bf16 parts; warps 9-16 add: a thread has a row and half of the columns, reads the base's from
 // shared memory (rows 16 bytes longer than their columns: no bank conflicts) and stores 32 bytes at a time, whole sectors.
 // Two tiles are in flight: while one is added up, the next one's base comes in.
+#ifndef LCD_ADAPTERS_UP_TC_CUH_
+#define LCD_ADAPTERS_UP_TC_CUH_
+
 #include "adapters_launch.h"
 #include "adapters_tc.cuh"
 
@@ -37,7 +40,8 @@ struct Shape {
   static_assert(kSmem <= kMostSmem && kPerSm * kTmem <= 512, "shared and tensor memory");
 };
 
-template <typename W, typename Y, int R, bool TRANSPOSED>
+// WIDE: rows of base and y start on 16 bytes and end on them.
+template <typename W, typename Y, int R, bool TRANSPOSED, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArgs P) {
   using S = Shape<W, Y, R, TRANSPOSED>;
   constexpr int NC = S::kNC;
@@ -105,6 +109,34 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
         ok = __all_sync(0xffffffffu, bar_wait(y_empty(b), ((it >> 1) & 1u) ^ 1u, abort_flag));
         if (!ok) break;
         const uint32_t to = at_y + (b * 128 + 32 * warp + lane / kPieces) * S::kPitch + piece * 16;
+        if (!WIDE) {                             // rows that do not start on 16 bytes: through registers
+          constexpr int kOwn = 16 / (int)sizeof(Y);
+          const long long c = c0 + piece * kOwn;
+          const int have = (int)max(0ll, min((long long)kOwn, P.a.K - c));
+          const bool within = c >= kOwn && c + 2 * kOwn <= P.a.K;
+          constexpr int kBatch = 32 / kRowsEach < 8 ? 32 / kRowsEach : 8;
+#pragma unroll 1
+          for (int i0 = 0; i0 < 32; i0 += kBatch * kRowsEach) {
+            Words<Y, kOwn> in[kBatch];
+            int r[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) r[i] = __shfl_sync(0xffffffffu, row, i0 + i * kRowsEach + lane / kPieces);
+            if (within && !P.wide_base) {
+              Around<Y, kOwn> around[kBatch];
+#pragma unroll
+              for (int i = 0; i < kBatch; ++i) load_around(around[i], from + max(r[i], 0) * P.ldbase, r[i] >= 0);
+#pragma unroll
+              for (int i = 0; i < kBatch; ++i) shift_words(in[i], around[i], from + max(r[i], 0) * P.ldbase);
+            } else {
+#pragma unroll
+              for (int i = 0; i < kBatch; ++i) load_words(in[i], from + max(r[i], 0) * P.ldbase, r[i] >= 0 ? have : 0, P.wide_base && (have <= 0 || have >= kOwn));
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) store16(to + (i0 + i * kRowsEach) * S::kPitch, make_uint4(in[i].w[0], in[i].w[1], in[i].w[2], in[i].w[3]));
+          }
+          bar_arrive(y_full(b));
+          continue;
+        }
 #pragma unroll 8
         for (int i = 0; i < 32; i += kRowsEach) {
           const int r = __shfl_sync(0xffffffffu, row, i + lane / kPieces);
@@ -267,11 +299,12 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
       const bool real = q.group < G;
       const uint32_t b = it & 1u, db = dt & 1u;
       look(tile + 1);
+      // (without base the buffers are this warp's own)
       if (P.base) ok = __all_sync(0xffffffffu, bar_wait(y_full(b), (it >> 1) & 1u, abort_flag));
       if (ok && real) ok = __all_sync(0xffffffffu, bar_wait(d_full(db), (dt >> 1) & 1u, abort_flag));
       if (!ok) break;
       after_sync();
-      const Y* own = reinterpret_cast<const Y*>(gen + at_y + (b * 128 + mine) * S::kPitch) + half * kHalf;
+      Y* own = reinterpret_cast<Y*>(gen + at_y + (b * 128 + mine) * S::kPitch) + half * kHalf;
       Y* y = static_cast<Y*>(P.y) + max(to_row, 0) * P.ldy + c0;
       const uint32_t from = tmem + ((uint32_t)(32 * quad) << 16) + db * NC + half * kHalf;
       uint32_t d[2][16];
@@ -297,13 +330,35 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = __fmaf_rn(s, __uint_as_float(d[(c / 16) & 1][i]), v[i]);
         }
+        if (!WIDE) {                                          // the sums go where the base was
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float part[8] = {v[8 * h], v[8 * h + 1], v[8 * h + 2], v[8 * h + 3], v[8 * h + 4], v[8 * h + 5], v[8 * h + 6], v[8 * h + 7]};
+            store8(own + c + 8 * h, part);
+          }
+          continue;
+        }
         if (to_row < 0 || c >= columns) continue;
         if (c + 16 <= columns) {
-          store16_values(y + c, v, P.wide_y);
-        } else {                                              // the row ends after four or eight, or twelve
+          store16_values(y + c, v, P.wide_y > 16);
+        } else {                                              // the row ends after four, eight or twelve
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             if (c + i < columns) y[c + i] = from_f32<Y>(v[i]);
+        }
+      }
+      if (!WIDE) {                                            // rows that do not start on 16 bytes: value by value, neighbours side by side
+        __syncwarp();
+        const Y* rows = reinterpret_cast<const Y*>(gen + at_y + (b * 128 + 32 * quad) * S::kPitch) + half * kHalf;
+#pragma unroll 4
+        for (int i = 0; i < 32; ++i) {
+          const int r = __shfl_sync(0xffffffffu, to_row, i);
+          if (r < 0) continue;
+          Y* to = static_cast<Y*>(P.y) + r * P.ldy + c0;
+          const Y* from_row = rows + i * (S::kPitch / (int)sizeof(Y));
+#pragma unroll
+          for (int c = lane; c < kHalf; c += 32)
+            if (c < columns) to[c] = from_row[c];
         }
       }
       before_sync();
@@ -324,10 +379,10 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
   if (threadIdx.x == 0 && *abort_flag && P.status) *P.status = LCD_ERR_TIMEOUT;
 }
 
-template <typename W, typename Y, int R, bool TRANSPOSED>
-lcd_status launch_shape(UpArgs P, cudaStream_t s) {
+template <typename W, typename Y, int R, bool TRANSPOSED, bool WIDE>
+lcd_status launch_shape(const UpArgs& P, cudaStream_t s) {
   using S = Shape<W, Y, R, TRANSPOSED>;
-  auto kern = adapters_up_tc_kernel<W, Y, R, TRANSPOSED>;
+  auto kern = adapters_up_tc_kernel<W, Y, R, TRANSPOSED, WIDE>;
   static PerDeviceFlag attr_set;
   int dev;
   if (attr_set.first(&dev)) {
@@ -335,36 +390,34 @@ lcd_status launch_shape(UpArgs P, cudaStream_t s) {
     if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
     attr_set.done(dev);
   }
-  P.a.wide_w = on_bytes(P.a.w, P.a.ldw, P.a.sw, sizeof(W), 16);
-  P.wide_y = on_bytes(P.y, P.ldy, 0, sizeof(Y), 32);
   const long long most = ((long long)P.a.rows / kPlaces + (P.a.G + 1 < P.a.rows ? P.a.G + 1 : P.a.rows)) * ((P.a.K + S::kNC - 1) / S::kNC);
   const long long room = (long long)current_sm_count() * S::kPerSm;
   return adapter_launched(launch_overlapping(kern, dim3((unsigned)(most < room ? most : room)), dim3(kThreads), S::kSmem, 1, s, P));
 }
 
-}  // namespace
-
-int adapters_up_tc_parts(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type) {
-  const int64_t size = y_type == LCD_DTYPE_F32 ? 4 : 2;
-  if (P.a.rows < 512 || ((long long)P.a.rows / kPlaces + P.a.G + 1) * ((P.a.K + 63) / 64) > 0x7fffffff) return 0;
-  if (!on_bytes(P.y, P.ldy, P.a.K, size, 16) || (P.base && !on_bytes(P.base, P.ldbase, 0, size, 16))) return 0;
-  if (P.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return 0;      // the parts do not fit
-  return w_type == LCD_DTYPE_BF16 && y_type == LCD_DTYPE_BF16 ? 2 : 3;
+template <typename W, typename Y, bool TRANSPOSED>
+lcd_status launch_up_tc_types(UpArgs P, cudaStream_t s) {
+  P.a.wide_w = on_bytes(P.a.w, P.a.ldw, P.a.sw, sizeof(W), 16);
+  P.wide_base = on_bytes(P.base, P.ldbase, P.a.K, sizeof(Y), 16);
+  P.wide_y = on_bytes(P.y, P.ldy, P.a.K, sizeof(Y), 16) ? on_bytes(P.y, P.ldy, 0, sizeof(Y), 32) ? 32 : 16 : 0;
+  const bool wide = P.wide_base && P.wide_y;
+  return by_rank(P.a.r, [&](auto rt) {
+    constexpr int R = 16 * decltype(rt)::value;
+    if constexpr (R <= 64 || (std::is_same<W, __nv_bfloat16>::value && sizeof(Y) == 2))
+      return wide ? launch_shape<W, Y, R, TRANSPOSED, true>(P, s) : launch_shape<W, Y, R, TRANSPOSED, false>(P, s);
+    return (lcd_status)LCD_ERR_UNSUPPORTED;
+  });
 }
 
-lcd_status launch_adapters_up_tc(const UpArgs& P, lcd_dtype w_type, lcd_dtype y_type, bool transposed, cudaStream_t s) {
-  return by_dtype(w_type, [&](auto w) {
-    return by_dtype(y_type, [&](auto y) {
-      using W = typename decltype(w)::type;
-      using Y = typename decltype(y)::type;
-      return by_rank(P.a.r, [&](auto rt) {
-        constexpr int R = 16 * decltype(rt)::value;
-        if constexpr (R <= 64 || (std::is_same<W, __nv_bfloat16>::value && sizeof(Y) == 2))
-          return transposed ? launch_shape<W, Y, R, true>(P, s) : launch_shape<W, Y, R, false>(P, s);
-        return (lcd_status)LCD_ERR_UNSUPPORTED;
-      });
-    });
+}  // namespace
+
+template <typename W>
+lcd_status launch_up_tc_weights(const UpArgs& P, lcd_dtype y_type, bool transposed, cudaStream_t s) {
+  return by_dtype(y_type, [&](auto y) {
+    using Y = typename decltype(y)::type;
+    return transposed ? launch_up_tc_types<W, Y, true>(P, s) : launch_up_tc_types<W, Y, false>(P, s);
   });
 }
 
 }  // namespace lcd
+#endif

@@ -66,12 +66,18 @@ lcd_status down(const DownArgs& d, lcd_dtype x_type, lcd_dtype w_type, bool back
 
 lcd_status up(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type, bool transposed, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (u.t_parts) return launch_adapters_up_tc(u, w_type, y_type, transposed, s);
+  const bool tc = u.t_parts != nullptr;
   switch (w_type) {
-    case LCD_DTYPE_F32: return launch_adapters_up_f32(u, y_type, transposed, s);
-    case LCD_DTYPE_F16: return launch_adapters_up_f16(u, y_type, transposed, s);
-    default: return launch_adapters_up_bf16(u, y_type, transposed, s);
+    case LCD_DTYPE_F32: return tc ? launch_adapters_up_tc_f32(u, y_type, transposed, s) : launch_adapters_up_f32(u, y_type, transposed, s);
+    case LCD_DTYPE_F16: return tc ? launch_adapters_up_tc_f16(u, y_type, transposed, s) : launch_adapters_up_f16(u, y_type, transposed, s);
+    default: return tc ? launch_adapters_up_tc_bf16(u, y_type, transposed, s) : launch_adapters_up_bf16(u, y_type, transposed, s);
   }
+}
+// The bf16 parts of t that the products for many rows need, 0 where the others run.
+int parts_of_t(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type) {
+  if (u.a.rows < kManyRows || ((int64_t)u.a.rows / 128 + u.a.G + 1) * ((u.a.K + 63) / 64) > 0x7fffffff) return 0;
+  if (u.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return 0;      // the parts do not fit into shared memory
+  return w_type == LCD_DTYPE_BF16 && y_type == LCD_DTYPE_BF16 ? 2 : 3;
 }
 
 }  // namespace
@@ -121,7 +127,7 @@ extern "C" lcd_status lcd_adapters_workspace_bytes(int64_t count, int64_t rank, 
   if (!bytes || !counted(count) || rank < 1) return LCD_ERR_INVALID_ARG;
   if (rank > kMostRank) return LCD_ERR_UNSUPPORTED;
   // t or dt, and for many rows its bf16 parts
-  *bytes = (size_t)count * (size_t)padded_rank(rank) * (count >= 512 ? 10 : 4);
+  *bytes = (size_t)count * (size_t)padded_rank(rank) * (count >= kManyRows ? 10 : 4);
   return LCD_OK;
 }
 
@@ -155,7 +161,7 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   u.ldy = ldy;
   u.early = 1;
   u.status = status_word_dev;
-  d.parts = adapters_up_tc_parts(u, weights->type, y_type);
+  d.parts = parts_of_t(u, weights->type, y_type);
   u.t_parts = d.t_parts = d.parts ? d.t + rows->count * padded_rank(weights->rank) : nullptr;
   st = down(d, x_type, weights->type, false, cuda_stream);
   if (st != LCD_OK) return st;
@@ -199,7 +205,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
     d.ldx = lddy;
     d.t = dt;
     d.status = status_word_dev;
-    d.parts = dx ? adapters_up_tc_parts(u, weights->type, type) : 0;
+    d.parts = dx ? parts_of_t(u, weights->type, type) : 0;
     u.t_parts = d.t_parts = d.parts ? dt + rows->count * padded_rank(weights->rank) : nullptr;
     st = down(d, type, weights->type, true, cuda_stream);
     if (st != LCD_OK) return st;

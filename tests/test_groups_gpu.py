@@ -264,7 +264,8 @@ def test_adapters_ragged(sizes):
         check_adapters(make_adapters(3, len(group), len(sizes), 20, 130, 150, "fp16", "fp16", "fp32", group=group, scale=False), ("fp16",))
 
 
-MANY = [(512, 1, 16, 96, 64), (700, 3, 8, 96, 264), (1500, 9, 33, 64, 128), (513, 2, 64, 64, 520), (640, 4, 128, 64, 200), (600, 700, 12, 32, 48)]
+MANY = [(512, 1, 16, 96, 64), (700, 3, 8, 96, 264), (1500, 9, 33, 64, 128), (513, 2, 64, 64, 520), (640, 4, 128, 64, 200), (600, 700, 12, 32, 48), (600, 5, 12, 333, 131),
+        (512, 1, 64, 130, 259), (777, 3, 128, 201, 1001), (530, 2, 31, 1000, 1)]
 
 
 @pytest.mark.parametrize("x,w", PAIRS)
@@ -373,6 +374,18 @@ def test_grad_of_many_rows(x, w, M, G, r, K, N):
     check_grad(c, x, (x, w), status_word=word, grad_dtype=torch.float32, base=False)
     whole = make_adapters(M + r, M, G, r, N, K, x, w, whole=True, pitch=8)
     check_grad(whole, x, whole=True, exact=x == "fp32", grad_dtype=torch.float32, types=(x, w), status_word=word)
+    assert word.item() == 0
+
+
+@pytest.mark.parametrize("x,w", PAIRS)
+@pytest.mark.parametrize("M,G,r,K,N", [(3000, 1, 16, 64, 72), (2500, 2, 40, 136, 64), (2100, 1, 8, 63, 65)])
+def test_grad_of_long_groups(x, w, M, G, r, K, N):
+    # a sum over more rows than the stages in flight hold, several times around them; rows of one group against sums in whole numbers
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    whole = make_adapters(M + r, M, G, r, K, N, x, w, whole=True)
+    whole["scale"] = None
+    check_grad(whole, x, whole=True, exact=x == "fp32", grad_dtype=torch.float32, types=(x, w), status_word=word)
+    check_grad(make_adapters(M + r, M, G, r, K, N, x, w), x, (x, w), status_word=word)
     assert word.item() == 0
 
 
