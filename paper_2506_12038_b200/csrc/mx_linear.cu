@@ -3,13 +3,13 @@
 // 128 weight rows by BN tokens over 64 columns, codes from shared memory, scales from tensor memory, sums in fp32.  So there
 // is no decoding, and few tokens (weights from HBM) and many (tensor pipe) are one kernel with token tiles of different width.
 //
-// Roles (11 warps; 15 with tiles of 256 tokens):
+// Roles (11 warps; 15 with tiles of 256 tokens; grouped, of 128 or more):
 //   warp 0      TMA producer of codes: stages of 256 columns, 128-byte swizzle
 //   warp 10     TMA producer of scales: 512 columns (16 bytes a row) at a time
 //   warps 2-5   scales to tensor memory: the unit reads row r's four scale bytes of 128 columns at lane r % 32, column r / 32, in
 //               every quarter of the lanes, so each of the four warps stores all rows' words into its own quarter
 //   warp 1      owns tensor memory; one elected lane issues the MMAs
-//   warps 6-9, 11-14  epilogue: tensor memory -> y, coalesced along the weight rows; up to four tokens come as they are, then these warps
+//   warps 6-9, 11-    epilogue: tensor memory -> y, coalesced along the weight rows; up to four tokens come as they are, then these warps
 //               quantise them into the stages first
 // Many tokens take pairs of CTAs (mx_pair_kernel below).
 // Products grouped by expert (lcd_mx_linear_grouped) are the same kernel with another list of tiles: the tokens' codes lie sorted by
@@ -53,11 +53,16 @@ struct Cfg {
   static constexpr int kUsed = kDBuffers * BN + kSfSlots * kSfCols;
   static constexpr int kTmemCols = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
   static constexpr int kPerSm = BN <= 64 ? 2 : 1;
-  static constexpr int kEpiHalves = kDBuffers == 1 || (GROUPED && BN == 192) ? 2 : 1;   // the one accumulator is drained by twice the warps
+  // Parts of the columns that are drained by warps of their own: two where there is one accumulator; grouped, where a tile's rows are scattered
+  // and its columns often few, always (three of 64 columns with tiles of 192 were slower).
+  // Grouped, the tokens of wide tiles come in boxes of 64 rows, as many as the tile has tokens for, and the MMAs are as wide: the loads from
+  // L2 bound prompts (a tile of 192 tokens reads 320 rows of codes), and an expert's last tile is often half empty.
+  static constexpr int kBox = GROUPED && BN >= 128 ? 64 : BN;
+  static constexpr int kEpiParts = (GROUPED && BN >= 128) || kDBuffers == 1 ? 2 : 1, kEpiColumns = BN / kEpiParts;
   // grouped: the token tiles before every expert and where its tokens begin, and for every epilogue warp where its columns go
   static constexpr int kPlanBytes = 8 * (kMostExperts + 1), kPlacesBytes = 4 * BN * 8;
   static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 256 + (GROUPED ? kPlanBytes + kPlacesBytes : 0);
-  static constexpr int kThreads = 32 * (11 + 4 * (kEpiHalves - 1));
+  static constexpr int kThreads = 32 * (11 + 4 * (kEpiParts - 1));
   // Whatever shares an SM has tensor memory enough, so that no CTA of a cluster waits for columns while another CTA of it holds some:
   // two of the narrow tiles fit, and beside a wide one nothing does (shared memory).
   static_assert(kUsed <= kTmemCols && kTmemCols * kPerSm <= 512, "tensor memory");
@@ -376,7 +381,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     }
     for (int b = 0; b < 2; ++b) {
       bar_init(d_full(b), 1);
-      bar_init(d_empty(b), 4 * C::kEpiHalves);
+      bar_init(d_empty(b), 4 * C::kEpiParts);
     }
     bar_init(drain, 1);
     *abort_flag = 0;
@@ -431,20 +436,26 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       constexpr bool codes = decltype(of_codes)::value;
       constexpr int slots = codes ? C::kStages : kScaleSlots;
       const int from = codes ? ks0 : ss0, to = codes ? ks1 : ss1;
-      constexpr uint32_t bytes = codes ? kAStage + (kReady ? C::kBStage : 0) : kReady ? C::kScaleBytes : kRows * 16;
+      auto bytes_of = [&](const Spot& q) {
+        if (!codes) return (uint32_t)(kReady ? C::kScaleBytes : kRows * 16);
+        return (uint32_t)(kAStage + (!kReady ? 0 : C::kBox < BN ? (q.tokens + C::kBox - 1) / C::kBox * (C::kBox * kStageK / 2) : C::kBStage));
+      };
       auto full_of = [&](int s) { return codes ? full(s) : sc_full(s); };
       auto copy_w = [&](int s, int k, const Spot& q) {
         if (GROUPED) copy_tile_of(codes ? a_base + s * kAStage : s_base + s * C::kScaleBytes, codes ? &map_w : &map_ws, k * (codes ? kStageK / 2 : 16), q.n0, q.expert, full_of(s));
         else if (codes) copy_tile(a_base + s * kAStage, &map_w, k * (kStageK / 2), q.n0, full(s));
         else copy_tile(s_base + s * C::kScaleBytes, &map_ws, k * 16, q.n0, sc_full(s));
       };
-      auto copy_x = [&](int s, int k, int row) {
-        if (codes) copy_tile(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), row, full(s));
-        else copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, row, sc_full(s));
+      auto copy_x = [&](int s, int k, const Spot& q) {
+        if (!codes) copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, q.m0, sc_full(s));
+        else if (C::kBox == BN) copy_tile(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), q.m0, full(s));
+        else
+          for (int r = 0; r < q.tokens; r += C::kBox) copy_tile(b_base + s * C::kBStage + r * (kStageK / 2), &map_x, k * (kStageK / 2), q.m0 + r, full(s));
       };
       const int ahead = P.early && tile0 < n_tiles ? min(slots, to - from) : 0;
       if (ahead > 0) {
         const Spot q = tiles.at(tile0);
+        const uint32_t bytes = bytes_of(q);
         for (int i = 0; i < ahead; ++i) {
           bar_expect_tx(full_of(i), bytes);
           copy_w(i, from + i, q);
@@ -456,6 +467,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       bool ok = true;
       for (int tile = tile0; tile < n_tiles && ok; tile += tile_step) {
         const Spot q = tiles.at(tile);
+        const uint32_t bytes = bytes_of(q);
         for (int k = from; k < to; ++k, ++it) {
           if (it >= ahead) {
             ok = bar_wait(codes ? empty(s) : sc_empty(s), round, abort_flag);
@@ -463,7 +475,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             bar_expect_tx(full_of(s), bytes);
             copy_w(s, k, q);
           }
-          if (kReady) copy_x(s, k, q.m0);
+          if (kReady) copy_x(s, k, q);
           if (++s == slots) {
             s = 0;
             round ^= 1u;
@@ -481,11 +493,16 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     __syncwarp();
   } else if (warp == kMmaWarp) {
     if (elect()) {
-      constexpr uint32_t idesc[2] = {instr_desc(BN, 0), instr_desc(BN, 1)};
+      uint32_t idesc[2] = {instr_desc(BN, 0), instr_desc(BN, 1)};
       const uint64_t a_desc0 = smem_desc(a_base), b_desc0 = smem_desc(b_base);
       uint32_t it = 0, sit = 0, tl = 0;
       bool ok = true;
       for (int tile = tile0; tile < n_tiles && ok; tile += tile_step, ++tl) {
+        if (C::kBox < BN) {
+          const int width = (tiles.at(tile).tokens + C::kBox - 1) / C::kBox * C::kBox;
+          idesc[0] = instr_desc(width, 0);
+          idesc[1] = instr_desc(width, 1);
+        }
         const uint32_t buf = tl % C::kDBuffers;
         ok = bar_wait(d_empty(buf), ((tl / C::kDBuffers) & 1u) ^ 1u, abort_flag);
         if (!ok) break;
@@ -551,6 +568,20 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const uint32_t quarter = (uint32_t)(32 * quad) << 16;
     uint32_t tl = 0;
     bool ok = true;
+    // grouped: the next tile, and the rows of y that this warp's columns of it go to, asked for while this one is drained
+    Spot next = {};
+    int next_row[(C::kEpiColumns + 31) / 32];
+    auto look = [&](int tile) {
+      if (tile >= n_tiles) return;
+      next = tiles.at(tile);
+      const int begin = (warp > kScaleCopyWarp ? (warp - kScaleCopyWarp + 3) / 4 : 0) * C::kEpiColumns;
+#pragma unroll
+      for (int i = 0; i < C::kEpiColumns; i += 32) {
+        const int c = begin + i + lane;
+        next_row[i / 32] = i + lane < C::kEpiColumns && c < next.tokens && next.m0 + c < P.M ? P.order[next.m0 + c] : -1;
+      }
+    };
+    if constexpr (GROUPED) look(tile0);
     for (int tile = tile0; tile < n_tiles && ok; tile += tile_step, ++tl) {
       if constexpr (!kReady) {
         if (tl == 0) begin_after_previous();
@@ -622,23 +653,27 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         if (!ok) break;
       }
       const uint32_t buf = tl % C::kDBuffers;
-      const Spot q = tiles.at(tile);
+      const Spot q = GROUPED ? next : tiles.at(tile);
       const int n = q.n0 + 32 * quad + lane, m0 = q.m0, tokens = q.tokens;
-      const int half = warp > kScaleCopyWarp ? BN / 2 : 0;
-      long long* mine = places + (warp > kScaleCopyWarp ? warp - kFirstEpiWarp - 1 : warp - kFirstEpiWarp) * (BN / C::kEpiHalves);
+      const int part = warp > kScaleCopyWarp ? (warp - kScaleCopyWarp + 3) / 4 : 0, begin = part * C::kEpiColumns;
+      const int end = min(tokens, begin + C::kEpiColumns);
+      long long* mine = places + (4 * part + quad) * C::kEpiColumns;
       if constexpr (GROUPED) {
         __syncwarp();
-        for (int i = lane; i < BN / C::kEpiHalves; i += 32) {
-          const int row = half + i < tokens ? planned_row(P, m0 + half + i) : -1;
-          mine[i] = row < 0 ? -1 : row * P.ldy;
+#pragma unroll
+        for (int i = 0; i < C::kEpiColumns; i += 32) {
+          if (i + lane < C::kEpiColumns) {
+            const int row = next_row[i / 32];
+            mine[i + lane] = (unsigned)row < (unsigned)P.M ? row * P.ldy : -1;
+          }
         }
         __syncwarp();
+        look(tile + tile_step);
       }
       ok = __all_sync(0xffffffffu, bar_wait(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       const uint32_t from = tmem + quarter + buf * BN;
-      const int begin = half, end = C::kEpiHalves == 2 && !begin ? min(tokens, BN / 2) : tokens;
       if (split > 1) {            // every copy into the stages has landed and been read: they hold the partial sums
         float* part = reinterpret_cast<float*>(gen) + 32 * quad + lane;
         drain_columns<(BN > 64)>(from, begin, end, [&](int c, const uint32_t (&v)[16]) {
@@ -662,7 +697,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         for (long long i = (long long)max(P.offsets[P.G], 0) + blockIdx.x; i < P.M; i += gridDim.x) {
           const int r = planned_row(P, (int)i);
           if (r < 0) continue;
-          for (int n = thread; n < P.N; n += 128 * C::kEpiHalves) y[(size_t)r * P.ldy + n] = from_f32<T>(0.0f);
+          for (int n = thread; n < P.N; n += 128 * C::kEpiParts) y[(size_t)r * P.ldy + n] = from_f32<T>(0.0f);
         }
       });
     }
@@ -1178,7 +1213,7 @@ lcd_status launch_grouped(const MxGrouped& p, int split, int32_t* status, cudaSt
   CUtensorMap w, x, ws, xs;
   if (!encode_experts(&w, p.w_codes, blocks * 16, p.N, p.ldwc, p.G, p.dwc, kStageK / 2, true) ||
       !encode_experts(&ws, p.w_scales, blocks, p.N, p.ldws, p.G, p.dws, 16, false) ||
-      !encode_rows(&x, p.x_codes, blocks * 16, p.rows.count, p.ldxc, kStageK / 2, BN, true) ||
+      !encode_rows(&x, p.x_codes, blocks * 16, p.rows.count, p.ldxc, kStageK / 2, C::kBox, true) ||
       !encode_rows(&xs, p.x_scales, blocks, p.rows.count, p.ldxs, 16, BN, false)) {
     set_cuda_error((int)cudaErrorInvalidValue);
     return LCD_ERR_CUDA;
