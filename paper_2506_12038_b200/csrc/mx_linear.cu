@@ -90,14 +90,14 @@ struct Spot { int n0, m0, tokens, expert; };
 // The tiles in order: along the weight rows, a weight tile's token tiles one after the other; grouped, one expert after the other.
 // first: the token tiles before every expert, and of all; begins: where the experts' tokens begin (shared memory).  Tiles are asked for in
 // ascending order.
-template <int BN, bool GROUPED>
+template <int BN, bool GROUPED, int ROWS = kRows>
 struct Tiles {
   const Args& P;
   const int *first, *begins;
   int expert = 0;
   __device__ __forceinline__ Spot at(int tile) {
     if constexpr (GROUPED) {
-      const int nt = (P.N + kRows - 1) / kRows;
+      const int nt = (P.N + ROWS - 1) / ROWS;
       if (expert + 1 < P.G && first[expert + 1] * nt <= tile) {
         int high = P.G - 1;                      // the last expert that begins at this tile or before
         while (expert < high) {
@@ -108,10 +108,10 @@ struct Tiles {
       }
       const int local = tile - first[expert] * nt, mt = max(1, first[expert + 1] - first[expert]);
       const int m0 = begins[expert] + local % mt * BN;
-      return {local / mt * kRows, m0, min(BN, begins[expert + 1] - m0), expert};
+      return {local / mt * ROWS, m0, min(BN, begins[expert + 1] - m0), expert};
     } else {
       const int m0 = tile % P.n_tiles_m * BN;
-      return {tile / P.n_tiles_m * kRows, m0, min(BN, P.M - m0), 0};
+      return {tile / P.n_tiles_m * ROWS, m0, min(BN, P.M - m0), 0};
     }
   }
 };
@@ -324,6 +324,43 @@ __device__ __forceinline__ void columns8(const Args& P, int m, int k, const Raw8
   }
 }
 
+// The lists that Tiles takes, by one warp.  The plan was there when the kernel before this one began (P.early).
+template <int BN>
+__device__ __forceinline__ void make_tiles(const Args& P, int* first, int* begins, int lane) {
+      int sum = 0;
+      for (int e0 = 0; e0 < P.G; e0 += 32) {
+        const int e = e0 + lane;
+        int tiles = 0;
+        if (e < P.G) {
+          const int begin = min(max(P.offsets[e], 0), P.M), end = min(max(P.offsets[e + 1], begin), P.M);
+          tiles = (end - begin + BN - 1) / BN;
+          begins[e] = begin;
+          if (e == P.G - 1) begins[P.G] = end;
+        }
+        int upto = tiles;
+  #pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+          const int v = __shfl_up_sync(0xffffffffu, upto, d);
+          if (lane >= d) upto += v;
+        }
+        if (e < P.G) first[e] = sum + upto - tiles;
+        sum += __shfl_sync(0xffffffffu, upto, 31);
+      }
+      if (lane == 0) first[P.G] = sum;
+}
+
+// Rows of y without an expert become zeros, CTAs in turn.
+__device__ __forceinline__ void zero_rows(const Args& P, int thread, int threads) {
+  by_type(P, [&](auto* y) {
+    using T = std::remove_pointer_t<decltype(y)>;
+    for (long long i = (long long)max(P.offsets[P.G], 0) + blockIdx.x; i < P.M; i += gridDim.x) {
+      const int r = planned_row(P, (int)i);
+      if (r < 0) continue;
+      for (int n = thread; n < P.N; n += threads) y[(size_t)r * P.ldy + n] = from_f32<T>(0.0f);
+    }
+  });
+}
+
 // X: the type of x where the kernel quantises its tokens itself (few tokens), void where codes and scales come ready.  Then the
 // epilogue warps, which wait for the sums, take the stages in turn: a CTA needs its own columns of x only and blocks are complete in
 // them, so it can be done in every CTA, and a launch is saved (times: mx_linear_quantizes); from eight tokens on it takes longer than the
@@ -393,29 +430,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                  ::"r"((uint32_t)__cvta_generic_to_shared(tmem_holder)), "r"((uint32_t)C::kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (GROUPED && warp == 2) {
-    // The plan was there when the kernel before this one began (P.early).
-    int sum = 0;
-    for (int e0 = 0; e0 < P.G; e0 += 32) {
-      const int e = e0 + lane;
-      int tiles = 0;
-      if (e < P.G) {
-        const int begin = min(max(P.offsets[e], 0), P.M), end = min(max(P.offsets[e + 1], begin), P.M);
-        tiles = (end - begin + BN - 1) / BN;
-        begins[e] = begin;
-        if (e == P.G - 1) begins[P.G] = end;
-      }
-      int upto = tiles;
-#pragma unroll
-      for (int d = 1; d < 32; d *= 2) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += v;
-      }
-      if (e < P.G) first[e] = sum + upto - tiles;
-      sum += __shfl_sync(0xffffffffu, upto, 31);
-    }
-    if (lane == 0) first[P.G] = sum;
-  }
+  if (GROUPED && warp == 2) make_tiles<BN>(P, first, begins, lane);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -690,17 +705,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
       if (lane == 0) bar_arrive(d_empty(buf));
       __syncwarp();
     }
-    if constexpr (GROUPED) {           // rows without an expert: zeros
-      const int thread = (warp > kScaleCopyWarp ? warp - 1 : warp) * 32 + lane - 32 * kFirstEpiWarp;
-      by_type(P, [&](auto* y) {
-        using T = std::remove_pointer_t<decltype(y)>;
-        for (long long i = (long long)max(P.offsets[P.G], 0) + blockIdx.x; i < P.M; i += gridDim.x) {
-          const int r = planned_row(P, (int)i);
-          if (r < 0) continue;
-          for (int n = thread; n < P.N; n += 128 * C::kEpiParts) y[(size_t)r * P.ldy + n] = from_f32<T>(0.0f);
-        }
-      });
-    }
+    if constexpr (GROUPED) zero_rows(P, (warp > kScaleCopyWarp ? warp - 1 : warp) * 32 + lane - 32 * kFirstEpiWarp, 128 * C::kEpiParts);
   }
   if (split > 1) {
     // Token t of the tile is added up by rank t % split, a warp for 32 rows; the loads from all ranks are on their way together.
@@ -756,7 +761,7 @@ mx_linear_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 // writes and reads 16 KB + BN / 2 rows a stage where it alone would need BN rows: shared memory's bandwidth, what bounds
 // the kernel above, is enough (256 tokens: 128 bytes a clock).  Roles as above; the MMAs are issued by the pair's first CTA, and the
 // copies of both CTAs' codes complete on its barriers.  The tokens' scales are needed by both and lie in both CTAs' tensor memory.
-template <int BN>
+template <int BN, bool GROUPED = false>
 struct PairCfg {
   static constexpr int kBStage = BN / 2 * kStageK / 2;
   static constexpr int kStages = 6;
@@ -765,7 +770,9 @@ struct PairCfg {
   static constexpr int kDBuffers = 2 * BN + kSfSlots * kSfCols <= 512 ? 2 : 1;
   static constexpr int kEpiHalves = 2;
   static constexpr int kThreads = 32 * 15;
-  static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 512;
+  static constexpr int kBox = GROUPED ? 32 : BN / 2;              // grouped: rows of a CTA's half that are copied together, see Cfg
+  static constexpr int kPlanBytes = 8 * (kMostExperts + 1), kPlacesBytes = 4 * BN * 8;
+  static constexpr int kSmem = 1024 + kStages * (kAStage + kBStage) + kScaleSlots * kScaleBytes + 512 + (GROUPED ? kPlanBytes + kPlacesBytes : 0);
   static_assert(kDBuffers * BN + kSfSlots * kSfCols <= 512 && kSmem <= 227 * 1024 && kSmem > 128 * 1024, "one CTA an SM");
 };
 
@@ -815,11 +822,16 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
 
-template <int BN>
-__global__ void __launch_bounds__(PairCfg<BN>::kThreads, 1)
+__device__ __forceinline__ void copy_tile_pair_of(uint32_t dst, const CUtensorMap* map, int x, int row, int expert, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(row), "r"(expert), "r"(bar) : "memory");
+}
+
+template <int BN, bool GROUPED>
+__global__ void __launch_bounds__(PairCfg<BN, GROUPED>::kThreads, 1)
 mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_xs, const Args P) {
-  using C = PairCfg<BN>;
+  using C = PairCfg<BN, GROUPED>;
   extern __shared__ uint8_t smem_raw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw_addr = (uint32_t)__cvta_generic_to_shared(smem_raw);
@@ -842,7 +854,12 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   // stages that this CTA has asked for copies of; the other CTA's flag and number, which it sends at its end
   volatile int *asked = abort_flag + 1, *other_abort = abort_flag + 2, *other_asked = abort_flag + 3;
-  constexpr uint32_t kStageBytes = kAStage + C::kBStage;       // of one CTA
+  long long* places = reinterpret_cast<long long*>(gen + kBarAt + 512);              // grouped
+  int* first_tiles = reinterpret_cast<int*>(gen + kBarAt + 512 + C::kPlacesBytes);
+  int* begins = first_tiles + kMostExperts + 1;
+  // Tokens of a tile that a CTA brings, and so the bytes of a stage: grouped, as many boxes as the tile has tokens for.
+  auto half_of = [](const Spot& q) { return GROUPED ? (q.tokens + 2 * C::kBox - 1) / (2 * C::kBox) * C::kBox : BN / 2; };
+  auto stage_bytes = [&](const Spot& q) { return (uint32_t)(kAStage + half_of(q) * (kStageK / 2)); };
   uint32_t rank;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const bool first = rank == 0;
@@ -871,6 +888,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  if (GROUPED && warp == 2) make_tiles<BN>(P, first_tiles, begins, lane);
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;"
                  ::"r"((uint32_t)__cvta_generic_to_shared(tmem_holder)) : "memory");
@@ -883,6 +901,8 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_holder;
   const uint32_t sf_tmem = tmem + C::kDBuffers * BN;
+  const int n_tiles = GROUPED ? min(P.n_tiles, first_tiles[P.G] * ((P.N + 2 * kRows - 1) / (2 * kRows))) : P.n_tiles;
+  Tiles<BN, GROUPED, 2 * kRows> tiles{P, first_tiles, begins};
   if (warp != 0 && warp != kScaleCopyWarp) wait_for_previous();      // as above
 
   if (warp == 0 || warp == kScaleCopyWarp) {
@@ -893,37 +913,47 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
       // Codes: the first CTA's thread announces the bytes of both CTAs' copies (those of the other may have landed by then; its arrival is
       // what the phase waits for).  The other is never a phase ahead: it waits for the MMAs that read what it overwrites.
       const uint32_t full_first = in_cta(full(0), 0);
-      auto announce = [&](int s) {
+      auto announce = [&](int s, uint32_t bytes) {
         if (!codes) bar_expect_tx(sc_full(s), C::kScaleBytes);
-        else if (first) bar_expect_tx(full(s), 2 * kStageBytes);
+        else if (first) bar_expect_tx(full(s), 2 * bytes);
       };
-      auto copy_w = [&](int s, int k, int row) {
-        if (codes) copy_tile_pair(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full_first + 8u * s);
+      auto copy_w = [&](int s, int k, const Spot& q) {
+        const int row = q.n0 + (int)rank * kRows;
+        if (GROUPED && codes) copy_tile_pair_of(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, q.expert, full_first + 8u * s);
+        else if (GROUPED) copy_tile_of(s_base + s * C::kScaleBytes, &map_ws, k * 16, row, q.expert, sc_full(s));
+        else if (codes) copy_tile_pair(a_base + s * kAStage, &map_w, k * (kStageK / 2), row, full_first + 8u * s);
         else copy_tile(s_base + s * C::kScaleBytes, &map_ws, k * 16, row, sc_full(s));
       };
-      auto copy_x = [&](int s, int k, int row) {
-        if (codes) copy_tile_pair(b_base + s * C::kBStage, &map_x, k * (kStageK / 2), row + (int)rank * (BN / 2), full_first + 8u * s);
-        else copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, row, sc_full(s));
+      auto copy_x = [&](int s, int k, const Spot& q, int half) {
+        const int row = q.m0 + (int)rank * half;
+        if (!codes) copy_tile(s_base + s * C::kScaleBytes + kRows * 16, &map_xs, k * 16, q.m0, sc_full(s));
+        else
+          for (int r = 0; r < half; r += C::kBox)
+            copy_tile_pair(b_base + s * C::kBStage + r * (kStageK / 2), &map_x, k * (kStageK / 2), row + r, full_first + 8u * s);
       };
-      const int ahead = P.early && tile0 < P.n_tiles ? min(slots, to) : 0;
-      for (int i = 0; i < ahead; ++i) {
-        announce(i);
-        copy_w(i, i, tile0 / P.n_tiles_m * 2 * kRows + (int)rank * kRows);
+      const int ahead = P.early && tile0 < n_tiles ? min(slots, to) : 0;
+      if (ahead > 0) {
+        const Spot q = tiles.at(tile0);
+        for (int i = 0; i < ahead; ++i) {
+          announce(i, stage_bytes(q));
+          copy_w(i, i, q);
+        }
       }
       begin_after_previous();
       int it = 0, s = 0;
       uint32_t round = 1;          // the parity of a stage's barrier
       bool ok = true;
-      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step) {
-        const int n0 = tile / P.n_tiles_m * 2 * kRows + (int)rank * kRows, m0 = tile % P.n_tiles_m * BN;
+      for (int tile = tile0; tile < n_tiles && ok; tile += tile_step) {
+        const Spot q = tiles.at(tile);
+        const int half = half_of(q);
         for (int k = 0; k < to; ++k, ++it) {
           if (it >= ahead) {
             ok = codes ? bar_wait_cluster(empty(s), round, abort_flag) : bar_wait(sc_empty(s), round, abort_flag);
             if (!ok) break;
-            announce(s);
-            copy_w(s, k, n0);
+            announce(s, stage_bytes(q));
+            copy_w(s, k, q);
           }
-          copy_x(s, k, m0);
+          copy_x(s, k, q, half);
           if (++s == slots) {
             s = 0;
             round ^= 1u;
@@ -947,11 +977,16 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   } else if (warp == kMmaWarp) {
     if (first && elect()) {
       constexpr uint32_t kM = (uint32_t)(2 * kRows >> 4) << 24 ^ (uint32_t)(kRows >> 4) << 24;     // M = 256 in place of 128
-      constexpr uint32_t idesc[2] = {instr_desc(BN, 0) ^ kM, instr_desc(BN, 1) ^ kM};
+      uint32_t idesc[2] = {instr_desc(BN, 0) ^ kM, instr_desc(BN, 1) ^ kM};
       const uint64_t a_desc0 = smem_desc(a_base), b_desc0 = smem_desc(b_base);
       uint32_t it = 0, sit = 0, tl = 0;
       bool ok = true;
-      for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+      for (int tile = tile0; tile < n_tiles && ok; tile += tile_step, ++tl) {
+        if (GROUPED) {
+          const int width = 2 * half_of(tiles.at(tile));
+          idesc[0] = instr_desc(width, 0) ^ kM;
+          idesc[1] = instr_desc(width, 1) ^ kM;
+        }
         const uint32_t buf = tl % C::kDBuffers;
         ok = bar_wait_cluster(d_empty(buf), ((tl / C::kDBuffers) & 1u) ^ 1u, abort_flag);
         if (!ok) break;
@@ -990,7 +1025,7 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     const uint32_t quarter = (uint32_t)(32 * (warp & 3)) << 16;
     uint32_t sit = 0;
     bool ok = true;
-    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step)
+    for (int tile = tile0; tile < n_tiles && ok; tile += tile_step)
       for (int ss = 0; ss < P.n_ss; ++ss, ++sit) {
         const uint32_t slot = sit % kScaleSlots, sb = sit % C::kSfSlots;
         ok = __all_sync(0xffffffffu, bar_wait(sc_full(slot), (sit / kScaleSlots) & 1u, abort_flag) &&
@@ -1013,22 +1048,47 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
   } else {
     const int quad = warp & 3;
     const uint32_t quarter = (uint32_t)(32 * quad) << 16;
-    const int begin = warp > kScaleCopyWarp ? BN / 2 : 0;
+    const int part = warp > kScaleCopyWarp;
+    long long* mine = places + (4 * part + quad) * (BN / 2);
     uint32_t tl = 0;
     bool ok = true;
-    for (int tile = tile0; tile < P.n_tiles && ok; tile += tile_step, ++tl) {
+    // grouped: as above
+    Spot next = {};
+    int next_row[BN / 64];
+    auto look = [&](int tile) {
+      if (tile >= n_tiles) return;
+      next = tiles.at(tile);
+      const int half = half_of(next);
+#pragma unroll
+      for (int i = 0; i < BN / 2; i += 32) {
+        const int c = part * half + i + lane;
+        next_row[i / 32] = i + lane < half && c < next.tokens && next.m0 + c < P.M ? P.order[next.m0 + c] : -1;
+      }
+    };
+    if constexpr (GROUPED) look(tile0);
+    for (int tile = tile0; tile < n_tiles && ok; tile += tile_step, ++tl) {
       const uint32_t buf = tl % C::kDBuffers;
-      const int n = tile / P.n_tiles_m * 2 * kRows + (int)rank * kRows + 32 * quad + lane, m0 = tile % P.n_tiles_m * BN;
-      const int tokens = min(BN, P.M - m0);
+      const Spot q = GROUPED ? next : tiles.at(tile);
+      const int n = q.n0 + (int)rank * kRows + 32 * quad + lane, m0 = q.m0, tokens = q.tokens, begin = part ? half_of(q) : 0;
+      if constexpr (GROUPED) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < BN / 2; i += 32) mine[i + lane] = (unsigned)next_row[i / 32] < (unsigned)P.M ? next_row[i / 32] * P.ldy : -1;
+        __syncwarp();
+        look(tile + tile_step);
+      }
       ok = __all_sync(0xffffffffu, bar_wait_cluster(d_full(buf), (tl / C::kDBuffers) & 1u, abort_flag));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      store_columns<true>(P, tmem + quarter + buf * BN, begin, begin ? tokens : min(tokens, BN / 2), m0, n);
+      const int end = part ? tokens : min(tokens, half_of(q));
+      if constexpr (GROUPED) scatter_columns<true>(P, tmem + quarter + buf * BN, begin, end, (uint32_t)__cvta_generic_to_shared(mine), n);
+      else store_columns<true>(P, tmem + quarter + buf * BN, begin, end, m0, n);
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane == 0) bar_arrive_first(d_empty(buf));
       __syncwarp();
     }
+    if constexpr (GROUPED) zero_rows(P, (warp > kScaleCopyWarp ? warp - 1 : warp) * 32 + lane - 32 * kFirstEpiWarp, 256);
   }
   // neither CTA leaves while the other may still read its shared memory or arrive at its barriers
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -1048,8 +1108,10 @@ mx_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
       const int own = *asked, other = *other_asked, most = max(own, other);
       for (int i = min(own, other); i < most; ++i) {
         const uint32_t bar = full(i % C::kStages);
-        if (other > own) bar_expect_tx(bar, kStageBytes);
-        else asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(kStageBytes) : "memory");
+        Tiles<BN, GROUPED, 2 * kRows> again{P, first_tiles, begins};
+        const uint32_t bytes = stage_bytes(again.at(tile0 + i / P.n_ks * tile_step));
+        if (other > own) bar_expect_tx(bar, bytes);
+        else asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
       }
       for (int i = max(0, most - C::kStages); i < most; ++i) bar_drain(full(i % C::kStages), (i / C::kStages) & 1u);
     }
@@ -1108,24 +1170,30 @@ Plan plan(int64_t M, int64_t N, int64_t n_ks) {
 }
 
 // The width and the cut of a product grouped by expert.  How many rows an expert has is not known here; from the mean m over the experts
-// that can occur, taken for exponentially distributed, an expert has 1 / (1 - exp(-w / m)) tiles of w tokens.  Times as above.
+// that can occur, taken for exponentially distributed, an expert has 1 / (1 - exp(-w / m)) tiles of w tokens.  Times of a stage and of a
+// tile's end in microseconds, from whole calls on B200 (widths 16 / 32 / 64 / 128 / 192 / 256 / pairs of 192 / of 256):
+//     2048 tokens x 4 of 32 experts, 4096 x 2048: 158 / 102 / 79 / 71 / 72 / 90 / 72 / 89 us; 4096 x 8192: - / - / 268 / 232 / 221 / 245 / 218 / 230
+//     4096 x 2 of 8, 14336 x 4096: - / - / 446 / 320 / 289 / 363 / 272 / 358;   512 x 4 of 32, 4096 x 2048: 53 / 40 / 36 / 38 / 46 / 54 / 45 / 52
+//     48 x 2 of 8, 11008 x 4096: 37 / 38 / 39 / 41 / 46 / 56;   200 x 4 of 32, 4096 x 2048: 34 / 31 / 33 / 35 / 41 / 46
 Plan plan_grouped(int64_t rows, int64_t G, int64_t N, int64_t n_ks) {
-  static constexpr struct { int width; double stage, epilogue; } kWidths[] = {{16, 0.33, 0.1}, {32, 0.33, 0.2}, {64, 0.34, 0.4},
-                                                                               {128, 0.31, 0.4}, {192, 0.39, 0.2}, {256, 0.35, 2.9}};
+  static constexpr struct { int width; double stage, end; bool pair; } kWidths[] = {
+      {16, 0.15, 0.1, false}, {32, 0.18, 0.1, false}, {64, 0.24, 0.2, false}, {128, 0.36, 0.4, false},
+      {192, 0.43, 1.1, false}, {256, 0.54, 2.7, false}, {192, 0.42, 1.2, true}, {256, 0.49, 3.1, true}};
   const double experts = (double)(G < rows ? G : rows), mean = (double)rows / experts, sms = current_sm_count();
-  const int64_t n_tiles_n = (N + kRows - 1) / kRows, n_ss = (n_ks + 1) / 2;
+  const int64_t n_ss = (n_ks + 1) / 2;
   Plan best = {256, 1, false};
   double least = 1e300;
   for (const auto& w : kWidths) {
-    const double tiles = experts * n_tiles_n / (1.0 - exp(-w.width / mean));
+    const int64_t n_tiles_n = w.pair ? (N + 2 * kRows - 1) / (2 * kRows) : (N + kRows - 1) / kRows;
+    const double tiles = experts * n_tiles_n / (1.0 - exp(-w.width / mean)), at_once = w.pair ? sms / 2 : sms;
     const int64_t bound = (rows / w.width + (int64_t)experts) * n_tiles_n;
-    for (int s = 1; s <= kMostSplit && s <= n_ss && (s == 1 || bound * s <= (int64_t)sms); s *= 2) {
+    for (int s = 1; s <= (w.pair ? 1 : kMostSplit) && s <= n_ss && (s == 1 || bound * s <= (int64_t)sms); s *= 2) {
       if (s > 4 && (w.width >= 128 || bound * s > (int64_t)sms / 2)) break;
-      const double waves = tiles < sms ? 1.0 : tiles / sms;
-      const double time = waves * (2 * w.stage * ((n_ss + s - 1) / s) + w.epilogue) + (s > 1 ? 2.0 + fmin(mean, w.width) / (64.0 * s) : 0.0);
+      const double waves = tiles < at_once ? 1.0 : tiles / at_once;
+      const double time = waves * (2 * w.stage * ((n_ss + s - 1) / s) + w.end) + (s > 1 ? 2.0 + fmin(mean, w.width) / (64.0 * s) : 0.0);
       if (time < least) {
         least = time;
-        best = {w.width, s, false};
+        best = {w.width, s, w.pair};
       }
     }
   }
@@ -1196,53 +1264,9 @@ bool encode_experts(CUtensorMap* map, const uint8_t* p, int64_t bytes, int64_t r
 }
 
 template <int BN>
-lcd_status launch_grouped(const MxGrouped& p, int split, int32_t* status, cudaStream_t s) {
-  using C = Cfg<BN, true>;
-  auto kern = mx_linear_kernel<BN, void, true>;
-  static PerDeviceFlag attr_set;
-  int dev;
-  if (attr_set.first(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
-    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
-    attr_set.done(dev);
-  }
-  const int64_t blocks = (p.K + kMxBlock - 1) / kMxBlock, n_tiles_n = (p.N + kRows - 1) / kRows;
-  // at most: every expert's last tile may hold one token
-  const int64_t tiles = (p.rows.count / BN + (p.G < p.rows.count ? p.G : p.rows.count)) * n_tiles_n;
-  if (tiles * split > 0x7fffffff) return LCD_ERR_UNSUPPORTED;
-  CUtensorMap w, x, ws, xs;
-  if (!encode_experts(&w, p.w_codes, blocks * 16, p.N, p.ldwc, p.G, p.dwc, kStageK / 2, true) ||
-      !encode_experts(&ws, p.w_scales, blocks, p.N, p.ldws, p.G, p.dws, 16, false) ||
-      !encode_rows(&x, p.x_codes, blocks * 16, p.rows.count, p.ldxc, kStageK / 2, C::kBox, true) ||
-      !encode_rows(&xs, p.x_scales, blocks, p.rows.count, p.ldxs, 16, BN, false)) {
-    set_cuda_error((int)cudaErrorInvalidValue);
-    return LCD_ERR_CUDA;
-  }
-  Args a = {};
-  a.y = p.y;
-  a.ldy = p.ldy;
-  a.y_type = (int)p.y_type;
-  a.M = (int)p.rows.count;
-  a.N = (int)p.N;
-  a.n_ks = (int)((blocks * kMxBlock + kStageK - 1) / kStageK);
-  a.n_ss = (a.n_ks + 1) / 2;
-  a.n_tiles = (int)tiles;
-  a.early = 1;
-  a.status = status;
-  a.order = p.rows.order;
-  a.offsets = p.rows.offsets;
-  a.G = (int)p.G;
-  const int64_t room = (int64_t)current_sm_count() * C::kPerSm;
-  const unsigned grid = (unsigned)(split > 1 ? tiles * split : tiles < room ? tiles : room);
-  const cudaError_t e = launch_overlapping(kern, dim3(grid), dim3(C::kThreads), C::kSmem, (unsigned)split, s, w, x, ws, xs, a);
-  if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
-  return LCD_OK;
-}
-
-template <int BN>
 lcd_status launch_pair(const MxProduct& p, bool early, int32_t* status, cudaStream_t s) {
   using C = PairCfg<BN>;
-  auto kern = mx_pair_kernel<BN>;
+  auto kern = mx_pair_kernel<BN, false>;
   static PerDeviceFlag attr_set;
   int dev;
   if (attr_set.first(&dev)) {
@@ -1275,6 +1299,56 @@ lcd_status launch_pair(const MxProduct& p, bool early, int32_t* status, cudaStre
   a.status = status;
   const int64_t pairs = current_sm_count() / 2;
   const cudaError_t e = launch_overlapping(kern, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs))), dim3(C::kThreads), C::kSmem, 2u, s, w, x, ws, xs, a);
+  if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+  return LCD_OK;
+}
+
+template <int BN, bool PAIR>
+lcd_status launch_grouped(const MxGrouped& p, int split, int32_t* status, cudaStream_t s) {
+  using C = std::conditional_t<PAIR, PairCfg<BN, true>, Cfg<BN, true>>;
+  auto kern = [] {
+    if constexpr (PAIR) return mx_pair_kernel<BN, true>;
+    else return mx_linear_kernel<BN, void, true>;
+  }();
+  static PerDeviceFlag attr_set;
+  int dev;
+  if (attr_set.first(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
+    if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
+    attr_set.done(dev);
+  }
+  const int64_t blocks = (p.K + kMxBlock - 1) / kMxBlock, rows = PAIR ? 2 * kRows : kRows, n_tiles_n = (p.N + rows - 1) / rows;
+  // at most: every expert's last tile may hold one token
+  const int64_t tiles = (p.rows.count / BN + (p.G < p.rows.count ? p.G : p.rows.count)) * n_tiles_n;
+  if (tiles * split > 0x7fffffff) return LCD_ERR_UNSUPPORTED;
+  CUtensorMap w, x, ws, xs;
+  if (!encode_experts(&w, p.w_codes, blocks * 16, p.N, p.ldwc, p.G, p.dwc, kStageK / 2, true) ||
+      !encode_experts(&ws, p.w_scales, blocks, p.N, p.ldws, p.G, p.dws, 16, false) ||
+      !encode_rows(&x, p.x_codes, blocks * 16, p.rows.count, p.ldxc, kStageK / 2, C::kBox, true) ||
+      !encode_rows(&xs, p.x_scales, blocks, p.rows.count, p.ldxs, 16, BN, false)) {
+    set_cuda_error((int)cudaErrorInvalidValue);
+    return LCD_ERR_CUDA;
+  }
+  Args a = {};
+  a.y = p.y;
+  a.ldy = p.ldy;
+  a.y_type = (int)p.y_type;
+  a.M = (int)p.rows.count;
+  a.N = (int)p.N;
+  a.n_ks = (int)((blocks * kMxBlock + kStageK - 1) / kStageK);
+  a.n_ss = (a.n_ks + 1) / 2;
+  a.n_tiles = (int)tiles;
+  a.early = 1;
+  a.status = status;
+  a.order = p.rows.order;
+  a.offsets = p.rows.offsets;
+  a.G = (int)p.G;
+  int64_t room = 0;
+  if constexpr (PAIR) room = current_sm_count() / 2;
+  else room = (int64_t)current_sm_count() * C::kPerSm;
+  const int64_t at_once = split > 1 || tiles < room ? tiles : room;
+  const cudaError_t e = launch_overlapping(kern, dim3((unsigned)(at_once * (PAIR ? 2 : split))), dim3(C::kThreads), C::kSmem,
+                                           PAIR ? 2u : (unsigned)split, s, w, x, ws, xs, a);
   if (e != cudaSuccess) { set_cuda_error((int)e); return LCD_ERR_CUDA; }
   return LCD_OK;
 }
@@ -1316,13 +1390,14 @@ lcd_status launch_mx_grouped(const MxGrouped& p, int32_t* status_word, void* str
   if (p.G > kMostExperts) return LCD_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Plan w = plan_grouped(p.rows.count, p.G, p.N, ((p.K + kMxBlock - 1) / kMxBlock * kMxBlock + kStageK - 1) / kStageK);
+  if (w.pair) return w.width == 192 ? launch_grouped<192, true>(p, 1, status_word, s) : launch_grouped<256, true>(p, 1, status_word, s);
   switch (w.width) {
-    case 16: return launch_grouped<16>(p, w.split, status_word, s);
-    case 32: return launch_grouped<32>(p, w.split, status_word, s);
-    case 64: return launch_grouped<64>(p, w.split, status_word, s);
-    case 128: return launch_grouped<128>(p, w.split, status_word, s);
-    case 192: return launch_grouped<192>(p, w.split, status_word, s);
-    default: return launch_grouped<256>(p, w.split, status_word, s);
+    case 16: return launch_grouped<16, false>(p, w.split, status_word, s);
+    case 32: return launch_grouped<32, false>(p, w.split, status_word, s);
+    case 64: return launch_grouped<64, false>(p, w.split, status_word, s);
+    case 128: return launch_grouped<128, false>(p, w.split, status_word, s);
+    case 192: return launch_grouped<192, false>(p, w.split, status_word, s);
+    default: return launch_grouped<256, false>(p, w.split, status_word, s);
   }
 }
 
