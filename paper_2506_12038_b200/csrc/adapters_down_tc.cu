@@ -275,7 +275,8 @@ lcd_status launch_type(DownArgs P, bool backward, cudaStream_t s) {
 }  // namespace
 
 bool adapters_down_tc_takes(const DownArgs& P, lcd_dtype x_type, lcd_dtype w_type) {
-  return x_type == w_type && x_type != LCD_DTYPE_F32 && P.a.rows >= kManyRows;
+  return x_type == w_type && x_type != LCD_DTYPE_F32 &&
+         P.a.rows >= (on_bytes(P.x, P.ldx, 0, 2, 16) && on_bytes(P.a.w, P.a.ldw, P.a.sw, 2, 16) ? kManyRows : 2 * kManyRows);
 }
 
 lcd_status launch_adapters_down_tc(const DownArgs& P, lcd_dtype type, bool backward, cudaStream_t s) {

@@ -54,6 +54,7 @@ __global__ void __launch_bounds__(32 * kUpWarps, ONE && RT == 1 ? 4 : ONE && RT 
   constexpr int CT = kUpTiles<W, RT>, R = 16 * RT, kOwn = 2 * CT;       // columns of a lane
   constexpr bool kBf16 = std::is_same<W, __nv_bfloat16>::value;
   constexpr int kTerms = kBf16 && sizeof(Y) == 4 ? 3 : 2;
+  __shared__ float s_out[kUpWarps][16][8 * CT + 1];
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const long long col0 = ((long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * 8 * CT;
   const long long own0 = col0 + kOwn * t;
@@ -226,6 +227,7 @@ __global__ void __launch_bounds__(32 * kUpWarps, ONE && RT == 1 ? 4 : ONE && RT 
             }
           }
         }
+        // rows that do not start on 16 bytes go through shared memory, so that neighbouring lanes store neighbouring columns
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           if (now.row[h] < 0) continue;
@@ -239,7 +241,24 @@ __global__ void __launch_bounds__(32 * kUpWarps, ONE && RT == 1 ? 4 : ONE && RT 
               out[CT + j] = __fmaf_rn(factor, d[j][2 * h + 1], out[CT + j]);
             }
           }
-          store_values(static_cast<Y*>(P.y) + (long long)now.row[h] * P.ldy + own0, out, have, P.wide_y);
+          if (P.wide_y) {
+            store_values(static_cast<Y*>(P.y) + (long long)now.row[h] * P.ldy + own0, out, have, true);
+          } else {
+#pragma unroll
+            for (int j = 0; j < kOwn; ++j) s_out[threadIdx.x >> 5][g + 8 * h][kOwn * t + j] = out[j];
+          }
+        }
+        if (!P.wide_y) {
+          __syncwarp();
+          const int columns = (int)max(0ll, min((long long)(8 * CT), P.a.K - col0));
+#pragma unroll 4
+          for (int r = 0; r < 16; ++r) {
+            const int row = __shfl_sync(0xffffffffu, r < 8 ? now.row[0] : now.row[1], r % 8 * 4);
+            if (row < 0) continue;
+            Y* to = static_cast<Y*>(P.y) + (long long)row * P.ldy + col0;
+            for (int c = lane; c < columns; c += 32) to[c] = from_f32<Y>(s_out[threadIdx.x >> 5][r][c]);
+          }
+          __syncwarp();
         }
         if (ONE) break;
         now = next;

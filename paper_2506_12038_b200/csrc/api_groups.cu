@@ -77,6 +77,8 @@ lcd_status up(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type, bool transpos
 int parts_of_t(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type) {
   if (u.a.rows < kManyRows || ((int64_t)u.a.rows / 128 + u.a.G + 1) * ((u.a.K + 63) / 64) > 0x7fffffff) return 0;
   if (u.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return 0;      // the parts do not fit into shared memory
+  const int64_t size = size_of(y_type);
+  if (u.a.rows < 2 * kManyRows && !(on_bytes(u.y, u.ldy, u.a.K, size, 16) && on_bytes(u.base, u.ldbase, u.a.K, size, 16))) return 0;
   return w_type == LCD_DTYPE_BF16 && y_type == LCD_DTYPE_BF16 ? 2 : 3;
 }
 
