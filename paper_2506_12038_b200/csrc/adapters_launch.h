@@ -45,7 +45,7 @@ struct OuterSide {
   long long columns;
   const float* scale;          // [G] or null
   void* out;                   // [G][r][columns], or [G][columns][r]
-  int by_column;
+  int by_column, wide_out;
 };
 struct OuterArgs {
   const int32_t *order, *offsets;

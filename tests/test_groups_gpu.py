@@ -378,7 +378,7 @@ def test_grad_of_many_rows(x, w, M, G, r, K, N):
 
 
 @pytest.mark.parametrize("x,w", PAIRS)
-@pytest.mark.parametrize("M,G,r,K,N", [(3000, 1, 16, 64, 72), (2500, 2, 40, 136, 64), (2100, 1, 8, 63, 65)])
+@pytest.mark.parametrize("M,G,r,K,N", [(3000, 1, 16, 64, 72), (2500, 2, 40, 136, 64), (2100, 1, 8, 63, 65), (1300, 30, 32, 1000, 72)])
 def test_grad_of_long_groups(x, w, M, G, r, K, N):
     # a sum over more rows than the stages in flight hold, several times around them; rows of one group against sums in whole numbers
     word = torch.zeros(1, dtype=torch.int32, device="cuda")
