@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblcd_b200.so")
 CALLS = os.path.join(HERE, "_host_calls.so")
 SOURCES = ["api.cu", "pack.cpp", "quantize.cu", "quantize8.cu", "smoothing.cu", "reclassify.cu", "dbci.cu", "dbci_sort.cu", "reference.cu", "lut_gemv.cu", "lut_smem.cu", "lut_gemv_tc.cu", "dense_tc.cu", "static_scratch.cu", "api_mx.cu", "mx.cu", "mx_linear.cu", "distill.cu",
-           "api_groups.cu", "group_rows.cu", "adapters_down_f32.cu", "adapters_down_f16.cu", "adapters_down_bf16.cu", "adapters_up_f32.cu", "adapters_up_f16.cu", "adapters_up_bf16.cu", "adapters_up_tc_f32.cu", "adapters_up_tc_f16.cu", "adapters_up_tc_bf16.cu", "adapters_down_tc.cu", "adapters_outer.cu", "adapters_outer_tc.cu"]
+           "api_groups.cu", "group_rows.cu", "adapters_down_f32.cu", "adapters_down_f16.cu", "adapters_down_bf16.cu", "adapters_up_f32.cu", "adapters_up_f16.cu", "adapters_up_bf16.cu", "adapters_up_tc_f32.cu", "adapters_up_tc_f16.cu", "adapters_up_tc_bf16.cu", "adapters_down_tc.cu", "adapters_down_parts.cu", "adapters_outer.cu", "adapters_outer_tc.cu"]
 
 
 def nvcc_path() -> str:

@@ -33,6 +33,8 @@ lcd_status launch_adapters_down_bf16(const DownArgs& P, lcd_dtype w_type, bool b
 
 bool adapters_down_tc_takes(const DownArgs& P, lcd_dtype x_type, lcd_dtype w_type);
 lcd_status launch_adapters_down_tc(const DownArgs& P, lcd_dtype type, bool backward, cudaStream_t s);
+bool adapters_down_parts_takes(const DownArgs& P, lcd_dtype x_type, lcd_dtype w_type);
+lcd_status launch_adapters_down_parts(const DownArgs& P, lcd_dtype x_type, lcd_dtype w_type, bool backward, cudaStream_t s);
 
 // The gradient of one adapter matrix: [r] x columns of z's, sums over an adapter's rows of u (r values a row, fp32) times z.
 struct OuterSide {

@@ -57,6 +57,7 @@ AdapterArgs args_of(const lcd_adapter_weights& w, const lcd_row_groups& rows, bo
 lcd_status down(const DownArgs& d, lcd_dtype x_type, lcd_dtype w_type, bool backward, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (adapters_down_tc_takes(d, x_type, w_type)) return launch_adapters_down_tc(d, x_type, backward, s);
+  if (adapters_down_parts_takes(d, x_type, w_type)) return launch_adapters_down_parts(d, x_type, w_type, backward, s);
   switch (x_type) {
     case LCD_DTYPE_F32: return launch_adapters_down_f32(d, w_type, backward, s);
     case LCD_DTYPE_F16: return launch_adapters_down_f16(d, w_type, backward, s);
