@@ -525,6 +525,7 @@ typedef struct {
  *   workspace: device scratch of lcd_adapters_workspace_bytes(count, rank) bytes, 16-byte aligned, contents ignored; calls that may overlap on the
  *             device need separate ones;
  *   status_word_dev: as for lcd_lut_linear.
+ * A row of x that is not finite, or an adapter that is not, makes its own rows' results not finite (NaN where an infinity would do), no others'.
  * Results are reproducible from run to run, but a row's last bits may differ with the rows beside it. */
 lcd_status lcd_adapters_workspace_bytes(int64_t count, int64_t rank, size_t* bytes);
 
@@ -537,7 +538,7 @@ lcd_status lcd_adapters(const lcd_adapter_weights* weights /* host struct */, co
  *     da_g = sum over g's rows of dt[m]^T x[m],     db_g = scale_g * sum over g's rows of dy[m]^T t[m];  groups without rows: zeros.
  *   dy:       device, [count][lddy], lddy >= N;   x: device, [count][ldx];   type: of dy, x, base and dx, types as for lcd_adapters;
  *   t:        device, fp32 [count][ldt], as lcd_adapters gave it for this x (may be NULL without db);
- *   base, dx: device, [count][ldbase], [count][lddx], as base and y of lcd_adapters; dx may be NULL: not wanted;
+ *   base, dx: device, [count][ldbase], [count][lddx], as base and y of lcd_adapters; dx may be NULL: not wanted.  dx may not be x or dy;
  *   da, db:   device out, grad_type, dense [G][rank][K] and [G][N][rank]; either may be NULL: not wanted;
  *   workspace, status_word_dev: as for lcd_adapters. */
 lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights /* host struct */, const void* dy, int64_t lddy, const void* x, int64_t ldx,

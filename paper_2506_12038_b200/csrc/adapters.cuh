@@ -1,10 +1,11 @@
-// Low-rank adapters beside a shared layer: what the three kernels have in common (adapters_down.cu: x a^T and dy b, adapters_up.cu: t b^T
+// Low-rank adapters beside a shared layer: what the three kernels have in common (adapters_down.cuh: x a^T and dy b, adapters_up.cuh: t b^T
 // and dt a, added to what is there, adapters_outer.cu: the adapters' gradients).
 //
-// All three are bound by the one pass over x, y, dy or dx (a rank of 64 needs 64 FLOP a byte of 16-bit activations), so operands go
-// from memory to registers in the fragment order of mma.sync and nothing is staged: a sum does not care for the order of its terms, so
-// a lane takes 16 consecutive bytes of its row for the slots that the instruction gives it, and both operands use the same order.
-// (A tcgen05 product would have to bring the gathered rows of x to shared memory first.)
+// All three are bound by the one pass over x, y, dy or dx (a rank of 64 needs 64 FLOP a byte of 16-bit activations), and with few rows by
+// latency.  There operands go from memory to registers in the fragment order of mma.sync and nothing is staged: a sum does not care for
+// the order of its terms, so a lane takes 16 consecutive bytes of its row for the slots that the instruction gives it, and both operands
+// use the same order.  With many rows registers do not hold enough loads to keep memory busy (4096 x 5120 x 13824, rank 64, bf16: 206 us
+// a call): those go through shared memory and tcgen05 (adapters_tc.cuh: 74 us).
 //
 // Arithmetic.  Two 16-bit operands of one type: their products are exact, sums are fp32.  The products with t or dt, which are fp32: with
 // bf16 beside them as two bf16 terms (16 bits, relative error 2^-16 where the result is rounded to 16-bit types) or three (24 bits, for

@@ -22,7 +22,8 @@ struct Shape {
   static constexpr int kStages = 4 * kStage <= 200 * 1024 ? 4 : 2;                // whoever fills a place has filled it the time before
   static constexpr int kPitch = R + 4;                                            // of the sums, fp32
   static constexpr int kSmem = 1024 + kStages * kStage + Plan::kBytes + 128;
-  static constexpr int kTmem = R < 32 ? 32 : R;
+  static constexpr int kTmem = (kSums<R> + 1) * R;
+  static_assert(kSmem > 114 * 1024 || kTmem <= 256, "tensor memory of CTAs that share an SM");
   static_assert(128 * kPitch * 4 <= kStages * kStage && kSmem <= 227 * 1024, "sums lie in the stages");
 };
 
@@ -70,7 +71,6 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_parts_kernel(const 
   if (warp == kMmaWarp) {
     if (elect()) {
       constexpr uint32_t idesc = instr_desc(R, true, false, TRANSPOSED);
-      uint32_t more = 0;
       for (int it = 0; it < n && ok; ++it) {
         const int s = it % S::kStages;
         ok = bar_wait(full(s), (it / S::kStages) & 1u, abort_flag);
@@ -84,8 +84,9 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_parts_kernel(const 
             if (px + pw >= 3) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              mma(tmem, xd + ((px * S::kX + 32 * i) >> 4), wd + ((pw * S::kW + (TRANSPOSED ? 2048 : 32) * i) >> 4), idesc, more);
-              more = 1;
+              const bool main = px + pw == 0;
+              mma(tmem + (main ? it % kSums<R> : kSums<R>) * R, xd + ((px * S::kX + 32 * i) >> 4), wd + ((pw * S::kW + (TRANSPOSED ? 2048 : 32) * i) >> 4), idesc,
+                  (uint32_t)(main ? it >= kSums<R> || i > 0 : it > 0 || i > 0 || px + 3 * pw != (S::kPartsW > 1 ? 3 : 1)));
             }
           }
         mma_commit(empty(s));
@@ -173,17 +174,10 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_parts_kernel(const 
       float* sum = reinterpret_cast<float*>(gen + base) + thread * S::kPitch;
 #pragma unroll
       for (int c = 0; c < R; c += 16) {
-        uint32_t v[16];
-        if (n > 0) {
-          tmem_ld16(tmem + ((uint32_t)(32 * warp) << 16) + c, v);
-          tmem_wait_ld();
-        } else {
+        float v[16] = {};
+        if (n > 0) read_sums<R>(tmem + ((uint32_t)(32 * warp) << 16) + c, n, true, v);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = 0u;
-        }
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<float4*>(sum + c + i) = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+        for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(sum + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
       }
     }
     before_sync();

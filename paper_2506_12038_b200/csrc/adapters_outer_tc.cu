@@ -32,9 +32,9 @@ struct Shape {
   static constexpr int kMmaWarp = kZWarps + kUWarps, kFirstEpiWarp = kMmaWarp + 1, kThreads = 32 * (kFirstEpiWarp + 4);
   static constexpr int kPitch = R + 4;                                            // of a cluster's sums, fp32
   static constexpr int kSmem = 1024 + kStages * kStage + 4 * (kMostGroups + 1) + 256;
-  static constexpr int kTmem = 2 * R < 32 ? 32 : 2 * R;
+  static constexpr int kTmem = 2 * (kSums<R> + 1) * R;
   static_assert(kStages % kZGroups == 0 && kStages % kUGroups == 0 && 128 * kPitch * 4 <= kStages * kStage && kSmem <= 227 * 1024, "shapes");
-  static_assert(kSmem > 114 * 1024 || kTmem <= 128, "tensor memory of CTAs that share an SM");
+  static_assert(kSmem > 114 * 1024 && kTmem <= 512, "one CTA an SM");
 };
 
 // The stages that a role walks through: sum after sum, this CTA's share of each.
@@ -132,7 +132,6 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
           if (!ok) break;
           after_sync();
           const uint64_t zd = tile_desc(base + s * S::kStage, kStageRows * 128), ud = tile_desc(base + s * S::kStage + S::kParts_z * S::kZPart, kStageRows * 128);
-          uint32_t more = it > 0;
 #pragma unroll
           for (int pz = 0; pz < S::kParts_z; ++pz)
 #pragma unroll
@@ -140,8 +139,9 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
               if (pz + pu >= S::kParts_u) continue;        // smaller than what the parts leave out
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
-                mma(tmem + b * R, zd + ((pz * S::kZPart + 2048 * i) >> 4), ud + ((pu * S::kUPart + 2048 * i) >> 4), idesc, more);
-                more = 1;
+                const bool main = pz + pu == 0;             // the others begin with pz = 0, pu = 1
+                mma(tmem + ((kSums<R> + 1) * b + (main ? it % kSums<R> : kSums<R>)) * R, zd + ((pz * S::kZPart + 2048 * i) >> 4), ud + ((pu * S::kUPart + 2048 * i) >> 4), idesc,
+                    (uint32_t)(main ? it >= kSums<R> || i > 0 : it > 0 || i > 0 || pz > 0 || pu > 1));
               }
             }
           mma_commit(empty(s));
@@ -315,25 +315,19 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
       float* sum = reinterpret_cast<float*>(gen + base) + mine * S::kPitch;       // a cluster's: it has one sum, whose stages are done with
 #pragma unroll
       for (int r0 = 0; r0 < R; r0 += 16) {
-        uint32_t v[16];
-        if (some) {
-          tmem_ld16(tmem + ((uint32_t)(32 * quad) << 16) + b * R + r0, v);
-          tmem_wait_ld();
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = 0u;
-        }
+        float v[16] = {};
+        if (some) read_sums<R>(tmem + ((uint32_t)(32 * quad) << 16) + (kSums<R> + 1) * b * R + r0, w.n, true, v);
         if (split > 1) {
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<float4*>(sum + r0 + i) = make_float4(__uint_as_float(v[i]), __uint_as_float(v[i + 1]), __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+            *reinterpret_cast<float4*>(sum + r0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
         } else if (inside) {
           // (a group without rows has zeros whatever its factor is)
           O* to = out + (E.by_column ? ((long long)w.group * E.columns + c) * P.r + r0 : ((long long)w.group * P.r + r0) * E.columns + c);
           const long long pitch = E.by_column ? 1 : E.columns;
           float x[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = some ? __uint_as_float(v[i]) * factor : 0.0f;
+          for (int i = 0; i < 16; ++i) x[i] = some ? v[i] * factor : 0.0f;
           if (E.wide_out && r0 + 16 <= P.r) {
             store16_values(to, x, false);
           } else {

@@ -4,7 +4,8 @@
 // It keeps its part of the adapter matrix in registers as the MMAs' B operand for all rows of an adapter; rows are the A operand, 16 at a
 // time, t in two or three terms (adapters.cuh).  Tile j's column c stands for column CT c + j, so that a lane ends up with 2 CT consecutive
 // columns of two rows, which it adds to the base's and stores.  The next rows' base and t are on their way meanwhile.
-// Reading base, writing y bounds it.  It begins while the kernel that makes t ends: the adapter matrix and the first base are loaded before.
+// Reading base, writing y bounds it, with few rows latency: the plan, then the matrix and base, then t (64 rows of 48 adapters to 11008 columns,
+// rank 16, bf16: 14 us with cold caches, bytes 3).  It begins while the kernel that makes t ends: the adapter matrix and the first base are loaded before.
 // TRANSPOSED: the adapter matrix is a [r][K]; rows are paired up with byte permutes.
 #ifndef LCD_ADAPTERS_UP_CUH_
 #define LCD_ADAPTERS_UP_CUH_

@@ -1,14 +1,16 @@
-// adapters_up.cu's products for many rows: y = base + s t b^T, dx = base + dt a.
+// adapters_up.cuh's products for many rows: y = base + s t b^T, dx = base + dt a.
 //
 // A tile is 128 rows of one adapter by NC columns.  Rows of base follow the plan through 16-byte cp.async copies, whole rows side by side (one bulk
 // copy a row takes a thread some 120 clocks, 128 of them three times as long as their bytes need); the product, t's parts times the adapter
 // matrix's, waits in tensor memory meanwhile.  A CTA has consecutive tiles of the list (columns, rows), so that the adapter's part stays
 // in shared memory from tile to tile.
 //
-// Roles (17 warps): warps 0-3 copy base in; warp 4 owns tensor memory, one elected lane issues the MMAs; warps 5-8 bring t and, where it
-// changes, the adapter matrix, split into bf16 parts; warps 9-16 add: a thread has a row and half of the columns, reads the base's from
+// Roles (17 warps): warps 0-3 copy base in; warp 4 owns tensor memory, one elected lane issues the MMAs; warps 5-8 bring the parts of t and, where it
+// changes, those of the adapter matrix; warps 9-16 add: a thread has a row and half of the columns, reads the base's from
 // shared memory (rows 16 bytes longer than their columns: no bank conflicts) and stores 32 bytes at a time, whole sectors.
 // Two tiles are in flight: while one is added up, the next one's base comes in.
+// 4096 x 13824, rank 64, bf16: 55 us, 4.1 TB/s (79 with t split here in place of where it is made, 61 with the matrix through registers).  A tile
+// takes 3.5 us: copies of base 3.5, adding and storing 2.5, both behind one another's memory traffic.
 #ifndef LCD_ADAPTERS_UP_TC_CUH_
 #define LCD_ADAPTERS_UP_TC_CUH_
 

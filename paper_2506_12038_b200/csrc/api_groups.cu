@@ -146,6 +146,7 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   lcd_status st = lcd_adapters_workspace_bytes(rows->count, weights->rank, &need);
   if (st != LCD_OK) return st;
   if (!workspace || workspace_bytes < need) return LCD_ERR_BUFFER_TOO_SMALL;
+  if (rows->count == 1) ldx = ldbase = ldy = 0;          // a single row has no pitch to be off 16 bytes
   DownArgs d = {};
   d.a = args_of(*weights, *rows, false);
   d.x = x;
@@ -178,7 +179,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
   if (!planned(rows) || !adapters_there(weights) || !dense_rows(dy, type, weights->N, lddy) || (!dx && !da && !db) ||
       (da && !dense_rows(x, type, weights->K, ldx)) || (db && (!t || ldt < weights->rank || !aligned(t, 4))) ||
       (dx && (!dense_rows(dx, type, weights->K, lddx) || (base && !dense_rows(base, type, weights->K, ldbase)) ||
-              (base == dx && ldbase != lddx && rows->count > 1))) ||
+              (base == dx && ldbase != lddx && rows->count > 1) || dx == dy || dx == x)) ||
       ((da || db) && (!known(grad_type) || !aligned(da, size_of(grad_type)) || !aligned(db, size_of(grad_type)))) || !aligned(workspace, 16) ||
       !aligned(status_word_dev, 4))
     return LCD_ERR_INVALID_ARG;
@@ -187,6 +188,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
   lcd_status st = lcd_adapters_workspace_bytes(rows->count, weights->rank, &need);
   if (st != LCD_OK) return st;
   if (!workspace || workspace_bytes < need) return LCD_ERR_BUFFER_TOO_SMALL;
+  if (rows->count == 1) lddy = ldx = ldt = ldbase = lddx = 0;
   float* dt = static_cast<float*>(workspace);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   UpArgs u = {};

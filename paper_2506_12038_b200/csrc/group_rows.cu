@@ -3,7 +3,8 @@
 // Every warp of a CTA, or of a cluster of eight where there are many rows, has one contiguous piece of the rows.  It counts its rows by
 // group in a column of its own in shared memory (match.any finds a group's rows among 32, one lane adds them, so there are no
 // atomics); the columns are summed over the warps of all CTAs, in their order, and over the groups; then every warp walks its piece
-// again and gives its rows their places.  What bounds it is latency: a dozen dependent steps (the figures are at the launch).
+// again and gives its rows their places.  What bounds it is latency: a dozen dependent steps (256 rows of 32 groups 3.0 us, 8192 in a
+// cluster of eight 7, 65536 of 128 groups 17; host and device together 5.7 and 19).
 #include "common.h"
 #include "device_util.h"
 

@@ -389,6 +389,23 @@ def test_grad_of_long_groups(x, w, M, G, r, K, N):
     assert word.item() == 0
 
 
+@pytest.mark.parametrize("x,w", [("fp32", "fp32"), ("fp16", "fp16"), ("bf16", "fp32")])
+def test_long_sums_keep_fp32s_precision(x, w):
+    # 8192 terms: 128 stages of four instructions, each of which cuts its sum off (2^-24 of it at most).  They go to seven accumulators in turn:
+    # 76 of them one after the other; the parts' products, the joining of the sums and what the parts leave out are within 2^-20
+    g = torch.Generator(device="cuda").manual_seed(3)
+    M = K = 8192
+    xs, dy, t = (torch.randn(M, n, generator=g, device="cuda") for n in (K, 64, 16))
+    a, b = torch.randn(1, 16, K, generator=g, device="cuda") / 64, torch.randn(1, 64, 16, generator=g, device="cuda")
+    xs, dy, a, b = xs.to(TYPES[x]), dy.to(TYPES[x]), a.to(TYPES[w]), b.to(TYPES[w])
+    rows = lcd.group_rows(torch.zeros(M, dtype=torch.int32, device="cuda"), 1)
+    _, got_t = lcd.adapters(xs, a, b, rows, want_t=True)
+    _, da, db = lcd.adapters_grad(dy, xs, a, b, t, rows, want_dx=False, grad_dtype=torch.float32)
+    want_t, dt = xs.double() @ a[0].double().t(), dy.double() @ b[0].double()
+    for got, want in ((got_t, want_t), (da[0], dt.t() @ xs.double()), (db[0], dy.double().t() @ t.double())):
+        assert (got.double() - want).norm() <= (76 * 2.0 ** -24 + 2.0 ** -20) * want.norm()
+
+
 @pytest.mark.parametrize("x,w", PAIRS)
 @pytest.mark.parametrize("M,G,r,K,N", [(1, 2, 16, 1000, 256), (33, 4, 8, 700, 256), (600, 3, 64, 130, 96), (257, 2, 128, 100, 64), (2000, 1, 16, 128, 64)])
 def test_grad_whole_numbers_are_exact(x, w, M, G, r, K, N):

@@ -58,7 +58,7 @@ WEIGHTS = [dict(w=weights(**kw)) for kw in (dict(a=None), dict(b=None), dict(typ
     (adapters, PLANS + WEIGHTS + [dict(x=None), dict(x_type=5), dict(ldx=63), dict(x=ctypes.c_void_p(1)), dict(y=None), dict(ldy=9), dict(y_type=3),
                                   dict(base=TWO), dict(ldbase=9), dict(y=A, ldy=12), dict(t=A, ldt=3), dict(t=TWO, ldt=4), dict(space=ODD), dict(word=TWO)]),
     (grad, PLANS + WEIGHTS + [dict(dy=None), dict(lddy=9), dict(x=None), dict(ldx=63), dict(type=3), dict(t=None), dict(ldt=3), dict(t=TWO),
-                              dict(base=ctypes.c_void_p(1)), dict(ldbase=63), dict(lddx=63), dict(dx=A, lddx=70), dict(dx=None, da=None, db=None),
+                              dict(base=ctypes.c_void_p(1)), dict(ldbase=63), dict(lddx=63), dict(dx=A, lddx=70), dict(dx=A, base=None), dict(dx=A, x=ODD, dy=ODD, lddx=72), dict(dx=None, da=None, db=None),
                               dict(grad_type=3), dict(da=TWO), dict(space=ODD), dict(word=TWO)])])
 def test_invalid_arguments(call, bad):
     for kw in bad:
