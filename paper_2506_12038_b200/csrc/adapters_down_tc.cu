@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
   uint32_t rank, split;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
-  begin_after_previous();
+  wait_for_previous();
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) {
       bar_init(full(s), kCopyThreads);
@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_down_tc_kernel(const Dow
   before_sync();
   __syncthreads();
   after_sync();
+  let_next_begin();          // not before this CTA has its tensor memory: the next kernel's may take some and then wait for this one
   const uint32_t tmem = *tmem_holder;
   const int tile = blockIdx.x / split, G = P.a.G;
   const Plan::Spot q = tile < plan.first[G + 1] ? plan.at(tile, G, kPlaces) : Plan::Spot{G, 0, 0};

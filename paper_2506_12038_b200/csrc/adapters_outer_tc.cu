@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
   uint32_t rank, split;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
-  begin_after_previous();
+  wait_for_previous();
   for (int g = threadIdx.x; g <= P.G; g += blockDim.x) offsets[g] = max(0, min(P.rows, P.offsets[g]));
   if (threadIdx.x == 0) {
     for (int s = 0; s < S::kStages; ++s) {
@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
   before_sync();
   __syncthreads();
   after_sync();
+  let_next_begin();          // not before this CTA has its tensor memory: the next kernel's may take some and then wait for this one
   const uint32_t tmem = *tmem_holder;
   const int slabs = (int)(P.slabs[0] + P.slabs[1]);
   Walk w{P, offsets, slabs, (int)(gridDim.x / split), (int)rank, (int)split, (long long)slabs * P.G, (long long)(blockIdx.x / split)};

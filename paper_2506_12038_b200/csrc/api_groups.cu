@@ -99,7 +99,7 @@ extern "C" lcd_status lcd_group_rows(const void* group, int idx_bytes, int64_t c
 
 extern "C" lcd_status lcd_mx_linear_grouped_workspace_bytes(int64_t count, int64_t K, size_t* bytes) {
   if (!bytes || !counted(count) || K < 1 || K > kMostColumns) return LCD_ERR_INVALID_ARG;
-  *bytes = (size_t)count * (size_t)(code_row(K) + on(blocks_of(K), 16));
+  *bytes = (size_t)count * (size_t)(code_row(K) + on(blocks_of(K), 16) + 4);       // codes, scales and where they are
   return LCD_OK;
 }
 
@@ -118,7 +118,8 @@ extern "C" lcd_status lcd_mx_linear_grouped(const uint8_t* w_codes, int64_t ldwc
   const int64_t ldc = code_row(K), lds = on(blocks_of(K), 16);
   uint8_t* codes = static_cast<uint8_t*>(workspace);
   uint8_t* scales = codes + rows->count * ldc;
-  const lcd_status st = launch_mx_quantize_rows(x, x_type, T, K, ldx, inv_smooth, *rows, G, codes, ldc, scales, lds, cuda_stream);
+  const lcd_status st = launch_mx_quantize_rows(x, x_type, T, K, ldx, inv_smooth, *rows, G, codes, ldc, scales, lds,
+                                                reinterpret_cast<int32_t*>(scales + rows->count * lds), cuda_stream);
   if (st != LCD_OK) return st;
   // one expert needs no distance, but the copies' description does
   const int64_t dwc = G == 1 ? N * ldwc : expert_codes, dws = G == 1 ? N * ldws : expert_scales;

@@ -124,9 +124,9 @@ constexpr int kMostGroups = 1024, kMostExperts = 512;
 // The rows of one batch that go to different weights (arguments are checked by api_groups.cu).
 lcd_status launch_group_rows(const void* group, int idx_bytes, int64_t rows, int64_t G, int32_t* order, int32_t* groups, int32_t* offsets,
                              void* stream);
-// Row i of the codes is x's row order[i] / (rows / T); rows without a group are left as they are.
+// Row i of the codes is x's row order[i] / (rows / T); rows without a group are left as they are.  place: room for as many numbers as rows.
 lcd_status launch_mx_quantize_rows(const void* x, lcd_dtype type, int64_t T, int64_t K, int64_t ldx, const float* inv, const lcd_row_groups& rows,
-                                   int64_t G, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, void* stream);
+                                   int64_t G, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, int32_t* place, void* stream);
 struct MxGrouped {
   const uint8_t *w_codes, *w_scales, *x_codes, *x_scales;      // of x: by place of the plan, written by the kernel launched directly before
   int64_t ldwc, dwc, ldws, dws, ldxc, ldxs, G, N, K;

@@ -61,9 +61,10 @@ inline cudaError_t launch_overlapping(void (*kern)(Params...), dim3 grid, dim3 b
 // Waits for the kernels before this one, and (the second) only then lets the next one begin: a kernel that has begun may take everything
 // before its direct predecessor for done.
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void begin_after_previous() {
   wait_for_previous();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  let_next_begin();
 }
 
 // Loads of what an earlier kernel of the stream writes, behind griddepcontrol.wait.  A kernel launched with programmatic

@@ -32,25 +32,27 @@ __device__ __forceinline__ Place place() {
   return {blockIdx.y * blockDim.x + threadIdx.x, (int64_t)blockIdx.x * EACH * blockDim.y + threadIdx.y};
 }
 
-// Rows by a plan: row i of the codes is row order[i] / each of x; rows from *end on are not needed.
+// Rows by a plan.  kGather: row i of the codes is row order[i] / each of x; rows from *end on are not needed.  kScatter: row m of x is quantised
+// once and written to the rows place[m * each] .. place[m * each + each - 1] of the codes, negative: nowhere.
+enum Rows { kAsTheyAre, kGather, kScatter };
 struct Gather {
-  const int32_t *order, *end;
+  const int32_t *order, *end, *place;
   int each;
 };
 
 // VEC: rows of x start on 16 bytes.
-template <typename T, bool VEC, int EACH, bool GATHER>
+template <typename T, bool VEC, int EACH, Rows ROWS>
 __global__ void __launch_bounds__(kMxThreads)
 mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc, uint8_t* scales,
                    int64_t lds, uint32_t units, Gather gather) {
   begin_after_previous();       // (no __restrict__: loads of what the kernel before wrote are coherent ones)
   const int64_t rows = M;
-  if (GATHER) {
+  if (ROWS == kGather) {
     M = min(M, (int64_t)*gather.end);
     if ((int64_t)blockIdx.x * EACH * blockDim.y >= M) return;
   }
   auto row_at = [&](int64_t row) {
-    if (!GATHER) return row;
+    if (ROWS != kGather) return row;
     const uint32_t from = (uint32_t)gather.order[row];
     return from < (uint64_t)rows ? (int64_t)(from / (uint32_t)gather.each) : (int64_t)0;
   };
@@ -113,6 +115,15 @@ mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* i
 #pragma unroll
       for (int i = 0; i < 8; ++i) t[i] = __fmul_rn(t[i], m);
       c = mx_codes8(t);
+    }
+    if (ROWS == kScatter) {
+      for (int j = 0; j < gather.each; ++j) {
+        const int64_t to = gather.place[row * gather.each + j];
+        if (to < 0) continue;
+        *reinterpret_cast<uint32_t*>(codes + to * ldc + (int64_t)at.unit * 4) = c;
+        if ((at.unit & 3u) == 0) scales[to * lds + (at.unit >> 2)] = (uint8_t)byte;
+      }
+      continue;
     }
     *reinterpret_cast<uint32_t*>(codes + row * ldc + (int64_t)at.unit * 4) = c;
     if ((at.unit & 3u) == 0) scales[row * lds + (at.unit >> 2)] = (uint8_t)byte;
@@ -197,16 +208,16 @@ Shape shape_of(int64_t rows, uint32_t units, uint32_t threads) {
   return {dim3((unsigned)((rows + per - 1) / per), columns), dim3(x, y), each};
 }
 
-template <typename T, bool GATHER = false>
+template <typename T, Rows ROWS = kAsTheyAre>
 lcd_status quantize_rows(const void* x, int64_t M, int64_t K, int64_t ldx, const float* inv, uint8_t* codes, int64_t ldc,
                          uint8_t* scales, int64_t lds, cudaStream_t s, const Gather& gather = {}) {
   const uint32_t units = (uint32_t)((K + kMxBlock - 1) / kMxBlock * 4);
-  const bool vec = on16(x, ldx, sizeof(T), GATHER ? M / gather.each : M);
+  const bool vec = on16(x, ldx, sizeof(T), ROWS == kGather ? M / gather.each : M);
   // (2048 x 5120 bf16: 128 threads 7.8 us, 256 8.9; through shared memory, 333 x 5001, 5.1 and 4.2)
   const Shape q = shape_of(M, units, vec ? kMxThreads / 2 : kMxThreads);
   if (q.grid.y > 65535) return LCD_ERR_UNSUPPORTED;
-  auto kern = vec ? (q.each ? mx_quantize_kernel<T, true, kRowsEach, GATHER> : mx_quantize_kernel<T, true, 1, GATHER>)
-                  : (q.each ? mx_quantize_kernel<T, false, kRowsEach, GATHER> : mx_quantize_kernel<T, false, 1, GATHER>);
+  auto kern = vec ? (q.each ? mx_quantize_kernel<T, true, kRowsEach, ROWS> : mx_quantize_kernel<T, true, 1, ROWS>)
+                  : (q.each ? mx_quantize_kernel<T, false, kRowsEach, ROWS> : mx_quantize_kernel<T, false, 1, ROWS>);
   return launched(launch_overlapping(kern, q.grid, q.block, 0, 1, s, static_cast<const T*>(x), M, K, ldx, inv, codes, ldc, scales, lds, units, gather));
 }
 
@@ -235,14 +246,35 @@ lcd_status launch_mx_quantize(const void* x, lcd_dtype type, int64_t M, int64_t 
   }
 }
 
+// Where a row of the plan's list stands in it, -1 for rows without a group.
+__global__ void __launch_bounds__(kMxThreads) places_kernel(const int32_t* order, const int32_t* end, int count, int32_t* place) {
+  begin_after_previous();
+  const int i = blockIdx.x * kMxThreads + threadIdx.x;
+  if (i >= count) return;
+  const uint32_t row = (uint32_t)order[i];
+  if (row < (uint32_t)count) place[row] = i < *end ? i : -1;
+}
+
+// A token of several choices is quantised once where there are many (2048 tokens of 2048 columns with four choices, bf16: 15 us of which three
+// quarters are arithmetic, four times over; the call to 4096 rows of 32 experts 88 us so, 82 with the places found first); few are not worth the launch that finds the places.
 lcd_status launch_mx_quantize_rows(const void* x, lcd_dtype type, int64_t T, int64_t K, int64_t ldx, const float* inv, const lcd_row_groups& rows,
-                                   int64_t G, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, void* stream) {
+                                   int64_t G, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, int32_t* place, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const Gather gather = {rows.order, rows.offsets + G, (int)(rows.count / T)};
+  const Gather gather = {rows.order, rows.offsets + G, place, (int)(rows.count / T)};
+  if (gather.each > 1 && rows.count * K >= (int64_t)1 << 22) {
+    const lcd_status st = launched(launch_overlapping(places_kernel, dim3((unsigned)((rows.count + kMxThreads - 1) / kMxThreads)), dim3(kMxThreads), 0, 1, s,
+                                                      rows.order, rows.offsets + G, (int)rows.count, place));
+    if (st != LCD_OK) return st;
+    switch (type) {
+      case LCD_DTYPE_F32: return quantize_rows<float, kScatter>(x, T, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+      case LCD_DTYPE_F16: return quantize_rows<__half, kScatter>(x, T, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+      default: return quantize_rows<__nv_bfloat16, kScatter>(x, T, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+    }
+  }
   switch (type) {
-    case LCD_DTYPE_F32: return quantize_rows<float, true>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
-    case LCD_DTYPE_F16: return quantize_rows<__half, true>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
-    default: return quantize_rows<__nv_bfloat16, true>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+    case LCD_DTYPE_F32: return quantize_rows<float, kGather>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+    case LCD_DTYPE_F16: return quantize_rows<__half, kGather>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
+    default: return quantize_rows<__nv_bfloat16, kGather>(x, rows.count, K, ldx, inv, codes, ldc, scales, lds, s, gather);
   }
 }
 

@@ -128,6 +128,14 @@ def test_every_width_of_tiles():
         check_experts(T, 1, 4, 130, 544, group=np.random.default_rng(T).integers(0, 4, size=T))
 
 
+@pytest.mark.parametrize("type", sorted(TYPES))
+def test_many_tokens_of_several_choices(type):
+    # a token is quantised once for its choices
+    check_experts(700, 3, 5, 96, 2048, type, smooth=True)
+    check_experts(1100, 4, 6, 40, 1001, type, pitch=1)
+    check_experts(1100, 2, 3, 40, 2016, type, group=np.full(2200, -1))
+
+
 def test_more_experts_than_a_warp_and_than_rows():
     check_experts(50, 2, 200, 40, 96)
     check_experts(2, 2, 512, 16, 64)

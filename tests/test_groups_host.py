@@ -70,14 +70,14 @@ def test_unsupported_and_short_workspaces():
     assert adapters(w=weights(rank=129, lda=64, adapter_a=64 * 129, ldb=129, adapter_b=1290)) == 2
     assert adapters(w=weights(type=2)) == 2 and grad(w=weights(type=2)) == 2              # fp16 beside bf16
     assert adapters(w=weights(G=1025)) == 2 and grad(w=weights(G=1025)) == 2
-    assert experts(bytes=6 * 48 - 1) == 3 and experts(space=None) == 3
+    assert experts(bytes=6 * 52 - 1) == 3 and experts(space=None) == 3
     assert adapters(bytes=6 * 64 - 1) == 3 and adapters(space=None) == 3 and grad(bytes=6 * 64 - 1) == 3
     need = ctypes.c_size_t()
     assert lib.lcd_adapters_workspace_bytes(6, 129, ctypes.byref(need)) == 2 and lib.lcd_adapters_workspace_bytes(0, 4, ctypes.byref(need)) == 1
     assert lib.lcd_adapters_workspace_bytes(6, 4, None) == 1 and lib.lcd_mx_linear_grouped_workspace_bytes(6, 0, ctypes.byref(need)) == 1
     for rank, padded in ((1, 16), (16, 16), (17, 32), (33, 64), (65, 128), (128, 128)):
         assert lcd.adapters_workspace_bytes(511, rank) == 511 * padded * 4 and lcd.adapters_workspace_bytes(512, rank) == 512 * padded * 10
-    assert lcd.mx_linear_grouped_workspace_bytes(6, 64) == 6 * 48
+    assert lcd.mx_linear_grouped_workspace_bytes(6, 64) == 6 * 52
 
 
 def test_binding_refuses_what_is_no_gpu_tensor():
