@@ -481,7 +481,7 @@ class RowGroups(NamedTuple):
 
 
 def group_rows(group, G: int, order=None, groups=None, offsets=None, stream=None) -> RowGroups:
-    """group: CUDA int32 or int64, one for every row (any shape, contiguous): the row's group, or anything outside [0, G) for none."""
+    """group: CUDA int32 or int64, one for every row (any shape, contiguous): the row's group, or anything outside [0, G) for none.  G is at most 1024."""
     r = (_host_calls or _calls()).group_rows(group, G, order, groups, offsets, stream)
     if r.__class__ is int:
         _check(r, "lcd_group_rows")
@@ -489,7 +489,7 @@ def group_rows(group, G: int, order=None, groups=None, offsets=None, stream=None
 
 
 def mx_linear_grouped(w_codes, w_scales, x, rows: RowGroups, inv_smooth=None, y=None, dtype=None, workspace=None, status_word=None, stream=None):
-    """A layer of G experts in microscaled 4-bit floating point.  w_codes: CUDA uint8 [G, N, 16 * blocks], w_scales uint8 [G, N, blocks], rows of
+    """A layer of G (up to 512) experts in microscaled 4-bit floating point.  w_codes: CUDA uint8 [G, N, 16 * blocks], w_scales uint8 [G, N, blocks], rows of
     both on 16 bytes as for mx_linear; x: fp32, fp16 or bf16 [T, K].  rows: the plan of the T * k pairs of a token and its choices (row p
     is token p // k), group_rows(choices [T, k], G).  y: CUDA [T * k, N], fp32 or dtype; rows without an expert are zeros.  workspace: CUDA
     scratch of at least mx_linear_grouped_workspace_bytes(T * k, K) bytes (allocated here if absent)."""
@@ -507,7 +507,7 @@ def mx_linear_grouped_workspace_bytes(count: int, K: int) -> int:
 
 def adapters(x, a, b, rows: RowGroups, base=None, y=None, scale=None, dtype=None, want_t=False, t=None, workspace=None, status_word=None,
              stream=None):
-    """y[m] = base[m] + scale[g] * (x[m] @ a[g].T) @ b[g].T, g the adapter of row m; rows without one keep base (zeros without base).
+    """y[m] = base[m] + scale[g] * (x[m] @ a[g].T) @ b[g].T, g the adapter (of rank up to 128) of row m; rows without one keep base (zeros without base).
     x: CUDA fp32, fp16 or bf16 [rows, K]; a [G, rank, K] and b [G, N, rank] of x's type or fp32 (any type if x is fp32); scale: fp32 [G];
     base: [rows, N], y's type; y: may be base itself.  Without base y has dtype, or x's type.  Returns y, and with want_t (or t given) also
     t = x a^T, fp32 [rows, rank], for adapters_grad.  workspace: CUDA scratch of at least adapters_workspace_bytes(rows, rank) bytes

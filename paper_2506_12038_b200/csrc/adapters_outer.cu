@@ -5,7 +5,7 @@
 // a lane loads CT consecutive columns and 2 RT consecutive ranks of four rows and pairs rows up with byte permutes.  Tile j's column c stands for
 // column CT c + j, m-tile i's rows c and c + 8 for ranks 2 RT c + 2 i and + 1.  t and dt go in as two or three terms (adapters.cuh).
 // The warps' sums meet in shared memory, the cluster's in distributed shared memory, in a fixed order.  Reading z bounds it.
-// For fewer rows than adapters_outer_tc.cu takes, and ranks above 64.
+// For fewer rows than adapters_outer_tc.cu takes.
 #include "adapters.cuh"
 #include "adapters_launch.h"
 

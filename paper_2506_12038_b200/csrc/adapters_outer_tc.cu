@@ -27,12 +27,13 @@ struct Shape {
   static constexpr int kStages = 6 * kStage <= 200 * 1024 ? 6 : 4 * kStage <= 200 * 1024 ? 4 : 2;
   // Groups that take stages in turn.  A stage's place belongs to the same ones every time: a wait for a parity passes two phases early, so
   // whoever fills a place has to have filled it the time before.
-  static constexpr int kZGroups = 2, kUGroups = kStages == 2 ? 2 : kStages / 2, kUWarpsEach = R == 64 ? 2 : 1;
+  static constexpr int kZGroups = R == 128 ? 1 : 2, kUGroups = kStages == 2 ? 2 : kStages / 2, kUWarpsEach = R <= 32 ? 1 : R / 32;
   static constexpr int kZWarps = 4 * kZGroups, kUWarps = kUGroups * kUWarpsEach;
   static constexpr int kMmaWarp = kZWarps + kUWarps, kFirstEpiWarp = kMmaWarp + 1, kThreads = 32 * (kFirstEpiWarp + 4);
   static constexpr int kPitch = R + 4;                                            // of a cluster's sums, fp32
   static constexpr int kSmem = 1024 + kStages * kStage + 4 * (kMostGroups + 1) + 256;
-  static constexpr int kTmem = 2 * (kSums<R> + 1) * R;
+  static constexpr int kBuffers = R == 128 ? 1 : 2;                                // sums in tensor memory: one is read while the next is made
+  static constexpr int kTmem = kBuffers * (kSums<R> + 1) * R;
   static_assert(kStages % kZGroups == 0 && kStages % kUGroups == 0 && 128 * kPitch * 4 <= kStages * kStage && kSmem <= 227 * 1024, "shapes");
   static_assert(kSmem > 114 * 1024 && kTmem <= 512, "one CTA an SM");
 };
@@ -125,8 +126,8 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
       uint32_t stage = 0, tl = 0;
       for (; w.sum < w.sums && ok; w.sum += w.step, w.n = 0, w.look()) {
         if (w.n <= 0) continue;
-        const uint32_t b = tl & 1u;
-        ok = bar_wait(d_empty(b), ((tl >> 1) & 1u) ^ 1u, abort_flag);
+        const uint32_t b = tl % S::kBuffers;
+        ok = bar_wait(d_empty(b), ((tl / S::kBuffers) & 1u) ^ 1u, abort_flag);
         for (int it = 0; it < w.n && ok; ++it, ++stage) {
           const uint32_t s = stage % S::kStages;
           ok = bar_wait(full(s), (stage / S::kStages) & 1u, abort_flag);
@@ -304,9 +305,9 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
     uint32_t tl = 0;
     for (; w.sum < w.sums && ok; w.sum += w.step, w.n = 0, w.look()) {
       const OuterSide& E = P.side[w.side];
-      const uint32_t b = tl & 1u;
+      const uint32_t b = tl % S::kBuffers;
       const bool some = w.n > 0;
-      if (some) ok = __all_sync(0xffffffffu, bar_wait(d_full(b), (tl >> 1) & 1u, abort_flag));
+      if (some) ok = __all_sync(0xffffffffu, bar_wait(d_full(b), (tl / S::kBuffers) & 1u, abort_flag));
       if (!ok) break;
       after_sync();
       const float factor = E.scale ? E.scale[w.group] : 1.0f;
@@ -416,7 +417,7 @@ bool adapters_outer_tc_takes(const OuterArgs& P, lcd_dtype z_type) {
   for (int i = 0; i < P.sides; ++i) {
     slabs += (P.side[i].columns + 127) / 128;
   }
-  return P.rows >= kManyRows && P.r <= 64 && slabs <= 0x7fffffff / kOuterSplit;
+  return P.rows >= kManyRows && slabs <= 0x7fffffff / kOuterSplit;
 }
 
 lcd_status launch_adapters_outer_tc(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s) {
@@ -427,7 +428,8 @@ lcd_status launch_adapters_outer_tc(const OuterArgs& P, lcd_dtype z_type, cudaSt
       switch (rank_tiles(P.r)) {
         case 1: return launch_shape<Z, O, 16>(P, s);
         case 2: return launch_shape<Z, O, 32>(P, s);
-        default: return launch_shape<Z, O, 64>(P, s);
+        case 4: return launch_shape<Z, O, 64>(P, s);
+        default: return launch_shape<Z, O, 128>(P, s);
       }
     });
   });

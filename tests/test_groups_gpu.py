@@ -386,7 +386,8 @@ def test_grad_of_many_rows(x, w, M, G, r, K, N):
 
 
 @pytest.mark.parametrize("x,w", PAIRS)
-@pytest.mark.parametrize("M,G,r,K,N", [(3000, 1, 16, 64, 72), (2500, 2, 40, 136, 64), (2100, 1, 8, 63, 65), (1300, 30, 32, 1000, 72)])
+@pytest.mark.parametrize("M,G,r,K,N", [(3000, 1, 16, 64, 72), (2500, 2, 40, 136, 64), (2100, 1, 8, 63, 65), (1300, 30, 32, 1000, 72), (1500, 2, 128, 200, 72),
+                                       (1100, 3, 100, 137, 65)])
 def test_grad_of_long_groups(x, w, M, G, r, K, N):
     # a sum over more rows than the stages in flight hold, several times around them; rows of one group against sums in whole numbers
     word = torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -496,6 +497,35 @@ def test_streams_devices_and_repeats():
     got = [work(s) for s in streams for _ in range(4)]
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for g in got for a, b in zip(first, g))
+
+
+@pytest.mark.parametrize("x,w,r", [("fp16", "fp16", 16), ("fp16", "fp32", 64), ("bf16", "bf16", 64), ("fp32", "fp32", 32), ("bf16", "bf16", 128)])
+def test_right_before_and_behind_products_that_begin_early(x, w, r):
+    # kernels that hold tensor memory and let the next one begin while they run, one behind the other, of several sizes
+    c = make_adapters(41, 640, 3, r, 256, 264, x, w)
+    few, many, xs = (torch.randn(n, 256, device="cuda") for n in (1, 700, 40))
+    codes, scales, _ = random_experts(9, 3, 300, 256)
+    dy, t = torch.randn(640, 264, device="cuda").to(TYPES[x]), torch.randn(640, r, device="cuda")
+    plan = lcd.group_rows(torch.arange(40, device="cuda") % 3, 3)
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def work():
+        out = []
+        for v in (few, many, xs):
+            out.append(lcd.adapters(c["x"], c["a"], c["b"], c["rows"], c["base"], scale=c["scale"], status_word=word))
+            out.append(lcd.mx_linear_fused(codes[0], scales[0], v, status_word=word))
+            out += lcd.adapters_grad(dy, c["x"], c["a"], c["b"], t, c["rows"], scale=c["scale"], status_word=word)
+            out.append(lcd.mx_linear_fused(codes[1], scales[1], v, status_word=word))
+            out.append(lcd.mx_linear_grouped(codes, scales, xs, plan, status_word=word))
+            out += lcd.adapters_grad(dy, c["x"], c["a"], c["b"], t, c["rows"], scale=c["scale"], want_dx=False, status_word=word)[1:]
+        return out
+
+    first = work()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        again = work()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, again)) and word.item() == 0
 
 
 def test_captured_and_replayed():
