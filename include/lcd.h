@@ -517,7 +517,8 @@ typedef struct {
 
 /* What the adapters of a batch's rows add to what a shared layer gave (lcd_lut_linear, lcd_mx_linear, any other):
  *     y[m] = base[m] + scale_g * (x[m] a_g^T) b_g^T, g the group of row m; rows without a group: y[m] = base[m].
- * Sums and t = x a_g^T are fp32; the result is rounded once to y's type.
+ * Sums and t = x a_g^T are fp32, products of fp32 numbers (t among them) within 2^-21 of their value, others exact; the result is rounded once to
+ * y's type.
  *   x:        device, [count][ldx], ldx >= K.  Types: x and the adapters alike, or either of them fp32 (else LCD_ERR_UNSUPPORTED);
  *   base:     device, y's type, [count][ldbase], ldbase >= N, or NULL: zeros.  May be y itself (with ldbase = ldy);
  *   y:        device out, [count][ldy], ldy >= N;

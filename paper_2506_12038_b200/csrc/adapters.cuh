@@ -7,9 +7,9 @@
 // use the same order.  With many rows registers do not hold enough loads to keep memory busy (4096 x 5120 x 13824, rank 64, bf16: 206 us
 // a call): those go through shared memory and tcgen05 (adapters_tc.cuh: 74 us).
 //
-// Arithmetic.  Two 16-bit operands of one type: their products are exact, sums are fp32.  The products with t or dt, which are fp32: with
-// bf16 beside them as two bf16 terms (16 bits, relative error 2^-16 where the result is rounded to 16-bit types) or three (24 bits, for
-// fp32 results), else as two tf32 terms (22 bits and their rounding; fp32 beside them likewise in two).
+// Arithmetic.  Two 16-bit operands of one type: their products are exact, sums are fp32.  The products with t or dt, which are fp32, whatever
+// the result's type (terms may cancel): with bf16 beside them as three bf16 terms (24 bits: exact), else as two tf32 terms (within 2^-23 of
+// the value; fp32 beside them likewise in two, the product of the rests, 2^-22, is left out).  On tcgen05 always as kPartsT bf16 terms.
 #ifndef LCD_ADAPTERS_CUH_
 #define LCD_ADAPTERS_CUH_
 
@@ -151,6 +151,11 @@ template <typename T, int N>
 __device__ __forceinline__ uint32_t pair_of(const Words<T, N>& a, const Words<T, N>& b, int i) {
   return __byte_perm(a.w[i / 2], b.w[i / 2], i % 2 ? 0x7632 : 0x5410);
 }
+
+// The bf16 parts of t and dt in the products behind them: 8 bits each.  (Two, 16 bits, left sums of cancelling terms off by 2^-16 of the
+// terms.  Times with two and with three, bf16: 4096 x 5120 x 13824, rank 64, 16 adapters 84 and 90 us, the gradient of 4096 x 5120 x 5120,
+// rank 32, 4 adapters 82 and 92.)
+constexpr int kPartsT = 3;
 
 // The plan of the rows and the adapters, as the kernels see them.
 struct AdapterArgs {

@@ -22,8 +22,7 @@ struct DownArgs {
   int window;
   float *t, *t_rows;           // by place, 16 * RT values a row; by row (may be null)
   long long ldt_rows;
-  void* t_parts;               // by place, [rows][parts][16 * RT] bf16 (may be null)
-  int parts;
+  void* t_parts;               // by place, [rows][kPartsT][16 * RT] bf16 (may be null)
   int32_t* status;
 };
 
@@ -31,10 +30,11 @@ struct DownArgs {
 __device__ __forceinline__ void store_t4(const DownArgs& P, int R, long long place, int r, const float (&v)[4]) {
   *reinterpret_cast<float4*>(P.t + place * R + r) = make_float4(v[0], v[1], v[2], v[3]);
   if (!P.t_parts) return;
-  uint2* to = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.t_parts) + place * P.parts * R + r);
+  uint2* to = reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(P.t_parts) + place * kPartsT * R + r);
   float w[4] = {v[0], v[1], v[2], v[3]};
-  for (int p = 0; p < P.parts; ++p) {
-    const bool last = p + 1 == P.parts;
+#pragma unroll
+  for (int p = 0; p < kPartsT; ++p) {
+    const bool last = p + 1 == kPartsT;
     to[p * R / 4] = last ? make_uint2(pair_rounded(w[0], w[1]), pair_rounded(w[2], w[3])) : make_uint2(pair_upper(w[0], w[1]), pair_upper(w[2], w[3]));
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = rest_of(w[i], upper_bf16(w[i]));

@@ -9,7 +9,7 @@ namespace lcd {
 struct UpArgs {
   AdapterArgs a;
   const float* t;              // by place, 16 * RT values a row
-  const void* t_parts;         // the same as bf16 parts, [rows][parts][16 * RT], where adapters_up_tc_parts says so
+  const void* t_parts;         // the same as bf16 parts, [rows][kPartsT][16 * RT]: the products for many rows run
   const void* base;            // or null
   void* y;
   long long ldbase, ldy;

@@ -3,7 +3,7 @@
 // A CTA has a slab of 8 CT columns of z (x or dy) and one adapter; its warps, and the CTAs of a cluster where there are few slabs, take
 // sixteen of the adapter's rows in turn.  The ranks are the 16 rows of mma.sync, the columns its 8, the sum runs over the batch's rows:
 // a lane loads CT consecutive columns and 2 RT consecutive ranks of four rows and pairs rows up with byte permutes.  Tile j's column c stands for
-// column CT c + j, m-tile i's rows c and c + 8 for ranks 2 RT c + 2 i and + 1.  t and dt go in as two or three terms (adapters.cuh).
+// column CT c + j, m-tile i's rows c and c + 8 for ranks 2 RT c + 2 i and + 1.  t and dt go in as terms (adapters.cuh).
 // The warps' sums meet in shared memory, the cluster's in distributed shared memory, in a fixed order.  Reading z bounds it.
 // For fewer rows than adapters_outer_tc.cu takes.
 #include "adapters.cuh"
@@ -36,7 +36,6 @@ __global__ void __launch_bounds__(32 * kOuterWarps) adapters_outer_kernel(const 
   const long long col0 = slab / halves * kColumns;
   const int from = max(0, min(P.rows, P.offsets[group])), to = max(from, min(P.rows, P.offsets[group + 1]));
   const int columns = (int)max(0ll, min((long long)CT, S.columns - col0 - CT * g)), ranks = max(0, min(2 * RT, P.r - r0 - 2 * RT * g));
-  const int three = P.out_type == LCD_DTYPE_F32;
 
   float acc[RT][CT][4];
 #pragma unroll
@@ -69,29 +68,22 @@ __global__ void __launch_bounds__(32 * kOuterWarps) adapters_outer_kernel(const 
       }
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        uint32_t a[3][4];
+        uint32_t a[kPartsT][4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           float x0 = value_of(f.u[2 * (q / 2)], 2 * i + q % 2), x1 = value_of(f.u[2 * (q / 2) + 1], 2 * i + q % 2);
-          a[0][q] = pair_upper(x0, x1);
-          x0 = rest_of(x0, upper_bf16(x0));
-          x1 = rest_of(x1, upper_bf16(x1));
-          if (three) {
-            a[1][q] = pair_upper(x0, x1);
-            a[2][q] = pair_rounded(rest_of(x0, upper_bf16(x0)), rest_of(x1, upper_bf16(x1)));
-          } else {
-            a[1][q] = pair_rounded(x0, x1);
+#pragma unroll
+          for (int term = 0; term < kPartsT - 1; ++term) {
+            a[term][q] = pair_upper(x0, x1);
+            x0 = rest_of(x0, upper_bf16(x0));
+            x1 = rest_of(x1, upper_bf16(x1));
           }
+          a[kPartsT - 1][q] = pair_rounded(x0, x1);
         }
 #pragma unroll
-        for (int j = 0; j < CT; ++j) {
-          mma16<Z>(acc[i][j], a[0][0], a[0][1], a[0][2], a[0][3], b[j][0], b[j][1]);
-          mma16<Z>(acc[i][j], a[1][0], a[1][1], a[1][2], a[1][3], b[j][0], b[j][1]);
-        }
-        if (three) {
+        for (int term = 0; term < kPartsT; ++term)
 #pragma unroll
-          for (int j = 0; j < CT; ++j) mma16<Z>(acc[i][j], a[2][0], a[2][1], a[2][2], a[2][3], b[j][0], b[j][1]);
-        }
+          for (int j = 0; j < CT; ++j) mma16<Z>(acc[i][j], a[term][0], a[term][1], a[term][2], a[term][3], b[j][0], b[j][1]);
       }
     } else {
 #pragma unroll

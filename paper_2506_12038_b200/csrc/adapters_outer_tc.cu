@@ -8,8 +8,8 @@
 // cluster's CTAs share one's rows and add up in distributed shared memory, in the order of the ranks.  Reading z bounds it.
 // Roles: kZWarps warps bring z and kUWarps t or dt, in groups that take stages in turn (finding a stage's rows and addresses takes longer than
 // its bytes), one owns tensor memory and an elected lane issues the MMAs, four store.
-// Rank 128 has one sum in tensor memory, which the next waits for: 4096 x 4096 x 4096, bf16, 93 us for one adapter and 122 for 16
-// (adapters_outer.cu 286 and 445); 512 rows 50 and 85 (67 and 286); fp32, 4096 rows, 206 and 255 (417 and 646).
+// Rank 128 has one sum in tensor memory, which the next waits for: 4096 x 4096 x 4096, bf16, 97 us for one adapter and 128 for 16
+// (adapters_outer.cu 286 and 445 with two parts of u); fp32, 4096 rows, 206 and 255 (417 and 646).
 #include "adapters_launch.h"
 #include "adapters_tc.cuh"
 
@@ -21,15 +21,16 @@ using namespace tc;
 
 constexpr int kStageRows = 64, kOuterSplit = 8;
 
-template <typename Z, typename O, int R>
+template <typename Z, int R>
 struct Shape {
-  static constexpr int kParts_u = kPartsFor<Z, O>, kParts_z = kParts<Z> < kParts_u ? kParts<Z> : kParts_u;
+  static constexpr int kParts_u = kPartsT, kParts_z = kParts<Z>;
   static constexpr int kZPart = 2 * kStageRows * 128, kUPart = (R + 63) / 64 * kStageRows * 128;
   static constexpr int kStage = kParts_z * kZPart + kParts_u * kUPart;
   static constexpr int kStages = 6 * kStage <= 200 * 1024 ? 6 : 4 * kStage <= 200 * 1024 ? 4 : 2;
   // Groups that take stages in turn.  A stage's place belongs to the same ones every time: a wait for a parity passes two phases early, so
-  // whoever fills a place has to have filled it the time before.
-  static constexpr int kZGroups = R == 128 ? 1 : 2, kUGroups = kStages == 2 ? 2 : kStages / 2, kUWarpsEach = R <= 32 ? 1 : R / 32;
+  // whoever fills a place has to have filled it the time before.  (Four places: two groups for u 71 us at 4096 x 5120 x 5120, rank 32, bf16, four
+  // 64; rank 64 103 and 94.)
+  static constexpr int kZGroups = R == 128 ? 1 : 2, kUGroups = kStages == 6 ? 3 : kStages, kUWarpsEach = R <= 32 ? 1 : R / 32;
   static constexpr int kZWarps = 4 * kZGroups, kUWarps = kUGroups * kUWarpsEach;
   static constexpr int kMmaWarp = kZWarps + kUWarps, kFirstEpiWarp = kMmaWarp + 1, kThreads = 32 * (kFirstEpiWarp + 4);
   static constexpr int kPitch = R + 4;                                            // of a cluster's sums, fp32
@@ -76,8 +77,8 @@ struct Walk {
 };
 
 template <typename Z, typename O, int R>
-__global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc_kernel(const __grid_constant__ OuterArgs P) {
-  using S = Shape<Z, O, R>;
+__global__ void __launch_bounds__(Shape<Z, R>::kThreads, 1) adapters_outer_tc_kernel(const __grid_constant__ OuterArgs P) {
+  using S = Shape<Z, R>;
   constexpr bool kCopied = S::kParts_z == 1;
   extern __shared__ uint8_t smem_raw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -389,7 +390,7 @@ __global__ void __launch_bounds__(Shape<Z, O, R>::kThreads, 1) adapters_outer_tc
 
 template <typename Z, typename O, int R>
 lcd_status launch_shape(OuterArgs P, cudaStream_t s) {
-  using S = Shape<Z, O, R>;
+  using S = Shape<Z, R>;
   auto kern = adapters_outer_tc_kernel<Z, O, R>;
   static PerDeviceFlag attr_set;
   int dev;

@@ -3,7 +3,7 @@
 // Operands are tiles of rows of 128 bytes in shared memory, 64 16-bit values a row, with the 128-byte swizzle (a 16-byte piece's number exclusive-or
 // the row's in its group of eight).  The same tile serves as a K-major operand (a row is a row of the operand, 16 columns of K are 32 bytes
 // further) or as an MN-major one (a row is a column of K: 16 of them are 2048 bytes further), so nothing is transposed: what the sum
-// runs over is told to the instruction.  fp32 and fp16 operands that meet t or dt go in as two or three bf16 parts, in tiles of their own.
+// runs over is told to the instruction.  t and dt, and fp32 and fp16 operands that meet them, go in as two or three bf16 parts, in tiles of their own.
 #ifndef LCD_ADAPTERS_TC_CUH_
 #define LCD_ADAPTERS_TC_CUH_
 
@@ -121,10 +121,6 @@ __device__ __forceinline__ void parts_of(float (&v)[8], uint4 (&out)[PARTS]) {
 }
 // The parts that a type's values take: bf16 is one, fp16 two (11 bits), fp32 three.
 template <typename T> constexpr int kParts = std::is_same<T, __nv_bfloat16>::value ? 1 : std::is_same<T, __half>::value ? 2 : 3;
-
-// The parts of t and dt beside an operand of type T for a result of type O: two where both are bf16 (2^-16 of a term is left out, half a step
-// of the result is 2^-9), else three.
-template <typename T, typename O> constexpr int kPartsFor = std::is_same<T, __nv_bfloat16>::value && std::is_same<O, __nv_bfloat16>::value ? 2 : 3;
 
 // How many CTAs of a cluster share the stages of a sum, when `tiles` sums of `stages` stages each run on `slots` places at a time: what takes least
 // time if starting and joining takes as long as six stages.

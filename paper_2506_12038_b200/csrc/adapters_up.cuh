@@ -2,7 +2,7 @@
 //
 // A warp has 8 CT columns (eight MMA tiles of eight, four or two where the rank is large) of a window of consecutive places of the plan.
 // It keeps its part of the adapter matrix in registers as the MMAs' B operand for all rows of an adapter; rows are the A operand, 16 at a
-// time, t in two or three terms (adapters.cuh).  Tile j's column c stands for column CT c + j, so that a lane ends up with 2 CT consecutive
+// time, t in terms (adapters.cuh).  Tile j's column c stands for column CT c + j, so that a lane ends up with 2 CT consecutive
 // columns of two rows, which it adds to the base's and stores.  The next rows' base and t are on their way meanwhile.
 // Reading base, writing y bounds it, with few rows latency: the plan, then the matrix and base, then t (64 rows of 48 adapters to 11008 columns,
 // rank 16, bf16: 14 us with cold caches, bytes 3).  It begins while the kernel that makes t ends: the adapter matrix and the first base are loaded before.
@@ -54,7 +54,6 @@ template <typename W, typename Y, int RT, bool TRANSPOSED, bool ONE>
 __global__ void __launch_bounds__(32 * kUpWarps, ONE && RT == 1 ? 4 : ONE && RT == 2 ? 3 : 1) adapters_up_kernel(const UpArgs P) {
   constexpr int CT = kUpTiles<W, RT>, R = 16 * RT, kOwn = 2 * CT;       // columns of a lane
   constexpr bool kBf16 = std::is_same<W, __nv_bfloat16>::value;
-  constexpr int kTerms = kBf16 && sizeof(Y) == 4 ? 3 : 2;
   __shared__ float s_out[kUpWarps][16][8 * CT + 1];
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const long long col0 = ((long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * 8 * CT;
@@ -180,20 +179,20 @@ __global__ void __launch_bounds__(32 * kUpWarps, ONE && RT == 1 ? 4 : ONE && RT 
           for (int i = 0; i < RT; ++i) {
             if constexpr (kBf16) {
               // words of ranks (4 i, 4 i + 1) of both rows, then (4 i + 2, 4 i + 3)
-              uint32_t a[kTerms][4];
+              uint32_t a[kPartsT][4];
 #pragma unroll
               for (int q = 0; q < 4; ++q) {
                 float x0 = v[q % 2][4 * i + 2 * (q / 2)], x1 = v[q % 2][4 * i + 2 * (q / 2) + 1];
 #pragma unroll
-                for (int term = 0; term < kTerms - 1; ++term) {
+                for (int term = 0; term < kPartsT - 1; ++term) {
                   a[term][q] = pair_upper(x0, x1);
                   x0 = rest_of(x0, upper_bf16(x0));
                   x1 = rest_of(x1, upper_bf16(x1));
                 }
-                a[kTerms - 1][q] = pair_rounded(x0, x1);
+                a[kPartsT - 1][q] = pair_rounded(x0, x1);
               }
 #pragma unroll
-              for (int term = 0; term < kTerms; ++term)
+              for (int term = 0; term < kPartsT; ++term)
 #pragma unroll
                 for (int j = 0; j < CT; ++j) mma16<__nv_bfloat16>(d[j], a[term][0], a[term][1], a[term][2], a[term][3], b[j][2 * i], b[j][2 * i + 1]);
             } else {

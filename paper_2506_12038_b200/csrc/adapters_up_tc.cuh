@@ -28,8 +28,7 @@ constexpr int kMostSmem = 227 * 1024;
 
 template <typename W, typename Y, int R, bool TRANSPOSED>
 struct Shape {
-  // (a third part of the matrix is smaller than what two parts of t leave out)
-  static constexpr int kParts_t = kPartsFor<W, Y>, kParts_w = kParts<W> < kParts_t ? kParts<W> : kParts_t, kSteps = R / 16;
+  static constexpr int kParts_t = kPartsT, kParts_w = kParts<W>, kSteps = R / 16;
   // t: [128 rows][parts][R], in blocks of 64 columns
   static constexpr int kT = (kParts_t * R + 63) / 64 * 128 * 128;
   static constexpr int w_bytes(int nc) { return TRANSPOSED ? nc / 64 * kParts_w * R * 128 : (kParts_w * R + 63) / 64 * nc * 128; }

@@ -74,13 +74,12 @@ lcd_status up(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type, bool transpos
     default: return tc ? launch_adapters_up_tc_bf16(u, y_type, transposed, s) : launch_adapters_up_bf16(u, y_type, transposed, s);
   }
 }
-// The bf16 parts of t that the products for many rows need, 0 where the others run.
-int parts_of_t(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type) {
-  if (u.a.rows < kManyRows || ((int64_t)u.a.rows / 128 + u.a.G + 1) * ((u.a.K + 63) / 64) > 0x7fffffff) return 0;
-  if (u.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return 0;      // the parts do not fit into shared memory
+// Whether the products for many rows run, which take t in bf16 parts.
+bool takes_parts_of_t(const UpArgs& u, lcd_dtype w_type, lcd_dtype y_type) {
+  if (u.a.rows < kManyRows || ((int64_t)u.a.rows / 128 + u.a.G + 1) * ((u.a.K + 63) / 64) > 0x7fffffff) return false;
+  if (u.a.r > 64 && (w_type != LCD_DTYPE_BF16 || y_type == LCD_DTYPE_F32)) return false;      // the parts do not fit into shared memory
   const int64_t size = size_of(y_type);
-  if (u.a.rows < 2 * kManyRows && !(on_bytes(u.y, u.ldy, u.a.K, size, 16) && on_bytes(u.base, u.ldbase, u.a.K, size, 16))) return 0;
-  return w_type == LCD_DTYPE_BF16 && y_type == LCD_DTYPE_BF16 ? 2 : 3;
+  return u.a.rows >= 2 * kManyRows || (on_bytes(u.y, u.ldy, u.a.K, size, 16) && on_bytes(u.base, u.ldbase, u.a.K, size, 16));
 }
 
 }  // namespace
@@ -166,8 +165,7 @@ extern "C" lcd_status lcd_adapters(const lcd_adapter_weights* weights, const voi
   u.ldy = ldy;
   u.early = 1;
   u.status = status_word_dev;
-  d.parts = parts_of_t(u, weights->type, y_type);
-  u.t_parts = d.t_parts = d.parts ? d.t + rows->count * padded_rank(weights->rank) : nullptr;
+  u.t_parts = d.t_parts = takes_parts_of_t(u, weights->type, y_type) ? d.t + rows->count * padded_rank(weights->rank) : nullptr;
   st = down(d, x_type, weights->type, false, cuda_stream);
   if (st != LCD_OK) return st;
   return up(u, weights->type, y_type, false, cuda_stream);
@@ -211,8 +209,7 @@ extern "C" lcd_status lcd_adapters_grad(const lcd_adapter_weights* weights, cons
     d.ldx = lddy;
     d.t = dt;
     d.status = status_word_dev;
-    d.parts = dx ? parts_of_t(u, weights->type, type) : 0;
-    u.t_parts = d.t_parts = d.parts ? dt + rows->count * padded_rank(weights->rank) : nullptr;
+    u.t_parts = d.t_parts = dx && takes_parts_of_t(u, weights->type, type) ? dt + rows->count * padded_rank(weights->rank) : nullptr;
     st = down(d, type, weights->type, true, cuda_stream);
     if (st != LCD_OK) return st;
   }
