@@ -33,7 +33,7 @@ __device__ __forceinline__ Place place() {
 }
 
 // Rows by a plan.  kGather: row i of the codes is row order[i] / each of x; rows from *end on are not needed.  kScatter: row m of x is quantised
-// once and written to the rows place[m * each] .. place[m * each + each - 1] of the codes, negative: nowhere.
+// once and written to the rows place[m * each] .. place[m * each + each - 1] of the codes, beyond them: nowhere.
 enum Rows { kAsTheyAre, kGather, kScatter };
 struct Gather {
   const int32_t *order, *end, *place;
@@ -118,8 +118,8 @@ mx_quantize_kernel(const T* x, int64_t M, int64_t K, int64_t ldx, const float* i
     }
     if (ROWS == kScatter) {
       for (int j = 0; j < gather.each; ++j) {
-        const int64_t to = gather.place[row * gather.each + j];
-        if (to < 0) continue;
+        const int64_t to = (uint32_t)gather.place[row * gather.each + j];
+        if (to >= rows * gather.each) continue;                   // without a group, or never set: a foreign plan need not name every row
         *reinterpret_cast<uint32_t*>(codes + to * ldc + (int64_t)at.unit * 4) = c;
         if ((at.unit & 3u) == 0) scales[to * lds + (at.unit >> 2)] = (uint8_t)byte;
       }
