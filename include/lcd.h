@@ -491,7 +491,7 @@ lcd_status lcd_group_rows(const void* group, int idx_bytes, int64_t count, int64
  * its k choices, row p belongs to token p / k, and
  *     y[p][n] = sum over k of x^[p / k][k] * w^[group of p][n][k],
  * x^ being what lcd_mx_quantize makes of x and inv_smooth; sums in fp32, rounded once to y's type.  Rows without a group: zeros.
- *   1 <= G <= 512 (more: LCD_ERR_UNSUPPORTED);
+ *   1 <= G <= 512 (more: LCD_ERR_UNSUPPORTED);  1 <= N, K <= 2^30;
  *   w_codes:  device, [G] matrices as lcd_mx_linear takes them, N rows each, expert_codes bytes apart (a multiple of 16);  w_scales likewise;
  *   x:        device, [T][ldx], ldx >= K, count a multiple of T;     inv_smooth: device fp32 [K] or NULL, for all experts;
  *   y:        device out, [count][ldy], ldy >= N;     status_word_dev: as for lcd_lut_linear;
@@ -506,7 +506,7 @@ lcd_status lcd_mx_linear_grouped(const uint8_t* w_codes, int64_t ldwc, int64_t e
                                  int64_t ldx, const float* inv_smooth, const lcd_row_groups* rows /* host struct */, void* y, lcd_dtype y_type,
                                  int64_t ldy, void* workspace, size_t workspace_bytes, int32_t* status_word_dev, void* cuda_stream);
 
-/* G low-rank adapters of one layer.  1 <= rank <= 128 (more: LCD_ERR_UNSUPPORTED). */
+/* G low-rank adapters of one layer.  1 <= G <= 1024, 1 <= rank <= 128 (more: LCD_ERR_UNSUPPORTED), 1 <= N, K <= 2^30. */
 typedef struct {
   const void* a;          /* device, [G][rank][K]: rows lda elements apart, adapters adapter_a elements apart */
   const void* b;          /* device, [G][N][rank]: rows ldb elements apart, adapters adapter_b elements apart */
