@@ -70,7 +70,7 @@ struct Words {
   uint32_t w[kCount];
 };
 // The same at any alignment: the aligned words around them, then shifted (apart, so that several rows' loads are on their way together).
-// Sixteen bytes of the row on either side are there.
+// The row has 16 bytes before them, and kCount words from their first on.
 template <typename T, int N>
 struct Around {
   static constexpr int kCount = (Words<T, N>::kCount + 3) / 4 * 4 + 4;

@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(32 * kUpWarps, ONE && RT == 1 ? 4 : ONE && RT 
   const long long own0 = col0 + kOwn * t;
   const int have = (int)max(0ll, min((long long)kOwn, P.a.K - own0));
   constexpr int kSide = 16 / sizeof(Y);
-  const bool inside = have >= kOwn && own0 >= kSide && own0 + kOwn + kSide <= P.a.K;
+  const bool inside = have >= kOwn && own0 >= kSide && own0 + Around<Y, kOwn>::kCount * 4 / (int)sizeof(Y) <= P.a.K;
   const int place0 = blockIdx.y * P.window, end = min(P.a.rows, place0 + P.window);
   if (!P.early) begin_after_previous();
   bool waited = !P.early;
