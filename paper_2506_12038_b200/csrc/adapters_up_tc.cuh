@@ -107,6 +107,8 @@ __global__ void __launch_bounds__(kThreads, 1) adapters_up_tc_kernel(const UpArg
         const bool inside = piece * 16 < columns_of(c0) * (int)sizeof(Y);
         const Y* from = static_cast<const Y*>(P.base) + c0 + piece * (16 / (int)sizeof(Y));
         look(tile + 1);
+        // Both buffers are on their way, the next waits for the epilogue: its time does not start before the kernel before this one has ended.
+        if (it == 2) begin_after_previous();
         ok = __all_sync(0xffffffffu, bar_wait(y_empty(b), ((it >> 1) & 1u) ^ 1u, abort_flag));
         if (!ok) break;
         const uint32_t to = at_y + (b * 128 + 32 * warp + lane / kPieces) * S::kPitch + piece * 16;
