@@ -520,7 +520,8 @@ typedef struct {
  * Sums and t = x a_g^T are fp32, products of fp32 numbers (t among them) within 2^-21 of their value, others exact; the result is rounded once to
  * y's type.
  *   x:        device, [count][ldx], ldx >= K.  Types: x and the adapters alike, or either of them fp32 (else LCD_ERR_UNSUPPORTED);
- *   base:     device, y's type, [count][ldbase], ldbase >= N, or NULL: zeros.  May be y itself (with ldbase = ldy);
+ *   base:     device, y's type, [count][ldbase], ldbase >= N, or NULL: zeros.  May be y itself (with ldbase = ldy); then rows without a
+ *             group are not touched;
  *   y:        device out, [count][ldy], ldy >= N;
  *   t:        device out, fp32 [count][ldt], ldt >= rank, or NULL: t, for lcd_adapters_grad (rows without a group: zeros);
  *   workspace: device scratch of lcd_adapters_workspace_bytes(count, rank) bytes, 16-byte aligned, contents ignored; calls that may overlap on the

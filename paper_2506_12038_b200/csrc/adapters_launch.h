@@ -13,7 +13,8 @@ struct UpArgs {
   const void* base;            // or null
   void* y;
   long long ldbase, ldy;
-  int window, wide_base, wide_y, in_place;
+  int window, wide_base, wide_y;
+  int in_place;                // y is base: rows without an adapter are left alone
   int32_t* status;
   int early;                   // the kernel before this one wrote t and nothing else that is read here, and began when all before it was done
 };

@@ -403,6 +403,7 @@ lcd_status launch_up_tc_types(UpArgs P, cudaStream_t s) {
   P.a.wide_w = on_bytes(P.a.w, P.a.ldw, P.a.sw, sizeof(W), 16);
   P.wide_base = on_bytes(P.base, P.ldbase, P.a.K, sizeof(Y), 16);
   P.wide_y = on_bytes(P.y, P.ldy, P.a.K, sizeof(Y), 16) ? on_bytes(P.y, P.ldy, 0, sizeof(Y), 32) ? 32 : 16 : 0;
+  P.in_place = P.base == P.y && P.ldbase == P.ldy;
   const bool wide = P.wide_base && P.wide_y;
   return by_rank(P.a.r, [&](auto rt) {
     constexpr int R = 16 * decltype(rt)::value;
