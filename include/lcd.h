@@ -506,6 +506,11 @@ lcd_status lcd_mx_linear_grouped(const uint8_t* w_codes, int64_t ldwc, int64_t e
                                  int64_t ldx, const float* inv_smooth, const lcd_row_groups* rows /* host struct */, void* y, lcd_dtype y_type,
                                  int64_t ldy, void* workspace, size_t workspace_bytes, int32_t* status_word_dev, void* cuda_stream);
 
+/* Which of its forms lcd_mx_linear_grouped runs for these sizes on the current device: tiles of tile_tokens tokens (16, 32, 64, 128, 192 or
+ * 256) of 128 weight rows, or of 256 by a pair of CTAs (paired = 1); the columns of a tile are cut among split CTAs. */
+lcd_status lcd_mx_linear_grouped_resolve(int64_t count, int64_t G, int64_t N, int64_t K, int* tile_tokens /* host out */,
+                                         int* split /* host out */, int* paired /* host out */);
+
 /* G low-rank adapters of one layer.  1 <= G <= 1024, 1 <= rank <= 128 (more: LCD_ERR_UNSUPPORTED), 1 <= N, K <= 2^30. */
 typedef struct {
   const void* a;          /* device, [G][rank][K]: rows lda elements apart, adapters adapter_a elements apart */

@@ -35,7 +35,7 @@ EXPORTS = ["lcd_status_string", "lcd_last_cuda_error", "lcd_packed_weights_bytes
            "lcd_smoothing_search_workspace_bytes", "lcd_smoothing_search", "lcd_reclassify",
            "lcd_dbci_workspace_bytes", "lcd_dbci", "lcd_mx_quantize", "lcd_mx_dequantize", "lcd_mx_linear",
            "lcd_mx_linear_fused_workspace_bytes", "lcd_mx_linear_fused", "lcd_distill_loss", "lcd_distill_grad",
-           "lcd_group_rows", "lcd_mx_linear_grouped_workspace_bytes", "lcd_mx_linear_grouped", "lcd_adapters_workspace_bytes",
+           "lcd_group_rows", "lcd_mx_linear_grouped_workspace_bytes", "lcd_mx_linear_grouped_resolve", "lcd_mx_linear_grouped", "lcd_adapters_workspace_bytes",
            "lcd_adapters", "lcd_adapters_grad"]
 STATIC_SCRATCH_BYTES = 4 << 20
 
@@ -142,6 +142,7 @@ def _load() -> ctypes.CDLL:
     rows, adapters = POINTER(RowGroupsC), POINTER(AdapterWeights)
     lib.lcd_group_rows.argtypes = [c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.lcd_mx_linear_grouped_workspace_bytes.argtypes = [c_int64, c_int64, POINTER(c_size_t)]
+    lib.lcd_mx_linear_grouped_resolve.argtypes = [c_int64] * 4 + [POINTER(c_int)] * 3
     lib.lcd_mx_linear_grouped.argtypes = [c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int64, c_int64] + matrix + [
         c_int64, c_int64, c_void_p, rows] + matrix + [c_int64, c_void_p, c_size_t, c_void_p, c_void_p]
     lib.lcd_adapters_workspace_bytes.argtypes = [c_int64, c_int64, POINTER(c_size_t)]
@@ -503,6 +504,14 @@ def mx_linear_grouped_workspace_bytes(count: int, K: int) -> int:
     out = c_size_t(0)
     _check(lib.lcd_mx_linear_grouped_workspace_bytes(count, K, byref(out)), "lcd_mx_linear_grouped_workspace_bytes")
     return out.value
+
+
+def resolve_mx_linear_grouped(count: int, G: int, N: int, K: int) -> tuple:
+    """The form of mx_linear_grouped that runs for count rows of G experts on the current device: (tokens of a tile, CTAs that share a tile's
+    columns, whether pairs of CTAs take a tile)."""
+    tokens, split, paired = c_int(0), c_int(0), c_int(0)
+    _check(lib.lcd_mx_linear_grouped_resolve(count, G, N, K, byref(tokens), byref(split), byref(paired)), "lcd_mx_linear_grouped_resolve")
+    return tokens.value, split.value, bool(paired.value)
 
 
 def adapters(x, a, b, rows: RowGroups, base=None, y=None, scale=None, dtype=None, want_t=False, t=None, workspace=None, status_word=None,

@@ -102,6 +102,16 @@ extern "C" lcd_status lcd_mx_linear_grouped_workspace_bytes(int64_t count, int64
   return LCD_OK;
 }
 
+extern "C" lcd_status lcd_mx_linear_grouped_resolve(int64_t count, int64_t G, int64_t N, int64_t K, int* tile_tokens, int* split, int* paired) {
+  if (!counted(count) || G < 1 || N < 1 || N > kMostColumns || K < 1 || K > kMostColumns || !tile_tokens || !split || !paired) return LCD_ERR_INVALID_ARG;
+  if (G > kMostExperts) return LCD_ERR_UNSUPPORTED;
+  const MxGroupedShape s = mx_grouped_shape(count, G, N, K);
+  *tile_tokens = s.width;
+  *split = s.split;
+  *paired = s.pair;
+  return LCD_OK;
+}
+
 extern "C" lcd_status lcd_mx_linear_grouped(const uint8_t* w_codes, int64_t ldwc, int64_t expert_codes, const uint8_t* w_scales, int64_t ldws,
                                             int64_t expert_scales, int64_t G, int64_t N, int64_t K, const void* x, lcd_dtype x_type, int64_t T,
                                             int64_t ldx, const float* inv_smooth, const lcd_row_groups* rows, void* y, lcd_dtype y_type,

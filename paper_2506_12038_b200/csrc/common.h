@@ -136,6 +136,8 @@ struct MxGrouped {
   int64_t ldy;
 };
 lcd_status launch_mx_grouped(const MxGrouped& p, int32_t* status_word, void* stream);
+struct MxGroupedShape { int width, split; bool pair; };
+MxGroupedShape mx_grouped_shape(int64_t count, int64_t G, int64_t N, int64_t K);
 struct Distillation {
   const void* logits;
   lcd_dtype type;

@@ -1386,10 +1386,15 @@ lcd_status launch_mx_linear(const MxProduct& p, bool x_just_written, int32_t* st
   }
 }
 
+MxGroupedShape mx_grouped_shape(int64_t count, int64_t G, int64_t N, int64_t K) {
+  const Plan w = plan_grouped(count, G, N, ((K + kMxBlock - 1) / kMxBlock * kMxBlock + kStageK - 1) / kStageK);
+  return {w.width, w.split, w.pair};
+}
+
 lcd_status launch_mx_grouped(const MxGrouped& p, int32_t* status_word, void* stream) {
   if (p.G > kMostExperts) return LCD_ERR_UNSUPPORTED;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const Plan w = plan_grouped(p.rows.count, p.G, p.N, ((p.K + kMxBlock - 1) / kMxBlock * kMxBlock + kStageK - 1) / kStageK);
+  const MxGroupedShape w = mx_grouped_shape(p.rows.count, p.G, p.N, p.K);
   if (w.pair) return w.width == 192 ? launch_grouped<192, true>(p, 1, status_word, s) : launch_grouped<256, true>(p, 1, status_word, s);
   switch (w.width) {
     case 16: return launch_grouped<16, false>(p, w.split, status_word, s);
