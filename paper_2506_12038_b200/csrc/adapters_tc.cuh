@@ -175,10 +175,12 @@ __device__ __forceinline__ void by_split(uint32_t split, F&& f) {
     default: f(std::integral_constant<int, 8>{});
   }
 }
-// Long sums.  An MMA adds to the fp32 sum and cuts off, toward zero, so a sum of n of them is short by up to n 2^-24 of itself.  So the stages
+// Long sums.  An MMA adds to the fp32 sum and cuts off, toward zero, so a sum of n of them is short by up to n 2^-23 of itself.  So the stages
 // go to several accumulators in turn, as many as tensor memory has room for, and the products of the parts behind the first to one more, a
 // smaller one; they are added when they are read.  Relative error of da, 512 rows of 4096 columns, fp16 with fp32 adapters: 5.3e-6 with one
-// accumulator, 2.0e-7 with eight; of x a^T, 8192 columns, fp32: 3.1e-5 and 7.2e-7 (plain fp32 sums 7.1e-7 and 1.6e-6).  Times are the same.
+// accumulator, 2.0e-7 with eight; of x a^T over 8192 columns, fp32: 3.1e-5 and 7.2e-7 (plain fp32 sums 7.1e-7 and 1.6e-6).  Times are the same.
+// With three accumulators, ranks above 32: over 8192 columns fp32 1.5e-6 and bf16 0.6e-6 (rank 64) to 1.4e-6 (rank 128; plain fp32 sums 1.6e-6 and
+// 1.0e-6), over 32768 6.5e-6 and 2.9e-6 to 6.0e-6 (3.2e-6 and 2.3e-6); da over 32768 rows 1.4e-6 to 1.6e-6 (0.8e-6).
 template <int R> constexpr int kSums = R <= 32 ? 7 : 3;
 // Sixteen columns of the accumulators of a sum, R columns apart, added up: the first `used` of the kSums, and the one more.
 template <int R>

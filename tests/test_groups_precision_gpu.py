@@ -57,3 +57,26 @@ def test_t_and_dt_enter_the_gradients_with_all_their_bits(x, w, M, N, K, r):
         assert torch.equal(dx.double(), wanted((M, K), {0: REST}))
         assert torch.equal(da.double(), wanted((1, r, K), {(0, 0): REST}))
         assert (lcd.adapters_grad(sums, xs, a, b, t, rows, grad_dtype=out, want_dx=False)[2].double() == REST).all()
+
+
+@pytest.mark.parametrize("x,w", [("fp32", "fp32"), ("fp16", "fp16"), ("bf16", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("r,most", [(16, 76), (40, 172), (64, 172), (128, 172)])
+@pytest.mark.parametrize("positive", [False, True])
+def test_long_sums_of_every_rank(x, w, r, most, positive):
+    # 8192 terms: 128 stages of four instructions, in turn to seven accumulators (ranks to 32) or three: `most` additions one after the other, each of
+    # which cuts off less than a step of its sum, 2^-23 of it.  Accumulators and parts are joined by ten additions at most (10 * 2^-24) and products
+    # of fp32 numbers are within 2^-21: together less than 2^-19.  Signed terms cancel: there errors are shares of the terms' root of squares, which
+    # the random walk of a sum does not exceed by more than a few times; all positive ones they are shares of the sum itself.
+    g = torch.Generator(device="cuda").manual_seed(r)
+    M = K = 8192
+    draw = (lambda *s: torch.rand(*s, generator=g, device="cuda")) if positive else (lambda *s: torch.randn(*s, generator=g, device="cuda"))
+    xs, dy, t = draw(M, K).to(TYPES[x]), draw(M, 64).to(TYPES[x]), draw(M, r)
+    a, b = draw(1, r, K).to(TYPES[w]), draw(1, 64, r).to(TYPES[w])
+    rows = lcd.group_rows(torch.zeros(M, dtype=torch.int32, device="cuda"), 1)
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    _, got_t = lcd.adapters(xs, a, b, rows, want_t=True, dtype=torch.float32, status_word=word)
+    _, da, db = lcd.adapters_grad(dy, xs, a, b, t, rows, want_dx=False, grad_dtype=torch.float32, status_word=word)
+    want_t, dt = xs.double() @ a[0].double().t(), dy.double() @ b[0].double()
+    for got, want in ((got_t, want_t), (da[0], dt.t() @ xs.double()), (db[0], dy.double().t() @ t.double())):
+        assert (got.double() - want).norm() <= (most * 2.0 ** -23 + 2.0 ** -19) * want.norm()
+    assert word.item() == 0
