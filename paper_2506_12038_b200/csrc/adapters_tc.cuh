@@ -233,8 +233,10 @@ constexpr int kPlaces = 128;
 struct Plan {
   int *first, *begins;
   static constexpr int kBytes = 2 * (kMostGroups + 2) * 4;
-  // By one warp.  step: places of a tile.
+  // By one warp.  step: places of a tile.  Offsets that do not ascend (no plan of lcd_group_rows) may make more tiles than there can be: those
+  // are left out, so that their number stays within an int.
   __device__ __forceinline__ void make(const AdapterArgs& a, int lane, int step) const {
+    const int most = a.rows / step + min(a.G + 1, a.rows);
     int sum = 0;
     for (int g0 = 0; g0 <= a.G; g0 += 32) {
       const int g = g0 + lane;
@@ -250,8 +252,8 @@ struct Plan {
         const int v = __shfl_up_sync(0xffffffffu, upto, d);
         if (lane >= d) upto += v;
       }
-      if (g <= a.G) first[g] = sum + upto - tiles;
-      sum += __shfl_sync(0xffffffffu, upto, 31);
+      if (g <= a.G) first[g] = min(sum + upto - tiles, most);
+      sum = min(sum + __shfl_sync(0xffffffffu, upto, 31), most);
     }
     if (lane == 0) {
       first[a.G + 1] = sum;
