@@ -5,7 +5,7 @@
 // latency.  There operands go from memory to registers in the fragment order of mma.sync and nothing is staged: a sum does not care for
 // the order of its terms, so a lane takes 16 consecutive bytes of its row for the slots that the instruction gives it, and both operands
 // use the same order.  With many rows registers do not hold enough loads to keep memory busy (4096 x 5120 x 13824, rank 64, bf16: 206 us
-// a call): those go through shared memory and tcgen05 (adapters_tc.cuh: 74 us).
+// a call): those go through shared memory and tcgen05 (adapters_tc.cuh: 79 us).
 //
 // Arithmetic.  Two 16-bit operands of one type: their products are exact, sums are fp32.  The products with t or dt, which are fp32, whatever
 // the result's type (terms may cancel): with bf16 beside them as three bf16 terms (24 bits: exact), else as two tf32 terms (within 2^-23 of
@@ -176,8 +176,22 @@ __device__ __forceinline__ int row_of(const int32_t* order, int at, int rows) { 
 // RT for a rank: 16 * RT is the rank padded.
 constexpr int rank_tiles(int64_t r) { return r <= 16 ? 1 : r <= 32 ? 2 : r <= 64 ? 4 : 8; }
 constexpr int kMostRank = 128;
-// From this many rows on the products run on tcgen05 (adapters_tc.cuh), from twice as many where they do not start on 16 bytes: 777 rows of
-// 5001 columns, fp16, to 5003, fp32, take 52 us there and 34 here, 4096 of 5001 to 8003 160 and 240.
+// From this many rows on the products run on tcgen05 (adapters_tc.cuh), from twice as many where base and y, or x and the adapters of one
+// 16-bit type, do not start on 16 bytes (never the gradients' sums).  Few rows' kernels and many's, us of a call / of the whole gradient, five
+// adapters of rank 16:
+//   rows                              384            512            768            1024           1536           2048
+//   bf16, 4096 to 4096     few    17 /  32       22 /  38       26 /  44       32 /  52       42 /  67       50 /  81
+//                          many   24 /  36       24 /  36       28 /  40       28 /  42       30 /  48       34 /  54
+//   bf16, 1000 to 1000     few    17 /  24       17 /  24       17 /  26       17 /  26       22 /  38       24 /  40
+//                          many   17 /  26       19 /  28       22 /  30       22 /  30       24 /  34       24 /  34
+//   fp32, 4096 to 4096     few    26 /  50       32 /  56       38 /  71       46 /  83       60 / 110       73 / 134
+//                          many   32 /  46       34 /  48       36 /  56       38 /  60       42 /  71       65 /  99
+//   bf16, 4097 to 4099     few    26 /  46       32 /  52       42 /  71       48 /  79       64 / 106       79 / 128
+//                          many   50 /  65       52 /  69       61 /  85       60 /  87       64 /  97       75 / 117
+//   bf16, 5001 to 5003     few    28 /  48       36 /  58       44 /  77       54 /  87       71 / 118       89 / 146
+//                          many   52 /  67       54 /  69       65 /  83       65 /  87       77 / 106       79 / 116
+//   fp32, 4097 to 4099     few    38 /  58       46 /  65       54 /  85       67 /  99       89 / 134      110 / 165
+//                          many   44 /  60       46 /  63       52 /  75       54 /  81       67 / 103       97 / 142
 constexpr int kManyRows = 512;
 
 template <typename F>

@@ -58,7 +58,7 @@ struct OuterArgs {
   int32_t* status;
 };
 lcd_status launch_adapters_outer(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s);
-bool adapters_outer_tc_takes(const OuterArgs& P, lcd_dtype z_type);
+bool adapters_outer_tc_takes(const OuterArgs& P);
 lcd_status launch_adapters_outer_tc(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s);
 
 }  // namespace lcd

@@ -222,7 +222,7 @@ lcd_status launch_outer(OuterArgs P, cudaStream_t s) {
 }  // namespace
 
 lcd_status launch_adapters_outer(const OuterArgs& P, lcd_dtype z_type, cudaStream_t s) {
-  if (adapters_outer_tc_takes(P, z_type)) return launch_adapters_outer_tc(P, z_type, s);
+  if (adapters_outer_tc_takes(P)) return launch_adapters_outer_tc(P, z_type, s);
   return by_dtype(z_type, [&](auto z) {
     using Z = typename decltype(z)::type;
     switch (rank_tiles(P.r)) {

@@ -4,7 +4,7 @@
 // MN-major as they lie.  Rows of z follow the plan through 16-byte copies (bf16 as it is where rows start on 16 bytes; else, and fp16 and
 // fp32, through registers, in one to three bf16 parts), those of t or dt are split into parts on their way.  One CTA an SM takes every
 // gridDim.x-th sum; while one is read from tensor memory and stored, the next one's stages come in (a CTA for each sum spent more time on
-// beginning and ending than on an adapter's 256 rows: 148 us at 4096 x 5120 x 13824, rank 64, 16 adapters).  Where there are few sums a
+// beginning and ending than on an adapter's 256 rows: 148 us at 4096 x 5120 x 13824, rank 64, 16 adapters, two parts of u).  Where there are few sums a
 // cluster's CTAs share one's rows and add up in distributed shared memory, in the order of the ranks.  Reading z bounds it.
 // Roles: kZWarps warps bring z and kUWarps t or dt, in groups that take stages in turn (finding a stage's rows and addresses takes longer than
 // its bytes), one owns tensor memory and an elected lane issues the MMAs, four store.
@@ -415,11 +415,9 @@ lcd_status launch_shape(OuterArgs P, cudaStream_t s) {
 
 }  // namespace
 
-bool adapters_outer_tc_takes(const OuterArgs& P, lcd_dtype z_type) {
+bool adapters_outer_tc_takes(const OuterArgs& P) {
   long long slabs = 0;
-  for (int i = 0; i < P.sides; ++i) {
-    slabs += (P.side[i].columns + 127) / 128;
-  }
+  for (int i = 0; i < P.sides; ++i) slabs += (P.side[i].columns + 127) / 128;
   return P.rows >= kManyRows && slabs <= 0x7fffffff / kOuterSplit;
 }
 

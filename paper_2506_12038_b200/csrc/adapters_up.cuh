@@ -22,7 +22,7 @@ constexpr int kUpWarps = 4;
 template <typename W, int RT>
 constexpr int kUpTiles = sizeof(W) == 2 ? (RT <= 4 ? 8 : 4) : (RT <= 2 ? 8 : RT == 4 ? 4 : 2);
 
-// N consecutive values of base, or zeros.
+// N consecutive values of a row, of which `have` lie inside it; wide: on 16 bytes.
 template <typename Y, int N>
 __device__ __forceinline__ void store_values(Y* p, const float (&v)[N], int have, bool wide) {
   if (wide && have >= N) {

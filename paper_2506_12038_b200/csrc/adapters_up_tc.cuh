@@ -9,7 +9,7 @@
 // changes, those of the adapter matrix; warps 9-16 add: a thread has a row and half of the columns, reads the base's from
 // shared memory (rows 16 bytes longer than their columns: no bank conflicts) and stores 32 bytes at a time, whole sectors.
 // Two tiles are in flight: while one is added up, the next one's base comes in.
-// 4096 x 13824, rank 64, bf16: 55 us, 4.1 TB/s (79 with t split here in place of where it is made, 61 with the matrix through registers).  A tile
+// 4096 x 13824, rank 64, bf16: 56 us, 4.0 TB/s (55 with two parts of t; then 79 with t split here in place of where it is made, 61 with the matrix through registers).  A tile
 // takes 3.5 us: copies of base 3.5, adding and storing 2.5, both behind one another's memory traffic.
 #ifndef LCD_ADAPTERS_UP_TC_CUH_
 #define LCD_ADAPTERS_UP_TC_CUH_

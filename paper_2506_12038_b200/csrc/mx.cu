@@ -256,7 +256,9 @@ __global__ void __launch_bounds__(kMxThreads) places_kernel(const int32_t* order
 }
 
 // A token of several choices is quantised once where there are many (2048 tokens of 2048 columns with four choices, bf16: 15 us of which three
-// quarters are arithmetic, four times over; the call to 4096 rows of 32 experts 88 us so, 82 with the places found first); few are not worth the launch that finds the places.
+// quarters are arithmetic, four times over); few are not worth the launch that finds the places.  The call to 512 rows of experts, each choice by
+// itself and once a token, us: 2^21 values (512 x 2 of 2048 columns) 17.4 and 17.4, (512 x 4 of 1001) 15.4 and 17.4; 2^22 (512 x 4 of 2048) 19.3
+// and 19.5, (128 x 8 of 4096) 23.6 and 21.6; 2^24 (2048 x 4 of 2048) 31.8 and 27.7.
 lcd_status launch_mx_quantize_rows(const void* x, lcd_dtype type, int64_t T, int64_t K, int64_t ldx, const float* inv, const lcd_row_groups& rows,
                                    int64_t G, uint8_t* codes, int64_t ldc, uint8_t* scales, int64_t lds, int32_t* place, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);

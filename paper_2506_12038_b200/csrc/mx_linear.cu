@@ -1171,7 +1171,8 @@ Plan plan(int64_t M, int64_t N, int64_t n_ks) {
 
 // The width and the cut of a product grouped by expert.  How many rows an expert has is not known here; from the mean m over the experts
 // that can occur, taken for exponentially distributed, an expert has 1 / (1 - exp(-w / m)) tiles of w tokens.  Times of a stage and of a
-// tile's end in microseconds, from whole calls on B200 (widths 16 / 32 / 64 / 128 / 192 / 256 / pairs of 192 / of 256):
+// tile's end in microseconds, from whole calls on B200 one behind the other over the same buffers, so that weights of less than L2's size come
+// from there (with others every time the 71 of the first, 128 wide, is 82; widths 16 / 32 / 64 / 128 / 192 / 256 / pairs of 192 / of 256):
 //     2048 tokens x 4 of 32 experts, 4096 x 2048: 158 / 102 / 79 / 71 / 72 / 90 / 72 / 89 us; 4096 x 8192: - / - / 268 / 232 / 221 / 245 / 218 / 230
 //     4096 x 2 of 8, 14336 x 4096: - / - / 446 / 320 / 289 / 363 / 272 / 358;   512 x 4 of 32, 4096 x 2048: 53 / 40 / 36 / 38 / 46 / 54 / 45 / 52
 //     48 x 2 of 8, 11008 x 4096: 37 / 38 / 39 / 41 / 46 / 56;   200 x 4 of 32, 4096 x 2048: 34 / 31 / 33 / 35 / 41 / 46
